@@ -265,6 +265,73 @@ int32_t flex_awd_loss(const flex_desc* desc, const void* Q, const void* K,
                       float* loss, float* dW1, float* dW2, float* dtau,
                       void* ws, size_t ws_bytes, void* stream);
 
+/* ---- Packed sequences ---------------------------------------------------
+ * The entry points below take sequences of different lengths packed one after
+ * the other: tensors of T rows (tokens) [T][heads][width], and an int32 array
+ * off [B+1] on the device with sequence b in rows off[b] .. off[b+1]-1
+ * (non-decreasing, off[B] <= T; a sequence may be empty).  Offsets are clamped
+ * to 0 .. T on the device, so wrong ones give wrong results but no access
+ * outside the tensors; rows of no sequence are neither read nor written.  The
+ * conventions at the top of this file hold, except:
+ *   - input rows may be strided (slices of one projection's output): *_stride
+ *     elements between consecutive rows, 0 for contiguous ones; at least
+ *     heads * width, a multiple of 16 bytes, at most 2^20 elements.  The heads
+ *     of a row are contiguous.  Outputs and upstream gradients are contiguous.
+ *   - several (query or value) heads may share a key head: head h uses key head
+ *     h / (heads / key heads).  A gradient of a shared head is the sum over its
+ *     group, formed in a fixed order.
+ *   - gradients are in io_dtype.
+ *   - a pointer may be NULL where its tensor has no rows. */
+
+/* Exact softmax attention, the one that Eq.(linear att) approximates and
+ * flex_awd_loss distils.  For sequence b with nq query rows and nk key rows
+ * (prefix-cached or slotted keys: nk and nq may differ), query i sees the keys
+ * j < nk, with causal also j <= i + nk - nq (the last query sees every key):
+ *     O_i = sum_j softmax_j(scale Q_i.K_j) V_j,  lse_i = log sum_j exp(scale Q_i.K_j)
+ * A query that sees no key has O_i = 0, lse_i = -inf and no gradient. */
+typedef struct {
+  int32_t B;              /* sequences                                              */
+  int32_t Hq, Hkv;        /* query heads; key heads (Hkv divides Hq)                */
+  int32_t d;              /* head size of Q, K and V: 32, 64 or 128                 */
+  int32_t Tq, Tk;         /* rows of Q, O and of K, V                               */
+  int32_t causal;
+  int32_t io_dtype;       /* flex_dtype of Q, K, V, O, dO and the gradients         */
+  int32_t q_stride, k_stride, v_stride;
+  float scale;            /* > 0; usually 1/sqrt(d)                                 */
+} flex_attn_desc;
+
+/* Bytes of workspace of a pass (FLEX_PASS_FWD, FLEX_PASS_BWD); 0 is possible,
+ * and then ws may be NULL. */
+int32_t flex_attn_workspace_size(const flex_attn_desc* desc, int32_t pass, size_t* bytes);
+
+/* Forward: prompts, and single tokens (or a few drafted ones) against a cache.
+ *   Q [Tq,Hq,d], K, V [Tk,Hkv,d]   io_dtype
+ *   q_off, k_off [B+1] int32
+ *   k_len [B] int32 or NULL        keys in use of each sequence's rows: a cache
+ *                                  with a slot of rows per sequence (clamped to
+ *                                  the slot); NULL: all rows
+ *   O [Tq,Hq,d] io_dtype, lse [Tq,Hq] fp32 or NULL
+ * Logits, statistics and sums are fp32; with FLEX_BF16 the probabilities are
+ * rounded to bf16 for the product with V.  With at most 64 rows (queries times
+ * heads of a group) per sequence on average the keys of a sequence are split over
+ * several workgroups, joined in a fixed order.
+ * A key row that a query does not see takes no part, whatever it holds. */
+int32_t flex_attn_fwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
+                      const int32_t* q_off, const int32_t* k_off, const int32_t* k_len,
+                      void* O, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Backward of flex_attn_fwd with k_len = NULL.
+ *   O, lse            the forward's outputs
+ *   dO [Tq,Hq,d]      io_dtype
+ *   dQ [Tq,Hq,d], dK, dV [Tk,Hkv,d]   io_dtype outputs: the rows of the
+ *                     sequences are overwritten
+ * With FLEX_BF16 the probabilities and the gradients of the logits are rounded to
+ * bf16 for the products over them. */
+int32_t flex_attn_bwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
+                      const int32_t* q_off, const int32_t* k_off, const void* O, const float* lse,
+                      const void* dO, void* dQ, void* dK, void* dV,
+                      void* ws, size_t ws_bytes, void* stream);
+
 /* ---- Kernel timing (profiling aid) --------------------------------------
  * Kernel classes of the library.  When timing is enabled for one class, every
  * launch of a kernel of that class is bracketed by two hipEvents recorded on
@@ -284,7 +351,9 @@ typedef enum {
   FLEX_KERNEL_DECODE = 9,       /* recurrent decode step                      */
   FLEX_KERNEL_AWD_FWD = 10,     /* distillation loss (and dphi(Q)) pass       */
   FLEX_KERNEL_AWD_BWD_K = 11,   /* distillation dphi(K) pass                  */
-  FLEX_KERNEL_AWD_WGRAD = 12    /* distillation chain rule to dW', dtau       */
+  FLEX_KERNEL_AWD_WGRAD = 12,   /* distillation chain rule to dW', dtau       */
+  FLEX_KERNEL_ATTN_FWD = 13,    /* exact attention, all kernels of a forward  */
+  FLEX_KERNEL_ATTN_BWD = 14     /* exact attention, all kernels of a backward */
 } flex_kernel;
 
 /* Select the kernel class to time (FLEX_KERNEL_NONE disables) and discard

@@ -21,10 +21,12 @@ EXPORTS = ("flex_abi_version", "flex_status_string", "flex_workspace_size",
            "flex_feature_map", "flex_linattn_fwd", "flex_linattn_prefill", "flex_linattn_fwd_noalloc",
            "flex_linattn_bwd",
            "flex_decode_step",
-           "flex_awd_loss", "flex_timing_enable", "flex_timing_read")
+           "flex_awd_loss", "flex_attn_workspace_size", "flex_attn_fwd", "flex_attn_bwd",
+           "flex_timing_enable", "flex_timing_read")
 KERNELS = {"none": 0, "fwd_state": 1, "fwd_sweep": 2, "scan": 3, "bwd_prepass": 4,
            "bwd_dq": 5, "bwd_dkv": 6, "bwd_reduce": 7, "feature_map": 8, "decode_step": 9,
-           "awd_fwd": 10, "awd_bwd_k": 11, "awd_wgrad": 12}
+           "awd_fwd": 10, "awd_bwd_k": 11, "awd_wgrad": 12,
+           "attn_fwd": 13, "attn_bwd": 14}
 
 
 class FlexError(RuntimeError):
@@ -40,6 +42,11 @@ class flex_desc(ctypes.Structure):
                 ("chunk", ctypes.c_int32), ("segments", ctypes.c_int32),
                 ("io_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
                 ("sigma", ctypes.c_float)]
+
+
+class flex_attn_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "d", "Tq", "Tk", "causal", "io_dtype",
+                                              "q_stride", "k_stride", "v_stride")] + [("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -83,6 +90,13 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.flex_decode_step.argtypes = [D] + [P] * 10
     lib.flex_awd_loss.restype = I
     lib.flex_awd_loss.argtypes = [D] + [P] * 10 + [S, P]
+    A = ctypes.POINTER(flex_attn_desc)
+    lib.flex_attn_workspace_size.restype = I
+    lib.flex_attn_workspace_size.argtypes = [A, I, ctypes.POINTER(S)]
+    lib.flex_attn_fwd.restype = I
+    lib.flex_attn_fwd.argtypes = [A] + [P] * 9 + [S, P]
+    lib.flex_attn_bwd.restype = I
+    lib.flex_attn_bwd.argtypes = [A] + [P] * 12 + [S, P]
     lib.flex_timing_enable.restype = I
     lib.flex_timing_enable.argtypes = [I]
     lib.flex_timing_read.restype = I
@@ -281,6 +295,104 @@ def flex_awd_loss(desc: flex_desc, Q, K, W1, W2, tau, grads=True, loss=None, dW1
                               _stream())
     _check(st, "flex_awd_loss")
     return dict(loss=loss, dW1=dW1, dW2=dW2, dtau=dtau)
+
+
+# ---------------------------------------------------------------------------
+# Packed sequences
+# ---------------------------------------------------------------------------
+def _size(fn, desc, *args):
+    n = ctypes.c_size_t(0)
+    _check(getattr(load(), fn)(ctypes.byref(desc), *args, ctypes.byref(n)), fn)
+    return n.value
+
+
+def _expect(what, dev, **tensors):
+    """Tensors against (shape, dtype, row stride or 0 for contiguous); None where one is left out."""
+    for name, (t, shape, dtype, stride) in tensors.items():
+        if t is None:
+            continue
+        rows = (stride, shape[2], 1) if stride and shape[0] > 1 else None
+        if (tuple(t.shape) != shape or t.dtype != dtype or t.device != dev or
+                (t.numel() and not (t[0].is_contiguous() and t.stride() == rows if rows else t.is_contiguous()))):
+            raise FlexError(FLEX_ERR_INVALID_ARG, f"{what}: {name} must be {dtype} {list(shape)} on {dev}, rows "
+                            + (f"{stride} elements apart" if stride else "contiguous"))
+
+
+def _io(desc):
+    import torch
+    return torch.bfloat16 if desc.io_dtype == FLEX_BF16 else torch.float32
+
+
+def _run(fn, dev, desc, *args):
+    """The call on the current stream of the tensors' device."""
+    import torch
+    with torch.cuda.device(dev):
+        _check(getattr(load(), fn)(ctypes.byref(desc), *args, _stream()), fn)
+
+
+def _seq_workspace(need, ws, dev):
+    import torch
+    if ws is None or ws.numel() * ws.element_size() < need:
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    return _ptr(ws), ws.numel() * ws.element_size()
+
+
+def make_attn_desc(B, Hq, Hkv, d, Tq, Tk, causal=True, io="bf16", scale=None, q_stride=0, k_stride=0,
+                   v_stride=0) -> flex_attn_desc:
+    """B sequences packed in Tq query and Tk key rows; strides in elements between rows (0: contiguous)."""
+    return flex_attn_desc(B, Hq, Hkv, d, Tq, Tk, 1 if causal else 0, FLEX_BF16 if io == "bf16" else FLEX_F32,
+                          q_stride, k_stride, v_stride, float(d ** -0.5 if scale is None else scale))
+
+
+def attn_workspace_size(desc: flex_attn_desc, pass_: int) -> int:
+    return _size("flex_attn_workspace_size", desc, pass_)
+
+
+def _attn_inputs(what, desc, Q, K, V, q_off, k_off, **more):
+    import torch
+    io, dev = _io(desc), Q.device
+    _expect(what, dev, Q=(Q, (desc.Tq, desc.Hq, desc.d), io, desc.q_stride),
+            K=(K, (desc.Tk, desc.Hkv, desc.d), io, desc.k_stride),
+            V=(V, (desc.Tk, desc.Hkv, desc.d), io, desc.v_stride),
+            q_off=(q_off, (desc.B + 1,), torch.int32, 0), k_off=(k_off, (desc.B + 1,), torch.int32, 0), **more)
+    return io, dev
+
+
+def flex_attn_fwd(desc: flex_attn_desc, Q, K, V, q_off, k_off, k_len=None, O=None, lse=None, ws=None,
+                  want_lse=True):
+    """Exact attention of packed sequences: Q [Tq,Hq,d] against K, V [Tk,Hkv,d], int32
+    offsets [B+1] (and the used key lengths k_len [B] of a slotted cache) on the
+    device.  Returns (O, lse)."""
+    import torch
+    rows, lrow = (desc.Tq, desc.Hq, desc.d), (desc.Tq, desc.Hq)
+    io, dev = _attn_inputs("flex_attn_fwd", desc, Q, K, V, q_off, k_off,
+                           k_len=(k_len, (desc.B,), torch.int32, 0), O=(O, rows, _io(desc), 0),
+                           lse=(lse, lrow, torch.float32, 0))
+    if O is None:
+        O = torch.empty(rows, dtype=io, device=dev)
+    if lse is None and want_lse:
+        lse = torch.empty(lrow, dtype=torch.float32, device=dev)
+    w = _seq_workspace(attn_workspace_size(desc, FLEX_PASS_FWD), ws, dev)
+    _run("flex_attn_fwd", dev, desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(q_off), _ptr(k_off), _ptr(k_len), _ptr(O),
+         _ptr(lse), *w)
+    return O, lse
+
+
+def flex_attn_bwd(desc: flex_attn_desc, Q, K, V, q_off, k_off, O, lse, dO, dQ=None, dK=None, dV=None, ws=None):
+    """Backward of flex_attn_fwd (k_len None) from its O and lse.  Returns dict(dQ, dK, dV)
+    in the io dtype; rows of no sequence are not written."""
+    import torch
+    rows, krow, io = (desc.Tq, desc.Hq, desc.d), (desc.Tk, desc.Hkv, desc.d), _io(desc)
+    _, dev = _attn_inputs("flex_attn_bwd", desc, Q, K, V, q_off, k_off, O=(O, rows, io, 0), dO=(dO, rows, io, 0),
+                          lse=(lse, rows[:2], torch.float32, 0), dQ=(dQ, rows, io, 0), dK=(dK, krow, io, 0),
+                          dV=(dV, krow, io, 0))
+    dQ = torch.empty(rows, dtype=io, device=dev) if dQ is None else dQ
+    dK = torch.empty(krow, dtype=io, device=dev) if dK is None else dK
+    dV = torch.empty(krow, dtype=io, device=dev) if dV is None else dV
+    w = _seq_workspace(attn_workspace_size(desc, FLEX_PASS_BWD), ws, dev)
+    _run("flex_attn_bwd", dev, desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(q_off), _ptr(k_off), _ptr(O), _ptr(lse),
+         _ptr(dO), _ptr(dQ), _ptr(dK), _ptr(dV), *w)
+    return dict(dQ=dQ, dK=dK, dV=dV)
 
 
 def flex_timing_enable(kernel: str) -> None:

@@ -1,0 +1,142 @@
+// C ABI of the packed-sequence operators: argument validation, workspace sizing and
+// the choice of kernels.
+#include "../../include/flex.h"
+#include "flex_seq_kernels.hpp"
+
+#include <math.h>
+#include <string.h>
+
+using namespace flex;
+
+namespace {
+
+constexpr int kMaxStride = 1 << 20;   // elements: a tile's window of rows stays within 32-bit byte offsets
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+int esize(int32_t io_dtype) { return io_dtype == FLEX_BF16 ? 2 : 4; }
+
+// A row stride: 0 (contiguous rows of `row` elements), or a whole number of 16-byte
+// units that rows fit in.
+bool stride_ok(int32_t stride, int64_t row, int e) {
+  if (stride == 0) return true;
+  return stride >= row && stride <= kMaxStride && (int64_t)stride * e % 16 == 0;
+}
+int stride_of(int32_t stride, int64_t row) { return stride ? stride : (int)row; }
+
+// a required tensor of `rows` rows, 16-byte aligned
+bool tensor_ok(const void* p, int64_t rows) { return rows == 0 || (p && aligned16(p)); }
+
+int32_t check_attn(const flex_attn_desc* d) {
+  if (!d) return FLEX_ERR_INVALID_ARG;
+  if (d->B <= 0 || d->Hq <= 0 || d->Hkv <= 0 || d->d <= 0 || d->Tq < 0 || d->Tk < 0) return FLEX_ERR_INVALID_ARG;
+  if (d->Hq % d->Hkv != 0) return FLEX_ERR_INVALID_ARG;
+  if (d->causal != 0 && d->causal != 1) return FLEX_ERR_INVALID_ARG;
+  if (d->io_dtype != FLEX_F32 && d->io_dtype != FLEX_BF16) return FLEX_ERR_INVALID_ARG;
+  if (!(d->scale > 0.0f) || !isfinite(d->scale)) return FLEX_ERR_INVALID_ARG;
+  if (d->d != 32 && d->d != 64 && d->d != 128) return FLEX_ERR_UNSUPPORTED;
+  const int64_t q = (int64_t)d->Hq * d->d, k = (int64_t)d->Hkv * d->d;
+  if (q > kMaxStride) return FLEX_ERR_UNSUPPORTED;
+  const int e = esize(d->io_dtype);
+  if (!stride_ok(d->q_stride, q, e) || !stride_ok(d->k_stride, k, e) || !stride_ok(d->v_stride, k, e))
+    return FLEX_ERR_INVALID_ARG;
+  // workgroups of a launch (row tiles and sequences times heads) fit 31 bits
+  if (((int64_t)d->Tq + d->B) * d->Hq >= (1LL << 31) || ((int64_t)d->Tk / 128 + d->B) * d->Hkv >= (1LL << 31))
+    return FLEX_ERR_INVALID_ARG;
+  return FLEX_OK;
+}
+
+// Parts of each sequence's keys in the forward; 0: the kernel for prompts.  The
+// split kernel takes 32 rows (queries times heads of a group) of a sequence at a
+// time and reads its keys for each 32, so it serves calls whose sequences have up to
+// twice that many on average.
+int attn_parts(const flex_attn_desc* d) {
+  if ((int64_t)d->Tq * (d->Hq / d->Hkv) > 64LL * d->B) return 0;
+  const int64_t wgs = (int64_t)d->B * d->Hkv, keys = d->Tk / d->B;
+  int64_t n = (1024 + wgs - 1) / wgs;
+  if (n > keys / 256) n = keys / 256;
+  return n < 1 ? 1 : (int)n;
+}
+size_t attn_part_rows(const flex_attn_desc* d) { return (size_t)d->Tq * d->Hq * (size_t)attn_parts(d); }
+
+size_t attn_ws_bytes(const flex_attn_desc* d, int32_t pass) {
+  if (pass == FLEX_PASS_BWD) return (size_t)2 * d->Tq * d->Hq * sizeof(float);
+  if (attn_parts(d) <= 1) return 0;
+  return align256(attn_part_rows(d) * d->d * sizeof(float)) + attn_part_rows(d) * 2 * sizeof(float);
+}
+
+AttnArgs attn_args(const flex_attn_desc* d, const void* Q, const void* K, const void* V, const int32_t* q_off,
+                   const int32_t* k_off) {
+  AttnArgs a;
+  memset(&a, 0, sizeof(a));
+  a.Q = Q; a.K = K; a.V = V; a.q_off = q_off; a.k_off = k_off;
+  a.B = d->B; a.Hq = d->Hq; a.Hkv = d->Hkv; a.Tq = d->Tq; a.Tk = d->Tk; a.causal = d->causal;
+  a.qs = stride_of(d->q_stride, (int64_t)d->Hq * d->d);
+  a.ks = stride_of(d->k_stride, (int64_t)d->Hkv * d->d);
+  a.vs = stride_of(d->v_stride, (int64_t)d->Hkv * d->d);
+  a.scale = d->scale;
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t flex_attn_workspace_size(const flex_attn_desc* desc, int32_t pass, size_t* bytes) {
+  if (!bytes) return FLEX_ERR_INVALID_ARG;
+  *bytes = 0;
+  if (pass != FLEX_PASS_FWD && pass != FLEX_PASS_BWD) return FLEX_ERR_INVALID_ARG;
+  const int32_t st = check_attn(desc);
+  if (st != FLEX_OK) return st;
+  *bytes = attn_ws_bytes(desc, pass);
+  return FLEX_OK;
+}
+
+int32_t flex_attn_fwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
+                      const int32_t* q_off, const int32_t* k_off, const int32_t* k_len, void* O, float* lse,
+                      void* ws, size_t ws_bytes, void* stream) {
+  const int32_t st = check_attn(desc);
+  if (st != FLEX_OK) return st;
+  if (!q_off || !k_off) return FLEX_ERR_INVALID_ARG;
+  if (!tensor_ok(Q, desc->Tq) || !tensor_ok(O, desc->Tq) || !tensor_ok(K, desc->Tk) || !tensor_ok(V, desc->Tk) ||
+      (lse && !aligned16(lse)))
+    return FLEX_ERR_INVALID_ARG;
+  const size_t need = attn_ws_bytes(desc, FLEX_PASS_FWD);
+  if (need > 0 && (!ws || ws_bytes < need || !aligned16(ws))) return FLEX_ERR_WORKSPACE;
+  if (desc->Tq == 0) return FLEX_OK;
+  AttnArgs a = attn_args(desc, Q, K, V, q_off, k_off);
+  a.k_len = k_len; a.O = O; a.lse = lse;
+  a.nsplit = attn_parts(desc);
+  if (need > 0) {
+    a.part_o = static_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) +
+                                         align256(attn_part_rows(desc) * desc->d * sizeof(float)));
+  }
+  const hipError_t e = launch_attn_fwd(a, desc->io_dtype == FLEX_BF16, desc->d, (hipStream_t)stream);
+  return e == hipSuccess ? FLEX_OK : FLEX_ERR_HIP;
+}
+
+int32_t flex_attn_bwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
+                      const int32_t* q_off, const int32_t* k_off, const void* O, const float* lse, const void* dO,
+                      void* dQ, void* dK, void* dV, void* ws, size_t ws_bytes, void* stream) {
+  const int32_t st = check_attn(desc);
+  if (st != FLEX_OK) return st;
+  if (!q_off || !k_off) return FLEX_ERR_INVALID_ARG;
+  const void* qt[] = {Q, O, lse, dO, dQ};
+  for (const void* p : qt)
+    if (!tensor_ok(p, desc->Tq)) return FLEX_ERR_INVALID_ARG;
+  const void* kt[] = {K, V, dK, dV};
+  for (const void* p : kt)
+    if (!tensor_ok(p, desc->Tk)) return FLEX_ERR_INVALID_ARG;
+  const size_t need = attn_ws_bytes(desc, FLEX_PASS_BWD);
+  if (need > 0 && (!ws || ws_bytes < need || !aligned16(ws))) return FLEX_ERR_WORKSPACE;
+  if (desc->Tq == 0 && desc->Tk == 0) return FLEX_OK;
+  AttnArgs a = attn_args(desc, Q, K, V, q_off, k_off);
+  a.O = const_cast<void*>(O); a.lse = const_cast<float*>(lse); a.dO = dO;
+  a.dQ = dQ; a.dK = dK; a.dV = dV;
+  a.delta = static_cast<float*>(ws);
+  const hipError_t e = launch_attn_bwd(a, desc->io_dtype == FLEX_BF16, desc->d, (hipStream_t)stream);
+  return e == hipSuccess ? FLEX_OK : FLEX_ERR_HIP;
+}
+
+}  // extern "C"
