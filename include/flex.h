@@ -332,6 +332,55 @@ int32_t flex_attn_bwd(const flex_attn_desc* desc, const void* Q, const void* K, 
                       const void* dO, void* dQ, void* dK, void* dV,
                       void* ws, size_t ws_bytes, void* stream);
 
+/* Gated delta rule: a recurrent state of associations that is decayed, corrected and
+ * read, per sequence and value head (with its key head's q and k):
+ *     S_t = a_t S_{t-1} + beta_t k_t (v_t - a_t S_{t-1}^T k_t)^T,   a_t = exp(g_t)
+ *     O_t = scale S_t^T q_t
+ * from S_0 = state0, or zero.  Rows of K are meant to have unit length (and beta
+ * 0 .. 2), which keeps the recurrence bounded; this is not checked.  g is a log
+ * decay, usually <= 0; -inf (a = 0: the state is cleared) is allowed in the
+ * forward and has gradient zero.  The prompt's forward and the backward work in
+ * chunks of 64 tokens. */
+typedef struct {
+  int32_t B, T;           /* sequences; rows of Q, K, V, g, beta, O                */
+  int32_t Hk, H;          /* query and key heads; value heads (Hk divides H)       */
+  int32_t d, dv;          /* head size of Q, K and of V: 64 or 128 each            */
+  int32_t io_dtype;       /* flex_dtype of Q, K, V, O, dO and the gradients        */
+  int32_t q_stride, k_stride, v_stride;
+  float scale;            /* > 0; usually 1/sqrt(d)                                */
+} flex_delta_desc;
+
+/* Bytes of workspace of a pass (FLEX_PASS_FWD, FLEX_PASS_BWD). */
+int32_t flex_delta_workspace_size(const flex_delta_desc* desc, int32_t pass, size_t* bytes);
+
+/* Bytes of what a forward keeps for its backward. */
+int32_t flex_delta_saved_size(const flex_delta_desc* desc, size_t* bytes);
+
+/* Forward over packed sequences.
+ *   Q, K [T,Hk,d], V [T,H,dv]   io_dtype
+ *   g, beta [T,H]               fp32
+ *   off [B+1] int32
+ *   state0 [B,H,d,dv] fp32 or NULL   the states to continue from
+ *   O [T,H,dv]                  io_dtype
+ *   state [B,H,d,dv] fp32 or NULL    the states after the last tokens (state0
+ *                               itself is allowed); an empty sequence's is its
+ *                               state0, or zero
+ *   saved                       flex_delta_saved_size() bytes for a backward, or
+ *                               NULL; with it ws is not used and may be NULL
+ * States, decays and sums are fp32; with FLEX_BF16 they enter products as two
+ * bf16 terms, so that a state is right to about 2^-17 of its terms. */
+int32_t flex_delta_fwd(const flex_delta_desc* desc, const void* Q, const void* K, const void* V,
+                       const float* g, const float* beta, const int32_t* off, const float* state0,
+                       void* O, float* state, void* saved, size_t saved_bytes,
+                       void* ws, size_t ws_bytes, void* stream);
+
+/* Single-token step: one token of every sequence (rows 0 .. B-1, T and the row
+ * offsets are not used), fp32 throughout but for the io rows.
+ *   q, k [B,Hk,d], v [B,H,dv], g, beta [B,H], state [B,H,d,dv] fp32 updated in
+ *   place, o [B,H,dv] */
+int32_t flex_delta_step(const flex_delta_desc* desc, const void* q, const void* k, const void* v,
+                        const float* g, const float* beta, float* state, void* o, void* stream);
+
 /* ---- Kernel timing (profiling aid) --------------------------------------
  * Kernel classes of the library.  When timing is enabled for one class, every
  * launch of a kernel of that class is bracketed by two hipEvents recorded on
@@ -353,7 +402,10 @@ typedef enum {
   FLEX_KERNEL_AWD_BWD_K = 11,   /* distillation dphi(K) pass                  */
   FLEX_KERNEL_AWD_WGRAD = 12,   /* distillation chain rule to dW', dtau       */
   FLEX_KERNEL_ATTN_FWD = 13,    /* exact attention, all kernels of a forward  */
-  FLEX_KERNEL_ATTN_BWD = 14     /* exact attention, all kernels of a backward */
+  FLEX_KERNEL_ATTN_BWD = 14,    /* exact attention, all kernels of a backward */
+  FLEX_KERNEL_DELTA_FWD = 15,   /* gated delta rule, all kernels of a forward  */
+  FLEX_KERNEL_DELTA_BWD = 16,   /* gated delta rule, all kernels of a backward */
+  FLEX_KERNEL_DELTA_STEP = 17   /* gated delta rule, single-token step        */
 } flex_kernel;
 
 /* Select the kernel class to time (FLEX_KERNEL_NONE disables) and discard

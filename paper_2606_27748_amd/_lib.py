@@ -22,11 +22,12 @@ EXPORTS = ("flex_abi_version", "flex_status_string", "flex_workspace_size",
            "flex_linattn_bwd",
            "flex_decode_step",
            "flex_awd_loss", "flex_attn_workspace_size", "flex_attn_fwd", "flex_attn_bwd",
+           "flex_delta_workspace_size", "flex_delta_saved_size", "flex_delta_fwd", "flex_delta_step",
            "flex_timing_enable", "flex_timing_read")
 KERNELS = {"none": 0, "fwd_state": 1, "fwd_sweep": 2, "scan": 3, "bwd_prepass": 4,
            "bwd_dq": 5, "bwd_dkv": 6, "bwd_reduce": 7, "feature_map": 8, "decode_step": 9,
            "awd_fwd": 10, "awd_bwd_k": 11, "awd_wgrad": 12,
-           "attn_fwd": 13, "attn_bwd": 14}
+           "attn_fwd": 13, "attn_bwd": 14, "delta_fwd": 15, "delta_bwd": 16, "delta_step": 17}
 
 
 class FlexError(RuntimeError):
@@ -47,6 +48,11 @@ class flex_desc(ctypes.Structure):
 class flex_attn_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "d", "Tq", "Tk", "causal", "io_dtype",
                                               "q_stride", "k_stride", "v_stride")] + [("scale", ctypes.c_float)]
+
+
+class flex_delta_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "Hk", "H", "d", "dv", "io_dtype", "q_stride", "k_stride",
+                                              "v_stride")] + [("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -97,6 +103,15 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.flex_attn_fwd.argtypes = [A] + [P] * 9 + [S, P]
     lib.flex_attn_bwd.restype = I
     lib.flex_attn_bwd.argtypes = [A] + [P] * 12 + [S, P]
+    G = ctypes.POINTER(flex_delta_desc)
+    lib.flex_delta_workspace_size.restype = I
+    lib.flex_delta_workspace_size.argtypes = [G, I, ctypes.POINTER(S)]
+    lib.flex_delta_saved_size.restype = I
+    lib.flex_delta_saved_size.argtypes = [G, ctypes.POINTER(S)]
+    lib.flex_delta_fwd.restype = I
+    lib.flex_delta_fwd.argtypes = [G] + [P] * 10 + [S, P, S, P]
+    lib.flex_delta_step.restype = I
+    lib.flex_delta_step.argtypes = [G] + [P] * 8
     lib.flex_timing_enable.restype = I
     lib.flex_timing_enable.argtypes = [I]
     lib.flex_timing_read.restype = I
@@ -393,6 +408,76 @@ def flex_attn_bwd(desc: flex_attn_desc, Q, K, V, q_off, k_off, O, lse, dO, dQ=No
     _run("flex_attn_bwd", dev, desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(q_off), _ptr(k_off), _ptr(O), _ptr(lse),
          _ptr(dO), _ptr(dQ), _ptr(dK), _ptr(dV), *w)
     return dict(dQ=dQ, dK=dK, dV=dV)
+
+
+def make_delta_desc(B, Hk, H, d, T, dv=None, io="bf16", scale=None, q_stride=0, k_stride=0,
+                    v_stride=0) -> flex_delta_desc:
+    """B sequences packed in T rows of Hk query/key heads and H value heads; strides in elements
+    between rows (0: contiguous)."""
+    return flex_delta_desc(B, T, Hk, H, d, d if dv is None else dv, FLEX_BF16 if io == "bf16" else FLEX_F32,
+                           q_stride, k_stride, v_stride, float(d ** -0.5 if scale is None else scale))
+
+
+def delta_workspace_size(desc: flex_delta_desc, pass_: int) -> int:
+    return _size("flex_delta_workspace_size", desc, pass_)
+
+
+def delta_saved_size(desc: flex_delta_desc) -> int:
+    """Bytes of the buffer in which a forward keeps what its backward reads."""
+    return _size("flex_delta_saved_size", desc)
+
+
+def _delta_inputs(what, desc, T, Q, K, V, g, beta, **more):
+    import torch
+    io, dev = _io(desc), Q.device
+    _expect(what, dev, Q=(Q, (T, desc.Hk, desc.d), io, desc.q_stride), K=(K, (T, desc.Hk, desc.d), io, desc.k_stride),
+            V=(V, (T, desc.H, desc.dv), io, desc.v_stride), g=(g, (T, desc.H), torch.float32, 0),
+            beta=(beta, (T, desc.H), torch.float32, 0), **more)
+    return io, dev
+
+
+def _saved(what, desc, saved):
+    n = saved.numel() * saved.element_size()
+    if n < delta_saved_size(desc) or not saved.is_contiguous():
+        raise FlexError(FLEX_ERR_WORKSPACE, f"{what}: saved")
+    return _ptr(saved), n
+
+
+def flex_delta_fwd(desc: flex_delta_desc, Q, K, V, g, beta, off, state0=None, O=None, state=None, saved=None,
+                   ws=None, want_state=False):
+    """Gated delta rule over packed sequences: Q, K [T,Hk,d], V [T,H,dv], g (log decay) and beta
+    [T,H] fp32, int32 offsets [B+1] on the device.  saved: a buffer of delta_saved_size bytes
+    for flex_delta_bwd.  Returns (O, state), state [B,H,d,dv] fp32 where one was given or
+    want_state."""
+    import torch
+    sshape = (desc.B, desc.H, desc.d, desc.dv)
+    io, dev = _delta_inputs("flex_delta_fwd", desc, desc.T, Q, K, V, g, beta, off=(off, (desc.B + 1,), torch.int32, 0),
+                            O=(O, (desc.T, desc.H, desc.dv), _io(desc), 0), state0=(state0, sshape, torch.float32, 0),
+                            state=(state, sshape, torch.float32, 0))
+    if O is None:
+        O = torch.empty(desc.T, desc.H, desc.dv, dtype=io, device=dev)
+    if state is None and want_state:
+        state = torch.empty(sshape, dtype=torch.float32, device=dev)
+    if saved is not None:
+        keep, w = _saved("flex_delta_fwd", desc, saved), (None, 0)
+    else:
+        keep, w = (None, 0), _seq_workspace(delta_workspace_size(desc, FLEX_PASS_FWD), ws, dev)
+    _run("flex_delta_fwd", dev, desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(g), _ptr(beta), _ptr(off), _ptr(state0), _ptr(O),
+         _ptr(state), *keep, *w)
+    return O, state
+
+
+def flex_delta_step(desc: flex_delta_desc, q, k, v, g, beta, state, o=None):
+    """One token of every sequence: q, k [B,Hk,d], v [B,H,dv], g, beta [B,H], state [B,H,d,dv]
+    fp32 updated in place.  Returns o [B,H,dv]."""
+    import torch
+    io, dev = _delta_inputs("flex_delta_step", desc, desc.B, q, k, v, g, beta,
+                            o=(o, (desc.B, desc.H, desc.dv), _io(desc), 0),
+                            state=(state, (desc.B, desc.H, desc.d, desc.dv), torch.float32, 0))
+    if o is None:
+        o = torch.empty(desc.B, desc.H, desc.dv, dtype=io, device=dev)
+    _run("flex_delta_step", dev, desc, _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(state), _ptr(o))
+    return o
 
 
 def flex_timing_enable(kernel: str) -> None:

@@ -791,7 +791,7 @@ extern "C" {
 int32_t flex_abi_version(void) { return FLEX_ABI_VERSION; }
 
 int32_t flex_timing_enable(int32_t kernel) {
-  if (kernel < FLEX_KERNEL_NONE || kernel > FLEX_KERNEL_ATTN_BWD) return FLEX_ERR_INVALID_ARG;
+  if (kernel < FLEX_KERNEL_NONE || kernel > FLEX_KERNEL_DELTA_STEP) return FLEX_ERR_INVALID_ARG;
   Timing& t = timing();
   std::lock_guard<std::mutex> lk(t.mu);
   t.kernel = kernel;

@@ -1,0 +1,431 @@
+// Gated delta rule, forward: the chunks' matrices (k_delta_prep), the sweep over the state
+// (k_delta_sweep) and the single-token step (k_delta_step).
+#include "flex_delta.hpp"
+#include "../../include/flex.h"
+
+namespace flex {
+
+namespace {
+__device__ __forceinline__ void lds_fence() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// c += a b for 16 x 16 fp32 tiles: a as its transpose's result layout, b as a result
+__device__ __forceinline__ void mm16(f32x4& c, const f32x4& a, const f32x4& b) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], b[r], c, 0, 0, 0);
+}
+}  // namespace
+
+// One wave per chunk and value head; everything in fp32 from exact products.
+// N = A^T is held as 16 x 16 tiles N(n, m) (rows j of block n, lane column i of block m), so
+// that the tiles of X = (I + N)^-1 = T^T come out as a lane per row i of T.  The diagonal
+// blocks are inverted by substitution, a lane per column, all four at once; the others
+// follow from X(n,m) = -X(n,n) sum_{n<k<=m} N(n,k) X(k,m) on the fp32 matrix cores.
+template <class T, int D>
+__global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
+  using S = typename Io<T>::type;
+  constexpr int KS = D / 32, LD = 20;
+  __shared__ __attribute__((aligned(16))) float lds_t[4][4 * 16 * LD];
+  __shared__ double lds_g[4][DC];
+  const int l = threadIdx.x % WAVE, r16 = l % 16, g = l / 16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int slots = seq_slots(a.T, a.B, DC);
+  const int id = blockIdx.x * 4 + w, slot = id / a.H, head = id % a.H;
+  if (slot >= slots) return;
+  const SeqTile t = find_tile<DC>(a.off, a.B, a.T, slot);
+  if (t.b < 0) return;
+  const int n = min(DC, t.n - t.tile * DC), row0 = t.row0 + t.tile * DC, kh = head / (a.H / a.Hk);
+  char* out = a.prep + (size_t)id * DELTA_PREP_BYTES;
+  float* Lt = lds_t[w];
+  double* Lg = lds_g[w];
+
+  // the decays, lane = token.  A decay of zero (g = -inf) is kept as a finite sum whose
+  // exponential is zero: differences of G stay defined.
+  float gv = 0.f, bv = 0.f;
+  if (l < n) {
+    gv = a.g[(size_t)(row0 + l) * a.H + head];
+    bv = a.beta[(size_t)(row0 + l) * a.H + head];
+  }
+  if (gv < -1e4f) gv = -1e4f;
+  double G = gv;
+#pragma unroll
+  for (int s = 1; s < WAVE; s *= 2) {
+    const double o = __shfl_up(G, s);
+    if (l >= s) G += o;
+  }
+  const double Gc = __shfl(G, DC - 1);
+  float* scal = reinterpret_cast<float*>(out + 2 * DELTA_MAT_BYTES);
+  scal[l] = expf((float)G);
+  scal[DC + l] = expf((float)(Gc - G));
+  scal[2 * DC + l] = bv;
+  Lg[l] = G;
+  lds_fence();
+
+  const auto rk = row_window(static_cast<const S*>(a.K) + kh * D, row0, a.ks, n, D);
+  Frag<T> kf[4][KS];
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+      kf[m][s] = window_frag<T>(rk, ((16 * m + r16) * a.ks + 32 * s + 8 * g) * (int)sizeof(S));
+  double Gi[4];   // G and b of this lane's column in each block
+  float bi[4];
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
+    Gi[m] = Lg[16 * m + r16];
+    bi[m] = __shfl(bv, 16 * m + r16);
+  }
+  auto decay = [&](double x) { return expf((float)x); };
+
+  // N(n, m), n <= m, and for n < m also A(m, n), which is N(n, m) as a left operand
+  f32x4 N[4][4], A[4][4];
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int nn = 0; nn <= m; ++nn) {
+      f32x4 c = zero4();
+#pragma unroll
+      for (int s = 0; s < KS; ++s) mma(c, kf[nn][s], kf[m][s]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int j = 16 * nn + 4 * g + e, i = 16 * m + r16;
+        N[nn][m][e] = j < i ? c[e] * (bi[m] * decay(Gi[m] - Lg[j])) : 0.f;
+      }
+      if (nn == m) {
+        *reinterpret_cast<f32x4*>(Lt + (m * 16 + r16) * LD + 4 * g) = N[m][m];   // A(m,m)[i][j]
+      } else {
+        f32x4 d = zero4();
+#pragma unroll
+        for (int s = 0; s < KS; ++s) mma(d, kf[m][s], kf[nn][s]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 16 * m + 4 * g + e;
+          A[m][nn][e] = d[e] * (__shfl(bv, i) * decay(Lg[i] - Gi[nn]));
+        }
+      }
+    }
+  lds_fence();
+  // T(g,g), lane column r16: t_i = [i == column] - sum_{k<i} A_ik t_k
+  float tc[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float x = i == r16 ? 1.f : 0.f;
+#pragma unroll
+    for (int k = 0; k < i; k += 4) {
+      const f32x4 ar = *reinterpret_cast<const f32x4*>(Lt + (g * 16 + i) * LD + k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (k + e < i) x = __builtin_fmaf(-ar[e], tc[k + e], x);
+    }
+    tc[i] = x;
+  }
+  lds_fence();
+#pragma unroll
+  for (int i = 0; i < 16; ++i) Lt[(g * 16 + i) * LD + r16] = tc[i];
+  lds_fence();
+  f32x4 X[4][4], Xl[4];   // X as results; the diagonal ones also as left operands
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
+    X[m][m] = *reinterpret_cast<const f32x4*>(Lt + (m * 16 + r16) * LD + 4 * g);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) Xl[m][e] = Lt[(m * 16 + 4 * g + e) * LD + r16];
+  }
+#pragma unroll
+  for (int dlt = 1; dlt < 4; ++dlt)
+#pragma unroll
+    for (int nn = 0; nn + dlt < 4; ++nn) {
+      const int m = nn + dlt;
+      f32x4 y = zero4(), x = zero4();
+#pragma unroll
+      for (int k = nn + 1; k <= m; ++k) mm16(y, A[k][nn], X[k][m]);
+      mm16(x, Xl[nn], y);
+      X[nn][m] = -x;
+    }
+  S* to = reinterpret_cast<S*>(out);
+  constexpr size_t LO = DC * DC;
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int nn = 0; nn <= (m | 1); ++nn)   // with the zero blocks that share a k step with the diagonal
+      store_split4(to + (16 * m + r16) * DC + 16 * nn + 4 * g, LO, nn <= m ? X[nn][m] : zero4());
+
+  S* po = reinterpret_cast<S*>(out + DELTA_MAT_BYTES);
+  const auto rq = row_window(static_cast<const S*>(a.Q) + kh * D, row0, a.qs, n, D);
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
+    Frag<T> qf[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+      qf[s] = window_frag<T>(rq, ((16 * m + r16) * a.qs + 32 * s + 8 * g) * (int)sizeof(S));
+#pragma unroll
+    for (int nn = 0; nn <= (m | 1); ++nn) {
+      f32x4 c = zero4();
+      if (nn <= m) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) mma(c, kf[nn][s], qf[s]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int j = 16 * nn + 4 * g + e, i = 16 * m + r16;
+          c[e] = j <= i ? c[e] * decay(Gi[m] - Lg[j]) : 0.f;
+        }
+      }
+      store_split4(po + (16 * m + r16) * DC + 16 * nn + 4 * g, LO, c);
+    }
+  }
+}
+
+// The sweep: one workgroup per sequence, value head and 16 NW columns of the state, a wave
+// per 16; the chunk's K, Q, T, P and scalars pass through LDS, V and O directly.
+template <class T, int D, int NW, bool SAVE>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1))) void k_delta_sweep(DeltaArgs a) {
+  using S = typename Io<T>::type;
+  using KT = Tile16<T, D>;
+  using MT = Pair16<T, DC>;
+  constexpr int KS = D / 32, DT = D / 16;
+  constexpr int ROWS = DC * D * (int)sizeof(T);                  // bytes of a K or Q tile
+  constexpr int MAT = DC * DC * (int)sizeof(T);                  // of one term of T or P
+  constexpr int BUF = 2 * ROWS + DELTA_PREP_BYTES;
+  constexpr int BUFS = 2 * BUF <= 160 * 1024 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) char lds[BUFS * BUF];
+  const int l = threadIdx.x % WAVE, r16 = l % 16, g = l / 16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int bh = blockIdx.x % (a.B * a.H), b = bh / a.H, head = bh % a.H, kh = head / (a.H / a.Hk);
+  const int col = (blockIdx.x / (a.B * a.H) * NW + w) * 16 + r16;   // this lane's column of the state
+  const SeqRange sq = seq_range(a.off, b, a.T);
+  const int nchunks = (sq.n + DC - 1) / DC, slot0 = sq.row0 / DC + b;
+
+  f32x4 st[DT];
+  const size_t sbase = ((size_t)bh * D) * a.dv + col;
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) st[i][e] = a.state0 ? a.state0[sbase + (size_t)(16 * i + 4 * g + e) * a.dv] : 0.f;
+
+  auto stage = [&](int c, int buf) {
+    const char* L = lds + buf * BUF;
+    const int row0 = sq.row0 + c * DC, n = min(DC, sq.n - c * DC);
+    stage_tile<T, D, DC, NW>(L, row_words(static_cast<const S*>(a.K) + kh * D, row0, a.ks, n, D),
+                             a.ks * (int)sizeof(S), w);
+    stage_tile<T, D, DC, NW>(L + ROWS, row_words(static_cast<const S*>(a.Q) + kh * D, row0, a.qs, n, D),
+                             a.qs * (int)sizeof(S), w);
+    const char* p = a.prep + ((size_t)(slot0 + c) * a.H + head) * DELTA_PREP_BYTES;
+    constexpr int TERMS = DELTA_MAT_BYTES / MAT;
+#pragma unroll
+    for (int i = 0; i < 2 * TERMS; ++i)
+      stage_tile<T, DC, DC, NW>(L + 2 * ROWS + i * MAT, row_words(reinterpret_cast<const S*>(p + i * MAT), 0, DC, DC, DC),
+                                DC * (int)sizeof(S), w);
+    stage_linear<1, NW>(L + 2 * ROWS + 2 * DELTA_MAT_BYTES, p + 2 * DELTA_MAT_BYTES, w);
+  };
+  S v[4][4];   // this lane's column of the chunk's V
+  auto load_v = [&](int c) {
+    const auto rs = row_window(static_cast<const S*>(a.V) + (size_t)head * a.dv, sq.row0 + c * DC, a.vs,
+                               min(DC, sq.n - c * DC), a.dv);
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[m][e] = load1(rs, ((16 * m + 4 * g + e) * a.vs + col) * (int)sizeof(S), S());
+  };
+  if (nchunks > 0) {
+    if (BUFS == 2) stage(0, 0);
+    load_v(0);
+  }
+  for (int c = 0; c < nchunks; ++c) {
+    if (BUFS == 1) {
+      sync_tiles();
+      stage(c, 0);
+    }
+    sync_tiles();   // chunk c has arrived; chunk c - 1 is no longer read
+    f32x4 vf[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) vf[m][e] = io_to_float(v[m][e]);
+    const char* LK = lds + (BUFS == 2 ? (c & 1) * BUF : 0);
+    const char* LQ = LK + ROWS;
+    const char* LT = LQ + ROWS;
+    const char* LP = LT + DELTA_MAT_BYTES;
+    const float* sc = reinterpret_cast<const float*>(LP + DELTA_MAT_BYTES);
+    if (c + 1 < nchunks) {
+      if (BUFS == 2) stage(c + 1, (c + 1) & 1);
+      load_v(c + 1);
+    }
+    const size_t blk = (size_t)(slot0 + c) * a.H + head;
+    if (SAVE) {
+      S* so = static_cast<S*>(a.st) + (blk * a.dv + col) * D;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) store_io4(so + 16 * i + 4 * g, st[i]);
+    }
+    // K S and Q S
+    f32x4 ks[4], qs[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) ks[m] = qs[m] = zero4();
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const Split<T> sb = split<T>(st[2 * s], st[2 * s + 1]);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        mma_xs(ks[m], KT::row(LK, 16 * m + r16, 32 * s + 4 * g, 32 * s + 16 + 4 * g), sb);
+        mma_xs(qs[m], KT::row(LQ, 16 * m + r16, 32 * s + 4 * g, 32 * s + 16 + 4 * g), sb);
+      }
+    }
+    // U = T b (V - e^G K S)
+    f32x4 eg[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      eg[m] = *reinterpret_cast<const f32x4*>(sc + 16 * m + 4 * g);
+      const f32x4 be = *reinterpret_cast<const f32x4*>(sc + 2 * DC + 16 * m + 4 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ks[m][e] = be[e] * (vf[m][e] - eg[m][e] * ks[m][e]);
+    }
+    f32x4 u[4];
+    {
+      const Split<T> r0 = split<T>(ks[0], ks[1]), r1 = split<T>(ks[2], ks[3]);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        u[m] = zero4();
+        mma_ss(u[m], MT::row(LT, MAT, 16 * m + r16, 4 * g, 16 + 4 * g), r0);
+        if (m >= 2) mma_ss(u[m], MT::row(LT, MAT, 16 * m + r16, 32 + 4 * g, 48 + 4 * g), r1);
+      }
+    }
+    if (SAVE) {
+      S* uo = static_cast<S*>(a.ut) + blk * (size_t)(DELTA_MAT_BYTES / MAT * DC) * a.dv + (size_t)col * DC;
+#pragma unroll
+      for (int m = 0; m < 4; ++m) store_split4(uo + 16 * m + 4 * g, (size_t)DC * a.dv, u[m]);
+    }
+    // S <- e^{G_63} S + K^T (w U)
+    {
+      f32x4 wu[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) wu[m] = u[m] * *reinterpret_cast<const f32x4*>(sc + DC + 16 * m + 4 * g);
+      const Split<T> w0 = split<T>(wu[0], wu[1]), w1 = split<T>(wu[2], wu[3]);
+      const float last = sc[DC - 1];
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        st[i] *= last;
+        mma_xs(st[i], KT::col(LK, 4 * g, 16 + 4 * g, 16 * i), w0);
+        mma_xs(st[i], KT::col(LK, 32 + 4 * g, 48 + 4 * g, 16 * i), w1);
+      }
+    }
+    // O = scale (e^G Q S + P U)
+    {
+      const Split<T> u0 = split<T>(u[0], u[1]), u1 = split<T>(u[2], u[3]);
+      const auto ro = row_window(static_cast<S*>(a.O) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
+                                 min(DC, sq.n - c * DC), a.dv);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        f32x4 o = qs[m] * eg[m];
+        mma_ss(o, MT::row(LP, MAT, 16 * m + r16, 4 * g, 16 + 4 * g), u0);
+        if (m >= 2) mma_ss(o, MT::row(LP, MAT, 16 * m + r16, 32 + 4 * g, 48 + 4 * g), u1);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          store1(ro, ((16 * m + 4 * g + e) * a.H * a.dv + col) * (int)sizeof(S), float_to_io<S>(o[e] * a.scale));
+      }
+    }
+  }
+  if (a.state) {
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a.state[sbase + (size_t)(16 * i + 4 * g + e) * a.dv] = st[i][e];
+  }
+}
+
+// One token of every sequence and value head against its state, fp32 throughout.  A
+// workgroup takes CW columns of one state: each thread four columns of ROWS rows, held in
+// registers between the read and the write.  One pass suffices: with x = S^T k and
+// y = S^T q of the old state, u = b (v - a x), S' = a S + k u^T and o = a y + (k.q) u.
+template <class T, int D, int CW>
+__global__ __launch_bounds__(256) void k_delta_step(DeltaArgs a) {
+  using S = typename Io<T>::type;
+  constexpr int C4 = CW / 4, RG = 256 / C4, ROWS = D / RG;
+  __shared__ float lk[D], lq[D];
+  __shared__ __attribute__((aligned(16))) float px[RG][CW + 4], py[RG][CW + 4];
+  const int t = threadIdx.x, c = t % C4, rg = t / C4;
+  const int parts = a.dv / CW, bh = blockIdx.x / parts, c0 = blockIdx.x % parts * CW;
+  const int b = bh / a.H, head = bh % a.H, kh = head / (a.H / a.Hk);
+  float* sp = a.state + ((size_t)bh * D + rg * ROWS) * a.dv + c0 + 4 * c;
+  f32x4 s[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) s[i] = *reinterpret_cast<const f32x4*>(sp + (size_t)i * a.dv);
+  if (t < D) {
+    lk[t] = io_to_float(static_cast<const S*>(a.K)[(size_t)b * a.ks + kh * D + t]);
+    lq[t] = io_to_float(static_cast<const S*>(a.Q)[(size_t)b * a.qs + kh * D + t]);
+  }
+  const float dec = expf(a.g[bh]), be = a.beta[bh];
+  f32x4 vv;
+  {
+    const S* vp = static_cast<const S*>(a.V) + (size_t)b * a.vs + (size_t)head * a.dv + c0 + 4 * c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) vv[e] = io_to_float(vp[e]);
+  }
+  __syncthreads();
+  f32x4 x = zero4(), y = zero4();
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    s[i] *= dec;
+    x += s[i] * lk[rg * ROWS + i];
+    y += s[i] * lq[rg * ROWS + i];
+  }
+  *reinterpret_cast<f32x4*>(&px[rg][4 * c]) = x;
+  *reinterpret_cast<f32x4*>(&py[rg][4 * c]) = y;
+  float kq = 0.f;   // the same sum in every wave
+  for (int i = t % WAVE; i < D; i += WAVE) kq = __builtin_fmaf(lk[i], lq[i], kq);
+  kq = group_sum(lane_sum<16>(kq));
+  __syncthreads();
+  x = zero4();
+  y = zero4();
+#pragma unroll
+  for (int i = 0; i < RG; ++i) {
+    x += *reinterpret_cast<const f32x4*>(&px[i][4 * c]);
+    y += *reinterpret_cast<const f32x4*>(&py[i][4 * c]);
+  }
+  const f32x4 u = (vv - x) * be;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) *reinterpret_cast<f32x4*>(sp + (size_t)i * a.dv) = s[i] + u * lk[rg * ROWS + i];
+  if (rg == 0) store_io4(static_cast<S*>(a.O) + (size_t)bh * a.dv + c0 + 4 * c, (y + u * kq) * a.scale);
+}
+
+namespace {
+template <class T, int D, int NW>
+void run_sweep(const DeltaArgs& a, hipStream_t st) {
+  const int wgs = a.B * a.H * (a.dv / (16 * NW));
+  if (a.st)
+    k_delta_sweep<T, D, NW, true><<<wgs, NW * 64, 0, st>>>(a);
+  else
+    k_delta_sweep<T, D, NW, false><<<wgs, NW * 64, 0, st>>>(a);
+}
+template <class T, int D>
+hipError_t run_fwd(const DeltaArgs& a, hipStream_t st) {
+  timing_mark(FLEX_KERNEL_DELTA_FWD, st, true);
+  if (a.T > 0) {
+    const int64_t waves = (int64_t)seq_slots(a.T, a.B, DC) * a.H;
+    k_delta_prep<T, D><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a);
+  }
+  if (a.waves == 4)
+    run_sweep<T, D, 4>(a, st);
+  else
+    run_sweep<T, D, 2>(a, st);
+  timing_mark(FLEX_KERNEL_DELTA_FWD, st, false);
+  return hipGetLastError();
+}
+template <class T, int D>
+hipError_t run_step(const DeltaArgs& a, hipStream_t st) {
+  timing_mark(FLEX_KERNEL_DELTA_STEP, st, true);
+  if (a.dv == 64)
+    k_delta_step<T, D, 64><<<a.B * a.H, 256, 0, st>>>(a);
+  else
+    k_delta_step<T, D, 128><<<a.B * a.H, 256, 0, st>>>(a);
+  timing_mark(FLEX_KERNEL_DELTA_STEP, st, false);
+  return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_delta_fwd(const DeltaArgs& a, bool bf16, hipStream_t st) {
+  if (bf16) return a.d == 64 ? run_fwd<__bf16, 64>(a, st) : run_fwd<__bf16, 128>(a, st);
+  return a.d == 64 ? run_fwd<float, 64>(a, st) : run_fwd<float, 128>(a, st);
+}
+hipError_t launch_delta_step(const DeltaArgs& a, bool bf16, hipStream_t st) {
+  if (bf16) return a.d == 64 ? run_step<__bf16, 64>(a, st) : run_step<__bf16, 128>(a, st);
+  return a.d == 64 ? run_step<float, 64>(a, st) : run_step<float, 128>(a, st);
+}
+
+}  // namespace flex

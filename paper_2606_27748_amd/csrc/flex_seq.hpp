@@ -237,7 +237,11 @@ __device__ __forceinline__ void store_io4(u16* p, f32x4 v) {
 __device__ __forceinline__ void store_io4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
 
 // This wave's loads to LDS have arrived, and its reads of LDS are done.
-__device__ __forceinline__ void wait_lds_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void wait_lds_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0); the compiler counts its own loads as arrived, too
+  asm volatile("" ::: "memory");
+}
 // This wave's loads to registers have arrived.  Before a loop that stages tiles: the
 // compiler would else wait for them at their first use, in every iteration, and so
 // for the tile that is on its way.

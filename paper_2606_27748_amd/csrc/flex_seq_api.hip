@@ -78,6 +78,58 @@ AttnArgs attn_args(const flex_attn_desc* d, const void* Q, const void* K, const 
   return a;
 }
 
+int32_t check_delta(const flex_delta_desc* d, bool step) {
+  if (!d) return FLEX_ERR_INVALID_ARG;
+  if (d->B <= 0 || d->T < 0 || d->Hk <= 0 || d->H <= 0 || d->d <= 0 || d->dv <= 0) return FLEX_ERR_INVALID_ARG;
+  if (d->H % d->Hk != 0) return FLEX_ERR_INVALID_ARG;
+  if (d->io_dtype != FLEX_F32 && d->io_dtype != FLEX_BF16) return FLEX_ERR_INVALID_ARG;
+  if (!(d->scale > 0.0f) || !isfinite(d->scale)) return FLEX_ERR_INVALID_ARG;
+  if ((d->d != 64 && d->d != 128) || (d->dv != 64 && d->dv != 128)) return FLEX_ERR_UNSUPPORTED;
+  const int64_t k = (int64_t)d->Hk * d->d, v = (int64_t)d->H * d->dv;
+  if (k > kMaxStride || v > kMaxStride) return FLEX_ERR_UNSUPPORTED;
+  const int e = esize(d->io_dtype);
+  if (!stride_ok(d->q_stride, k, e) || !stride_ok(d->k_stride, k, e) || !stride_ok(d->v_stride, v, e))
+    return FLEX_ERR_INVALID_ARG;
+  // workgroups of a launch fit 31 bits
+  const int64_t slots = step ? 0 : (int64_t)d->T / DELTA_CHUNK + d->B;
+  if (slots * d->H >= (1LL << 31) || (int64_t)d->B * d->H * 8 >= (1LL << 31)) return FLEX_ERR_INVALID_ARG;
+  return FLEX_OK;
+}
+
+// Chunk slots times value heads, and the bytes of what is kept per such block.
+size_t delta_blocks(const flex_delta_desc* d) { return ((size_t)d->T / DELTA_CHUNK + d->B) * d->H; }
+size_t delta_state_bytes(const flex_delta_desc* d) { return (size_t)d->d * d->dv * esize(d->io_dtype); }
+size_t delta_rows_bytes(const flex_delta_desc* d) { return (size_t)DELTA_CHUNK * d->dv * 4; }   // hi and lo, or fp32
+size_t delta_prep_bytes(const flex_delta_desc* d) { return delta_blocks(d) * DELTA_PREP_BYTES; }
+size_t delta_saved_bytes(const flex_delta_desc* d) {
+  return delta_blocks(d) * (DELTA_PREP_BYTES + delta_state_bytes(d) + delta_rows_bytes(d));
+}
+size_t delta_ws_bytes(const flex_delta_desc* d, int32_t pass) {
+  if (pass == FLEX_PASS_FWD) return delta_prep_bytes(d);
+  return delta_blocks(d) * (delta_state_bytes(d) + delta_rows_bytes(d));
+}
+
+DeltaArgs delta_args(const flex_delta_desc* d, const void* Q, const void* K, const void* V, const float* g,
+                     const float* beta, const int32_t* off) {
+  DeltaArgs a;
+  memset(&a, 0, sizeof(a));
+  a.Q = Q; a.K = K; a.V = V; a.g = g; a.beta = beta; a.off = off;
+  a.B = d->B; a.T = d->T; a.Hk = d->Hk; a.H = d->H; a.d = d->d; a.dv = d->dv;
+  a.qs = stride_of(d->q_stride, (int64_t)d->Hk * d->d);
+  a.ks = stride_of(d->k_stride, (int64_t)d->Hk * d->d);
+  a.vs = stride_of(d->v_stride, (int64_t)d->H * d->dv);
+  a.scale = d->scale;
+  // the sweep's waves per workgroup: more workgroups where they would not fill the CUs
+  a.waves = (int64_t)d->B * d->H * (d->dv / 64) >= 256 ? 4 : 2;
+  return a;
+}
+void delta_saved(DeltaArgs& a, const flex_delta_desc* d, void* saved) {
+  char* p = static_cast<char*>(saved);
+  a.prep = p;
+  a.st = p + delta_prep_bytes(d);
+  a.ut = static_cast<char*>(a.st) + delta_blocks(d) * delta_state_bytes(d);
+}
+
 }  // namespace
 
 extern "C" {
@@ -136,6 +188,61 @@ int32_t flex_attn_bwd(const flex_attn_desc* desc, const void* Q, const void* K, 
   a.dQ = dQ; a.dK = dK; a.dV = dV;
   a.delta = static_cast<float*>(ws);
   const hipError_t e = launch_attn_bwd(a, desc->io_dtype == FLEX_BF16, desc->d, (hipStream_t)stream);
+  return e == hipSuccess ? FLEX_OK : FLEX_ERR_HIP;
+}
+
+int32_t flex_delta_workspace_size(const flex_delta_desc* desc, int32_t pass, size_t* bytes) {
+  if (!bytes) return FLEX_ERR_INVALID_ARG;
+  *bytes = 0;
+  if (pass != FLEX_PASS_FWD && pass != FLEX_PASS_BWD) return FLEX_ERR_INVALID_ARG;
+  const int32_t st = check_delta(desc, false);
+  if (st != FLEX_OK) return st;
+  *bytes = delta_ws_bytes(desc, pass);
+  return FLEX_OK;
+}
+
+int32_t flex_delta_saved_size(const flex_delta_desc* desc, size_t* bytes) {
+  if (!bytes) return FLEX_ERR_INVALID_ARG;
+  *bytes = 0;
+  const int32_t st = check_delta(desc, false);
+  if (st != FLEX_OK) return st;
+  *bytes = delta_saved_bytes(desc);
+  return FLEX_OK;
+}
+
+int32_t flex_delta_fwd(const flex_delta_desc* desc, const void* Q, const void* K, const void* V, const float* g,
+                       const float* beta, const int32_t* off, const float* state0, void* O, float* state, void* saved,
+                       size_t saved_bytes, void* ws, size_t ws_bytes, void* stream) {
+  const int32_t st = check_delta(desc, false);
+  if (st != FLEX_OK) return st;
+  if (!off) return FLEX_ERR_INVALID_ARG;
+  const void* rows[] = {Q, K, V, g, beta, O};
+  for (const void* p : rows)
+    if (!tensor_ok(p, desc->T)) return FLEX_ERR_INVALID_ARG;
+  if ((state0 && !aligned16(state0)) || (state && !aligned16(state))) return FLEX_ERR_INVALID_ARG;
+  if (saved ? saved_bytes < delta_saved_bytes(desc) || !aligned16(saved)
+            : !ws || ws_bytes < delta_ws_bytes(desc, FLEX_PASS_FWD) || !aligned16(ws))
+    return FLEX_ERR_WORKSPACE;
+  DeltaArgs a = delta_args(desc, Q, K, V, g, beta, off);
+  a.state0 = state0; a.state = state; a.O = O;
+  if (saved)
+    delta_saved(a, desc, saved);
+  else
+    a.prep = static_cast<char*>(ws);
+  const hipError_t e = launch_delta_fwd(a, desc->io_dtype == FLEX_BF16, (hipStream_t)stream);
+  return e == hipSuccess ? FLEX_OK : FLEX_ERR_HIP;
+}
+
+int32_t flex_delta_step(const flex_delta_desc* desc, const void* q, const void* k, const void* v, const float* g,
+                        const float* beta, float* state, void* o, void* stream) {
+  const int32_t st = check_delta(desc, true);
+  if (st != FLEX_OK) return st;
+  const void* rows[] = {q, k, v, g, beta, state, o};
+  for (const void* p : rows)
+    if (!p || !aligned16(p)) return FLEX_ERR_INVALID_ARG;
+  DeltaArgs a = delta_args(desc, q, k, v, g, beta, nullptr);
+  a.state = state; a.O = o;
+  const hipError_t e = launch_delta_step(a, desc->io_dtype == FLEX_BF16, (hipStream_t)stream);
   return e == hipSuccess ? FLEX_OK : FLEX_ERR_HIP;
 }
 

@@ -39,4 +39,46 @@ struct AttnArgs {
 hipError_t launch_attn_fwd(const AttnArgs& a, bool bf16, int d, hipStream_t st);
 hipError_t launch_attn_bwd(const AttnArgs& a, bool bf16, int d, hipStream_t st);
 
+// Gated delta rule.  What the chunks of 64 tokens need beside the rows is kept per chunk
+// slot and value head (block slot * H + head):
+//   prep   T as hi and lo bf16 [64][64] (fp32: one [64][64]), P the same, then
+//          e^G [64], w [64], b [64] (fp32) in 1 KB
+//   st     the state at the chunk's start, transposed [dv][d], io type   (training)
+//   ut     U transposed [dv][64], hi and lo (fp32: one)                  (training)
+constexpr int DELTA_CHUNK = 64;
+constexpr int DELTA_MAT_BYTES = 64 * 64 * 4;   // T or P: hi and lo, or fp32
+constexpr int DELTA_PREP_BYTES = 2 * DELTA_MAT_BYTES + 1024;
+
+struct DeltaArgs {
+  const void* Q;
+  const void* K;
+  const void* V;
+  const float* g;
+  const float* beta;
+  const int32_t* off;
+  const float* state0;   // NULL: zero
+  float* state;          // NULL: not wanted
+  void* O;
+  int B, T, Hk, H, d, dv;
+  int qs, ks, vs;
+  float scale;
+  int waves;             // waves (of 16 state columns) per workgroup of the sweeps
+  char* prep;
+  void* st;              // NULL: not kept
+  void* ut;
+  // backward
+  const void* dO;
+  void* dst;             // gradient of the state at the chunk's end, transposed [dv][d], io type
+  void* drt;             // gradient of T^-1 U = b (V - e^G K S), transposed [dv][64], hi and lo
+  void* dQ;
+  void* dK;
+  void* dV;
+  void* dg;
+  void* dbeta;
+};
+
+hipError_t launch_delta_fwd(const DeltaArgs& a, bool bf16, hipStream_t st);
+hipError_t launch_delta_bwd(const DeltaArgs& a, bool bf16, hipStream_t st);
+hipError_t launch_delta_step(const DeltaArgs& a, bool bf16, hipStream_t st);
+
 }  // namespace flex

@@ -90,3 +90,35 @@ def check(name, got, ref, mag, terms, dtype):
     bound = terms * u * mag + u * ref.abs() + 1e-30
     bad = ~((got - ref).abs() <= bound)
     assert not bad.any(), (name, int(bad.sum()), float(((got - ref).abs() / bound).nan_to_num(1e30).max()))
+
+
+def delta_oracle(Q, K, V, g, beta, off, state0=None, scale=None, dO=None):
+    """O, final states and, with dO, the gradients in float64: the recurrence token by token."""
+    names = ("Q", "K", "V", "g", "beta")
+    leaf = {n: x.double().clone().requires_grad_(dO is not None) for n, x in zip(names, (Q, K, V, g, beta))}
+    T, Hk, d = Q.shape
+    H, dv, B = V.shape[1], V.shape[2], len(off) - 1
+    scale = d ** -0.5 if scale is None else scale
+    head = torch.arange(H) // (H // Hk)
+    q, k = leaf["Q"][:, head], leaf["K"][:, head]
+    O, states = torch.zeros(T, H, dv, dtype=torch.float64), []
+    rows = [None] * T
+    for b in range(B):
+        S = torch.zeros(H, d, dv, dtype=torch.float64) if state0 is None else state0[b].double()
+        for t in range(int(off[b]), int(off[b + 1])):
+            S = S * torch.exp(leaf["g"][t])[:, None, None]
+            u = leaf["beta"][t, :, None] * (leaf["V"][t] - (S * k[t, :, :, None]).sum(1))
+            S = S + k[t, :, :, None] * u[:, None, :]
+            rows[t] = scale * (S * q[t, :, :, None]).sum(1)
+        states.append(S.detach())
+    kept = [t for t in range(T) if rows[t] is not None]
+    out = {"state": torch.stack(states)}
+    if kept:
+        y = torch.stack([rows[t] for t in kept])
+        O[kept] = y.detach()
+        if dO is not None:
+            y.backward(dO.double()[kept])
+    out["O"] = O
+    if dO is not None:
+        out.update({"d" + n: torch.zeros_like(x) if x.grad is None else x.grad for n, x in leaf.items()})
+    return out
