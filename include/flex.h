@@ -374,6 +374,20 @@ int32_t flex_delta_fwd(const flex_delta_desc* desc, const void* Q, const void* K
                        void* O, float* state, void* saved, size_t saved_bytes,
                        void* ws, size_t ws_bytes, void* stream);
 
+/* Backward of flex_delta_fwd from states of zero (state0 = NULL) and without a gradient of
+ * the final states.
+ *   saved             written by the forward of the same descriptor and inputs
+ *   dO [T,H,dv]       io_dtype
+ *   dQ, dK [T,Hk,d], dV [T,H,dv], dg, dbeta [T,H]   io_dtype outputs: the rows of
+ *                     the sequences are overwritten
+ * With FLEX_BF16 the gradients of states and rows are carried in fp32 (in products as two
+ * bf16 terms); each product that a result sums has one operand rounded to bf16. */
+int32_t flex_delta_bwd(const flex_delta_desc* desc, const void* Q, const void* K, const void* V,
+                       const float* g, const float* beta, const int32_t* off,
+                       const void* saved, size_t saved_bytes, const void* dO,
+                       void* dQ, void* dK, void* dV, void* dg, void* dbeta,
+                       void* ws, size_t ws_bytes, void* stream);
+
 /* Single-token step: one token of every sequence (rows 0 .. B-1, T and the row
  * offsets are not used), fp32 throughout but for the io rows.
  *   q, k [B,Hk,d], v [B,H,dv], g, beta [B,H], state [B,H,d,dv] fp32 updated in

@@ -8,7 +8,7 @@ from ._lib import (FlexError, flex_desc, make_desc, workspace_size, flex_feature
                    flex_awd_loss, decode_state,
                    flex_attn_desc, make_attn_desc, attn_workspace_size, flex_attn_fwd, flex_attn_bwd,
                    flex_delta_desc, make_delta_desc, delta_workspace_size, delta_saved_size, flex_delta_fwd,
-                   flex_delta_step,
+                   flex_delta_bwd, flex_delta_step,
                    decode_state_views, load, status_string,
                    FLEX_OK, FLEX_ERR_INVALID_ARG, FLEX_ERR_UNSUPPORTED, FLEX_ERR_WORKSPACE,
                    FLEX_ERR_HIP, FLEX_PASS_FEATURE_MAP, FLEX_PASS_FWD, FLEX_PASS_BWD, FLEX_PASS_AWD,

@@ -22,7 +22,8 @@ EXPORTS = ("flex_abi_version", "flex_status_string", "flex_workspace_size",
            "flex_linattn_bwd",
            "flex_decode_step",
            "flex_awd_loss", "flex_attn_workspace_size", "flex_attn_fwd", "flex_attn_bwd",
-           "flex_delta_workspace_size", "flex_delta_saved_size", "flex_delta_fwd", "flex_delta_step",
+           "flex_delta_workspace_size", "flex_delta_saved_size", "flex_delta_fwd", "flex_delta_bwd",
+           "flex_delta_step",
            "flex_timing_enable", "flex_timing_read")
 KERNELS = {"none": 0, "fwd_state": 1, "fwd_sweep": 2, "scan": 3, "bwd_prepass": 4,
            "bwd_dq": 5, "bwd_dkv": 6, "bwd_reduce": 7, "feature_map": 8, "decode_step": 9,
@@ -110,6 +111,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.flex_delta_saved_size.argtypes = [G, ctypes.POINTER(S)]
     lib.flex_delta_fwd.restype = I
     lib.flex_delta_fwd.argtypes = [G] + [P] * 10 + [S, P, S, P]
+    lib.flex_delta_bwd.restype = I
+    lib.flex_delta_bwd.argtypes = [G] + [P] * 7 + [S] + [P] * 7 + [S, P]
     lib.flex_delta_step.restype = I
     lib.flex_delta_step.argtypes = [G] + [P] * 8
     lib.flex_timing_enable.restype = I
@@ -465,6 +468,25 @@ def flex_delta_fwd(desc: flex_delta_desc, Q, K, V, g, beta, off, state0=None, O=
     _run("flex_delta_fwd", dev, desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(g), _ptr(beta), _ptr(off), _ptr(state0), _ptr(O),
          _ptr(state), *keep, *w)
     return O, state
+
+
+def flex_delta_bwd(desc: flex_delta_desc, Q, K, V, g, beta, off, dO, saved, dQ=None, dK=None, dV=None, dg=None,
+                   dbeta=None, ws=None):
+    """Backward of flex_delta_fwd (state0 None) from what it kept in saved.  Returns dict(dQ,
+    dK, dV, dg, dbeta) in the io dtype; rows of no sequence are not written."""
+    import torch
+    io = _io(desc)
+    shapes = {"dQ": (desc.T, desc.Hk, desc.d), "dK": (desc.T, desc.Hk, desc.d), "dV": (desc.T, desc.H, desc.dv),
+              "dg": (desc.T, desc.H), "dbeta": (desc.T, desc.H)}
+    out = {"dQ": dQ, "dK": dK, "dV": dV, "dg": dg, "dbeta": dbeta}
+    _, dev = _delta_inputs("flex_delta_bwd", desc, desc.T, Q, K, V, g, beta, off=(off, (desc.B + 1,), torch.int32, 0),
+                           dO=(dO, shapes["dV"], io, 0), **{n: (out[n], shapes[n], io, 0) for n in out})
+    out = {n: torch.empty(shapes[n], dtype=io, device=dev) if t is None else t for n, t in out.items()}
+    keep = _saved("flex_delta_bwd", desc, saved)
+    w = _seq_workspace(delta_workspace_size(desc, FLEX_PASS_BWD), ws, dev)
+    _run("flex_delta_bwd", dev, desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(g), _ptr(beta), _ptr(off), *keep, _ptr(dO),
+         *(_ptr(out[n]) for n in ("dQ", "dK", "dV", "dg", "dbeta")), *w)
+    return out
 
 
 def flex_delta_step(desc: flex_delta_desc, q, k, v, g, beta, state, o=None):

@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libflexattn.so")
 SOURCES = ["flex_api.hip", "flex_fwd.hip", "flex_bwd.hip", "flex_bwd_dq.hip", "flex_decode.hip", "flex_awd.hip",
-           "flex_seq_api.hip", "flex_attn_fwd.hip", "flex_attn_bwd.hip", "flex_delta_fwd.hip"]
+           "flex_seq_api.hip", "flex_attn_fwd.hip", "flex_attn_bwd.hip", "flex_delta_fwd.hip", "flex_delta_bwd.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -191,4 +191,52 @@ __device__ __forceinline__ void stage_linear(const char* L, const void* src, int
   }
 }
 
+// What a chunk's sweep step reads, through LDS: K and Q tiles, T and P (their terms as tiles),
+// e^G, w and b.
+template <class T, int D>
+struct ChunkLds {
+  static constexpr int ROWS = DC * D * (int)sizeof(T);     // bytes of a K or Q tile
+  static constexpr int MAT = DC * DC * (int)sizeof(T);     // of one term of T or P
+  static constexpr int BYTES = 2 * ROWS + 2 * DELTA_MAT_BYTES + 1024;
+  static constexpr int BUFS = 2 * BYTES <= 160 * 1024 ? 2 : 1;
+  const char* L;
+  __device__ __forceinline__ const char* k() const { return L; }
+  __device__ __forceinline__ const char* q() const { return L + ROWS; }
+  __device__ __forceinline__ const char* t() const { return L + 2 * ROWS; }
+  __device__ __forceinline__ const char* p() const { return L + 2 * ROWS + DELTA_MAT_BYTES; }
+  // rows 16 m + 4 g .. + 3 of e^G (0), w (1), b (2)
+  __device__ __forceinline__ f32x4 scal(int which, int m, int g) const {
+    return *reinterpret_cast<const f32x4*>(L + 2 * ROWS + 2 * DELTA_MAT_BYTES + (which * DC + 16 * m + 4 * g) * 4);
+  }
+  // exp of the chunk's whole decay
+  __device__ __forceinline__ float last() const {
+    return *reinterpret_cast<const float*>(L + 2 * ROWS + 2 * DELTA_MAT_BYTES + (DC - 1) * 4);
+  }
+  template <int NW>
+  __device__ __forceinline__ void stage(const DeltaArgs& a, int row0, int n, int kh, size_t blk, int w) const {
+    using S = typename Io<T>::type;
+    stage_tile<T, D, DC, NW>(k(), row_words(static_cast<const S*>(a.K) + kh * D, row0, a.ks, n, D),
+                             a.ks * (int)sizeof(S), w);
+    stage_tile<T, D, DC, NW>(q(), row_words(static_cast<const S*>(a.Q) + kh * D, row0, a.qs, n, D),
+                             a.qs * (int)sizeof(S), w);
+    const char* p = a.prep + blk * DELTA_PREP_BYTES;
+#pragma unroll
+    for (int i = 0; i < 2 * DELTA_MAT_BYTES / MAT; ++i)
+      stage_tile<T, DC, DC, NW>(t() + i * MAT, row_words(reinterpret_cast<const S*>(p + i * MAT), 0, DC, DC, DC),
+                                DC * (int)sizeof(S), w);
+    stage_linear<1, NW>(t() + 2 * DELTA_MAT_BYTES, p + 2 * DELTA_MAT_BYTES, w);
+  }
+};
+
+// A lane's column `col` of a chunk's rows (rows 16 m + 4 g + e), rows behind the sequence as zeros.
+template <class S>
+__device__ __forceinline__ void load_column(S (&v)[4][4], const S* base, int row0, int stride, int n, int width, int col) {
+  const int g = threadIdx.x % WAVE / 16;
+  const auto rs = row_window(base, row0, stride, n, width);
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[m][e] = load1(rs, ((16 * m + 4 * g + e) * stride + col) * (int)sizeof(S), S());
+}
+
 }  // namespace flex

@@ -1,0 +1,399 @@
+// Gated delta rule, backward.  With dO' = scale dO, dS the gradient of the state at a chunk's
+// end, and the matrices of flex_delta.hpp:
+//   dU = P^T dO' + w K dS         dR = T^T dU           (R = b (V - e^G K S), U = T R)
+//   dS <- e^{G_63} dS + Q^T (e^G dO') - K^T (b e^G dR)                (the chunk's start)
+// runs backwards over the chunks (k_delta_rsweep, the same wave per 16 columns as the forward's
+// sweep), which also gives dV = b dR.  The rest is independent per chunk (k_delta_grad), from
+// the states S, dS and the rows U, dR that the sweeps leave:
+//   dP = low(dO' U^T), dA = -low(dR U^T), M = b dA D
+//   dQ = e^G dO' S^T + (dP D) K
+//   dK = (dP D)^T Q + (M + M^T) K - b F + w U dS^T,     F = e^G dR S^T
+//   dbeta_i = dR_i.V_i - k_i.F_i + sum_j dA_ij D_ij k_i.k_j
+//   dG_i = q_i.(e^G dO' S^T)_i - b_i k_i.F_i - Z_i + sum_j (X_ij - X_ji),  dG_63 += sum_i Z_i + e^{G_63} <S, dS>
+//          with X = dP P + dA A (elementwise), Z_i = k_i.(w U dS^T)_i;  dg_t = sum_{i>=t} dG_i
+// X enters as a row sum and as a column sum of the same fp32 numbers, so that pairs on one
+// side of t cancel in dg_t exactly.
+#include "flex_delta.hpp"
+#include "../../include/flex.h"
+
+namespace flex {
+
+template <class T, int D, int NW>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1))) void k_delta_rsweep(DeltaArgs a) {
+  using S = typename Io<T>::type;
+  using KT = Tile16<T, D>;
+  using MT = Pair16<T, DC>;
+  using CL = ChunkLds<T, D>;
+  constexpr int KS = D / 32, DT = D / 16, MAT = CL::MAT;
+  __shared__ __attribute__((aligned(16))) char lds[CL::BUFS * CL::BYTES];
+  const int l = threadIdx.x % WAVE, r16 = l % 16, g = l / 16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int bh = blockIdx.x % (a.B * a.H), b = bh / a.H, head = bh % a.H, kh = head / (a.H / a.Hk);
+  const int col = (blockIdx.x / (a.B * a.H) * NW + w) * 16 + r16;
+  const SeqRange sq = seq_range(a.off, b, a.T);
+  const int nchunks = (sq.n + DC - 1) / DC, slot0 = sq.row0 / DC + b;
+
+  f32x4 st[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i) st[i] = zero4();
+  auto stage = [&](int c, int buf) {
+    CL{lds + buf * CL::BYTES}.template stage<NW>(a, sq.row0 + c * DC, min(DC, sq.n - c * DC), kh,
+                                                 (size_t)(slot0 + c) * a.H + head, w);
+  };
+  S v[4][4];   // this lane's column of the chunk's dO
+  auto load_g = [&](int c) {
+    load_column(v, static_cast<const S*>(a.dO) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
+                min(DC, sq.n - c * DC), a.dv, col);
+  };
+  if (nchunks > 0) {
+    if (CL::BUFS == 2) stage(nchunks - 1, (nchunks - 1) & 1);
+    load_g(nchunks - 1);
+  }
+  for (int c = nchunks - 1; c >= 0; --c) {
+    if (CL::BUFS == 1) {
+      sync_tiles();
+      stage(c, 0);
+    }
+    sync_tiles();   // chunk c has arrived; chunk c + 1 is no longer read
+    Frag<T> go[2];   // dO as an operand over the tokens, and as values
+    f32x4 gf[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        go[m / 2].v[4 * (m % 2) + e] = io_to_op<T>(v[m][e]);
+        gf[m][e] = io_to_float(v[m][e]) * a.scale;
+      }
+    const CL L{lds + (CL::BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
+    if (c > 0) {
+      if (CL::BUFS == 2) stage(c - 1, (c - 1) & 1);
+      load_g(c - 1);
+    }
+    const size_t blk = (size_t)(slot0 + c) * a.H + head;
+    S* so = static_cast<S*>(a.dst) + (blk * a.dv + col) * D;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) store_io4(so + 16 * i + 4 * g, st[i]);
+    // dU = P^T dO' + w K dS
+    f32x4 du[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) du[m] = zero4();
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const Split<T> sb = split<T>(st[2 * s], st[2 * s + 1]);
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+        mma_xs(du[m], KT::row(L.k(), 16 * m + r16, 32 * s + 4 * g, 32 * s + 16 + 4 * g), sb);
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      f32x4 y = zero4();
+      if (m < 2) mma_sx(y, MT::col(L.p(), MAT, 4 * g, 16 + 4 * g, 16 * m), go[0]);
+      mma_sx(y, MT::col(L.p(), MAT, 32 + 4 * g, 48 + 4 * g, 16 * m), go[1]);
+      du[m] = du[m] * L.scal(1, m, g) + y * a.scale;
+    }
+    // dR = T^T dU, dV = b dR
+    f32x4 dr[4];
+    {
+      const Split<T> d0 = split<T>(du[0], du[1]), d1 = split<T>(du[2], du[3]);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        dr[m] = zero4();
+        if (m < 2) mma_ss(dr[m], MT::col(L.t(), MAT, 4 * g, 16 + 4 * g, 16 * m), d0);
+        mma_ss(dr[m], MT::col(L.t(), MAT, 32 + 4 * g, 48 + 4 * g, 16 * m), d1);
+      }
+    }
+    S* ro = static_cast<S*>(a.drt) + blk * (size_t)(DELTA_MAT_BYTES / MAT * DC) * a.dv + (size_t)col * DC;
+    const auto rv = row_window(static_cast<S*>(a.dV) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
+                               min(DC, sq.n - c * DC), a.dv);
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      store_split4(ro + 16 * m + 4 * g, (size_t)DC * a.dv, dr[m]);
+      const f32x4 dv = dr[m] * L.scal(2, m, g);
+      const f32x4 eg = L.scal(0, m, g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        store1(rv, ((16 * m + 4 * g + e) * a.H * a.dv + col) * (int)sizeof(S), float_to_io<S>(dv[e]));
+      dr[m] = -(dv * eg);      // -b e^G dR
+      gf[m] *= eg;             // e^G dO'
+    }
+    // dS <- e^{G_63} dS + Q^T (e^G dO') - K^T (b e^G dR)
+    const Split<T> q0 = split<T>(gf[0], gf[1]), q1 = split<T>(gf[2], gf[3]);
+    const Split<T> k0 = split<T>(dr[0], dr[1]), k1 = split<T>(dr[2], dr[3]);
+    const float last = L.last();
+#pragma unroll
+    for (int i = 0; i < DT; ++i) {
+      st[i] *= last;
+      mma_xs(st[i], KT::col(L.q(), 4 * g, 16 + 4 * g, 16 * i), q0);
+      mma_xs(st[i], KT::col(L.q(), 32 + 4 * g, 48 + 4 * g, 16 * i), q1);
+      mma_xs(st[i], KT::col(L.k(), 4 * g, 16 + 4 * g, 16 * i), k0);
+      mma_xs(st[i], KT::col(L.k(), 32 + 4 * g, 48 + 4 * g, 16 * i), k1);
+    }
+  }
+}
+
+// One workgroup per chunk and key head, over the value heads of its group in order; wave w has
+// the tokens 16 w .. + 15, a lane per token, and holds the rows of dQ^T and dK^T
+// ([d x 16 tokens]).  S, dS, U, dR, dO and V pass through LDS in blocks of VB value columns.
+template <class T, int D, int VB>
+__global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
+  using S = typename Io<T>::type;
+  using KT = Tile16<T, D>;
+  using VT = Tile16<T, VB>;
+  using MT = Tile16<T, DC>;
+  using PT = Pair16<T, DC>;
+  constexpr int KS = D / 32, DT = D / 16, VS = VB / 32;
+  constexpr int TERMS = IsBf16<T>::value ? 2 : 1;
+  constexpr int ROWS = DC * D * (int)sizeof(T), MAT = DC * DC * (int)sizeof(T);
+  constexpr int VROWS = DC * VB * (int)sizeof(T);     // a block of dO or V, or of one term of U or dR
+  constexpr int SROWS = VB * D * (int)sizeof(T);      // a block of S or dS
+  constexpr int BLOCK = 2 * VROWS + 2 * SROWS + 2 * TERMS * VROWS;
+  __shared__ __attribute__((aligned(16))) char lds[2 * ROWS + (BLOCK > 2 * MAT ? BLOCK : 2 * MAT)];
+  __shared__ double lG[DC];
+  __shared__ float col_x[4][DC], row_g[DC], sum_z[4], sum_s[4];
+  const char* LK = lds;
+  const char* LQ = lds + ROWS;
+  const char* LG = lds + 2 * ROWS;            // dO
+  const char* LV = LG + VROWS;
+  const char* LS = LV + VROWS;                // S
+  const char* LD = LS + SROWS;                // dS
+  const char* LU = LD + SROWS;                // U
+  const char* LR = LU + TERMS * VROWS;        // dR
+  char* LP = lds + 2 * ROWS;                  // afterwards: dP D and M, rows i
+  char* LM = LP + MAT;
+
+  const int l = threadIdx.x % WAVE, r16 = l % 16, g = l / 16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int slot = blockIdx.x / a.Hk, kh = blockIdx.x % a.Hk, grp = a.H / a.Hk;
+  const SeqTile t = find_tile<DC>(a.off, a.B, a.T, slot);
+  if (t.b < 0) return;
+  const int n = min(DC, t.n - t.tile * DC), row0 = t.row0 + t.tile * DC;
+  const int tok = 16 * w + r16;
+  stage_tile<T, D, DC, 4>(LK, row_words(static_cast<const S*>(a.K) + kh * D, row0, a.ks, n, D), a.ks * (int)sizeof(S), w);
+  stage_tile<T, D, DC, 4>(LQ, row_words(static_cast<const S*>(a.Q) + kh * D, row0, a.qs, n, D), a.qs * (int)sizeof(S), w);
+
+  f32x4 dq[DT], dk[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i) dq[i] = dk[i] = zero4();
+
+  for (int h = 0; h < grp; ++h) {
+    const int head = kh * grp + h;
+    const size_t blk = (size_t)slot * a.H + head;
+    const char* prep = a.prep + blk * DELTA_PREP_BYTES + 2 * DELTA_MAT_BYTES;
+    const float* scal = reinterpret_cast<const float*>(prep);
+    const float eg = scal[tok], wt = scal[DC + tok], be = scal[2 * DC + tok], last = scal[DC - 1];
+    f32x4 qi[DT], fi[DT], wi[DT];   // dO S^T, dR S^T, U dS^T, transposed
+#pragma unroll
+    for (int i = 0; i < DT; ++i) qi[i] = fi[i] = wi[i] = zero4();
+    f32x4 dp[4], da[4];   // dO U^T and dR U^T, transposed: rows j, lane column i
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dp[i] = da[i] = zero4();
+    float rv = 0.f, ss = 0.f;
+    for (int v0 = 0; v0 < a.dv; v0 += VB) {
+      sync_tiles();   // what was staged or written before is no longer read
+      stage_tile<T, VB, DC, 4>(LG, row_words(static_cast<const S*>(a.dO) + (size_t)head * a.dv + v0, row0, a.H * a.dv, n, VB),
+                               a.H * a.dv * (int)sizeof(S), w);
+      stage_tile<T, VB, DC, 4>(LV, row_words(static_cast<const S*>(a.V) + (size_t)head * a.dv + v0, row0, a.vs, n, VB),
+                               a.vs * (int)sizeof(S), w);
+      stage_tile<T, D, VB, 4>(LS, row_words(static_cast<const S*>(a.st) + (blk * a.dv + v0) * D, 0, D, VB, D),
+                              D * (int)sizeof(S), w);
+      stage_tile<T, D, VB, 4>(LD, row_words(static_cast<const S*>(a.dst) + (blk * a.dv + v0) * D, 0, D, VB, D),
+                              D * (int)sizeof(S), w);
+#pragma unroll
+      for (int i = 0; i < TERMS; ++i) {
+        const size_t at = ((blk * TERMS + i) * a.dv + v0) * DC;
+        stage_tile<T, DC, VB, 4>(LU + i * VROWS, row_words(static_cast<const S*>(a.ut) + at, 0, DC, VB, DC),
+                                 DC * (int)sizeof(S), w);
+        stage_tile<T, DC, VB, 4>(LR + i * VROWS, row_words(static_cast<const S*>(a.drt) + at, 0, DC, VB, DC),
+                                 DC * (int)sizeof(S), w);
+      }
+      if (threadIdx.x < DC) lG[threadIdx.x] = reinterpret_cast<const double*>(prep + 1024)[threadIdx.x];
+      sync_tiles();
+#pragma unroll
+      for (int s = 0; s < VS; ++s) {
+        const int c0 = 32 * s + 8 * g;   // value columns c0 .. c0 + 7 in this lane's slots
+        const Frag<T> go = VT::row(LG, tok, c0, c0 + 4), vv = VT::row(LV, tok, c0, c0 + 4);
+        const Split<T> dr = PT::col(LR, VROWS, c0, c0 + 4, 16 * w), u = PT::col(LU, VROWS, c0, c0 + 4, 16 * w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          float r = dr.hi.get(j);
+          if constexpr (IsBf16<T>::value) r += dr.lo.get(j);
+          rv = __builtin_fmaf(r, vv.get(j), rv);
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          const Frag<T> sf = KT::col(LS, c0, c0 + 4, 16 * i), df = KT::col(LD, c0, c0 + 4, 16 * i);
+          mma(qi[i], sf, go);
+          mma_xs(fi[i], sf, dr);
+          mma_xs(wi[i], df, u);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j <= w) {
+            const Split<T> uj = PT::col(LU, VROWS, c0, c0 + 4, 16 * j);
+            mma_sx(dp[j], uj, go);
+            mma_xs(da[j], uj.hi, dr);
+          }
+      }
+      for (int i = threadIdx.x; i < SROWS / 16; i += 256) {   // <S, dS>: the same place in both tiles
+        if constexpr (IsBf16<T>::value) {
+          const bf16x8 x = *reinterpret_cast<const bf16x8*>(LS + 16 * i), y = *reinterpret_cast<const bf16x8*>(LD + 16 * i);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) ss = __builtin_fmaf((float)x[j], (float)y[j], ss);
+        } else {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(LS + 16 * i), y = *reinterpret_cast<const f32x4*>(LD + 16 * i);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) ss = __builtin_fmaf(x[j], y[j], ss);
+        }
+      }
+    }
+    // the rows' parts of dG and dbeta
+    float dot_q = 0.f, dot_f = 0.f, dot_z = 0.f;
+    const float ge = eg * a.scale;
+#pragma unroll
+    for (int i = 0; i < DT; ++i) {
+      const f32x4 kr = KT::quad_f(LK, tok, 16 * i + 4 * g), qr = KT::quad_f(LQ, tok, 16 * i + 4 * g);
+      qi[i] *= ge;
+      fi[i] *= eg;
+      wi[i] *= wt;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        dot_q = __builtin_fmaf(qr[e], qi[i][e], dot_q);
+        dot_f = __builtin_fmaf(kr[e], fi[i][e], dot_f);
+        dot_z = __builtin_fmaf(kr[e], wi[i][e], dot_z);
+      }
+      dq[i] += qi[i];
+      dk[i] += wi[i] - fi[i] * be;
+    }
+    dot_q = group_sum(dot_q);
+    dot_f = group_sum(dot_f);
+    dot_z = group_sum(dot_z);
+    rv = group_sum(rv);
+    // dP D, M, and the sums of X
+    float row_x = 0.f, row_b = 0.f;
+    const double Gi = lG[tok];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f32x4 x = zero4();
+      if (j <= w) {
+        f32x4 kk = zero4(), qk = zero4();
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const Frag<T> kj = KT::row(LK, 16 * j + r16, 32 * s + 8 * g, 32 * s + 8 * g + 4);
+          mma(kk, kj, KT::row(LK, tok, 32 * s + 8 * g, 32 * s + 8 * g + 4));
+          mma(qk, kj, KT::row(LQ, tok, 32 * s + 8 * g, 32 * s + 8 * g + 4));
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int tj = 16 * j + 4 * g + e;
+          const float D_ij = tj <= tok ? expf((float)(Gi - lG[tj])) : 0.f;
+          dp[j][e] *= a.scale * D_ij;
+          const float dad = tj < tok ? -da[j][e] * D_ij : 0.f;
+          da[j][e] = dad * be;
+          row_b = __builtin_fmaf(dad, kk[e], row_b);
+          x[e] = dp[j][e] * qk[e] + da[j][e] * kk[e];
+          row_x += x[e];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float c = lane_sum<16>(x[e]);
+        if (r16 == 0) col_x[w][16 * j + 4 * g + e] = c;
+      }
+    }
+    row_x = group_sum(row_x);
+    row_b = group_sum(row_b);
+    if (g == 0) row_g[tok] = dot_q - be * dot_f - dot_z + row_x;
+    if (g == 0 && tok < n) {
+      const size_t at = (size_t)(row0 + tok) * a.H + head;
+      static_cast<S*>(a.dbeta)[at] = float_to_io<S>(rv - dot_f + row_b);
+    }
+    const float z16 = lane_sum<16>(dot_z);
+    ss = group_sum(lane_sum<16>(ss));
+    if (l == 0) {
+      sum_z[w] = z16;
+      sum_s[w] = ss;
+    }
+    __syncthreads();   // the last block of S, dS, U, dR is no longer read
+    if (w == 0) {
+      const float gv = l < n ? a.g[(size_t)(row0 + l) * a.H + head] : 0.f;
+      float x = row_g[l] - ((col_x[0][l] + col_x[1][l]) + (col_x[2][l] + col_x[3][l]));
+      if (l == DC - 1)
+        x += (sum_z[0] + sum_z[1]) + (sum_z[2] + sum_z[3]) + last * ((sum_s[0] + sum_s[1]) + (sum_s[2] + sum_s[3]));
+#pragma unroll
+      for (int s = 1; s < WAVE; s *= 2) {
+        const float o = __shfl_down(x, s);
+        if (l + s < WAVE) x += o;
+      }
+      // a decay of zero has no slope
+      if (l < n) static_cast<S*>(a.dg)[(size_t)(row0 + l) * a.H + head] = float_to_io<S>(gv < -1e4f ? 0.f : x);
+    }
+    // (dP D) and M as rows i in LDS, with the zero blocks that share a k step with the diagonal
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j <= (w | 1)) {
+        store_io4(reinterpret_cast<S*>(const_cast<char*>(MT::quad(LP, tok, 16 * j + 4 * g))), dp[j]);
+        store_io4(reinterpret_cast<S*>(const_cast<char*>(MT::quad(LM, tok, 16 * j + 4 * g))), da[j]);
+      }
+    // dQ += (dP D) K, dK += M K over this wave's own rows
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+      if (2 * s <= w) {
+        Frag<T> pf, mf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          pf.set(e, dp[2 * s][e]);
+          pf.set(4 + e, dp[2 * s + 1][e]);
+          mf.set(e, da[2 * s][e]);
+          mf.set(4 + e, da[2 * s + 1][e]);
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          const Frag<T> kc = KT::col(LK, 32 * s + 4 * g, 32 * s + 16 + 4 * g, 16 * i);
+          mma(dq[i], kc, pf);
+          mma(dk[i], kc, mf);
+        }
+      }
+    __syncthreads();
+    // dK += (dP D)^T Q + M^T K over the rows that follow
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+      if (2 * s + 1 >= w) {
+        const Frag<T> pf = MT::col(LP, 32 * s + 4 * g, 32 * s + 16 + 4 * g, 16 * w);
+        const Frag<T> mf = MT::col(LM, 32 * s + 4 * g, 32 * s + 16 + 4 * g, 16 * w);
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          mma(dk[i], KT::col(LQ, 32 * s + 4 * g, 32 * s + 16 + 4 * g, 16 * i), pf);
+          mma(dk[i], KT::col(LK, 32 * s + 4 * g, 32 * s + 16 + 4 * g, 16 * i), mf);
+        }
+      }
+  }
+  if (tok >= n) return;
+  const size_t at = ((size_t)(row0 + tok) * a.Hk + kh) * D;
+#pragma unroll
+  for (int i = 0; i < DT; ++i) {
+    store_io4(static_cast<S*>(a.dQ) + at + 16 * i + 4 * g, dq[i]);
+    store_io4(static_cast<S*>(a.dK) + at + 16 * i + 4 * g, dk[i]);
+  }
+}
+
+namespace {
+template <class T, int D>
+hipError_t run_bwd(const DeltaArgs& a, hipStream_t st) {
+  timing_mark(FLEX_KERNEL_DELTA_BWD, st, true);
+  const int bh = a.B * a.H;
+  if (a.waves == 4)
+    k_delta_rsweep<T, D, 4><<<bh * (a.dv / 64), 256, 0, st>>>(a);
+  else
+    k_delta_rsweep<T, D, 2><<<bh * (a.dv / 32), 128, 0, st>>>(a);
+  k_delta_grad<T, D, 32><<<seq_slots(a.T, a.B, DC) * a.Hk, 256, 0, st>>>(a);
+  timing_mark(FLEX_KERNEL_DELTA_BWD, st, false);
+  return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_delta_bwd(const DeltaArgs& a, bool bf16, hipStream_t st) {
+  if (bf16) return a.d == 64 ? run_bwd<__bf16, 64>(a, st) : run_bwd<__bf16, 128>(a, st);
+  return a.d == 64 ? run_bwd<float, 64>(a, st) : run_bwd<float, 128>(a, st);
+}
+
+}  // namespace flex

@@ -57,6 +57,7 @@ __global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
   scal[l] = expf((float)G);
   scal[DC + l] = expf((float)(Gc - G));
   scal[2 * DC + l] = bv;
+  reinterpret_cast<double*>(out + 2 * DELTA_MAT_BYTES + 1024)[l] = G;
   Lg[l] = G;
   lds_fence();
 
@@ -180,12 +181,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1))) vo
   using S = typename Io<T>::type;
   using KT = Tile16<T, D>;
   using MT = Pair16<T, DC>;
-  constexpr int KS = D / 32, DT = D / 16;
-  constexpr int ROWS = DC * D * (int)sizeof(T);                  // bytes of a K or Q tile
-  constexpr int MAT = DC * DC * (int)sizeof(T);                  // of one term of T or P
-  constexpr int BUF = 2 * ROWS + DELTA_PREP_BYTES;
-  constexpr int BUFS = 2 * BUF <= 160 * 1024 ? 2 : 1;
-  __shared__ __attribute__((aligned(16))) char lds[BUFS * BUF];
+  using CL = ChunkLds<T, D>;
+  constexpr int KS = D / 32, DT = D / 16, MAT = CL::MAT;
+  __shared__ __attribute__((aligned(16))) char lds[CL::BUFS * CL::BYTES];
   const int l = threadIdx.x % WAVE, r16 = l % 16, g = l / 16;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int bh = blockIdx.x % (a.B * a.H), b = bh / a.H, head = bh % a.H, kh = head / (a.H / a.Hk);
@@ -201,35 +199,20 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1))) vo
     for (int e = 0; e < 4; ++e) st[i][e] = a.state0 ? a.state0[sbase + (size_t)(16 * i + 4 * g + e) * a.dv] : 0.f;
 
   auto stage = [&](int c, int buf) {
-    const char* L = lds + buf * BUF;
-    const int row0 = sq.row0 + c * DC, n = min(DC, sq.n - c * DC);
-    stage_tile<T, D, DC, NW>(L, row_words(static_cast<const S*>(a.K) + kh * D, row0, a.ks, n, D),
-                             a.ks * (int)sizeof(S), w);
-    stage_tile<T, D, DC, NW>(L + ROWS, row_words(static_cast<const S*>(a.Q) + kh * D, row0, a.qs, n, D),
-                             a.qs * (int)sizeof(S), w);
-    const char* p = a.prep + ((size_t)(slot0 + c) * a.H + head) * DELTA_PREP_BYTES;
-    constexpr int TERMS = DELTA_MAT_BYTES / MAT;
-#pragma unroll
-    for (int i = 0; i < 2 * TERMS; ++i)
-      stage_tile<T, DC, DC, NW>(L + 2 * ROWS + i * MAT, row_words(reinterpret_cast<const S*>(p + i * MAT), 0, DC, DC, DC),
-                                DC * (int)sizeof(S), w);
-    stage_linear<1, NW>(L + 2 * ROWS + 2 * DELTA_MAT_BYTES, p + 2 * DELTA_MAT_BYTES, w);
+    CL{lds + buf * CL::BYTES}.template stage<NW>(a, sq.row0 + c * DC, min(DC, sq.n - c * DC), kh,
+                                                 (size_t)(slot0 + c) * a.H + head, w);
   };
   S v[4][4];   // this lane's column of the chunk's V
   auto load_v = [&](int c) {
-    const auto rs = row_window(static_cast<const S*>(a.V) + (size_t)head * a.dv, sq.row0 + c * DC, a.vs,
-                               min(DC, sq.n - c * DC), a.dv);
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[m][e] = load1(rs, ((16 * m + 4 * g + e) * a.vs + col) * (int)sizeof(S), S());
+    load_column(v, static_cast<const S*>(a.V) + (size_t)head * a.dv, sq.row0 + c * DC, a.vs, min(DC, sq.n - c * DC),
+                a.dv, col);
   };
   if (nchunks > 0) {
-    if (BUFS == 2) stage(0, 0);
+    if (CL::BUFS == 2) stage(0, 0);
     load_v(0);
   }
   for (int c = 0; c < nchunks; ++c) {
-    if (BUFS == 1) {
+    if (CL::BUFS == 1) {
       sync_tiles();
       stage(c, 0);
     }
@@ -239,13 +222,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1))) vo
     for (int m = 0; m < 4; ++m)
 #pragma unroll
       for (int e = 0; e < 4; ++e) vf[m][e] = io_to_float(v[m][e]);
-    const char* LK = lds + (BUFS == 2 ? (c & 1) * BUF : 0);
-    const char* LQ = LK + ROWS;
-    const char* LT = LQ + ROWS;
-    const char* LP = LT + DELTA_MAT_BYTES;
-    const float* sc = reinterpret_cast<const float*>(LP + DELTA_MAT_BYTES);
+    const CL L{lds + (CL::BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
     if (c + 1 < nchunks) {
-      if (BUFS == 2) stage(c + 1, (c + 1) & 1);
+      if (CL::BUFS == 2) stage(c + 1, (c + 1) & 1);
       load_v(c + 1);
     }
     const size_t blk = (size_t)(slot0 + c) * a.H + head;
@@ -263,16 +242,16 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1))) vo
       const Split<T> sb = split<T>(st[2 * s], st[2 * s + 1]);
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        mma_xs(ks[m], KT::row(LK, 16 * m + r16, 32 * s + 4 * g, 32 * s + 16 + 4 * g), sb);
-        mma_xs(qs[m], KT::row(LQ, 16 * m + r16, 32 * s + 4 * g, 32 * s + 16 + 4 * g), sb);
+        mma_xs(ks[m], KT::row(L.k(), 16 * m + r16, 32 * s + 4 * g, 32 * s + 16 + 4 * g), sb);
+        mma_xs(qs[m], KT::row(L.q(), 16 * m + r16, 32 * s + 4 * g, 32 * s + 16 + 4 * g), sb);
       }
     }
     // U = T b (V - e^G K S)
     f32x4 eg[4];
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-      eg[m] = *reinterpret_cast<const f32x4*>(sc + 16 * m + 4 * g);
-      const f32x4 be = *reinterpret_cast<const f32x4*>(sc + 2 * DC + 16 * m + 4 * g);
+      eg[m] = L.scal(0, m, g);
+      const f32x4 be = L.scal(2, m, g);
 #pragma unroll
       for (int e = 0; e < 4; ++e) ks[m][e] = be[e] * (vf[m][e] - eg[m][e] * ks[m][e]);
     }
@@ -282,8 +261,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1))) vo
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
         u[m] = zero4();
-        mma_ss(u[m], MT::row(LT, MAT, 16 * m + r16, 4 * g, 16 + 4 * g), r0);
-        if (m >= 2) mma_ss(u[m], MT::row(LT, MAT, 16 * m + r16, 32 + 4 * g, 48 + 4 * g), r1);
+        mma_ss(u[m], MT::row(L.t(), MAT, 16 * m + r16, 4 * g, 16 + 4 * g), r0);
+        if (m >= 2) mma_ss(u[m], MT::row(L.t(), MAT, 16 * m + r16, 32 + 4 * g, 48 + 4 * g), r1);
       }
     }
     if (SAVE) {
@@ -295,14 +274,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1))) vo
     {
       f32x4 wu[4];
 #pragma unroll
-      for (int m = 0; m < 4; ++m) wu[m] = u[m] * *reinterpret_cast<const f32x4*>(sc + DC + 16 * m + 4 * g);
+      for (int m = 0; m < 4; ++m) wu[m] = u[m] * L.scal(1, m, g);
       const Split<T> w0 = split<T>(wu[0], wu[1]), w1 = split<T>(wu[2], wu[3]);
-      const float last = sc[DC - 1];
+      const float last = L.last();
 #pragma unroll
       for (int i = 0; i < DT; ++i) {
         st[i] *= last;
-        mma_xs(st[i], KT::col(LK, 4 * g, 16 + 4 * g, 16 * i), w0);
-        mma_xs(st[i], KT::col(LK, 32 + 4 * g, 48 + 4 * g, 16 * i), w1);
+        mma_xs(st[i], KT::col(L.k(), 4 * g, 16 + 4 * g, 16 * i), w0);
+        mma_xs(st[i], KT::col(L.k(), 32 + 4 * g, 48 + 4 * g, 16 * i), w1);
       }
     }
     // O = scale (e^G Q S + P U)
@@ -313,8 +292,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1))) vo
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
         f32x4 o = qs[m] * eg[m];
-        mma_ss(o, MT::row(LP, MAT, 16 * m + r16, 4 * g, 16 + 4 * g), u0);
-        if (m >= 2) mma_ss(o, MT::row(LP, MAT, 16 * m + r16, 32 + 4 * g, 48 + 4 * g), u1);
+        mma_ss(o, MT::row(L.p(), MAT, 16 * m + r16, 4 * g, 16 + 4 * g), u0);
+        if (m >= 2) mma_ss(o, MT::row(L.p(), MAT, 16 * m + r16, 32 + 4 * g, 48 + 4 * g), u1);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           store1(ro, ((16 * m + 4 * g + e) * a.H * a.dv + col) * (int)sizeof(S), float_to_io<S>(o[e] * a.scale));

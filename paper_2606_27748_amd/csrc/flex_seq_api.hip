@@ -233,6 +233,27 @@ int32_t flex_delta_fwd(const flex_delta_desc* desc, const void* Q, const void* K
   return e == hipSuccess ? FLEX_OK : FLEX_ERR_HIP;
 }
 
+int32_t flex_delta_bwd(const flex_delta_desc* desc, const void* Q, const void* K, const void* V, const float* g,
+                       const float* beta, const int32_t* off, const void* saved, size_t saved_bytes, const void* dO,
+                       void* dQ, void* dK, void* dV, void* dg, void* dbeta, void* ws, size_t ws_bytes, void* stream) {
+  const int32_t st = check_delta(desc, false);
+  if (st != FLEX_OK) return st;
+  if (!off) return FLEX_ERR_INVALID_ARG;
+  const void* rows[] = {Q, K, V, g, beta, dO, dQ, dK, dV, dg, dbeta};
+  for (const void* p : rows)
+    if (!tensor_ok(p, desc->T)) return FLEX_ERR_INVALID_ARG;
+  if (!saved || saved_bytes < delta_saved_bytes(desc) || !aligned16(saved)) return FLEX_ERR_WORKSPACE;
+  if (!ws || ws_bytes < delta_ws_bytes(desc, FLEX_PASS_BWD) || !aligned16(ws)) return FLEX_ERR_WORKSPACE;
+  if (desc->T == 0) return FLEX_OK;
+  DeltaArgs a = delta_args(desc, Q, K, V, g, beta, off);
+  delta_saved(a, desc, const_cast<void*>(saved));
+  a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV; a.dg = dg; a.dbeta = dbeta;
+  a.dst = ws;
+  a.drt = static_cast<char*>(ws) + delta_blocks(desc) * delta_state_bytes(desc);
+  const hipError_t e = launch_delta_bwd(a, desc->io_dtype == FLEX_BF16, (hipStream_t)stream);
+  return e == hipSuccess ? FLEX_OK : FLEX_ERR_HIP;
+}
+
 int32_t flex_delta_step(const flex_delta_desc* desc, const void* q, const void* k, const void* v, const float* g,
                         const float* beta, float* state, void* o, void* stream) {
   const int32_t st = check_delta(desc, true);
