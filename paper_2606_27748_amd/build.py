@@ -23,7 +23,8 @@ FLAGS = [
 # Per-source additions: the dQ sweep places MFMA results in VGPRs (its results
 # mostly feed vector code; fewer accumulator-register copies).  Measured slower
 # for the other kernels.
-FILE_FLAGS = {"flex_bwd_dq.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+_VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+FILE_FLAGS = {"flex_bwd_dq.hip": _VGPR_FORM, "flex_delta_fwd.hip": _VGPR_FORM, "flex_delta_bwd.hip": _VGPR_FORM}
 
 
 def _run(cmd):

@@ -18,116 +18,191 @@
 
 namespace flex {
 
-template <class T, int D, int NW>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1))) void k_delta_rsweep(DeltaArgs a) {
+// As the forward's sweep: per 16 columns one wave carries dS (dS -> K dS -> dU -> dR -> dS) and a
+// second forms Q^T (e^G dO'), which does not depend on it, and stores dR and dV; NL
+// waves stage the chunks.
+template <class T, int D, int NC>
+__global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_delta_rsweep(DeltaArgs a) {
   using S = typename Io<T>::type;
   using KT = Tile16<T, D>;
-  using MT = Pair16<T, DC>;
-  using CL = ChunkLds<T, D>;
-  constexpr int KS = D / 32, DT = D / 16, MAT = CL::MAT;
-  __shared__ __attribute__((aligned(16))) char lds[CL::BUFS * CL::BYTES];
+  using LT = LowTri<T>;
+  using CL = ChunkLds<T, D, 16 * NC>;
+  constexpr int KS = D / 32, DT = D / 16, TERMS = IsBf16<T>::value ? 2 : 1;
+  constexpr int BOX = (4 + DT) * WAVE * 16;          // dR, Q^T (e^G dO')
+  constexpr int BUFS = 2 * CL::BYTES + NC * BOX <= 160 * 1024 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) char lds[BUFS * CL::BYTES + NC * BOX];
   const int l = threadIdx.x % WAVE, r16 = l % 16, g = l / 16;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  const int bh = blockIdx.x % (a.B * a.H), b = bh / a.H, head = bh % a.H, kh = head / (a.H / a.Hk);
-  const int col = (blockIdx.x / (a.B * a.H) * NW + w) * 16 + r16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), pair = w % NC;
+  const int parts = a.dv / (16 * NC);
+  const SweepCoord sc = sweep_coord(a.B * a.H, parts);
+  const int bh = sc.bh, b = bh / a.H, head = bh % a.H, kh = head / (a.H / a.Hk);
+  const int col0 = sc.part * NC * 16, col = col0 + 16 * pair + r16;
   const SeqRange sq = seq_range(a.off, b, a.T);
   const int nchunks = (sq.n + DC - 1) / DC, slot0 = sq.row0 / DC + b;
+  f32x4* box = reinterpret_cast<f32x4*>(lds + BUFS * CL::BYTES + pair * BOX) + l;   // tile i at box[i * WAVE]
+  // every wave passes the same barriers in a chunk: (1) the chunk is in LDS, (2) Q^T (e^G dO') and
+  // dR are, and with one buffer (3) the chunk is no longer read
 
-  f32x4 st[DT];
-#pragma unroll
-  for (int i = 0; i < DT; ++i) st[i] = zero4();
-  auto stage = [&](int c, int buf) {
-    CL{lds + buf * CL::BYTES}.template stage<NW>(a, sq.row0 + c * DC, min(DC, sq.n - c * DC), kh,
-                                                 (size_t)(slot0 + c) * a.H + head, w);
-  };
-  S v[4][4];   // this lane's column of the chunk's dO
-  auto load_g = [&](int c) {
-    load_column(v, static_cast<const S*>(a.dO) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
-                min(DC, sq.n - c * DC), a.dv, col);
-  };
-  if (nchunks > 0) {
-    if (CL::BUFS == 2) stage(nchunks - 1, (nchunks - 1) & 1);
-    load_g(nchunks - 1);
-  }
-  for (int c = nchunks - 1; c >= 0; --c) {
-    if (CL::BUFS == 1) {
-      sync_tiles();
-      stage(c, 0);
+  if (w >= 2 * NC) {   // staging
+    const S* X = static_cast<const S*>(a.dO) + (size_t)head * a.dv + col0;
+    const int xs = a.H * a.dv, lw = w - 2 * NC;
+    auto stage = [&](int c) {
+      CL{lds + (BUFS == 2 ? (c & 1) * CL::BYTES : 0)}.template stage<NL>(
+          a, sq.row0 + c * DC, min(DC, sq.n - c * DC), kh, (size_t)(slot0 + c) * a.H + head, X, xs, lw);
+    };
+    constexpr int PER = (CL::LINES + 2 * NL * WAVE - 1) / (2 * NL * WAVE);   // two workgroups share a head at least
+    unsigned seen[PER] = {};
+    auto prefetch = [&](int c) {
+      CL{nullptr}.template prefetch<NL, PER>(seen, a, sq.row0 + c * DC, min(DC, sq.n - c * DC), kh,
+                                             (size_t)(slot0 + c) * a.H + head, X, xs, sc.part, parts, lw);
+    };
+    const int first = nchunks - 1, end = -1, step = -1;
+    if (nchunks > 0) {
+      stage(first);
+      if (nchunks > 1) prefetch(first + step);
     }
-    sync_tiles();   // chunk c has arrived; chunk c + 1 is no longer read
-    Frag<T> go[2];   // dO as an operand over the tokens, and as values
-    f32x4 gf[4];
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        go[m / 2].v[4 * (m % 2) + e] = io_to_op<T>(v[m][e]);
-        gf[m][e] = io_to_float(v[m][e]) * a.scale;
+    for (int c = first; c != end; c += step) {
+      const bool more = c + step != end, far = more && c + 2 * step != end;
+      // the chunk, not what was asked for after it
+      if (BUFS == 2 && more)
+        sync_tiles_but<PER>();
+      else
+        sync_tiles();
+      if (BUFS == 2) {
+        if (more) stage(c + step);
+        if (far) prefetch(c + 2 * step);
       }
-    const CL L{lds + (CL::BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
-    if (c > 0) {
-      if (CL::BUFS == 2) stage(c - 1, (c - 1) & 1);
-      load_g(c - 1);
-    }
-    const size_t blk = (size_t)(slot0 + c) * a.H + head;
-    S* so = static_cast<S*>(a.dst) + (blk * a.dv + col) * D;
-#pragma unroll
-    for (int i = 0; i < DT; ++i) store_io4(so + 16 * i + 4 * g, st[i]);
-    // dU = P^T dO' + w K dS
-    f32x4 du[4];
-#pragma unroll
-    for (int m = 0; m < 4; ++m) du[m] = zero4();
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const Split<T> sb = split<T>(st[2 * s], st[2 * s + 1]);
-#pragma unroll
-      for (int m = 0; m < 4; ++m)
-        mma_xs(du[m], KT::row(L.k(), 16 * m + r16, 32 * s + 4 * g, 32 * s + 16 + 4 * g), sb);
+      sync_lds();
+      if (BUFS == 1) {
+        sync_lds();
+        if (more) stage(c + step);
+        if (far) prefetch(c + 2 * step);
+      }
     }
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      f32x4 y = zero4();
-      if (m < 2) mma_sx(y, MT::col(L.p(), MAT, 4 * g, 16 + 4 * g, 16 * m), go[0]);
-      mma_sx(y, MT::col(L.p(), MAT, 32 + 4 * g, 48 + 4 * g, 16 * m), go[1]);
-      du[m] = du[m] * L.scal(1, m, g) + y * a.scale;
-    }
-    // dR = T^T dU, dV = b dR
-    f32x4 dr[4];
-    {
-      const Split<T> d0 = split<T>(du[0], du[1]), d1 = split<T>(du[2], du[3]);
+    for (int u = 0; u < PER; ++u) asm volatile("" ::"v"(seen[u]));
+    return;
+  }
+
+  if (w < NC) {   // dS
+    f32x4 st[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) st[i] = zero4();
+    for (int c = nchunks - 1; c >= 0; --c) {
+      const CL L{lds + (BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
+      S* so = static_cast<S*>(a.dst) + (((size_t)(slot0 + c) * a.H + head) * a.dv + col) * D + 8 * g;
+      Split<T> sb[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        sb[s] = split<T>(st[2 * s], st[2 * s + 1]);
+        store_terms(so + 32 * s, 0, sb[s]);
+      }
+      sync_lds();
+      // dU = P^T dO' + w K dS, dR = T^T dU
+      f32x4 y[4], dr[4];
+      {
+        Split<T> a0[2], a1[4];
+        LT::transposed(a0, a1, L.p(), g);
+        Frag<T> go[2];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const auto x = L.col(m, g, 16 * pair);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) go[m / 2].v[4 * (m % 2) + e] = x[e];
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          dr[m] = y[m] = zero4();
+          mma_sx(y[m], a1[m], go[1]);
+          if (m < 2) mma_sx(y[m], a0[m], go[0]);
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        Frag<T> kr[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) kr[m] = KT::row8(L.k(), tile_row(m, r16), 32 * s + 8 * g);
+        mma_xs4(dr, kr, sb[s]);
+      }
+#pragma unroll
+      for (int m = 0; m < 4; ++m) dr[m] = dr[m] * L.scal(1, m, g) + y[m] * a.scale;
+      LT::apply_t(dr, L.t(), g);
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        dr[m] = zero4();
-        if (m < 2) mma_ss(dr[m], MT::col(L.t(), MAT, 4 * g, 16 + 4 * g, 16 * m), d0);
-        mma_ss(dr[m], MT::col(L.t(), MAT, 32 + 4 * g, 48 + 4 * g, 16 * m), d1);
+        box[m * WAVE] = dr[m];
+        dr[m] = -(dr[m] * L.scal(2, m, g) * L.scal(0, m, g));   // -b e^G dR
       }
+      const Split<T> k0 = split<T>(dr[0], dr[1]), k1 = split<T>(dr[2], dr[3]);
+      const float last = L.last();
+      sync_lds();
+      // dS <- e^{G_63} dS + Q^T (e^G dO') - K^T (b e^G dR)
+#pragma unroll
+      for (int i = 0; i < DT; i += 4) {
+        Frag<T> kc[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          kc[m] = KT::col8(L.k(), 8 * g, i + m);
+          st[i + m] = st[i + m] * last + box[(4 + i + m) * WAVE];
+        }
+        mma_xs4(*reinterpret_cast<f32x4(*)[4]>(&st[i]), kc, k0);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) kc[m] = KT::col8(L.k(), 32 + 8 * g, i + m);
+        mma_xs4(*reinterpret_cast<f32x4(*)[4]>(&st[i]), kc, k1);
+      }
+      if (BUFS == 1) sync_lds();
     }
-    S* ro = static_cast<S*>(a.drt) + blk * (size_t)(DELTA_MAT_BYTES / MAT * DC) * a.dv + (size_t)col * DC;
-    const auto rv = row_window(static_cast<S*>(a.dV) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
-                               min(DC, sq.n - c * DC), a.dv);
+    return;
+  }
+
+  for (int c = nchunks - 1; c >= 0; --c) {
+    const CL L{lds + (BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
+    sync_lds();
+    f32x4 gf[4], be[4];
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-      store_split4(ro + 16 * m + 4 * g, (size_t)DC * a.dv, dr[m]);
-      const f32x4 dv = dr[m] * L.scal(2, m, g);
-      const f32x4 eg = L.scal(0, m, g);
+      const auto x = L.col(m, g, 16 * pair);
+      const f32x4 eg = L.scal(0, m, g) * a.scale;
+      be[m] = L.scal(2, m, g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) gf[m][e] = (float)x[e] * eg[e];
+    }
+    {
+      const Split<T> q0 = split<T>(gf[0], gf[1]), q1 = split<T>(gf[2], gf[3]);
+#pragma unroll
+      for (int i = 0; i < DT; i += 4) {
+        f32x4 y[4];
+        Frag<T> qc[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          y[m] = zero4();
+          qc[m] = KT::col8(L.q(), 8 * g, i + m);
+        }
+        mma_xs4(y, qc, q0);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) qc[m] = KT::col8(L.q(), 32 + 8 * g, i + m);
+        mma_xs4(y, qc, q1);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) box[(4 + i + m) * WAVE] = y[m];
+      }
+    }
+    sync_lds();
+    const size_t blk = (size_t)(slot0 + c) * a.H + head;
+    S* ro = static_cast<S*>(a.drt) + blk * (size_t)(TERMS * DC) * a.dv + (size_t)col * DC + 8 * g;
+    const auto rv = row_window(static_cast<S*>(a.dV) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
+                               min(DC, sq.n - c * DC), a.dv);
+    f32x4 dr[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) dr[m] = box[m * WAVE];
+    store_terms(ro, (size_t)DC * a.dv, split<T>(dr[0], dr[1]));
+    store_terms(ro + 32, (size_t)DC * a.dv, split<T>(dr[2], dr[3]));
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      dr[m] *= be[m];
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        store1(rv, ((16 * m + 4 * g + e) * a.H * a.dv + col) * (int)sizeof(S), float_to_io<S>(dv[e]));
-      dr[m] = -(dv * eg);      // -b e^G dR
-      gf[m] *= eg;             // e^G dO'
+        store1(rv, (tile_row(m, 4 * g + e) * a.H * a.dv + col) * (int)sizeof(S), float_to_io<S>(dr[m][e]));
     }
-    // dS <- e^{G_63} dS + Q^T (e^G dO') - K^T (b e^G dR)
-    const Split<T> q0 = split<T>(gf[0], gf[1]), q1 = split<T>(gf[2], gf[3]);
-    const Split<T> k0 = split<T>(dr[0], dr[1]), k1 = split<T>(dr[2], dr[3]);
-    const float last = L.last();
-#pragma unroll
-    for (int i = 0; i < DT; ++i) {
-      st[i] *= last;
-      mma_xs(st[i], KT::col(L.q(), 4 * g, 16 + 4 * g, 16 * i), q0);
-      mma_xs(st[i], KT::col(L.q(), 32 + 4 * g, 48 + 4 * g, 16 * i), q1);
-      mma_xs(st[i], KT::col(L.k(), 4 * g, 16 + 4 * g, 16 * i), k0);
-      mma_xs(st[i], KT::col(L.k(), 32 + 4 * g, 48 + 4 * g, 16 * i), k1);
-    }
+    if (BUFS == 1) sync_lds();
   }
 }
 
@@ -381,10 +456,7 @@ template <class T, int D>
 hipError_t run_bwd(const DeltaArgs& a, hipStream_t st) {
   timing_mark(FLEX_KERNEL_DELTA_BWD, st, true);
   const int bh = a.B * a.H;
-  if (a.waves == 4)
-    k_delta_rsweep<T, D, 4><<<bh * (a.dv / 64), 256, 0, st>>>(a);
-  else
-    k_delta_rsweep<T, D, 2><<<bh * (a.dv / 32), 128, 0, st>>>(a);
+  k_delta_rsweep<T, D, 2><<<bh * (a.dv / 32), 256 + NL * 64, 0, st>>>(a);
   k_delta_grad<T, D, 32><<<seq_slots(a.T, a.B, DC) * a.Hk, 256, 0, st>>>(a);
   timing_mark(FLEX_KERNEL_DELTA_BWD, st, false);
   return hipGetLastError();

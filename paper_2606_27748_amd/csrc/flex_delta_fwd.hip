@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
   scal[l] = expf((float)G);
   scal[DC + l] = expf((float)(Gc - G));
   scal[2 * DC + l] = bv;
-  reinterpret_cast<double*>(out + 2 * DELTA_MAT_BYTES + 1024)[l] = G;
+  reinterpret_cast<double*>(out + DELTA_SWEEP_BYTES)[l] = G;
   Lg[l] = G;
   lds_fence();
 
@@ -141,15 +141,14 @@ __global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
       mm16(x, Xl[nn], y);
       X[nn][m] = -x;
     }
-  S* to = reinterpret_cast<S*>(out);
-  constexpr size_t LO = DC * DC;
+  constexpr size_t LO = LowTri<T>::TERM / sizeof(S);
 #pragma unroll
   for (int m = 0; m < 4; ++m)
 #pragma unroll
     for (int nn = 0; nn <= (m | 1); ++nn)   // with the zero blocks that share a k step with the diagonal
-      store_split4(to + (16 * m + r16) * DC + 16 * nn + 4 * g, LO, nn <= m ? X[nn][m] : zero4());
+      store_split4(reinterpret_cast<S*>(out + LowTri<T>::at(16 * m + r16, 16 * nn + 4 * g)), LO,
+                   nn <= m ? X[nn][m] : zero4());
 
-  S* po = reinterpret_cast<S*>(out + DELTA_MAT_BYTES);
   const auto rq = row_window(static_cast<const S*>(a.Q) + kh * D, row0, a.qs, n, D);
 #pragma unroll
   for (int m = 0; m < 4; ++m) {
@@ -169,142 +168,180 @@ __global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
           c[e] = j <= i ? c[e] * decay(Gi[m] - Lg[j]) : 0.f;
         }
       }
-      store_split4(po + (16 * m + r16) * DC + 16 * nn + 4 * g, LO, c);
+      store_split4(reinterpret_cast<S*>(out + DELTA_MAT_BYTES + LowTri<T>::at(16 * m + r16, 16 * nn + 4 * g)), LO, c);
     }
   }
 }
 
-// The sweep: one workgroup per sequence, value head and 16 NW columns of the state, a wave
-// per 16; the chunk's K, Q, T, P and scalars pass through LDS, V and O directly.
-template <class T, int D, int NW, bool SAVE>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1))) void k_delta_sweep(DeltaArgs a) {
+// The sweep: one workgroup per sequence, value head and 16 NC columns of the state.  What the
+// next chunk waits for is one wave's per 16 columns (S -> K S -> U -> S, the state in its
+// registers); a second forms Q S and O beside it from the operands that the first leaves in
+// LDS, and writes O and what a backward needs; NL waves stage the chunks.  Left to one wave, all of it
+// took 4.3 us a chunk at d = 128 (256 waves for 32 heads, three quarters of the SIMDs without
+// work), with the second wave doing the staging too 2.9.
+template <class T, int D, int NC, bool SAVE>
+__global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_delta_sweep(DeltaArgs a) {
   using S = typename Io<T>::type;
   using KT = Tile16<T, D>;
-  using MT = Pair16<T, DC>;
-  using CL = ChunkLds<T, D>;
-  constexpr int KS = D / 32, DT = D / 16, MAT = CL::MAT;
-  __shared__ __attribute__((aligned(16))) char lds[CL::BUFS * CL::BYTES];
+  using LT = LowTri<T>;
+  using CL = ChunkLds<T, D, 16 * NC>;
+  using FB = FragBox<T>;
+  constexpr int KS = D / 32, DT = D / 16, TERMS = IsBf16<T>::value ? 2 : 1;
+  constexpr int BOX = (KS + 2) * FB::BYTES;                          // S, then U
+  constexpr int BUFS = 2 * CL::BYTES + NC * BOX <= 160 * 1024 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) char lds[BUFS * CL::BYTES + NC * BOX];
   const int l = threadIdx.x % WAVE, r16 = l % 16, g = l / 16;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  const int bh = blockIdx.x % (a.B * a.H), b = bh / a.H, head = bh % a.H, kh = head / (a.H / a.Hk);
-  const int col = (blockIdx.x / (a.B * a.H) * NW + w) * 16 + r16;   // this lane's column of the state
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), pair = w % NC;
+  const int parts = a.dv / (16 * NC);
+  const SweepCoord sc = sweep_coord(a.B * a.H, parts);
+  const int bh = sc.bh, b = bh / a.H, head = bh % a.H, kh = head / (a.H / a.Hk);
+  const int col0 = sc.part * NC * 16, col = col0 + 16 * pair + r16;   // this lane's column of the state
   const SeqRange sq = seq_range(a.off, b, a.T);
   const int nchunks = (sq.n + DC - 1) / DC, slot0 = sq.row0 / DC + b;
+  char* box = lds + BUFS * CL::BYTES + pair * BOX;
+  // every wave passes the same barriers in a chunk: (1) the chunk and S are in LDS, (2) U is, and with
+  // one buffer (3) the chunk is no longer read
 
-  f32x4 st[DT];
-  const size_t sbase = ((size_t)bh * D) * a.dv + col;
+  if (w >= 2 * NC) {   // staging
+    const S* X = static_cast<const S*>(a.V) + (size_t)head * a.dv + col0;
+    const int xs = a.vs, lw = w - 2 * NC;
+    auto stage = [&](int c) {
+      CL{lds + (BUFS == 2 ? (c & 1) * CL::BYTES : 0)}.template stage<NL>(
+          a, sq.row0 + c * DC, min(DC, sq.n - c * DC), kh, (size_t)(slot0 + c) * a.H + head, X, xs, lw);
+    };
+    constexpr int PER = (CL::LINES + 2 * NL * WAVE - 1) / (2 * NL * WAVE);   // two workgroups share a head at least
+    unsigned seen[PER] = {};
+    auto prefetch = [&](int c) {
+      CL{nullptr}.template prefetch<NL, PER>(seen, a, sq.row0 + c * DC, min(DC, sq.n - c * DC), kh,
+                                             (size_t)(slot0 + c) * a.H + head, X, xs, sc.part, parts, lw);
+    };
+    const int first = 0, end = nchunks, step = 1;
+    if (nchunks > 0) {
+      stage(first);
+      if (nchunks > 1) prefetch(first + step);
+    }
+    for (int c = first; c != end; c += step) {
+      const bool more = c + step != end, far = more && c + 2 * step != end;
+      // the chunk, not what was asked for after it
+      if (BUFS == 2 && more)
+        sync_tiles_but<PER>();
+      else
+        sync_tiles();
+      if (BUFS == 2) {
+        if (more) stage(c + step);
+        if (far) prefetch(c + 2 * step);
+      }
+      sync_lds();
+      if (BUFS == 1) {
+        sync_lds();
+        if (more) stage(c + step);
+        if (far) prefetch(c + 2 * step);
+      }
+    }
 #pragma unroll
-  for (int i = 0; i < DT; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) st[i][e] = a.state0 ? a.state0[sbase + (size_t)(16 * i + 4 * g + e) * a.dv] : 0.f;
+    for (int u = 0; u < PER; ++u) asm volatile("" ::"v"(seen[u]));
+    return;
+  }
 
-  auto stage = [&](int c, int buf) {
-    CL{lds + buf * CL::BYTES}.template stage<NW>(a, sq.row0 + c * DC, min(DC, sq.n - c * DC), kh,
-                                                 (size_t)(slot0 + c) * a.H + head, w);
-  };
-  S v[4][4];   // this lane's column of the chunk's V
-  auto load_v = [&](int c) {
-    load_column(v, static_cast<const S*>(a.V) + (size_t)head * a.dv, sq.row0 + c * DC, a.vs, min(DC, sq.n - c * DC),
-                a.dv, col);
-  };
-  if (nchunks > 0) {
-    if (CL::BUFS == 2) stage(0, 0);
-    load_v(0);
-  }
-  for (int c = 0; c < nchunks; ++c) {
-    if (CL::BUFS == 1) {
-      sync_tiles();
-      stage(c, 0);
-    }
-    sync_tiles();   // chunk c has arrived; chunk c - 1 is no longer read
-    f32x4 vf[4];
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) vf[m][e] = io_to_float(v[m][e]);
-    const CL L{lds + (CL::BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
-    if (c + 1 < nchunks) {
-      if (CL::BUFS == 2) stage(c + 1, (c + 1) & 1);
-      load_v(c + 1);
-    }
-    const size_t blk = (size_t)(slot0 + c) * a.H + head;
-    if (SAVE) {
-      S* so = static_cast<S*>(a.st) + (blk * a.dv + col) * D;
-#pragma unroll
-      for (int i = 0; i < DT; ++i) store_io4(so + 16 * i + 4 * g, st[i]);
-    }
-    // K S and Q S
-    f32x4 ks[4], qs[4];
-#pragma unroll
-    for (int m = 0; m < 4; ++m) ks[m] = qs[m] = zero4();
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const Split<T> sb = split<T>(st[2 * s], st[2 * s + 1]);
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        mma_xs(ks[m], KT::row(L.k(), 16 * m + r16, 32 * s + 4 * g, 32 * s + 16 + 4 * g), sb);
-        mma_xs(qs[m], KT::row(L.q(), 16 * m + r16, 32 * s + 4 * g, 32 * s + 16 + 4 * g), sb);
-      }
-    }
-    // U = T b (V - e^G K S)
-    f32x4 eg[4];
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      eg[m] = L.scal(0, m, g);
-      const f32x4 be = L.scal(2, m, g);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) ks[m][e] = be[e] * (vf[m][e] - eg[m][e] * ks[m][e]);
-    }
-    f32x4 u[4];
-    {
-      const Split<T> r0 = split<T>(ks[0], ks[1]), r1 = split<T>(ks[2], ks[3]);
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        u[m] = zero4();
-        mma_ss(u[m], MT::row(L.t(), MAT, 16 * m + r16, 4 * g, 16 + 4 * g), r0);
-        if (m >= 2) mma_ss(u[m], MT::row(L.t(), MAT, 16 * m + r16, 32 + 4 * g, 48 + 4 * g), r1);
-      }
-    }
-    if (SAVE) {
-      S* uo = static_cast<S*>(a.ut) + blk * (size_t)(DELTA_MAT_BYTES / MAT * DC) * a.dv + (size_t)col * DC;
-#pragma unroll
-      for (int m = 0; m < 4; ++m) store_split4(uo + 16 * m + 4 * g, (size_t)DC * a.dv, u[m]);
-    }
-    // S <- e^{G_63} S + K^T (w U)
-    {
-      f32x4 wu[4];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) wu[m] = u[m] * L.scal(1, m, g);
-      const Split<T> w0 = split<T>(wu[0], wu[1]), w1 = split<T>(wu[2], wu[3]);
-      const float last = L.last();
-#pragma unroll
-      for (int i = 0; i < DT; ++i) {
-        st[i] *= last;
-        mma_xs(st[i], KT::col(L.k(), 4 * g, 16 + 4 * g, 16 * i), w0);
-        mma_xs(st[i], KT::col(L.k(), 32 + 4 * g, 48 + 4 * g, 16 * i), w1);
-      }
-    }
-    // O = scale (e^G Q S + P U)
-    {
-      const Split<T> u0 = split<T>(u[0], u[1]), u1 = split<T>(u[2], u[3]);
-      const auto ro = row_window(static_cast<S*>(a.O) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
-                                 min(DC, sq.n - c * DC), a.dv);
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        f32x4 o = qs[m] * eg[m];
-        mma_ss(o, MT::row(L.p(), MAT, 16 * m + r16, 4 * g, 16 + 4 * g), u0);
-        if (m >= 2) mma_ss(o, MT::row(L.p(), MAT, 16 * m + r16, 32 + 4 * g, 48 + 4 * g), u1);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          store1(ro, ((16 * m + 4 * g + e) * a.H * a.dv + col) * (int)sizeof(S), float_to_io<S>(o[e] * a.scale));
-      }
-    }
-  }
-  if (a.state) {
+  if (w < NC) {   // the state
+    f32x4 st[DT];
+    const size_t sbase = ((size_t)bh * D) * a.dv + col;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) a.state[sbase + (size_t)(16 * i + 4 * g + e) * a.dv] = st[i][e];
+      for (int e = 0; e < 4; ++e) st[i][e] = a.state0 ? a.state0[sbase + (size_t)tile_row(i, 4 * g + e) * a.dv] : 0.f;
+    for (int c = 0; c < nchunks; ++c) {
+      const CL L{lds + (BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
+      Split<T> sb[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        sb[s] = split<T>(st[2 * s], st[2 * s + 1]);
+        FB::put(box + s * FB::BYTES, l, sb[s]);
+      }
+      sync_lds();
+      f32x4 u[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) u[m] = zero4();
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        Frag<T> kr[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) kr[m] = KT::row8(L.k(), tile_row(m, r16), 32 * s + 8 * g);
+        mma_xs4(u, kr, sb[s]);
+      }
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const f32x4 eg = L.scal(0, m, g), be = L.scal(2, m, g);
+        const auto vc = L.col(m, g, 16 * pair);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[m][e] = be[e] * ((float)vc[e] - eg[e] * u[m][e]);
+      }
+      LT::apply(u, L.t(), r16, g);
+      FB::put(box + KS * FB::BYTES, l, split<T>(u[0], u[1]));
+      FB::put(box + (KS + 1) * FB::BYTES, l, split<T>(u[2], u[3]));
+#pragma unroll
+      for (int m = 0; m < 4; ++m) u[m] *= L.scal(1, m, g);
+      const Split<T> w0 = split<T>(u[0], u[1]), w1 = split<T>(u[2], u[3]);
+      const float last = L.last();
+      sync_lds();
+#pragma unroll
+      for (int i = 0; i < DT; i += 4) {
+        Frag<T> kc[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          kc[m] = KT::col8(L.k(), 8 * g, i + m);
+          st[i + m] *= last;
+        }
+        mma_xs4(*reinterpret_cast<f32x4(*)[4]>(&st[i]), kc, w0);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) kc[m] = KT::col8(L.k(), 32 + 8 * g, i + m);
+        mma_xs4(*reinterpret_cast<f32x4(*)[4]>(&st[i]), kc, w1);
+      }
+      if (BUFS == 1) sync_lds();
+    }
+    if (a.state) {
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a.state[sbase + (size_t)tile_row(i, 4 * g + e) * a.dv] = st[i][e];
+    }
+    return;
+  }
+
+  for (int c = 0; c < nchunks; ++c) {   // O
+    const CL L{lds + (BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
+    sync_lds();
+    const size_t blk = (size_t)(slot0 + c) * a.H + head;
+    f32x4 o[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) o[m] = zero4();
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const Split<T> sb = FB::get(box + s * FB::BYTES, l);
+      Frag<T> qr[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) qr[m] = KT::row8(L.q(), tile_row(m, r16), 32 * s + 8 * g);
+      mma_xs4(o, qr, sb);
+      if (SAVE) store_terms(static_cast<S*>(a.st) + (blk * a.dv + col) * D + 32 * s + 8 * g, 0, sb);
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) o[m] *= L.scal(0, m, g);
+    sync_lds();
+    const Split<T> u0 = FB::get(box + KS * FB::BYTES, l), u1 = FB::get(box + (KS + 1) * FB::BYTES, l);
+    if (SAVE) {
+      S* uo = static_cast<S*>(a.ut) + blk * (size_t)(TERMS * DC) * a.dv + (size_t)col * DC + 8 * g;
+      store_terms(uo, (size_t)DC * a.dv, u0);
+      store_terms(uo + 32, (size_t)DC * a.dv, u1);
+    }
+    const auto ro = row_window(static_cast<S*>(a.O) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
+                               min(DC, sq.n - c * DC), a.dv);
+    LT::mul(o, L.p(), r16, g, u0, u1);
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        store1(ro, (tile_row(m, 4 * g + e) * a.H * a.dv + col) * (int)sizeof(S), float_to_io<S>(o[m][e] * a.scale));
+    if (BUFS == 1) sync_lds();
   }
 }
 
@@ -364,13 +401,13 @@ __global__ __launch_bounds__(256) void k_delta_step(DeltaArgs a) {
 }
 
 namespace {
-template <class T, int D, int NW>
+template <class T, int D, int NC>
 void run_sweep(const DeltaArgs& a, hipStream_t st) {
-  const int wgs = a.B * a.H * (a.dv / (16 * NW));
+  const int wgs = a.B * a.H * (a.dv / (16 * NC));
   if (a.st)
-    k_delta_sweep<T, D, NW, true><<<wgs, NW * 64, 0, st>>>(a);
+    k_delta_sweep<T, D, NC, true><<<wgs, NC * 128 + NL * 64, 0, st>>>(a);
   else
-    k_delta_sweep<T, D, NW, false><<<wgs, NW * 64, 0, st>>>(a);
+    k_delta_sweep<T, D, NC, false><<<wgs, NC * 128 + NL * 64, 0, st>>>(a);
 }
 template <class T, int D>
 hipError_t run_fwd(const DeltaArgs& a, hipStream_t st) {
@@ -379,10 +416,7 @@ hipError_t run_fwd(const DeltaArgs& a, hipStream_t st) {
     const int64_t waves = (int64_t)seq_slots(a.T, a.B, DC) * a.H;
     k_delta_prep<T, D><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(a);
   }
-  if (a.waves == 4)
-    run_sweep<T, D, 4>(a, st);
-  else
-    run_sweep<T, D, 2>(a, st);
+  run_sweep<T, D, 2>(a, st);
   timing_mark(FLEX_KERNEL_DELTA_FWD, st, false);
   return hipGetLastError();
 }

@@ -246,6 +246,20 @@ __device__ __forceinline__ void wait_lds_loads() {
 // compiler would else wait for them at their first use, in every iteration, and so
 // for the tile that is on its way.
 __device__ __forceinline__ void wait_reg_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
+// Every wave's loads to LDS have arrived, and its reads are done; up to LATER of the wave's
+// last memory instructions may be on their way.  Counted in issue order: at least LATER must
+// have been issued after the loads to LDS (stores of the step, which a wait for all would
+// otherwise wait out, a memory latency each time).
+template <int LATER>
+__device__ __forceinline__ void sync_tiles_but() {
+  static_assert(LATER < 64, "six bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((LATER & 15) | (LATER >> 4) << 14 | 0x0070);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// Every wave's reads and writes of LDS are done; loads may be on their way.
+__device__ __forceinline__ void sync_lds() { sync_tiles_but<63>(); }
 // Every wave's loads to LDS have arrived, and its reads are done.
 __device__ __forceinline__ void sync_tiles() {
   wait_lds_loads();

@@ -119,8 +119,6 @@ DeltaArgs delta_args(const flex_delta_desc* d, const void* Q, const void* K, con
   a.ks = stride_of(d->k_stride, (int64_t)d->Hk * d->d);
   a.vs = stride_of(d->v_stride, (int64_t)d->H * d->dv);
   a.scale = d->scale;
-  // the sweep's waves per workgroup: more workgroups where they would not fill the CUs
-  a.waves = (int64_t)d->B * d->H * (d->dv / 64) >= 256 ? 4 : 2;
   return a;
 }
 void delta_saved(DeltaArgs& a, const flex_delta_desc* d, void* saved) {

@@ -41,13 +41,15 @@ hipError_t launch_attn_bwd(const AttnArgs& a, bool bf16, int d, hipStream_t st);
 
 // Gated delta rule.  What the chunks of 64 tokens need beside the rows is kept per chunk
 // slot and value head (block slot * H + head):
-//   prep   T as hi and lo bf16 [64][64] (fp32: one [64][64]), P the same, then
-//          e^G [64], w [64], b [64] (fp32) in 1 KB, then G [64] (fp64) in 1 KB
+//   prep   T, then P (lower triangular [64][64]): hi and lo bf16, or fp32, each as the rows 0..31
+//          of the columns 0..31 and the rows 32..63, in the order of the sweeps' LDS tiles;
+//          e^G [64], w [64], b [64] (fp32) in 1 KB; G [64] (fp64) in 1 KB
 //   st     the state at the chunk's start, transposed [dv][d], io type   (training)
 //   ut     U transposed [dv][64], hi and lo (fp32: one)                  (training)
 constexpr int DELTA_CHUNK = 64;
-constexpr int DELTA_MAT_BYTES = 64 * 64 * 4;   // T or P: hi and lo, or fp32
-constexpr int DELTA_PREP_BYTES = 2 * DELTA_MAT_BYTES + 2048;
+constexpr int DELTA_MAT_BYTES = (32 * 32 + 32 * 64) * 4;   // T or P: hi and lo, or fp32
+constexpr int DELTA_SWEEP_BYTES = 2 * DELTA_MAT_BYTES + 1024;
+constexpr int DELTA_PREP_BYTES = DELTA_SWEEP_BYTES + 1024;
 
 struct DeltaArgs {
   const void* Q;
@@ -62,7 +64,6 @@ struct DeltaArgs {
   int B, T, Hk, H, d, dv;
   int qs, ks, vs;
   float scale;
-  int waves;             // waves (of 16 state columns) per workgroup of the sweeps
   char* prep;
   void* st;              // NULL: not kept
   void* ut;
