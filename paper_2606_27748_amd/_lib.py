@@ -324,14 +324,18 @@ def _size(fn, desc, *args):
     return n.value
 
 
-def _expect(what, dev, **tensors):
-    """Tensors against (shape, dtype, row stride or 0 for contiguous); None where one is left out."""
-    for name, (t, shape, dtype, stride) in tensors.items():
+def _expect(what, dev, tensors):
+    """Each (name, tensor, shape, dtype, row stride or 0 for contiguous) as it must be; None where one
+    is left out."""
+    for name, t, shape, dtype, stride in tensors:
         if t is None:
             continue
-        rows = (stride, shape[2], 1) if stride and shape[0] > 1 else None
-        if (tuple(t.shape) != shape or t.dtype != dtype or t.device != dev or
-                (t.numel() and not (t[0].is_contiguous() and t.stride() == rows if rows else t.is_contiguous()))):
+        ok = t.shape == shape and t.dtype is dtype and t.device == dev
+        if ok and stride and shape[0] > 1:
+            ok = t.stride() == (stride, shape[2], 1)
+        elif ok:
+            ok = t.is_contiguous()
+        if not ok:
             raise FlexError(FLEX_ERR_INVALID_ARG, f"{what}: {name} must be {dtype} {list(shape)} on {dev}, rows "
                             + (f"{stride} elements apart" if stride else "contiguous"))
 
@@ -341,18 +345,30 @@ def _io(desc):
     return torch.bfloat16 if desc.io_dtype == FLEX_BF16 else torch.float32
 
 
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
 def _run(fn, dev, desc, *args):
-    """The call on the current stream of the tensors' device."""
+    """The call on the current stream of the tensors' device, with that device current."""
     import torch
-    with torch.cuda.device(dev):
-        _check(getattr(load(), fn)(ctypes.byref(desc), *args, _stream()), fn)
+    f = getattr(load(), fn)
+    if dev.index == torch.cuda.current_device():
+        st = f(ctypes.byref(desc), *args, torch._C._cuda_getCurrentRawStream(dev.index))
+    else:
+        with torch.cuda.device(dev):
+            st = f(ctypes.byref(desc), *args, torch.cuda.current_stream().cuda_stream)
+    if st != FLEX_OK:
+        raise FlexError(st, fn)
 
 
 def _seq_workspace(need, ws, dev):
-    import torch
     if ws is None or ws.numel() * ws.element_size() < need:
+        if not need:
+            return None, 0
+        import torch
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
-    return _ptr(ws), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def make_attn_desc(B, Hq, Hkv, d, Tq, Tk, causal=True, io="bf16", scale=None, q_stride=0, k_stride=0,
@@ -366,13 +382,13 @@ def attn_workspace_size(desc: flex_attn_desc, pass_: int) -> int:
     return _size("flex_attn_workspace_size", desc, pass_)
 
 
-def _attn_inputs(what, desc, Q, K, V, q_off, k_off, **more):
+def _attn_inputs(what, desc, Q, K, V, q_off, k_off, *more):
     import torch
-    io, dev = _io(desc), Q.device
-    _expect(what, dev, Q=(Q, (desc.Tq, desc.Hq, desc.d), io, desc.q_stride),
-            K=(K, (desc.Tk, desc.Hkv, desc.d), io, desc.k_stride),
-            V=(V, (desc.Tk, desc.Hkv, desc.d), io, desc.v_stride),
-            q_off=(q_off, (desc.B + 1,), torch.int32, 0), k_off=(k_off, (desc.B + 1,), torch.int32, 0), **more)
+    io, dev, i32, off = _io(desc), Q.device, torch.int32, (desc.B + 1,)
+    kv = (desc.Tk, desc.Hkv, desc.d)
+    _expect(what, dev, (("Q", Q, (desc.Tq, desc.Hq, desc.d), io, desc.q_stride), ("K", K, kv, io, desc.k_stride),
+                        ("V", V, kv, io, desc.v_stride), ("q_off", q_off, off, i32, 0),
+                        ("k_off", k_off, off, i32, 0)) + more)
     return io, dev
 
 
@@ -382,17 +398,16 @@ def flex_attn_fwd(desc: flex_attn_desc, Q, K, V, q_off, k_off, k_len=None, O=Non
     offsets [B+1] (and the used key lengths k_len [B] of a slotted cache) on the
     device.  Returns (O, lse)."""
     import torch
-    rows, lrow = (desc.Tq, desc.Hq, desc.d), (desc.Tq, desc.Hq)
-    io, dev = _attn_inputs("flex_attn_fwd", desc, Q, K, V, q_off, k_off,
-                           k_len=(k_len, (desc.B,), torch.int32, 0), O=(O, rows, _io(desc), 0),
-                           lse=(lse, lrow, torch.float32, 0))
+    rows, f32 = (desc.Tq, desc.Hq, desc.d), torch.float32
+    io, dev = _attn_inputs("flex_attn_fwd", desc, Q, K, V, q_off, k_off, ("k_len", k_len, (desc.B,), torch.int32, 0),
+                           ("O", O, rows, _io(desc), 0), ("lse", lse, rows[:2], f32, 0))
     if O is None:
         O = torch.empty(rows, dtype=io, device=dev)
     if lse is None and want_lse:
-        lse = torch.empty(lrow, dtype=torch.float32, device=dev)
+        lse = torch.empty(rows[:2], dtype=f32, device=dev)
     w = _seq_workspace(attn_workspace_size(desc, FLEX_PASS_FWD), ws, dev)
-    _run("flex_attn_fwd", dev, desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(q_off), _ptr(k_off), _ptr(k_len), _ptr(O),
-         _ptr(lse), *w)
+    _run("flex_attn_fwd", dev, desc, Q.data_ptr(), K.data_ptr(), V.data_ptr(), q_off.data_ptr(), k_off.data_ptr(),
+         _at(k_len), O.data_ptr(), _at(lse), *w)
     return O, lse
 
 
@@ -401,15 +416,14 @@ def flex_attn_bwd(desc: flex_attn_desc, Q, K, V, q_off, k_off, O, lse, dO, dQ=No
     in the io dtype; rows of no sequence are not written."""
     import torch
     rows, krow, io = (desc.Tq, desc.Hq, desc.d), (desc.Tk, desc.Hkv, desc.d), _io(desc)
-    _, dev = _attn_inputs("flex_attn_bwd", desc, Q, K, V, q_off, k_off, O=(O, rows, io, 0), dO=(dO, rows, io, 0),
-                          lse=(lse, rows[:2], torch.float32, 0), dQ=(dQ, rows, io, 0), dK=(dK, krow, io, 0),
-                          dV=(dV, krow, io, 0))
+    _, dev = _attn_inputs("flex_attn_bwd", desc, Q, K, V, q_off, k_off, ("O", O, rows, io, 0), ("dO", dO, rows, io, 0),
+                          ("lse", lse, rows[:2], torch.float32, 0), ("dQ", dQ, rows, io, 0), ("dK", dK, krow, io, 0),
+                          ("dV", dV, krow, io, 0))
     dQ = torch.empty(rows, dtype=io, device=dev) if dQ is None else dQ
     dK = torch.empty(krow, dtype=io, device=dev) if dK is None else dK
     dV = torch.empty(krow, dtype=io, device=dev) if dV is None else dV
     w = _seq_workspace(attn_workspace_size(desc, FLEX_PASS_BWD), ws, dev)
-    _run("flex_attn_bwd", dev, desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(q_off), _ptr(k_off), _ptr(O), _ptr(lse),
-         _ptr(dO), _ptr(dQ), _ptr(dK), _ptr(dV), *w)
+    _run("flex_attn_bwd", dev, desc, *(t.data_ptr() for t in (Q, K, V, q_off, k_off, O, lse, dO, dQ, dK, dV)), *w)
     return dict(dQ=dQ, dK=dK, dV=dV)
 
 
@@ -430,20 +444,20 @@ def delta_saved_size(desc: flex_delta_desc) -> int:
     return _size("flex_delta_saved_size", desc)
 
 
-def _delta_inputs(what, desc, T, Q, K, V, g, beta, **more):
+def _delta_inputs(what, desc, T, Q, K, V, g, beta, *more):
     import torch
-    io, dev = _io(desc), Q.device
-    _expect(what, dev, Q=(Q, (T, desc.Hk, desc.d), io, desc.q_stride), K=(K, (T, desc.Hk, desc.d), io, desc.k_stride),
-            V=(V, (T, desc.H, desc.dv), io, desc.v_stride), g=(g, (T, desc.H), torch.float32, 0),
-            beta=(beta, (T, desc.H), torch.float32, 0), **more)
+    io, dev, f32, qk = _io(desc), Q.device, torch.float32, (T, desc.Hk, desc.d)
+    _expect(what, dev, (("Q", Q, qk, io, desc.q_stride), ("K", K, qk, io, desc.k_stride),
+                        ("V", V, (T, desc.H, desc.dv), io, desc.v_stride), ("g", g, (T, desc.H), f32, 0),
+                        ("beta", beta, (T, desc.H), f32, 0)) + more)
     return io, dev
 
 
-def _saved(what, desc, saved):
+def _saved(what, desc, saved, dev):
     n = saved.numel() * saved.element_size()
-    if n < delta_saved_size(desc) or not saved.is_contiguous():
-        raise FlexError(FLEX_ERR_WORKSPACE, f"{what}: saved")
-    return _ptr(saved), n
+    if n < delta_saved_size(desc) or not saved.is_contiguous() or saved.device != dev:
+        raise FlexError(FLEX_ERR_WORKSPACE, f"{what}: saved must hold delta_saved_size bytes on {dev}")
+    return saved.data_ptr(), n
 
 
 def flex_delta_fwd(desc: flex_delta_desc, Q, K, V, g, beta, off, state0=None, O=None, state=None, saved=None,
@@ -453,20 +467,20 @@ def flex_delta_fwd(desc: flex_delta_desc, Q, K, V, g, beta, off, state0=None, O=
     for flex_delta_bwd.  Returns (O, state), state [B,H,d,dv] fp32 where one was given or
     want_state."""
     import torch
-    sshape = (desc.B, desc.H, desc.d, desc.dv)
-    io, dev = _delta_inputs("flex_delta_fwd", desc, desc.T, Q, K, V, g, beta, off=(off, (desc.B + 1,), torch.int32, 0),
-                            O=(O, (desc.T, desc.H, desc.dv), _io(desc), 0), state0=(state0, sshape, torch.float32, 0),
-                            state=(state, sshape, torch.float32, 0))
+    sshape, rows, f32 = (desc.B, desc.H, desc.d, desc.dv), (desc.T, desc.H, desc.dv), torch.float32
+    io, dev = _delta_inputs("flex_delta_fwd", desc, desc.T, Q, K, V, g, beta, ("off", off, (desc.B + 1,), torch.int32, 0),
+                            ("O", O, rows, _io(desc), 0), ("state0", state0, sshape, f32, 0),
+                            ("state", state, sshape, f32, 0))
     if O is None:
-        O = torch.empty(desc.T, desc.H, desc.dv, dtype=io, device=dev)
+        O = torch.empty(rows, dtype=io, device=dev)
     if state is None and want_state:
-        state = torch.empty(sshape, dtype=torch.float32, device=dev)
+        state = torch.empty(sshape, dtype=f32, device=dev)
     if saved is not None:
-        keep, w = _saved("flex_delta_fwd", desc, saved), (None, 0)
+        keep, w = _saved("flex_delta_fwd", desc, saved, dev), (None, 0)
     else:
         keep, w = (None, 0), _seq_workspace(delta_workspace_size(desc, FLEX_PASS_FWD), ws, dev)
-    _run("flex_delta_fwd", dev, desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(g), _ptr(beta), _ptr(off), _ptr(state0), _ptr(O),
-         _ptr(state), *keep, *w)
+    _run("flex_delta_fwd", dev, desc, *(t.data_ptr() for t in (Q, K, V, g, beta, off)), _at(state0), O.data_ptr(),
+         _at(state), *keep, *w)
     return O, state
 
 
@@ -475,30 +489,29 @@ def flex_delta_bwd(desc: flex_delta_desc, Q, K, V, g, beta, off, dO, saved, dQ=N
     """Backward of flex_delta_fwd (state0 None) from what it kept in saved.  Returns dict(dQ,
     dK, dV, dg, dbeta) in the io dtype; rows of no sequence are not written."""
     import torch
-    io = _io(desc)
-    shapes = {"dQ": (desc.T, desc.Hk, desc.d), "dK": (desc.T, desc.Hk, desc.d), "dV": (desc.T, desc.H, desc.dv),
-              "dg": (desc.T, desc.H), "dbeta": (desc.T, desc.H)}
-    out = {"dQ": dQ, "dK": dK, "dV": dV, "dg": dg, "dbeta": dbeta}
-    _, dev = _delta_inputs("flex_delta_bwd", desc, desc.T, Q, K, V, g, beta, off=(off, (desc.B + 1,), torch.int32, 0),
-                           dO=(dO, shapes["dV"], io, 0), **{n: (out[n], shapes[n], io, 0) for n in out})
-    out = {n: torch.empty(shapes[n], dtype=io, device=dev) if t is None else t for n, t in out.items()}
-    keep = _saved("flex_delta_bwd", desc, saved)
+    io, qk, rows, gates = _io(desc), (desc.T, desc.Hk, desc.d), (desc.T, desc.H, desc.dv), (desc.T, desc.H)
+    out = (("dQ", dQ, qk, io, 0), ("dK", dK, qk, io, 0), ("dV", dV, rows, io, 0), ("dg", dg, gates, io, 0),
+           ("dbeta", dbeta, gates, io, 0))
+    _, dev = _delta_inputs("flex_delta_bwd", desc, desc.T, Q, K, V, g, beta, ("off", off, (desc.B + 1,), torch.int32, 0),
+                           ("dO", dO, rows, io, 0), *out)
+    grads = {n: torch.empty(shape, dtype=io, device=dev) if t is None else t for n, t, shape, _, _ in out}
+    keep = _saved("flex_delta_bwd", desc, saved, dev)
     w = _seq_workspace(delta_workspace_size(desc, FLEX_PASS_BWD), ws, dev)
-    _run("flex_delta_bwd", dev, desc, _ptr(Q), _ptr(K), _ptr(V), _ptr(g), _ptr(beta), _ptr(off), *keep, _ptr(dO),
-         *(_ptr(out[n]) for n in ("dQ", "dK", "dV", "dg", "dbeta")), *w)
-    return out
+    _run("flex_delta_bwd", dev, desc, *(t.data_ptr() for t in (Q, K, V, g, beta, off)), *keep, dO.data_ptr(),
+         *(t.data_ptr() for t in grads.values()), *w)
+    return grads
 
 
 def flex_delta_step(desc: flex_delta_desc, q, k, v, g, beta, state, o=None):
     """One token of every sequence: q, k [B,Hk,d], v [B,H,dv], g, beta [B,H], state [B,H,d,dv]
     fp32 updated in place.  Returns o [B,H,dv]."""
     import torch
-    io, dev = _delta_inputs("flex_delta_step", desc, desc.B, q, k, v, g, beta,
-                            o=(o, (desc.B, desc.H, desc.dv), _io(desc), 0),
-                            state=(state, (desc.B, desc.H, desc.d, desc.dv), torch.float32, 0))
+    rows = (desc.B, desc.H, desc.dv)
+    io, dev = _delta_inputs("flex_delta_step", desc, desc.B, q, k, v, g, beta, ("o", o, rows, _io(desc), 0),
+                            ("state", state, (desc.B, desc.H, desc.d, desc.dv), torch.float32, 0))
     if o is None:
-        o = torch.empty(desc.B, desc.H, desc.dv, dtype=io, device=dev)
-    _run("flex_delta_step", dev, desc, _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(state), _ptr(o))
+        o = torch.empty(rows, dtype=io, device=dev)
+    _run("flex_delta_step", dev, desc, *(t.data_ptr() for t in (q, k, v, g, beta, state, o)))
     return o
 
 

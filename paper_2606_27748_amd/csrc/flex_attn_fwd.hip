@@ -281,30 +281,51 @@ __global__ __launch_bounds__(256) void k_attn_split(AttnArgs a) {
   }
 }
 
-// Joins the parts of k_attn_split in their order: one group of D / 4 lanes per row.
+// Joins the parts of k_attn_split: one workgroup per row, D / 4 lanes across and 1024 / D
+// groups of lanes that take the parts in turn, added up in a fixed order.  (One group for all parts
+// of a row waited out a memory latency per part: 67 us for 156 parts, where the parts themselves
+// took 20.)
 template <class T, int D>
 __global__ __launch_bounds__(256) void k_attn_combine(AttnArgs a) {
   using S = typename Io<T>::type;
-  constexpr int L4 = D / 4;
-  const size_t row = (size_t)blockIdx.x * (256 / L4) + threadIdx.x / L4;
-  const int d = threadIdx.x % L4 * 4;
+  constexpr int L4 = D / 4, G = 256 / L4;
+  __shared__ float fac[ATTN_PARTS];
+  __shared__ __attribute__((aligned(16))) f32x4 acc[G][L4];
+  __shared__ float red[8];
+  const size_t row = blockIdx.x;
+  const int t = threadIdx.x, c = t % L4, grp = t / L4;
   const int q = (int)(row / a.Hq);
   if (q < clamp_off(a.q_off[0], a.Tq) || q >= clamp_off(a.q_off[a.B], a.Tq)) return;
   const float* ml = a.part_ml + row * a.nsplit * 2;
+  const float* po = a.part_o + row * a.nsplit * D + 4 * c;
   const float sl2 = a.scale * LOG2E;
-  float m = -INFINITY;
-  for (int i = 0; i < a.nsplit; ++i) m = fmaxf(m, ml[2 * i]);
+  const int n = a.nsplit;   // at most ATTN_PARTS, a thread each
+  const float m_t = t < n ? ml[2 * t] : -INFINITY, l_t = t < n ? ml[2 * t + 1] : 0.f;
+  float m = m_t;
+#pragma unroll
+  for (int s = 1; s < WAVE; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
+  if (t % WAVE == 0) red[t / WAVE] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
   const float ref = m == -INFINITY ? 0.f : m;
-  float sum = 0.f;
+  const float f_t = __builtin_amdgcn_exp2f((m_t - ref) * sl2);
+  if (t < n) fac[t] = f_t;
+  float sum = l_t * f_t;
+  sum = group_sum(lane_sum<16>(sum));
+  if (t % WAVE == 0) red[4 + t / WAVE] = sum;
+  __syncthreads();
+  sum = (red[4] + red[5]) + (red[6] + red[7]);
   f32x4 v = zero4();
-  for (int i = 0; i < a.nsplit; ++i) {
-    const float f = __builtin_amdgcn_exp2f((ml[2 * i] - ref) * sl2);
-    sum += ml[2 * i + 1] * f;
-    v += *reinterpret_cast<const f32x4*>(a.part_o + (row * a.nsplit + i) * D + d) * f;
-  }
+#pragma unroll 4
+  for (int i = grp; i < n; i += G) v += *reinterpret_cast<const f32x4*>(po + (size_t)i * D) * fac[i];
+  acc[grp][c] = v;
+  __syncthreads();
+  if (grp != 0) return;
+#pragma unroll
+  for (int i = 1; i < G; ++i) v += acc[i][c];
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  store_io4(static_cast<S*>(a.O) + row * D + d, v * inv);
-  if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : m * a.scale + __logf(sum);
+  store_io4(static_cast<S*>(a.O) + row * D + 4 * c, v * inv);
+  if (a.lse && c == 0) a.lse[row] = sum == 0.f ? -INFINITY : m * a.scale + __logf(sum);
 }
 
 namespace {
@@ -314,8 +335,7 @@ hipError_t run_fwd(const AttnArgs& a, hipStream_t st) {
   if (a.nsplit > 0) {
     k_attn_split<T, D><<<a.B * a.Hkv * a.nsplit, 256, 0, st>>>(a);
     if (a.nsplit > 1) {
-      const size_t rows = (size_t)a.Tq * a.Hq, per = 256 / (D / 4);
-      k_attn_combine<T, D><<<(unsigned)((rows + per - 1) / per), 256, 0, st>>>(a);
+      k_attn_combine<T, D><<<(unsigned)((size_t)a.Tq * a.Hq), 256, 0, st>>>(a);
     }
   } else {
     constexpr int KT = sizeof(T) == 4 && D == 128 ? 32 : 64;

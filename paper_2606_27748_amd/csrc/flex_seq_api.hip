@@ -55,6 +55,7 @@ int attn_parts(const flex_attn_desc* d) {
   const int64_t wgs = (int64_t)d->B * d->Hkv, keys = d->Tk / d->B;
   int64_t n = (1024 + wgs - 1) / wgs;
   if (n > keys / 256) n = keys / 256;
+  if (n > ATTN_PARTS) n = ATTN_PARTS;
   return n < 1 ? 1 : (int)n;
 }
 size_t attn_part_rows(const flex_attn_desc* d) { return (size_t)d->Tq * d->Hq * (size_t)attn_parts(d); }

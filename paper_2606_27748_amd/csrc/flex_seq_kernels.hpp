@@ -11,6 +11,7 @@ void timing_mark(int kernel_class, hipStream_t st, bool begin);
 
 // Exact attention.  Strides are between consecutive rows, in elements; O, dO and
 // the gradients are contiguous.
+constexpr int ATTN_PARTS = 256;   // of one sequence's keys, at most
 struct AttnArgs {
   const void* Q;
   const void* K;
