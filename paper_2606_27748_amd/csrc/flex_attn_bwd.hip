@@ -11,6 +11,9 @@ namespace flex {
 namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr int BM = 128;   // rows per workgroup, 32 per wave
+// Blocks of 32 keys whose products a wave of the dQ sweep forms together: more to work on while the
+// exponentials of one are formed, and more registers.
+constexpr int blocks_at_once(int d) { return d <= 64 ? 2 : 1; }
 }  // namespace
 
 // Per row and head, transposed to [Hq][Tq] so that the sweeps read the statistics
@@ -32,7 +35,8 @@ __global__ __launch_bounds__(256) void k_attn_delta(AttnArgs a) {
   for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(o.get(j), g.get(j), sum);
   sum = lane_sum<L>(sum);
   if (in && e == 0) {
-    a.delta[(size_t)head * a.Tq + q] = a.lse[row] * LOG2E;
+    // a query that sees no key: all its products are masked, exp2(-inf - 0) = 0
+    a.delta[(size_t)head * a.Tq + q] = a.lse[row] == -INFINITY ? 0.f : a.lse[row] * LOG2E;
     a.delta[((size_t)a.Hq + head) * a.Tq + q] = sum;
   }
 }
@@ -40,10 +44,10 @@ __global__ __launch_bounds__(256) void k_attn_delta(AttnArgs a) {
 // dQ: the forward's tiles and orientation.  Per block of 32 keys S^T = K Q^T,
 // dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T.
 template <class T, int D, int KT>
-__global__ __launch_bounds__(256) void k_attn_dq(AttnArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, D>::ROW > 256 ? 1 : 2))) void k_attn_dq(AttnArgs a) {
   using S = typename Io<T>::type;
   using RT = RowTile<T, D>;
-  constexpr int KS = D / 16, NB = KT / 32, DT = D / 32;
+  constexpr int KS = D / 16, NB = KT / 32, DT = D / 32, GB = blocks_at_once(D) < NB ? blocks_at_once(D) : NB;
   constexpr int TILE = KT * RT::ROW;
   __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
   const int l = threadIdx.x % WAVE, c = l % 32, h = l / 32;
@@ -97,28 +101,39 @@ __global__ __launch_bounds__(256) void k_attn_dq(AttnArgs a) {
     if (i + 1 < ntiles) stage(i + 1);
     const char* LK = lds + (i & 1) * 2 * TILE;
     const char* LV = LK + TILE;
+    if (i * KT >= lim_hi) continue;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int j0 = i * KT + 32 * b;
-      if (j0 >= lim_hi) continue;
-      f32x16 s = zero16(), p = zero16();
+    for (int b0 = 0; b0 < NB; b0 += GB) {
+      f32x16 s[GB], p[GB];
 #pragma unroll
-      for (int k = 0; k < KS; ++k) mma32(s, RT::row(LK, 32 * b + c, k, h), q[k]);
+      for (int b = 0; b < GB; ++b) {
+        s[b] = p[b] = zero16();
 #pragma unroll
-      for (int k = 0; k < KS; ++k) mma32(p, RT::row(LV, 32 * b + c, k, h), g[k]);
+        for (int k = 0; k < KS; ++k) mma32(s[b], RT::row(LK, 32 * (b0 + b) + c, k, h), q[k]);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], sl2, -lse2)) * (p[e] - delta);
-      if (j0 + 32 > lim_lo) {
+        for (int k = 0; k < KS; ++k) mma32(p[b], RT::row(LV, 32 * (b0 + b) + c, k, h), g[k]);
+      }
+      if (i * KT + KT > lim_lo) {   // a hidden key's probability is zero
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (j0 + res_row(e, h) >= lim) s[e] = 0.f;
+        for (int b = 0; b < GB; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (i * KT + 32 * (b0 + b) + res_row(e, h) >= lim) {
+              s[b][e] = -INFINITY;
+              p[b][e] = 0.f;
+            }
       }
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const Frag<T> ds = frag_of<T>(s, k);
+      for (int b = 0; b < GB; ++b)
 #pragma unroll
-        for (int d = 0; d < DT; ++d) mma32(dq[d], RT::col(LK, 32 * b + 16 * k + 4 * h, 32 * d), ds);
-      }
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+          for (int e = 8 * k; e < 8 * k + 8; ++e)
+            s[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], sl2, -lse2)) * (p[b][e] - delta);
+          const Frag<T> ds = frag_of<T>(s[b], k);
+#pragma unroll
+          for (int d = 0; d < DT; ++d) mma32(dq[d], RT::col(LK, 32 * (b0 + b) + 16 * k + 4 * h, 32 * d), ds);
+        }
     }
   }
   if (qi >= t.n) return;
@@ -130,106 +145,159 @@ __global__ __launch_bounds__(256) void k_attn_dq(AttnArgs a) {
       store_io4(out + 32 * d + res_row(e, h), f32x4{dq[d][e], dq[d][e + 1], dq[d][e + 2], dq[d][e + 3]} * a.scale);
 }
 
-// dK and dV: 128 keys of one key head per workgroup, 32 per wave, their rows of K and
-// V in registers; the queries of every head of the group pass by in tiles of QT
-// rows.  S = Q K^T and dP = dO V^T come out with a lane per key and rows over queries,
-// as dV^T += dO^T P and dK^T += Q^T dS take them.
-template <class T, int D, int QT>
-__global__ __launch_bounds__(256) void k_attn_dkv(AttnArgs a) {
+// dK and dV: 128 keys of one key head per workgroup, 32 per wave; the queries of every head of
+// the group pass by in tiles of QT rows, divided among WQ groups of four waves, whose shares of the
+// sums are added up at the end.  S = Q K^T and dP = dO V^T come out with a lane per
+// key and rows over queries, as dV^T += dO^T P and dK^T += Q^T dS take them.
+// At d = 128 two wave groups halve the longest workgroup, that of the first keys under a causal mask (it
+// meets all queries of all heads): at 2 x 8192 tokens, 4 key heads, d = 128 the grid is 520
+// workgroups, all resident at once with one group, and waited for that one.  The rows of K and V
+// are in registers, or with KL in LDS: at d = 128 a wave then fits half a SIMD's registers
+// without spilling (a reload in the loop waits for the tile that is on its way, too).
+template <class T, int D, int QT, int WQ, bool KL>
+__global__ __launch_bounds__(256 * WQ) __attribute__((amdgpu_waves_per_eu(RowTile<T, D>::ROW > 256 ? 1 : 2))) void k_attn_dkv(
+    AttnArgs a) {
   using S = typename Io<T>::type;
   using RT = RowTile<T, D>;
-  constexpr int KS = D / 16, NB = QT / 32, DT = D / 32;
+  constexpr int KS = D / 16, DT = D / 32, NW = 4 * WQ, WR = QT / WQ, NB = WR / 32;
   constexpr int TILE = QT * RT::ROW;
-  __shared__ __attribute__((aligned(16))) char lds[4 * TILE];
+  constexpr int STAT = 64 * 4;
+  constexpr int BUF = 2 * TILE + 2 * STAT;   // Q and dO, their lse and delta
+  constexpr int JOIN = WQ > 1 ? BM * (D + 4) * 4 : 0;
+  constexpr int LDS = 2 * BUF + (KL ? 2 * BM * RT::ROW : 0);
+  __shared__ __attribute__((aligned(16))) char lds[LDS > JOIN ? LDS : JOIN];
+  const char* LKeys = lds + 2 * BUF;
+  const char* LVals = LKeys + BM * RT::ROW;
   const int l = threadIdx.x % WAVE, c = l % 32, h = l / 32;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), wk = w % 4, wq = w / 4;
   const TileCoord tc = tile_coord(seq_slots(a.Tk, a.B, BM), a.Hkv, false);
   const SeqTile t = find_tile<BM>(a.k_off, a.B, a.Tk, tc.slot);
   if (t.b < 0) return;
   const SeqRange qr = seq_range(a.q_off, t.b, a.Tq);
   const int grp = a.Hq / a.Hkv, kvh = tc.head;
-  const int rows = min(BM, t.n - t.tile * BM), first = t.tile * BM + 32 * w, shift = t.n - qr.n;
+  const int rows = min(BM, t.n - t.tile * BM), first = t.tile * BM + 32 * wk, shift = t.n - qr.n;
   const int kj = first + c;
   // the first query that sees a key of the workgroup, and of the wave
   const int q_wg = a.causal ? max(t.tile * BM - shift, 0) : 0;
   const int q_w = a.causal ? first - shift : 0;
-  const int tile0 = q_wg / QT, ntiles = max((qr.n + QT - 1) / QT - tile0, 0);
+  // from the last query tile down, all heads of each: workgroups of different keys then read the same
+  // rows at about the same time, through one L2
+  const int last = (qr.n + QT - 1) / QT - 1, total = grp * max(last + 1 - q_wg / QT, 0);
+  auto stage = [&](int i) {
+    char* L = lds + (i & 1) * BUF;
+    const int head = kvh * grp + i % grp, q0 = (last - i / grp) * QT, n = min(qr.n - q0, QT);
+    stage_tile<T, D, QT, NW>(L, row_words(static_cast<const S*>(a.Q) + head * D, qr.row0 + q0, a.qs, n, D),
+                             a.qs * (int)sizeof(S), w);
+    stage_tile<T, D, QT, NW>(L + TILE, row_words(static_cast<const S*>(a.dO) + head * D, qr.row0 + q0, a.Hq * D, n, D),
+                             a.Hq * D * (int)sizeof(S), w);
+    if (w < 2)   // lse, delta
+      stage_floats(L + 2 * TILE + w * STAT, row_words(a.delta + ((size_t)w * a.Hq + head) * a.Tq, qr.row0 + q0, 1, n, 1));
+  };
 
-  Frag<T> kf[KS], vf[KS];
+  Frag<T> kf[KL ? 1 : KS], vf[KL ? 1 : KS];
   {
-    const int r = 32 * w + c;
+    const int r = 32 * wk + c;
     const size_t row0 = t.row0 + t.tile * BM;
-    const auto rk = row_window(static_cast<const S*>(a.K) + kvh * D, row0, a.ks, rows, D);
-    const auto rv = row_window(static_cast<const S*>(a.V) + kvh * D, row0, a.vs, rows, D);
+    const S* K = static_cast<const S*>(a.K) + kvh * D;
+    const S* V = static_cast<const S*>(a.V) + kvh * D;
+    if constexpr (KL) {
+      stage_tile<T, D, BM, NW>(LKeys, row_words(K, row0, a.ks, rows, D), a.ks * (int)sizeof(S), w);
+      stage_tile<T, D, BM, NW>(LVals, row_words(V, row0, a.vs, rows, D), a.vs * (int)sizeof(S), w);
+    } else {
+      const auto rk = row_window(K, row0, a.ks, rows, D), rv = row_window(V, row0, a.vs, rows, D);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      kf[s] = window_frag<T>(rk, (r * a.ks + 16 * s + 8 * h) * (int)sizeof(S));
-      vf[s] = window_frag<T>(rv, (r * a.vs + 16 * s + 8 * h) * (int)sizeof(S));
+      for (int s = 0; s < KS; ++s) {
+        kf[s] = window_frag<T>(rk, (r * a.ks + 16 * s + 8 * h) * (int)sizeof(S));
+        vf[s] = window_frag<T>(rv, (r * a.vs + 16 * s + 8 * h) * (int)sizeof(S));
+      }
     }
   }
   f32x16 dk[DT], dv[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i) dk[i] = dv[i] = zero16();
   const float sl2 = a.scale * LOG2E;
-  const int total = grp * ntiles;
-  auto stage = [&](int i) {
-    char* L = lds + (i & 1) * 2 * TILE;
-    const int head = kvh * grp + i / ntiles, q0 = (tile0 + i % ntiles) * QT, n = min(qr.n - q0, QT);
-    stage_tile<T, D, QT, 4>(L, row_words(static_cast<const S*>(a.Q) + head * D, qr.row0 + q0, a.qs, n, D),
-                            a.qs * (int)sizeof(S), w);
-    stage_tile<T, D, QT, 4>(L + TILE, row_words(static_cast<const S*>(a.dO) + head * D, qr.row0 + q0, a.Hq * D, n, D),
-                            a.Hq * D * (int)sizeof(S), w);
-  };
   if (total > 0) stage(0);
   wait_reg_loads();
   for (int i = 0; i < total; ++i) {
     sync_tiles();   // tile i has arrived; tile i - 1 is no longer read
     if (i + 1 < total) stage(i + 1);
-    const char* LQ = lds + (i & 1) * 2 * TILE;
+    const char* LQ = lds + (i & 1) * BUF;
     const char* LG = LQ + TILE;
-    const int head = kvh * grp + i / ntiles, q0 = (tile0 + i % ntiles) * QT, n = min(qr.n - q0, QT);
-    const auto rl = row_window(a.delta + (size_t)head * a.Tq, qr.row0 + q0, 1, n, 1);
-    const auto rd = row_window(a.delta + ((size_t)a.Hq + head) * a.Tq, qr.row0 + q0, 1, n, 1);
+    const float* Ls = reinterpret_cast<const float*>(LG + TILE) + WR * wq;
+    const int q0 = (last - i / grp) * QT + WR * wq;   // this wave's rows
+    if (q0 + WR <= q_w || q0 >= qr.n) continue;
+    f32x16 s[NB], p[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const int i0 = q0 + 32 * b;
-      if (i0 + 31 < q_w || i0 >= qr.n) continue;
-      f32x4 ls[4], de[4];   // rows 8a + 4h + i
+      const int r = WR * wq + 32 * b + c;
+      s[b] = p[b] = zero16();
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int off = (32 * b + 8 * x + 4 * h) * 4;
+      for (int k = 0; k < KS; ++k)
+        mma32(s[b], RT::row(LQ, r, k, h), KL ? RT::row(LKeys, 32 * wk + c, k, h) : kf[KL ? 0 : k]);
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          ls[x][y] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rl, off + 4 * y, 0, 0));
-          de[x][y] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rd, off + 4 * y, 0, 0));
-        }
-      }
-      f32x16 s = zero16(), p = zero16();
+      for (int k = 0; k < KS; ++k)
+        mma32(p[b], RT::row(LG, r, k, h), KL ? RT::row(LVals, 32 * wk + c, k, h) : vf[KL ? 0 : k]);
+    }
+    if (a.causal && q0 < q_w + 31) {   // a hidden key's probability is zero
 #pragma unroll
-      for (int k = 0; k < KS; ++k) mma32(s, RT::row(LQ, 32 * b + c, k, h), kf[k]);
-#pragma unroll
-      for (int k = 0; k < KS; ++k) mma32(p, RT::row(LG, 32 * b + c, k, h), vf[k]);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], sl2, -ls[e / 4][e % 4]));
-        p[e] = s[e] * (p[e] - de[e / 4][e % 4]);
-      }
-      if (a.causal && i0 < q_w + 31) {
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (i0 + res_row(e, h) + shift < kj) s[e] = p[e] = 0.f;
-      }
+          if (q0 + 32 * b + res_row(e, h) + shift < kj) {
+            s[b][e] = -INFINITY;
+            p[b][e] = 0.f;
+          }
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const Frag<T> pf = frag_of<T>(s, k), df = frag_of<T>(p, k);
-        const int kb = 32 * b + 16 * k + 4 * h;
+#pragma unroll
+        for (int x = 2 * k; x < 2 * k + 2; ++x) {   // rows 8x + 4h + y; those behind the sequence are zeros
+          const f32x4 ls = *reinterpret_cast<const f32x4*>(Ls + 32 * b + 8 * x + 4 * h);
+          const f32x4 de = *reinterpret_cast<const f32x4*>(Ls + 64 + 32 * b + 8 * x + 4 * h);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int e = 4 * x + y;
+            s[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], sl2, -ls[y]));
+            p[b][e] = s[b][e] * (p[b][e] - de[y]);
+          }
+        }
+        const Frag<T> pf = frag_of<T>(s[b], k), df = frag_of<T>(p[b], k);
+        const int kb = WR * wq + 32 * b + 16 * k + 4 * h;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           mma32(dv[d], RT::col(LG, kb, 32 * d), pf);
           mma32(dk[d], RT::col(LQ, kb, 32 * d), df);
         }
       }
-    }
+  }
+  if (WQ > 1) {   // the second group's sums to the first, through LDS, dK and then dV
+    float* J = reinterpret_cast<float*>(lds) + (32 * wk + c) * (D + 4);
+    auto join = [&](f32x16 (&x)[DT]) {
+      __syncthreads();
+      if (wq == 1) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<f32x4*>(J + 32 * d + res_row(e, h)) = f32x4{x[d][e], x[d][e + 1], x[d][e + 2], x[d][e + 3]};
+      }
+      __syncthreads();
+      if (wq == 0) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(J + 32 * d + res_row(e, h));
+#pragma unroll
+            for (int y = 0; y < 4; ++y) x[d][e + y] += v[y];
+          }
+      }
+    };
+    join(dk);
+    join(dv);
+    if (wq != 0) return;
   }
   if (kj >= t.n) return;
   const size_t at = ((size_t)(t.row0 + kj) * a.Hkv + kvh) * D;
@@ -254,7 +322,10 @@ hipError_t run_bwd(const AttnArgs& a, hipStream_t st) {
     const size_t rows = (size_t)a.Tq * a.Hq, per = 256 / (D / 8);
     k_attn_delta<T, D><<<(unsigned)((rows + per - 1) / per), 256, 0, st>>>(a);
   }
-  if (a.Tk > 0) k_attn_dkv<T, D, R><<<seq_slots(a.Tk, a.B, BM) * a.Hkv, 256, 0, st>>>(a);
+  constexpr bool KL = IsBf16<T>::value && D == 128;
+  // us at 8279 packed tokens, 12 heads of 64: one group 84, two 105; at 16384 tokens, 16 heads of 128 on 4:
+  // one 1565 (one wave per SIMD), two 1340
+  if (a.Tk > 0) k_attn_dkv<T, D, R, KL ? 2 : 1, KL><<<seq_slots(a.Tk, a.B, BM) * a.Hkv, KL ? 512 : 256, 0, st>>>(a);
   if (a.Tq > 0) k_attn_dq<T, D, R><<<seq_slots(a.Tq, a.B, BM) * a.Hq, 256, 0, st>>>(a);
   timing_mark(FLEX_KERNEL_ATTN_BWD, st, false);
   return hipGetLastError();

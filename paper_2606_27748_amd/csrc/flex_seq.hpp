@@ -295,4 +295,11 @@ __device__ __forceinline__ void stage_tile(const char* L, u32x4 rs, int stride_b
   }
 }
 
+// 64 consecutive floats of a window to LDS, by one wave; zeros behind it.
+__device__ __forceinline__ void stage_floats(const char* L, u32x4 rs) {
+  const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) const char*)L);
+  const int off = threadIdx.x % WAVE * 4;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(rs) : "memory");
+}
+
 }  // namespace flex
