@@ -101,10 +101,23 @@ __device__ __forceinline__ void mma_ss(f32x4& c, const Split<__bf16>& a, const S
 }
 __device__ __forceinline__ void mma_ss(f32x4& c, const Split<float>& a, const Split<float>& b) { mma(c, a.hi, b.hi); }
 
-// Operand reads of a RowTile by 16 x 16 products.
+// Rows kept as the sweeps' lanes hold them: row r, columns c .. c+7 are lane (c / 8 % 4) 16 + r % 16's part
+// of the operand of columns c / 32 of the rows r / 16, 16 bytes a lane (fp32: two halves).  A store of
+// one is 1 KB in a row; as rows of D elements it would touch sixteen of them.
 template <class T, int D>
-struct Tile16 : RowTile<T, D> {
-  using R = RowTile<T, D>;
+struct FragRows {
+  static constexpr int E = 16 / sizeof(T);
+  static constexpr int FRAG = WAVE * 8 * (int)sizeof(T);   // bytes
+  static __device__ __forceinline__ int at(int r, int ch) {
+    const int c = ch * E;
+    return (r / 16 * (D / 32) + c / 32) * FRAG + (c % 8) / E * (WAVE * 16) + ((c / 8 % 4) * 16 + r % 16) * 16;
+  }
+};
+
+// Operand reads of a tile of rows in LDS by 16 x 16 products.
+template <class T, int D, class Rows = RowTile<T, D>>
+struct Tile16 : Rows {
+  using R = Rows;
   // four elements of row r from column c on (c a multiple of 4)
   static __device__ __forceinline__ const char* quad(const char* L, int r, int c) {
     return L + R::at(r, c / R::E) + (c % R::E) * (int)sizeof(T);
@@ -201,9 +214,9 @@ struct Tile16 : RowTile<T, D> {
 };
 
 // Two terms of a matrix kept as hi and lo tiles, `bytes` apart (fp32: one tile).
-template <class T, int D>
+template <class T, int D, class Rows = RowTile<T, D>>
 struct Pair16 {
-  using R = Tile16<T, D>;
+  using R = Tile16<T, D, Rows>;
   template <class F>
   static __device__ __forceinline__ Split<T> both(const char* L, int bytes, F read) {
     Split<T> s;
@@ -335,29 +348,39 @@ struct FragBox {
     return s;
   }
 };
-// The eight values of an operand's terms, the second term `lo` elements behind the first (0: not).
-__device__ __forceinline__ void store_terms(u16* p, size_t lo, const Split<__bf16>& s) {
+// Operand `frag` of a FragRows array, the second term `lo` elements behind the first (0: not).
+__device__ __forceinline__ void store_frag(u16* base, int frag, size_t lo, const Split<__bf16>& s) {
+  u16* p = base + (size_t)frag * (WAVE * 8) + threadIdx.x % WAVE * 8;
   *reinterpret_cast<bf16x8*>(p) = s.hi.v;
   if (lo) *reinterpret_cast<bf16x8*>(p + lo) = s.lo.v;
 }
-__device__ __forceinline__ void store_terms(float* p, size_t, const Split<float>& s) {
+__device__ __forceinline__ void store_frag(float* base, int frag, size_t, const Split<float>& s) {
+  float* p = base + (size_t)frag * (WAVE * 8) + threadIdx.x % WAVE * 4;
   *reinterpret_cast<f32x4*>(p) = f32x4{s.hi.v[0], s.hi.v[1], s.hi.v[2], s.hi.v[3]};
-  *reinterpret_cast<f32x4*>(p + 4) = f32x4{s.hi.v[4], s.hi.v[5], s.hi.v[6], s.hi.v[7]};
+  *reinterpret_cast<f32x4*>(p + WAVE * 4) = f32x4{s.hi.v[4], s.hi.v[5], s.hi.v[6], s.hi.v[7]};
 }
 
-// one element of a window, in the io type
-__device__ __forceinline__ u16 load1(__amdgpu_buffer_rsrc_t rs, int off, u16) {
-  return __builtin_amdgcn_raw_buffer_load_b16(rs, off, 0, 0);
-}
-__device__ __forceinline__ float load1(__amdgpu_buffer_rsrc_t rs, int off, float) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0));
-}
-__device__ __forceinline__ void store1(__amdgpu_buffer_rsrc_t rs, int off, u16 v) {
-  __builtin_amdgcn_raw_buffer_store_b16(v, rs, off, 0, 0);
-}
-__device__ __forceinline__ void store1(__amdgpu_buffer_rsrc_t rs, int off, float v) {
-  __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), rs, off, 0, 0);
-}
+// A wave's 16 columns of a chunk's rows (result tiles x), rounded to the io type and written as rows of
+// 32 bytes (fp32: 64) through the wave's own `box` in LDS: 16 bytes a lane in place of one element.
+template <class S>
+struct RowBox {
+  static constexpr int LD = 16 * (int)sizeof(S) + 16;   // bytes per row
+  static constexpr int BYTES = DC * LD;
+  static __device__ __forceinline__ void store(char* box, __amdgpu_buffer_rsrc_t rs, int stride, int col, const f32x4 (&x)[4]) {
+    const int l = threadIdx.x % WAVE, r16 = l % 16, g = l / 16;
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<S*>(box + tile_row(m, 4 * g + e) * LD + r16 * (int)sizeof(S)) = float_to_io<S>(x[m][e]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(S); ++i) {   // row l, its 16-byte units
+      const u32x4 v = *reinterpret_cast<const u32x4*>(box + l * LD + 16 * i);
+      __builtin_amdgcn_raw_buffer_store_b128(v, rs, (l * stride + col) * (int)sizeof(S) + 16 * i, 0, 0);
+    }
+  }
+};
 
 // four values as one or two terms, `lo` elements behind the first
 __device__ __forceinline__ void store_split4(u16* p, size_t lo, const f32x4& v) {

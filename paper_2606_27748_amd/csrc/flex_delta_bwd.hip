@@ -28,7 +28,8 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
   using LT = LowTri<T>;
   using CL = ChunkLds<T, D, 16 * NC>;
   constexpr int KS = D / 32, DT = D / 16, TERMS = IsBf16<T>::value ? 2 : 1;
-  constexpr int BOX = (4 + DT) * WAVE * 16;          // dR, Q^T (e^G dO')
+  // dR, Q^T (e^G dO'), and room to turn dV's columns into rows
+  constexpr int BOX_V = (4 + DT) * WAVE * 16, BOX = BOX_V + RowBox<S>::BYTES;
   constexpr int BUFS = 2 * CL::BYTES + NC * BOX <= 160 * 1024 ? 2 : 1;
   __shared__ __attribute__((aligned(16))) char lds[BUFS * CL::BYTES + NC * BOX];
   const int l = threadIdx.x % WAVE, r16 = l % 16, g = l / 16;
@@ -88,15 +89,18 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
     f32x4 st[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) st[i] = zero4();
-    for (int c = nchunks - 1; c >= 0; --c) {
-      const CL L{lds + (BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
-      S* so = static_cast<S*>(a.dst) + (((size_t)(slot0 + c) * a.H + head) * a.dv + col) * D + 8 * g;
-      Split<T> sb[KS];
+    Split<T> sb[KS];
+    auto keep_state = [&](int c) {
+      S* so = static_cast<S*>(a.dst) + ((size_t)(slot0 + c) * a.H + head) * a.dv * D;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         sb[s] = split<T>(st[2 * s], st[2 * s + 1]);
-        store_terms(so + 32 * s, 0, sb[s]);
+        store_frag(so, (col0 / 16 + pair) * KS + s, 0, sb[s]);
       }
+    };
+    if (nchunks > 0) keep_state(nchunks - 1);
+    for (int c = nchunks - 1; c >= 0; --c) {
+      const CL L{lds + (BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
       sync_lds();
       // dU = P^T dO' + w K dS, dR = T^T dU
       f32x4 y[4], dr[4];
@@ -149,6 +153,7 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
         for (int m = 0; m < 4; ++m) kc[m] = KT::col8(L.k(), 32 + 8 * g, i + m);
         mma_xs4(*reinterpret_cast<f32x4(*)[4]>(&st[i]), kc, k1);
       }
+      if (c > 0) keep_state(c - 1);
       if (BUFS == 1) sync_lds();
     }
     return;
@@ -187,21 +192,18 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
     }
     sync_lds();
     const size_t blk = (size_t)(slot0 + c) * a.H + head;
-    S* ro = static_cast<S*>(a.drt) + blk * (size_t)(TERMS * DC) * a.dv + (size_t)col * DC + 8 * g;
-    const auto rv = row_window(static_cast<S*>(a.dV) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
-                               min(DC, sq.n - c * DC), a.dv);
+    S* ro = static_cast<S*>(a.drt) + blk * (size_t)(TERMS * DC) * a.dv;
     f32x4 dr[4];
 #pragma unroll
     for (int m = 0; m < 4; ++m) dr[m] = box[m * WAVE];
-    store_terms(ro, (size_t)DC * a.dv, split<T>(dr[0], dr[1]));
-    store_terms(ro + 32, (size_t)DC * a.dv, split<T>(dr[2], dr[3]));
+    store_frag(ro, (col0 / 16 + pair) * 2, (size_t)DC * a.dv, split<T>(dr[0], dr[1]));
+    store_frag(ro, (col0 / 16 + pair) * 2 + 1, (size_t)DC * a.dv, split<T>(dr[2], dr[3]));
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      dr[m] *= be[m];
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        store1(rv, (tile_row(m, 4 * g + e) * a.H * a.dv + col) * (int)sizeof(S), float_to_io<S>(dr[m][e]));
-    }
+    for (int m = 0; m < 4; ++m) dr[m] *= be[m];
+    RowBox<S>::store(lds + BUFS * CL::BYTES + pair * BOX + BOX_V,
+                     row_window(static_cast<S*>(a.dV) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
+                                min(DC, sq.n - c * DC), a.dv),
+                     a.H * a.dv, col0 + 16 * pair, dr);
     if (BUFS == 1) sync_lds();
   }
 }
@@ -215,7 +217,8 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
   using KT = Tile16<T, D>;
   using VT = Tile16<T, VB>;
   using MT = Tile16<T, DC>;
-  using PT = Pair16<T, DC>;
+  using ST = Tile16<T, D, FragRows<T, D>>;
+  using PT = Pair16<T, DC, FragRows<T, DC>>;
   constexpr int KS = D / 32, DT = D / 16, VS = VB / 32;
   constexpr int TERMS = IsBf16<T>::value ? 2 : 1;
   constexpr int ROWS = DC * D * (int)sizeof(T), MAT = DC * DC * (int)sizeof(T);
@@ -269,17 +272,13 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
                                a.H * a.dv * (int)sizeof(S), w);
       stage_tile<T, VB, DC, 4>(LV, row_words(static_cast<const S*>(a.V) + (size_t)head * a.dv + v0, row0, a.vs, n, VB),
                                a.vs * (int)sizeof(S), w);
-      stage_tile<T, D, VB, 4>(LS, row_words(static_cast<const S*>(a.st) + (blk * a.dv + v0) * D, 0, D, VB, D),
-                              D * (int)sizeof(S), w);
-      stage_tile<T, D, VB, 4>(LD, row_words(static_cast<const S*>(a.dst) + (blk * a.dv + v0) * D, 0, D, VB, D),
-                              D * (int)sizeof(S), w);
+      stage_linear<SROWS / 1024, 4>(LS, static_cast<const S*>(a.st) + (blk * a.dv + v0) * D, w);
+      stage_linear<SROWS / 1024, 4>(LD, static_cast<const S*>(a.dst) + (blk * a.dv + v0) * D, w);
 #pragma unroll
       for (int i = 0; i < TERMS; ++i) {
         const size_t at = ((blk * TERMS + i) * a.dv + v0) * DC;
-        stage_tile<T, DC, VB, 4>(LU + i * VROWS, row_words(static_cast<const S*>(a.ut) + at, 0, DC, VB, DC),
-                                 DC * (int)sizeof(S), w);
-        stage_tile<T, DC, VB, 4>(LR + i * VROWS, row_words(static_cast<const S*>(a.drt) + at, 0, DC, VB, DC),
-                                 DC * (int)sizeof(S), w);
+        stage_linear<VROWS / 1024, 4>(LU + i * VROWS, static_cast<const S*>(a.ut) + at, w);
+        stage_linear<VROWS / 1024, 4>(LR + i * VROWS, static_cast<const S*>(a.drt) + at, w);
       }
       if (threadIdx.x < DC) lG[threadIdx.x] = reinterpret_cast<const double*>(prep + 1024)[threadIdx.x];
       sync_tiles();
@@ -296,7 +295,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
         }
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
-          const Frag<T> sf = KT::col(LS, c0, c0 + 4, 16 * i), df = KT::col(LD, c0, c0 + 4, 16 * i);
+          const Frag<T> sf = ST::col(LS, c0, c0 + 4, 16 * i), df = ST::col(LD, c0, c0 + 4, 16 * i);
           mma(qi[i], sf, go);
           mma_xs(fi[i], sf, dr);
           mma_xs(wi[i], df, u);

@@ -187,7 +187,8 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
   using CL = ChunkLds<T, D, 16 * NC>;
   using FB = FragBox<T>;
   constexpr int KS = D / 32, DT = D / 16, TERMS = IsBf16<T>::value ? 2 : 1;
-  constexpr int BOX = (KS + 2) * FB::BYTES;                          // S, then U
+  // S as operands, U as results, and room to turn O's columns into rows
+  constexpr int BOX_U = KS * FB::BYTES, BOX_O = BOX_U + 4 * WAVE * 16, BOX = BOX_O + RowBox<S>::BYTES;
   constexpr int BUFS = 2 * CL::BYTES + NC * BOX <= 160 * 1024 ? 2 : 1;
   __shared__ __attribute__((aligned(16))) char lds[BUFS * CL::BYTES + NC * BOX];
   const int l = threadIdx.x % WAVE, r16 = l % 16, g = l / 16;
@@ -250,14 +251,18 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
     for (int i = 0; i < DT; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) st[i][e] = a.state0 ? a.state0[sbase + (size_t)tile_row(i, 4 * g + e) * a.dv] : 0.f;
-    for (int c = 0; c < nchunks; ++c) {
-      const CL L{lds + (BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
-      Split<T> sb[KS];
+    f32x4* box_u = reinterpret_cast<f32x4*>(box + BOX_U) + l;
+    Split<T> sb[KS];
+    auto put_state = [&]() {
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         sb[s] = split<T>(st[2 * s], st[2 * s + 1]);
         FB::put(box + s * FB::BYTES, l, sb[s]);
       }
+    };
+    put_state();
+    for (int c = 0; c < nchunks; ++c) {
+      const CL L{lds + (BUFS == 2 ? (c & 1) * CL::BYTES : 0)};
       sync_lds();
       f32x4 u[4];
 #pragma unroll
@@ -277,10 +282,11 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
         for (int e = 0; e < 4; ++e) u[m][e] = be[e] * ((float)vc[e] - eg[e] * u[m][e]);
       }
       LT::apply(u, L.t(), r16, g);
-      FB::put(box + KS * FB::BYTES, l, split<T>(u[0], u[1]));
-      FB::put(box + (KS + 1) * FB::BYTES, l, split<T>(u[2], u[3]));
 #pragma unroll
-      for (int m = 0; m < 4; ++m) u[m] *= L.scal(1, m, g);
+      for (int m = 0; m < 4; ++m) {
+        box_u[m * WAVE] = u[m];
+        u[m] *= L.scal(1, m, g);
+      }
       const Split<T> w0 = split<T>(u[0], u[1]), w1 = split<T>(u[2], u[3]);
       const float last = L.last();
       sync_lds();
@@ -297,6 +303,7 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
         for (int m = 0; m < 4; ++m) kc[m] = KT::col8(L.k(), 32 + 8 * g, i + m);
         mma_xs4(*reinterpret_cast<f32x4(*)[4]>(&st[i]), kc, w1);
       }
+      put_state();   // the box is free: its reader has passed the second barrier
       if (BUFS == 1) sync_lds();
     }
     if (a.state) {
@@ -322,25 +329,25 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
 #pragma unroll
       for (int m = 0; m < 4; ++m) qr[m] = KT::row8(L.q(), tile_row(m, r16), 32 * s + 8 * g);
       mma_xs4(o, qr, sb);
-      if (SAVE) store_terms(static_cast<S*>(a.st) + (blk * a.dv + col) * D + 32 * s + 8 * g, 0, sb);
+      if (SAVE) store_frag(static_cast<S*>(a.st) + blk * a.dv * D, (col0 / 16 + pair) * KS + s, 0, sb);
     }
 #pragma unroll
     for (int m = 0; m < 4; ++m) o[m] *= L.scal(0, m, g);
     sync_lds();
-    const Split<T> u0 = FB::get(box + KS * FB::BYTES, l), u1 = FB::get(box + (KS + 1) * FB::BYTES, l);
+    const f32x4* box_u = reinterpret_cast<const f32x4*>(box + BOX_U) + l;
+    const Split<T> u0 = split<T>(box_u[0], box_u[WAVE]), u1 = split<T>(box_u[2 * WAVE], box_u[3 * WAVE]);
     if (SAVE) {
-      S* uo = static_cast<S*>(a.ut) + blk * (size_t)(TERMS * DC) * a.dv + (size_t)col * DC + 8 * g;
-      store_terms(uo, (size_t)DC * a.dv, u0);
-      store_terms(uo + 32, (size_t)DC * a.dv, u1);
+      S* uo = static_cast<S*>(a.ut) + blk * (size_t)(TERMS * DC) * a.dv;
+      store_frag(uo, (col0 / 16 + pair) * 2, (size_t)DC * a.dv, u0);
+      store_frag(uo, (col0 / 16 + pair) * 2 + 1, (size_t)DC * a.dv, u1);
     }
-    const auto ro = row_window(static_cast<S*>(a.O) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
-                               min(DC, sq.n - c * DC), a.dv);
     LT::mul(o, L.p(), r16, g, u0, u1);
 #pragma unroll
-    for (int m = 0; m < 4; ++m)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        store1(ro, (tile_row(m, 4 * g + e) * a.H * a.dv + col) * (int)sizeof(S), float_to_io<S>(o[m][e] * a.scale));
+    for (int m = 0; m < 4; ++m) o[m] *= a.scale;
+    RowBox<S>::store(box + BOX_O,
+                     row_window(static_cast<S*>(a.O) + (size_t)head * a.dv, sq.row0 + c * DC, a.H * a.dv,
+                                min(DC, sq.n - c * DC), a.dv),
+                     a.H * a.dv, col0 + 16 * pair, o);
     if (BUFS == 1) sync_lds();
   }
 }

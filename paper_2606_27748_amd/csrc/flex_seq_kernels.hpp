@@ -45,8 +45,8 @@ hipError_t launch_attn_bwd(const AttnArgs& a, bool bf16, int d, hipStream_t st);
 //   prep   T, then P (lower triangular [64][64]): hi and lo bf16, or fp32, each as the rows 0..31
 //          of the columns 0..31 and the rows 32..63, in the order of the sweeps' LDS tiles;
 //          e^G [64], w [64], b [64] (fp32) in 1 KB; G [64] (fp64) in 1 KB
-//   st     the state at the chunk's start, transposed [dv][d], io type   (training)
-//   ut     U transposed [dv][64], hi and lo (fp32: one)                  (training)
+//   st     the state at the chunk's start as FragRows [dv][d], io type   (training)
+//   ut     U as FragRows [dv][64], hi and lo (fp32: one)                 (training)
 constexpr int DELTA_CHUNK = 64;
 constexpr int DELTA_MAT_BYTES = (32 * 32 + 32 * 64) * 4;   // T or P: hi and lo, or fp32
 constexpr int DELTA_SWEEP_BYTES = 2 * DELTA_MAT_BYTES + 1024;
@@ -70,8 +70,8 @@ struct DeltaArgs {
   void* ut;
   // backward
   const void* dO;
-  void* dst;             // gradient of the state at the chunk's end, transposed [dv][d], io type
-  void* drt;             // gradient of T^-1 U = b (V - e^G K S), transposed [dv][64], hi and lo
+  void* dst;             // gradient of the state at the chunk's end, as st
+  void* drt;             // gradient of T^-1 U = b (V - e^G K S), as ut
   void* dQ;
   void* dK;
   void* dV;
