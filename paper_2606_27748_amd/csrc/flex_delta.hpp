@@ -31,7 +31,7 @@ constexpr int DC = DELTA_CHUNK;
 
 // Waves of a sweep's workgroup that stage its chunks.  Loads to LDS (or to registers) of one wave
 // alone move 18 bytes a clock from L2, of two 27, of four 40, of eight 43.
-constexpr int NL = 4;
+constexpr int NL = 2;
 
 // Workgroup of a sweep -> sequence and value head, and which of `parts` blocks of its columns: the
 // workgroups of one head are a multiple of eight apart, on one XCD, where that is possible.

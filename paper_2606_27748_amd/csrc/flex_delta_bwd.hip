@@ -210,7 +210,8 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
 
 // One workgroup per chunk and key head, over the value heads of its group in order; wave w has
 // the tokens 16 w .. + 15, a lane per token, and holds the rows of dQ^T and dK^T
-// ([d x 16 tokens]).  S, dS, U, dR, dO and V pass through LDS in blocks of VB value columns.
+// ([d x 16 tokens]).  S, dS, U, dR, dO and V pass through LDS in blocks of VB value columns, the next
+// block on its way while one is worked on where two fit.
 template <class T, int D, int VB>
 __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
   using S = typename Io<T>::type;
@@ -224,20 +225,15 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
   constexpr int ROWS = DC * D * (int)sizeof(T), MAT = DC * DC * (int)sizeof(T);
   constexpr int VROWS = DC * VB * (int)sizeof(T);     // a block of dO or V, or of one term of U or dR
   constexpr int SROWS = VB * D * (int)sizeof(T);      // a block of S or dS
-  constexpr int BLOCK = 2 * VROWS + 2 * SROWS + 2 * TERMS * VROWS;
-  __shared__ __attribute__((aligned(16))) char lds[2 * ROWS + (BLOCK > 2 * MAT ? BLOCK : 2 * MAT)];
+  constexpr int STAGED = 2 * VROWS + 2 * SROWS + 2 * TERMS * VROWS;
+  constexpr int BLOCK = STAGED > 2 * MAT ? STAGED : 2 * MAT;
+  // rows of 256 bytes and more take a SIMD's registers per wave: one workgroup per CU, and room for two blocks
+  constexpr int BUFS = D * (int)sizeof(T) >= 256 && 2 * ROWS + 2 * BLOCK <= 156 * 1024 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) char lds[2 * ROWS + BUFS * BLOCK];
   __shared__ double lG[DC];
   __shared__ float col_x[4][DC], row_g[DC], sum_z[4], sum_s[4];
   const char* LK = lds;
   const char* LQ = lds + ROWS;
-  const char* LG = lds + 2 * ROWS;            // dO
-  const char* LV = LG + VROWS;
-  const char* LS = LV + VROWS;                // S
-  const char* LD = LS + SROWS;                // dS
-  const char* LU = LD + SROWS;                // U
-  const char* LR = LU + TERMS * VROWS;        // dR
-  char* LP = lds + 2 * ROWS;                  // afterwards: dP D and M, rows i
-  char* LM = LP + MAT;
 
   const int l = threadIdx.x % WAVE, r16 = l % 16, g = l / 16;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
@@ -253,6 +249,29 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
 #pragma unroll
   for (int i = 0; i < DT; ++i) dq[i] = dk[i] = zero4();
 
+  const int nvb = a.dv / VB;
+  auto stage = [&](int i) {   // block i % nvb of head i / nvb
+    const int head = kh * grp + i / nvb, v0 = i % nvb * VB;
+    const size_t blk = (size_t)slot * a.H + head;
+    const char* L = lds + 2 * ROWS + (BUFS == 2 ? (i & 1) * BLOCK : 0);
+    stage_tile<T, VB, DC, 4>(L, row_words(static_cast<const S*>(a.dO) + (size_t)head * a.dv + v0, row0, a.H * a.dv, n, VB),
+                             a.H * a.dv * (int)sizeof(S), w);
+    L += VROWS;
+    stage_tile<T, VB, DC, 4>(L, row_words(static_cast<const S*>(a.V) + (size_t)head * a.dv + v0, row0, a.vs, n, VB),
+                             a.vs * (int)sizeof(S), w);
+    L += VROWS;
+    stage_linear<SROWS / 1024, 4>(L, static_cast<const S*>(a.st) + (blk * a.dv + v0) * D, w);
+    stage_linear<SROWS / 1024, 4>(L + SROWS, static_cast<const S*>(a.dst) + (blk * a.dv + v0) * D, w);
+    L += 2 * SROWS;
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) {
+      const size_t at = ((blk * TERMS + k) * a.dv + v0) * DC;
+      stage_linear<VROWS / 1024, 4>(L + k * VROWS, static_cast<const S*>(a.ut) + at, w);
+      stage_linear<VROWS / 1024, 4>(L + (TERMS + k) * VROWS, static_cast<const S*>(a.drt) + at, w);
+    }
+  };
+  if (BUFS == 2) stage(0);
+  int it = 0;
   for (int h = 0; h < grp; ++h) {
     const int head = kh * grp + h;
     const size_t blk = (size_t)slot * a.H + head;
@@ -266,22 +285,21 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) dp[i] = da[i] = zero4();
     float rv = 0.f, ss = 0.f;
-    for (int v0 = 0; v0 < a.dv; v0 += VB) {
-      sync_tiles();   // what was staged or written before is no longer read
-      stage_tile<T, VB, DC, 4>(LG, row_words(static_cast<const S*>(a.dO) + (size_t)head * a.dv + v0, row0, a.H * a.dv, n, VB),
-                               a.H * a.dv * (int)sizeof(S), w);
-      stage_tile<T, VB, DC, 4>(LV, row_words(static_cast<const S*>(a.V) + (size_t)head * a.dv + v0, row0, a.vs, n, VB),
-                               a.vs * (int)sizeof(S), w);
-      stage_linear<SROWS / 1024, 4>(LS, static_cast<const S*>(a.st) + (blk * a.dv + v0) * D, w);
-      stage_linear<SROWS / 1024, 4>(LD, static_cast<const S*>(a.dst) + (blk * a.dv + v0) * D, w);
-#pragma unroll
-      for (int i = 0; i < TERMS; ++i) {
-        const size_t at = ((blk * TERMS + i) * a.dv + v0) * DC;
-        stage_linear<VROWS / 1024, 4>(LU + i * VROWS, static_cast<const S*>(a.ut) + at, w);
-        stage_linear<VROWS / 1024, 4>(LR + i * VROWS, static_cast<const S*>(a.drt) + at, w);
+    const double Gl = threadIdx.x < DC ? reinterpret_cast<const double*>(prep + 1024)[threadIdx.x] : 0.0;
+    for (int vb = 0; vb < nvb; ++vb, ++it) {
+      if (BUFS == 1) {
+        sync_tiles();   // what was staged or written before is no longer read
+        stage(it);
       }
-      if (threadIdx.x < DC) lG[threadIdx.x] = reinterpret_cast<const double*>(prep + 1024)[threadIdx.x];
       sync_tiles();
+      if (BUFS == 2 && it + 1 < grp * nvb) stage(it + 1);
+      if (vb == 0 && threadIdx.x < DC) lG[threadIdx.x] = Gl;
+      const char* LG = lds + 2 * ROWS + (BUFS == 2 ? (it & 1) * BLOCK : 0);   // dO, V, S, dS, U, dR
+      const char* LV = LG + VROWS;
+      const char* LS = LV + VROWS;
+      const char* LD = LS + SROWS;
+      const char* LU = LD + SROWS;
+      const char* LR = LU + TERMS * VROWS;
 #pragma unroll
       for (int s = 0; s < VS; ++s) {
         const int c0 = 32 * s + 8 * g;   // value columns c0 .. c0 + 7 in this lane's slots
@@ -320,6 +338,9 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
         }
       }
     }
+    // the last block's place takes dP D and M, rows i
+    char* LP = lds + 2 * ROWS + (BUFS == 2 ? ((it - 1) & 1) * BLOCK : 0);
+    char* LM = LP + MAT;
     // the rows' parts of dG and dbeta
     float dot_q = 0.f, dot_f = 0.f, dot_z = 0.f;
     const float ge = eg * a.scale;
@@ -387,7 +408,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
       sum_z[w] = z16;
       sum_s[w] = ss;
     }
-    __syncthreads();   // the last block of S, dS, U, dR is no longer read
+    sync_lds();   // the last block is no longer read; the next may be on its way
     if (w == 0) {
       const float gv = l < n ? a.g[(size_t)(row0 + l) * a.H + head] : 0.f;
       float x = row_g[l] - ((col_x[0][l] + col_x[1][l]) + (col_x[2][l] + col_x[3][l]));
@@ -427,7 +448,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
           mma(dk[i], kc, mf);
         }
       }
-    __syncthreads();
+    sync_lds();
     // dK += (dP D)^T Q + M^T K over the rows that follow
 #pragma unroll
     for (int s = 0; s < 2; ++s)
