@@ -315,7 +315,7 @@ int32_t flex_attn_workspace_size(const flex_attn_desc* desc, int32_t pass, size_
  * rounded to bf16 for the product with V.  With at most 64 rows (queries times
  * heads of a group) per sequence on average the keys of a sequence are split over
  * several workgroups, joined in a fixed order.
- * A key row that a query does not see takes no part, whatever it holds. */
+ * Key rows that a query does not see take no part, whatever they hold. */
 int32_t flex_attn_fwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
                       const int32_t* q_off, const int32_t* k_off, const int32_t* k_len,
                       void* O, float* lse, void* ws, size_t ws_bytes, void* stream);
@@ -326,7 +326,10 @@ int32_t flex_attn_fwd(const flex_attn_desc* desc, const void* Q, const void* K, 
  *   dQ [Tq,Hq,d], dK, dV [Tk,Hkv,d]   io_dtype outputs: the rows of the
  *                     sequences are overwritten
  * With FLEX_BF16 the probabilities and the gradients of the logits are rounded to
- * bf16 for the products over them. */
+ * bf16 for the products over them.  Rows of other sequences and behind the last
+ * one take no part; within a sequence, NaN or infinities in a row of K, V or dO
+ * may also reach the gradients of rows that the causal mask hides from it, in
+ * the same block of 64. */
 int32_t flex_attn_bwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
                       const int32_t* q_off, const int32_t* k_off, const void* O, const float* lse,
                       const void* dO, void* dQ, void* dK, void* dV,

@@ -327,6 +327,8 @@ def _size(fn, desc, *args):
 def _expect(what, dev, tensors):
     """Each (name, tensor, shape, dtype, row stride or 0 for contiguous) as it must be; None where one
     is left out."""
+    if dev.type != "cuda":
+        raise FlexError(FLEX_ERR_INVALID_ARG, f"{what}: tensors must be on the GPU")
     for name, t, shape, dtype, stride in tensors:
         if t is None:
             continue

@@ -45,6 +45,48 @@ struct Soft {
   }
 };
 
+// A hidden key has the probability zero, and zero times a V row with NaN or infinities is NaN.  Where
+// a wave's sums are not finite, this forms them again over the keys that each query sees, one key
+// at a time (keys lo .. hi - 1 of the sequence, lane limits lim, final maximum m).
+template <class T, int D>
+__device__ __forceinline__ bool not_finite(const f32x16 (&o)[D / 32]) {
+  float x = 0.f;   // NaN from the first NaN or infinity on
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x = __builtin_fmaf(o[d][e], 0.f, x);
+  return x != 0.f;
+}
+template <class T, int D>
+__device__ __forceinline__ void sum_seen(f32x16 (&o)[D / 32], const Frag<T> (&q)[D / 16],
+                                                   const typename Io<T>::type* K, const typename Io<T>::type* V, int ks,
+                                                   int vs, int lo, int hi, int lim, float m, float sl2) {
+  using S = typename Io<T>::type;
+  const int h = threadIdx.x % WAVE / 32;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) o[d] = zero16();
+  for (int j = lo; j < hi; ++j) {
+    const S* k = K + (size_t)j * ks + 8 * h;
+    const S* v = V + (size_t)j * vs;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      Frag<T> f;
+      load8(f, k + 16 * i, true);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = __builtin_fmaf(f.get(e), q[i].get(e), s);
+    }
+    s = half_sum(s);
+    const float p = (float)(T)__builtin_amdgcn_exp2f((s - m) * sl2);
+    if (j < lim) {
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] = __builtin_fmaf(p, io_to_float(v[32 * d + res_row(e, h)]), o[d][e]);
+    }
+  }
+}
+
 }  // namespace
 
 // Prompts.  One workgroup: 128 queries of one head, 32 per wave (in registers as
@@ -131,6 +173,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, 
         for (int d = 0; d < DT; ++d) mma32(o[d], RT::col(LV, 32 * b + 16 * k + 4 * h, 32 * d), p);
       }
   }
+  if (a.causal && __any(qi < t.n && not_finite<T, D>(o)))
+    sum_seen<T, D>(o, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, 0, min(lim_hi, kr.n), lim,
+                   sm.m, sl2);
   if (qi >= t.n) return;
   const float l_all = half_sum(sm.l);
   const float inv = l_all > 0.f ? 1.f / l_all : (l_all == 0.f ? 0.f : l_all);   // no key: zeros; NaN stays
@@ -226,6 +271,20 @@ __global__ __launch_bounds__(256) void k_attn_split(AttnArgs a) {
         for (int d = 0; d < DT; ++d) mma32(o[d], RT::col(LV, 16 * k + 4 * h, 32 * d), p);
       }
       if (BUFS == 2) buf ^= 1;
+    }
+    if (a.causal && __any(valid && not_finite<T, D>(o))) {   // this wave's blocks, one after the other
+      f32x16 x[DT];
+      f32x16 total[DT];
+#pragma unroll
+      for (int d = 0; d < DT; ++d) total[d] = zero16();
+      for (int j0 = start; j0 < hi; j0 += 128) {
+        sum_seen<T, D>(x, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, j0, min(j0 + 32, hi), lim,
+                       sm.m, sl2);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) total[d] += x[d];
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] = total[d];
     }
     // join the four waves: statistics, then the scaled sums through LDS
     const float lw = half_sum(sm.l);

@@ -323,7 +323,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
           if (j <= w) {
             const Split<T> uj = PT::col(LU, VROWS, c0, c0 + 4, 16 * j);
             mma_sx(dp[j], uj, go);
-            mma_xs(da[j], uj.hi, dr);
+            mma_ss(da[j], uj, dr);
           }
       }
       for (int i = threadIdx.x; i < SROWS / 16; i += 256) {   // <S, dS>: the same place in both tiles
@@ -433,19 +433,12 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
       if (2 * s <= w) {
-        Frag<T> pf, mf;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          pf.set(e, dp[2 * s][e]);
-          pf.set(4 + e, dp[2 * s + 1][e]);
-          mf.set(e, da[2 * s][e]);
-          mf.set(4 + e, da[2 * s + 1][e]);
-        }
+        const Split<T> pf = split<T>(dp[2 * s], dp[2 * s + 1]), mf = split<T>(da[2 * s], da[2 * s + 1]);
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
           const Frag<T> kc = KT::col(LK, 32 * s + 4 * g, 32 * s + 16 + 4 * g, 16 * i);
-          mma(dq[i], kc, pf);
-          mma(dk[i], kc, mf);
+          mma_xs(dq[i], kc, pf);
+          mma_xs(dk[i], kc, mf);
         }
       }
     sync_lds();
