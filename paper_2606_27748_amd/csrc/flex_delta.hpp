@@ -29,8 +29,10 @@ namespace flex {
 
 constexpr int DC = DELTA_CHUNK;
 
-// Waves of a sweep's workgroup that stage its chunks.  Loads to LDS (or to registers) of one wave
-// alone move 18 bytes a clock from L2, of two 27, of four 40, of eight 43.
+// Waves of a sweep's workgroup that stage its chunks.  Two, although loads of one wave alone move 18 bytes a
+// clock from L2, of two 27, of four 40: four hold up the carrying waves' SIMDs and the stores.  us of
+// the forward and reverse sweeps at d = 128, 32 heads, 8192 tokens with one, two and four: 279, 260,
+// 296 and 281, 284, 316; the forward over 9 ragged prompts 126, 127, 124.
 constexpr int NL = 2;
 
 // Workgroup of a sweep -> sequence and value head, and which of `parts` blocks of its columns: the

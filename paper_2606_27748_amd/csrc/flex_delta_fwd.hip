@@ -176,9 +176,11 @@ __global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
 // The sweep: one workgroup per sequence, value head and 16 NC columns of the state.  What the
 // next chunk waits for is one wave's per 16 columns (S -> K S -> U -> S, the state in its
 // registers); a second forms Q S and O beside it from the operands that the first leaves in
-// LDS, and writes O and what a backward needs; NL waves stage the chunks.  Left to one wave, all of it
-// took 4.3 us a chunk at d = 128 (256 waves for 32 heads, three quarters of the SIMDs without
-// work), with the second wave doing the staging too 2.9.
+// LDS, and writes O and what a backward needs; NL waves stage the chunks.  What bounds it is that
+// chain: 82 matrix instructions of 16 clocks and the splits between them, about 4200 clocks a
+// chunk at d = 128, of which the instructions fill 1300.  One wave for all of it took 4.3 us a chunk
+// (256 waves for 32 heads of 128, three quarters of the SIMDs without work), two waves 2.9, these
+// 2.0 (with what a backward needs kept: 12 KB of it and 4 KB of O per chunk and workgroup).
 template <class T, int D, int NC, bool SAVE>
 __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_delta_sweep(DeltaArgs a) {
   using S = typename Io<T>::type;
