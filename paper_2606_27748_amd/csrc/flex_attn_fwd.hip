@@ -190,7 +190,30 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, 
   if (a.lse && h == 0) a.lse[row] = l_all == 0.f ? -INFINITY : sm.m * a.scale + __logf(l_all);
 }
 
-// Few rows against many keys.  One workgroup: one sequence, one key head and one
+// Blocks of 32 rows (queries times the `grp` heads that share a key head) in slots: the first B are the
+// sequences' first blocks, so that single tokens need no search and what has no block comes
+// last; those behind a sequence's first start at slot B + off grp / 32, which leaves room for any lengths.
+// (One workgroup for all blocks of a sequence: 965 us for a prompt of 2000 among 63 single tokens with 8
+// heads of 64, these 64.  A slot that may be empty next to each full one cost 18 of 55 us: a
+// workgroup takes a CU's LDS, and the full one behind it waits.)
+struct RowBlock {
+  int b, block;
+};
+inline int block_slots(int T, int B, int grp) { return B + (T > 0 ? (T * grp - 1) / 32 : 0); }
+__device__ __forceinline__ RowBlock find_block(const int32_t* __restrict__ off, int B, int T, int grp, int slot) {
+  if (slot < B) return {slot, 0};
+  const int l = threadIdx.x % WAVE, e = slot - B;
+  int cnt = 0;   // sequences whose further blocks start by here; the first's do
+  for (int b0 = 0; b0 < B; b0 += WAVE) {
+    const int c = __popcll(__ballot(b0 + l < B && clamp_off(off[min(b0 + l, B - 1)], T) * grp / 32 <= e));
+    cnt += c;
+    if (c < WAVE) break;
+  }
+  const int b = max(cnt - 1, 0), k = e - clamp_off(off[b], T) * grp / 32;
+  return {__builtin_amdgcn_readfirstlane(b), __builtin_amdgcn_readfirstlane(k < 0 ? 1 << 25 : k + 1)};
+}
+
+// Few rows against many keys.  One workgroup: 32 rows of a sequence, one key head and one
 // part of its keys; the columns are the rows of all the query heads that share it
 // (row r: query r / group, head r % group).  Its waves take every fourth block of
 // 32 keys, each through its own LDS, without a barrier, and join at the end.
@@ -208,135 +231,138 @@ __global__ __launch_bounds__(256) void k_attn_split(AttnArgs a) {
   const int l = threadIdx.x % WAVE, c = l % 32, h = l / 32;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int grp = a.Hq / a.Hkv;
-  const int part = blockIdx.x % a.nsplit, bk = blockIdx.x / a.nsplit;
-  const int kvh = bk % a.Hkv, b = bk / a.Hkv;
-  const int q0 = clamp_off(a.q_off[b], a.Tq), nq = max(clamp_off(a.q_off[b + 1], a.Tq) - q0, 0);
-  const SeqRange kr = seq_range(a.k_off, b, a.Tk, a.k_len);
+  const int part = blockIdx.x % a.nsplit, id = blockIdx.x / a.nsplit;
+  const int kvh = id % a.Hkv;
+  const RowBlock rb = find_block(a.q_off, a.B, a.Tq, grp, id / a.Hkv);
+  const SeqRange qr = seq_range(a.q_off, rb.b, a.Tq);
+  const int q0 = qr.row0, nq = qr.n, r0 = 32 * rb.block;
+  if (r0 >= nq * grp) return;
+  const SeqRange kr = seq_range(a.k_off, rb.b, a.Tk, a.k_len);
   const int per = ((kr.n + a.nsplit - 1) / a.nsplit + 127) / 128 * 128;
-  const int lo = min(part * per, kr.n), hi = min(lo + per, kr.n), shift = kr.n - nq;
+  const int shift = kr.n - nq, lo = min(part * per, kr.n);
+  // the part's end: at the last key that one of the rows sees
+  const int hi = min(min(lo + per, kr.n), a.causal ? min(r0 + 31, nq * grp - 1) / grp + shift + 1 : kr.n);
   const float sl2 = a.scale * LOG2E;
   const S* K = static_cast<const S*>(a.K) + kvh * D;
   const S* V = static_cast<const S*>(a.V) + kvh * D;
   char* mine = dyn + w * BUFS * 2 * TILE;
 
-  for (int r0 = 0; r0 < nq * grp; r0 += 32) {
-    const int r = r0 + c, qi = r / grp, head = kvh * grp + r % grp;
-    const bool valid = r < nq * grp;
-    const int lim = a.causal ? min(hi, qi + shift + 1) : hi;
-    const int lim_lo = a.causal ? min(hi, r0 / grp + shift + 1) : hi;
-    Frag<T> q[KS];
-    const S* qrow = static_cast<const S*>(a.Q) + (valid ? (size_t)(q0 + qi) * a.qs + head * D : 0);
+  const int r = r0 + c, qi = r / grp, head = kvh * grp + r % grp;
+  const bool valid = r < nq * grp;
+  const int lim = a.causal ? min(hi, qi + shift + 1) : hi;
+  const int lim_lo = a.causal ? min(hi, r0 / grp + shift + 1) : hi;
+  Frag<T> q[KS];
+  const S* qrow = static_cast<const S*>(a.Q) + (valid ? (size_t)(q0 + qi) * a.qs + head * D : 0);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) load8(q[s], qrow + 16 * s + 8 * h, valid);
-    f32x16 o[DT];
+  for (int s = 0; s < KS; ++s) load8(q[s], qrow + 16 * s + 8 * h, valid);
+  f32x16 o[DT];
 #pragma unroll
-    for (int i = 0; i < DT; ++i) o[i] = zero16();
-    Soft sm;
-    auto stage = [&](int j0, int buf) {
-      char* L = mine + buf * 2 * TILE;
-      stage_tile<T, D, 32, 1>(L, row_words(K, kr.row0 + j0, a.ks, hi - j0, D), a.ks * (int)sizeof(S), 0);
-      stage_tile<T, D, 32, 1>(L + TILE, row_words(V, kr.row0 + j0, a.vs, hi - j0, D), a.vs * (int)sizeof(S), 0);
-    };
-    int buf = 0;
-    const int start = lo + 32 * w;
-    if (BUFS == 2 && start < hi) stage(start, 0);
-    wait_reg_loads();
-    for (int j0 = start; j0 < hi; j0 += 128) {
-      if (BUFS == 1) {
-        wait_lds_loads();
-        stage(j0, 0);
-      }
+  for (int i = 0; i < DT; ++i) o[i] = zero16();
+  Soft sm;
+  auto stage = [&](int j0, int buf) {
+    char* L = mine + buf * 2 * TILE;
+    const int n = min(hi - j0, 32);   // of a tile: the bytes of a long sequence pass 32 bits
+    stage_tile<T, D, 32, 1>(L, row_words(K, kr.row0 + j0, a.ks, n, D), a.ks * (int)sizeof(S), 0);
+    stage_tile<T, D, 32, 1>(L + TILE, row_words(V, kr.row0 + j0, a.vs, n, D), a.vs * (int)sizeof(S), 0);
+  };
+  int buf = 0;
+  const int start = lo + 32 * w;
+  if (BUFS == 2 && start < hi) stage(start, 0);
+  wait_reg_loads();
+  for (int j0 = start; j0 < hi; j0 += 128) {
+    if (BUFS == 1) {
       wait_lds_loads();
-      if (BUFS == 2 && j0 + 128 < hi) stage(j0 + 128, buf ^ 1);
-      const char* LK = mine + buf * 2 * TILE;
-      const char* LV = LK + TILE;
-      f32x16 s[1];
-      s[0] = zero16();
-#pragma unroll
-      for (int k = 0; k < KS; ++k) mma32(s[0], RT::row(LK, c, k, h), q[k]);
-      if (j0 + 32 > lim_lo) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (j0 + res_row(e, h) >= lim) s[0][e] = -INFINITY;
-      }
-      const float alpha = sm.template step<T>(s, sl2);
-      if (__any(alpha != 1.f)) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[d] *= alpha;
-      }
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const Frag<T> p = frag_of<T>(s[0], k);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) mma32(o[d], RT::col(LV, 16 * k + 4 * h, 32 * d), p);
-      }
-      if (BUFS == 2) buf ^= 1;
+      stage(j0, 0);
     }
-    if (a.causal && __any(valid && not_finite<T, D>(o))) {   // this wave's blocks, one after the other
-      f32x16 x[DT];
-      f32x16 total[DT];
+    wait_lds_loads();
+    if (BUFS == 2 && j0 + 128 < hi) stage(j0 + 128, buf ^ 1);
+    const char* LK = mine + buf * 2 * TILE;
+    const char* LV = LK + TILE;
+    f32x16 s[1];
+    s[0] = zero16();
 #pragma unroll
-      for (int d = 0; d < DT; ++d) total[d] = zero16();
-      for (int j0 = start; j0 < hi; j0 += 128) {
-        sum_seen<T, D>(x, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, j0, min(j0 + 32, hi), lim,
-                       sm.m, sl2);
+    for (int k = 0; k < KS; ++k) mma32(s[0], RT::row(LK, c, k, h), q[k]);
+    if (j0 + 32 > lim_lo) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) total[d] += x[d];
+      for (int e = 0; e < 16; ++e)
+        if (j0 + res_row(e, h) >= lim) s[0][e] = -INFINITY;
+    }
+    const float alpha = sm.template step<T>(s, sl2);
+    if (__any(alpha != 1.f)) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= alpha;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const Frag<T> p = frag_of<T>(s[0], k);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) mma32(o[d], RT::col(LV, 16 * k + 4 * h, 32 * d), p);
+    }
+    if (BUFS == 2) buf ^= 1;
+  }
+  if (a.causal && __any(valid && not_finite<T, D>(o))) {   // this wave's blocks, one after the other
+    f32x16 x[DT];
+    f32x16 total[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) total[d] = zero16();
+    for (int j0 = start; j0 < hi; j0 += 128) {
+      sum_seen<T, D>(x, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, j0, min(j0 + 32, hi), lim,
+                     sm.m, sl2);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) total[d] += x[d];
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = total[d];
+  }
+  // join the four waves: statistics, then the scaled sums through LDS
+  const float lw = half_sum(sm.l);
+  __syncthreads();
+  if (h == 0) {
+    ml[(w * 32 + c) * 2] = sm.m;
+    ml[(w * 32 + c) * 2 + 1] = lw;
+  }
+  __syncthreads();
+  float m_all = -INFINITY, l_all = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m_all = fmaxf(m_all, ml[(i * 32 + c) * 2]);
+  const float ref = m_all == -INFINITY ? 0.f : m_all;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    l_all += ml[(i * 32 + c) * 2 + 1] * __builtin_amdgcn_exp2f((ml[(i * 32 + c) * 2] - ref) * sl2);
+  const float f = __builtin_amdgcn_exp2f((sm.m - ref) * sl2);
+  float* acc = reinterpret_cast<float*>(dyn);   // [4 waves][32 columns][D + 4]
+  constexpr int LD = D + 4;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      *reinterpret_cast<f32x4*>(acc + (w * 32 + c) * LD + 32 * d + res_row(e, h)) =
+          f32x4{o[d][e] * f, o[d][e + 1] * f, o[d][e + 2] * f, o[d][e + 3] * f};
+  float* tot = ml + 256;   // [32][2]: maximum and sum of this part
+  if (threadIdx.x < 32) {
+    tot[2 * c] = m_all;
+    tot[2 * c + 1] = l_all;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
+    const int col = i / (D / 4), d = i % (D / 4) * 4, rr = r0 + col;
+    if (rr >= nq * grp) break;
+    f32x4 v = *reinterpret_cast<const f32x4*>(acc + col * LD + d);
+#pragma unroll
+    for (int k = 1; k < 4; ++k) v += *reinterpret_cast<const f32x4*>(acc + (k * 32 + col) * LD + d);
+    const size_t row = (size_t)(q0 + rr / grp) * a.Hq + kvh * grp + rr % grp;
+    const float m_row = tot[2 * col], l_row = tot[2 * col + 1];
+    if (a.nsplit == 1) {
+      const float inv = l_row == 0.f ? 0.f : 1.f / l_row;
+      store_io4(static_cast<S*>(a.O) + row * D + d, v * inv);
+      if (a.lse && d == 0) a.lse[row] = l_row == 0.f ? -INFINITY : m_row * a.scale + __logf(l_row);
+    } else {
+      *reinterpret_cast<f32x4*>(a.part_o + (row * a.nsplit + part) * D + d) = v;
+      if (d == 0) {
+        a.part_ml[(row * a.nsplit + part) * 2] = m_row;
+        a.part_ml[(row * a.nsplit + part) * 2 + 1] = l_row;
       }
-#pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] = total[d];
     }
-    // join the four waves: statistics, then the scaled sums through LDS
-    const float lw = half_sum(sm.l);
-    __syncthreads();
-    if (h == 0) {
-      ml[(w * 32 + c) * 2] = sm.m;
-      ml[(w * 32 + c) * 2 + 1] = lw;
-    }
-    __syncthreads();
-    float m_all = -INFINITY, l_all = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m_all = fmaxf(m_all, ml[(i * 32 + c) * 2]);
-    const float ref = m_all == -INFINITY ? 0.f : m_all;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      l_all += ml[(i * 32 + c) * 2 + 1] * __builtin_amdgcn_exp2f((ml[(i * 32 + c) * 2] - ref) * sl2);
-    const float f = __builtin_amdgcn_exp2f((sm.m - ref) * sl2);
-    float* acc = reinterpret_cast<float*>(dyn);   // [4 waves][32 columns][D + 4]
-    constexpr int LD = D + 4;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4)
-        *reinterpret_cast<f32x4*>(acc + (w * 32 + c) * LD + 32 * d + res_row(e, h)) =
-            f32x4{o[d][e] * f, o[d][e + 1] * f, o[d][e + 2] * f, o[d][e + 3] * f};
-    float* tot = ml + 256;   // [32][2]: maximum and sum of this part
-    if (threadIdx.x < 32) {
-      tot[2 * c] = m_all;
-      tot[2 * c + 1] = l_all;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 32 * (D / 4); i += 256) {
-      const int col = i / (D / 4), d = i % (D / 4) * 4, rr = r0 + col;
-      if (rr >= nq * grp) break;
-      f32x4 v = *reinterpret_cast<const f32x4*>(acc + col * LD + d);
-#pragma unroll
-      for (int k = 1; k < 4; ++k) v += *reinterpret_cast<const f32x4*>(acc + (k * 32 + col) * LD + d);
-      const size_t row = (size_t)(q0 + rr / grp) * a.Hq + kvh * grp + rr % grp;
-      const float m_row = tot[2 * col], l_row = tot[2 * col + 1];
-      if (a.nsplit == 1) {
-        const float inv = l_row == 0.f ? 0.f : 1.f / l_row;
-        store_io4(static_cast<S*>(a.O) + row * D + d, v * inv);
-        if (a.lse && d == 0) a.lse[row] = l_row == 0.f ? -INFINITY : m_row * a.scale + __logf(l_row);
-      } else {
-        *reinterpret_cast<f32x4*>(a.part_o + (row * a.nsplit + part) * D + d) = v;
-        if (d == 0) {
-          a.part_ml[(row * a.nsplit + part) * 2] = m_row;
-          a.part_ml[(row * a.nsplit + part) * 2 + 1] = l_row;
-        }
-      }
-    }
-    __syncthreads();
   }
 }
 
@@ -392,7 +418,7 @@ template <class T, int D>
 hipError_t run_fwd(const AttnArgs& a, hipStream_t st) {
   timing_mark(FLEX_KERNEL_ATTN_FWD, st, true);
   if (a.nsplit > 0) {
-    k_attn_split<T, D><<<a.B * a.Hkv * a.nsplit, 256, 0, st>>>(a);
+    k_attn_split<T, D><<<block_slots(a.Tq, a.B, a.Hq / a.Hkv) * a.Hkv * a.nsplit, 256, 0, st>>>(a);
     if (a.nsplit > 1) {
       k_attn_combine<T, D><<<(unsigned)((size_t)a.Tq * a.Hq), 256, 0, st>>>(a);
     }

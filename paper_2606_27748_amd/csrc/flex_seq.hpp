@@ -89,7 +89,7 @@ __device__ __forceinline__ SeqTile find_tile(const int32_t* __restrict__ off, in
   t.row0 = clamp_off(off[b], T);
   t.n = max(clamp_off(off[b + 1], T) - t.row0, 0);
   t.tile = slot - (t.row0 / M + b);
-  if ((long long)t.tile * M < t.n) t.b = b;
+  if (t.tile >= 0 && (long long)t.tile * M < t.n) t.b = b;   // offsets that fall may give tiles below 0
   t.b = __builtin_amdgcn_readfirstlane(t.b);
   t.row0 = __builtin_amdgcn_readfirstlane(t.row0);
   t.n = __builtin_amdgcn_readfirstlane(t.n);

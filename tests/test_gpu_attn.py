@@ -118,3 +118,36 @@ def test_rows_behind_the_last_sequence_are_left(F):
     gr = F.flex_attn_bwd(desc, q, k, v, a, b, O, lse, g, dQ=mark(82, 4, 64), dK=mark(82, 2, 64), dV=mark(82, 2, 64))
     for x in (O, lse, *gr.values()):
         assert (x[73:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d,Hq,Hkv,prompt", [(64, 2, 2, 333), (128, 8, 2, 100), (32, 6, 2, 65)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompt_among_single_tokens(F, causal, d, Hq, Hkv, prompt, dtype):
+    """One prompt and single tokens in a call, few rows on average: every block of 32 rows has workgroups of its own."""
+    nq = [1, 1, prompt, 0, 1, 2] + [1] * 6
+    nk = [900, 1, prompt + 70, 50, 0, 400] + [64, 65, 31, 32, 700, 5]
+    Q, K, V, _, qo, ko = _inputs(nq, nk, Hq, Hkv, d, dtype, seed=prompt, pad=1)
+    out, mag = attn_oracle(Q, K, V, qo, ko, causal=causal)
+    desc = _desc(F, Q, K, V, len(nq), causal, dtype)
+    assert sum(nq) * (Hq // Hkv) <= 64 * len(nq)
+    O, lse = F.flex_attn_fwd(desc, *(to_dev(x) for x in (Q, K, V, qo, ko)))
+    _check_fwd(out, mag, O, lse, dtype)
+
+
+@pytest.mark.parametrize("rows_,empty", [(2058, 511), (4200, 40)])
+def test_rows_far_apart(F, rows_, empty):
+    """Rows 2 MB apart, a sequence of over 4 GB: the bytes between its first and last row pass 32 bits."""
+    gen = torch.Generator().manual_seed(rows_)
+    Q, K, V = (rows(gen, n, 1, 32, BF16) for n in (1, rows_, rows_))
+    qo, ko = offsets([0, 1] + [0] * empty), offsets([0, rows_] + [0] * empty)
+    out, mag = attn_oracle(Q, K, V, qo, ko)
+    far = 1 << 20
+    desc = F.make_attn_desc(len(qo) - 1, 1, 1, 32, 1, rows_, k_stride=far, v_stride=far)
+
+    def apart(x):
+        y = torch.empty(rows_ * far, dtype=BF16, device="cuda").as_strided((rows_, 1, 32), (far, 32, 1))
+        return y.copy_(x)
+
+    O, lse = F.flex_attn_fwd(desc, Q.cuda(), apart(K), apart(V), qo.cuda(), ko.cuda())
+    _check_fwd(out, mag, O, lse, BF16)
