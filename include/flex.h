@@ -281,6 +281,8 @@ int32_t flex_awd_loss(const flex_desc* desc, const void* Q, const void* K,
  *     h / (heads / key heads).  A gradient of a shared head is the sum over its
  *     group, formed in a fixed order.
  *   - gradients are in io_dtype.
+ *   - sizes whose launches would have 2^32 threads (with 16 heads of 128, some 170000
+ *     sequences of the delta rule, 500000 of attention) are FLEX_ERR_INVALID_ARG.
  *   - a pointer may be NULL where its tensor has no rows. */
 
 /* Exact softmax attention, the one that Eq.(linear att) approximates and
@@ -314,7 +316,8 @@ int32_t flex_attn_workspace_size(const flex_attn_desc* desc, int32_t pass, size_
  * Logits, statistics and sums are fp32; with FLEX_BF16 the probabilities are
  * rounded to bf16 for the product with V.  With at most 64 rows (queries times
  * heads of a group) per sequence on average the keys of a sequence are split over
- * several workgroups, joined in a fixed order.
+ * several workgroups, joined in a fixed order.  Prompts and single tokens may come in
+ * one call.
  * Key rows that a query does not see take no part, whatever they hold. */
 int32_t flex_attn_fwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
                       const int32_t* q_off, const int32_t* k_off, const int32_t* k_len,

@@ -365,6 +365,8 @@ def _run(fn, dev, desc, *args):
 
 
 def _seq_workspace(need, ws, dev):
+    if ws is not None and (ws.device != dev or not ws.is_contiguous()):
+        raise FlexError(FLEX_ERR_WORKSPACE, f"ws must be contiguous on {dev}")
     if ws is None or ws.numel() * ws.element_size() < need:
         if not need:
             return None, 0

@@ -355,7 +355,7 @@ hipError_t run_bwd(const AttnArgs& a, hipStream_t st) {
   if (a.Tq > 0) k_attn_dq<T, D, R><<<seq_slots(a.Tq, a.B, BM) * a.Hq, 256, 0, st>>>(a);
   constexpr bool KL = IsBf16<T>::value && D == 128;
   // us at 8279 packed tokens, 12 heads of 64: one group 84, two 105; at 16384 tokens, 16 heads of 128 on 4:
-  // one 1565 (one wave per SIMD), two 1340
+  // one 1565 (one wave per SIMD), two 1258
   if (a.Tk > 0) k_attn_dkv<T, D, R, KL ? 2 : 1, KL><<<seq_slots(a.Tk, a.B, BM) * a.Hkv, KL ? 512 : 256, 0, st>>>(a);
   timing_mark(FLEX_KERNEL_ATTN_BWD, st, false);
   return hipGetLastError();

@@ -11,6 +11,7 @@ using namespace flex;
 namespace {
 
 constexpr int kMaxStride = 1 << 20;   // elements: a tile's window of rows stays within 32-bit byte offsets
+constexpr int64_t kMaxThreads = (1LL << 32) - 1;   // of a launch
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -27,6 +28,11 @@ int stride_of(int32_t stride, int64_t row) { return stride ? stride : (int)row; 
 // a required tensor of `rows` rows, 16-byte aligned
 bool tensor_ok(const void* p, int64_t rows) { return rows == 0 || (p && aligned16(p)); }
 
+// The calls of the split kernel, which takes 32 rows (queries times heads of a group) of a sequence
+// and reads its keys for each 32: those whose sequences have up to twice that many on average.
+bool few_rows(const flex_attn_desc* d) { return (int64_t)d->Tq * (d->Hq / d->Hkv) <= 64LL * d->B; }
+int64_t row_blocks(const flex_attn_desc* d) { return (int64_t)d->Tq * (d->Hq / d->Hkv) / 32 + d->B; }
+
 int32_t check_attn(const flex_attn_desc* d) {
   if (!d) return FLEX_ERR_INVALID_ARG;
   if (d->B <= 0 || d->Hq <= 0 || d->Hkv <= 0 || d->d <= 0 || d->Tq < 0 || d->Tk < 0) return FLEX_ERR_INVALID_ARG;
@@ -40,22 +46,22 @@ int32_t check_attn(const flex_attn_desc* d) {
   const int e = esize(d->io_dtype);
   if (!stride_ok(d->q_stride, q, e) || !stride_ok(d->k_stride, k, e) || !stride_ok(d->v_stride, k, e))
     return FLEX_ERR_INVALID_ARG;
-  // workgroups of a launch (row tiles and sequences times heads) fit 31 bits
-  if (((int64_t)d->Tq + d->B) * d->Hq >= (1LL << 31) || ((int64_t)d->Tk / 128 + d->B) * d->Hkv >= (1LL << 31))
+  // row and head indexes fit 31 bits, and the largest launches (tiles of 128 rows with 256 threads, of keys
+  // with 512, statistics with d / 8 threads a row; 32 rows of a group with 256) their threads 32
+  const int64_t B = d->B, q_tiles = d->Tq / 128 + B, k_tiles = d->Tk / 128 + B;
+  if ((d->Tq + B) * d->Hq >= (1LL << 31) || q_tiles * d->Hq * 256 > kMaxThreads || k_tiles * d->Hkv * 512 > kMaxThreads ||
+      ((int64_t)d->Tq * d->Hq + 255) * (d->d / 8) > kMaxThreads || (few_rows(d) && row_blocks(d) * d->Hkv * 256 > kMaxThreads))
     return FLEX_ERR_INVALID_ARG;
   return FLEX_OK;
 }
 
-// Parts of each sequence's keys in the forward; 0: the kernel for prompts.  The
-// split kernel takes 32 rows (queries times heads of a group) of a sequence at a
-// time and reads its keys for each 32, so it serves calls whose sequences have up to
-// twice that many on average.
+// Parts of each sequence's keys in the forward; 0: the kernel for prompts.
 // A workgroup of it fills a CU at d = 128: one part per CU where few heads and sequences share them,
 // and two where many do, whose lengths differ.  us with 256, 512 and 1024 workgroups: one
 // token against 40000 rows, 4 key heads, 20.6, 24.0 and 26; 64 tokens against 253385 rows in slots
 // of 8192, 2 key heads, 65.5, 63.0 and 66.
 int attn_parts(const flex_attn_desc* d) {
-  if ((int64_t)d->Tq * (d->Hq / d->Hkv) > 64LL * d->B) return 0;
+  if (!few_rows(d)) return 0;
   const int64_t wgs = (int64_t)d->B * d->Hkv, keys = d->Tk / d->B;
   const int64_t target = wgs < 64 ? 256 : 512;
   int64_t n = (target + wgs - 1) / wgs;
@@ -96,9 +102,12 @@ int32_t check_delta(const flex_delta_desc* d, bool step) {
   const int e = esize(d->io_dtype);
   if (!stride_ok(d->q_stride, k, e) || !stride_ok(d->k_stride, k, e) || !stride_ok(d->v_stride, v, e))
     return FLEX_ERR_INVALID_ARG;
-  // workgroups of a launch fit 31 bits
-  const int64_t slots = step ? 0 : (int64_t)d->T / DELTA_CHUNK + d->B;
-  if (slots * d->H >= (1LL << 31) || (int64_t)d->B * d->H * 8 >= (1LL << 31)) return FLEX_ERR_INVALID_ARG;
+  // the threads of a launch: a state's in the step, its columns' 12 waves per 64 in the sweeps, a chunk's for
+  // each key head
+  const int64_t states = (int64_t)d->B * d->H, slots = step ? 0 : (int64_t)d->T / DELTA_CHUNK + d->B;
+  if (states * (step ? 256 : d->dv / 32 * 384) > kMaxThreads || (slots * d->H + 3) * 64 > kMaxThreads ||
+      slots * d->Hk * 256 > kMaxThreads)
+    return FLEX_ERR_INVALID_ARG;
   return FLEX_OK;
 }
 

@@ -122,6 +122,26 @@ def test_binding_checks_tensors():
         assert e.value.status == BAD
 
 
+def test_largest_launches():
+    """Sizes whose launches would have 2^32 threads are refused, the next below are not."""
+    size = lambda fn, d: _size(fn, d, F.FLEX_PASS_FWD)[0]  # noqa: E731
+    for B_, status in ((174762, OK), (174763, BAD)):   # 384 threads per 32 of 128 columns of 16 states
+        assert size("flex_delta_workspace_size", F.make_delta_desc(B_, 16, 16, 128, 1000)) == status
+    for B_, status in ((524280, OK), (524288, BAD)):   # 512 threads per sequence and key head
+        assert size("flex_attn_workspace_size", F.make_attn_desc(B_, 16, 16, 128, 1000, 1000)) == status
+    for Tq, status in ((1 << 23, OK), (1 << 24, BAD)):   # d / 8 threads per row and head
+        assert size("flex_attn_workspace_size", F.make_attn_desc(1, 16, 1, 128, Tq, 1000)) == status
+
+
+def test_workspace_of_another_device():
+    import torch
+    from paper_2606_27748_amd import _lib
+    for need in (0, 16):
+        with pytest.raises(F.FlexError) as e:
+            _lib._seq_workspace(need, torch.empty(64, dtype=torch.uint8), torch.device("cuda", 0))
+        assert e.value.status == WS
+
+
 ASAN_DRIVER = r"""
 #include <cstdio>
 #include <cstring>
