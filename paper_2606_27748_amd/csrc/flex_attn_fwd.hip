@@ -202,13 +202,9 @@ struct RowBlock {
 inline int block_slots(int T, int B, int grp) { return B + (T > 0 ? (T * grp - 1) / 32 : 0); }
 __device__ __forceinline__ RowBlock find_block(const int32_t* __restrict__ off, int B, int T, int grp, int slot) {
   if (slot < B) return {slot, 0};
-  const int l = threadIdx.x % WAVE, e = slot - B;
-  int cnt = 0;   // sequences whose further blocks start by here; the first's do
-  for (int b0 = 0; b0 < B; b0 += WAVE) {
-    const int c = __popcll(__ballot(b0 + l < B && clamp_off(off[min(b0 + l, B - 1)], T) * grp / 32 <= e));
-    cnt += c;
-    if (c < WAVE) break;
-  }
+  const int e = slot - B;
+  // sequences whose further blocks start by here
+  const int cnt = leading(B, [=](int b) { return clamp_off(off[b], T) * grp / 32 <= e; });
   const int b = max(cnt - 1, 0), k = e - clamp_off(off[b], T) * grp / 32;
   return {__builtin_amdgcn_readfirstlane(b), __builtin_amdgcn_readfirstlane(k < 0 ? 1 << 25 : k + 1)};
 }

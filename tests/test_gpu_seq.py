@@ -167,3 +167,25 @@ def test_binding_refuses(F):
     with pytest.raises(F.FlexError) as e:   # a state of another shape
         F.flex_delta_fwd(desc, *args, state0=torch.zeros(1, 1, 64, 32, device="cuda"))
     assert e.value.status == F.FLEX_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("B", [64, 65, 129, 4096, 4100])
+def test_many_short_sequences(F, B):
+    """As many sequences as the search of a tile's takes one round for, or two, or three, of 0 to 5 tokens; every
+    fiftieth has 70 (further blocks, further tiles)."""
+    g = torch.Generator().manual_seed(B)
+    lengths = [70 if b % 50 == 7 else int(torch.randint(0, 6, (1,), generator=g)) for b in range(B - 1)] + [3]
+    x, t, ddesc, adesc = _layers(F, F32, lengths, 61)
+    saved = torch.empty(F.delta_saved_size(ddesc), dtype=torch.uint8, device="cuda")
+    got = _step(F, x, t, ddesc, adesc, saved)
+    pick = sorted({0, 1, 7, B // 2, B - 2, B - 1} | {b for b in range(0, B, 501)})   # the oracle's share
+    part = {n: torch.cat([x[n][int(x["off"][b]):int(x["off"][b + 1])] for b in pick]) for n in (*NAMES[:5], "dO", "Q2", "K2", "dY")}
+    off = offsets([lengths[b] for b in pick])
+    take = lambda y: torch.cat([y.cpu()[int(x["off"][b]):int(x["off"][b + 1])] for b in pick])  # noqa: E731
+    fwd = delta_oracle(*(part[n] for n in NAMES[:5]), off)
+    att, _ = attn_oracle(part["Q2"], part["K2"], fwd["O"], off, off, dO=part["dY"])
+    bwd = delta_oracle(*(part[n] for n in NAMES[:5]), off, dO=att["dV"])
+    near("O", take(got["O"]), fwd["O"], NORM[F32]["O"])
+    near("Y", take(got["Y"]), att["O"], 1e-5)
+    for n, r in (("dQ2", att["dQ"]), ("dK2", att["dK"]), *((n, bwd[n]) for n in ("dQ", "dK", "dV", "dg", "dbeta"))):
+        near(n, take(got[n]), r, 2 * NORM[F32]["grad"])
