@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void k_attn_delta(AttnArgs a) {
 // error against dS goes with 1 / sqrt of their number: gradients of sequences of some hundred
 // rows are off by 3.2e-3 with it, against 2.4e-3 from the other roundings).  Query tiles that see
 // at most EXACT keys sum delta = sum_j P_ij dP_ij in a pass of its own first, for the key sweep
-// too; that is 1 % of the work of a sequence of 8192.
+// too; that is 1 % of the work of a sequence of 8192.  (Not with fp32 rows, whose O has no such rounding.)
 template <class T, int D, int KT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, D>::ROW > 256 ? 1 : 2))) void k_attn_dq(AttnArgs a) {
   using S = typename Io<T>::type;
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, 
         p[e] = 0.f;
       }
   };
-  if (lim_wg <= EXACT) {
+  if (IsBf16<T>::value && lim_wg <= EXACT) {
     if (ntiles > 0) stage(0);
     wait_reg_loads();
     float sum = 0.f;
