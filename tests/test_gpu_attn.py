@@ -151,3 +151,26 @@ def test_rows_far_apart(F, rows_, empty):
 
     O, lse = F.flex_attn_fwd(desc, Q.cuda(), apart(K), apart(V), qo.cuda(), ko.cuda())
     _check_fwd(out, mag, O, lse, BF16)
+
+
+def test_backward_against_differences(F):
+    """<gradient, r> against the change of sum(dO O) along r, by the float64 definition: within 128 roundings of the
+    sums of absolute terms times r's, and the difference's own error, step^2 = 1e-10 of the like."""
+    nq, nk = [70, 5], [70, 40]
+    Q, K, V, dO, qo, ko = _inputs(nq, nk, 4, 2, 64, F32, seed=12)
+    _, mag = attn_oracle(Q, K, V, qo, ko, dO=dO)
+    t = [x.cuda() for x in (Q, K, V, qo, ko)]
+    desc = _desc(F, Q, K, V, 2, True, F32)
+    O, lse = F.flex_attn_fwd(desc, *t)
+    grads = F.flex_attn_bwd(desc, *t, O, lse, dO.cuda())
+    gen, h = torch.Generator().manual_seed(13), 1e-5
+    for i, n in enumerate("QKV"):
+        r = torch.randn((Q, K, V)[i].shape, generator=gen, dtype=torch.float64)
+        ends = []
+        for s in (1, -1):
+            x = [y.double() for y in (Q, K, V)]
+            x[i] = x[i] + s * h * r
+            ends.append((attn_oracle(*x, qo, ko)[0]["O"] * dO.double()).sum())
+        g = grads["d" + n].cpu().double()
+        bound = ((128 * 2.0 ** -24 + 1e-8) * mag["d" + n] * r.abs()).sum()
+        assert abs((g * r).sum() - (ends[0] - ends[1]) / (2 * h)) <= bound, n

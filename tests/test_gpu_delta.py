@@ -158,3 +158,39 @@ def test_backward(F, lengths, d, dv, Hk, H, dtype):
             assert (grads[n].float().abs() <= 1e-30).all()
             continue
         near(n, grads[n], ref[n], NORM[dtype]["grad"])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_backward_over_a_decay_of_zero(F, dtype):
+    """g = -inf: what came before has no influence, and the decay itself no slope."""
+    x = make([150, 64], 1, 2, 64, 64, dtype, seed=8)
+    cut = [0, 70, 71, 128, 150]
+    x["g"][cut] = -float("inf")
+    names = ("Q", "K", "V", "g", "beta", "off")
+    ref = delta_oracle(*(x[n] for n in names), dO=x["dO"])
+    t, desc = dev(x), desc_of(F, x, dtype)
+    saved = torch.empty(F.delta_saved_size(desc), dtype=torch.uint8, device="cuda")
+    F.flex_delta_fwd(desc, *(t[n] for n in names), saved=saved)
+    grads = F.flex_delta_bwd(desc, *(t[n] for n in names), t["dO"], saved)
+    assert (grads["dg"][cut] == 0).all()
+    for n in ("dQ", "dK", "dV", "dg", "dbeta"):
+        near(n, grads[n], ref[n], NORM[dtype]["grad"])
+
+
+def test_backward_against_differences(F):
+    """<gradient, r> against the change of sum(dO O) along r, by the float64 recurrence: within the gradient's
+    tolerance times both norms, and the difference's own error, step^2 = 1e-10 of derivatives that are of the
+    gradient's size here."""
+    x = make([70, 65], 2, 4, 64, 64, F32, seed=9)
+    names = ("Q", "K", "V", "g", "beta", "off")
+    t, desc = dev(x), desc_of(F, x, F32)
+    saved = torch.empty(F.delta_saved_size(desc), dtype=torch.uint8, device="cuda")
+    F.flex_delta_fwd(desc, *(t[n] for n in names), saved=saved)
+    grads = F.flex_delta_bwd(desc, *(t[n] for n in names), t["dO"], saved)
+    gen, h = torch.Generator().manual_seed(10), 1e-5
+    for n in names[:5]:
+        r = torch.randn(x[n].shape, generator=gen, dtype=torch.float64)
+        ends = [(delta_oracle(*(x[m].double() + s * h * r if m == n else x[m] for m in names))["O"] * x["dO"].double()).sum()
+                for s in (1, -1)]
+        g = grads["d" + n].cpu().double()
+        assert abs((g * r).sum() - (ends[0] - ends[1]) / (2 * h)) <= (NORM[F32]["grad"] + 1e-6) * g.norm() * r.norm(), n

@@ -189,3 +189,38 @@ def test_many_short_sequences(F, B):
     near("Y", take(got["Y"]), att["O"], 1e-5)
     for n, r in (("dQ2", att["dQ"]), ("dK2", att["dK"]), *((n, bwd[n]) for n in ("dQ", "dK", "dV", "dg", "dbeta"))):
         near(n, take(got[n]), r, 2 * NORM[F32]["grad"])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_before_the_first_sequence(F, dtype):
+    """Offsets from 37 on: the results of the same rows on their own, and what lies before them left."""
+    lengths, skip = [70, 0, 131], 37
+    x, t, ddesc, adesc = _layers(F, dtype, lengths, 71)
+    saved = torch.empty(F.delta_saved_size(ddesc), dtype=torch.uint8, device="cuda")
+    ref = _step(F, x, t, ddesc, adesc, saved)
+    T = sum(lengths) + skip
+    late = {n: torch.cat([torch.full((skip, *v.shape[1:]), float("nan"), dtype=v.dtype, device="cuda"), v])
+            for n, v in t.items() if n not in ("off", "state0")}
+    late["off"] = t["off"] + skip
+    io = "bf16" if dtype == BF16 else "f32"
+    ddesc, adesc = F.make_delta_desc(3, 2, 4, 64, T, io=io), F.make_attn_desc(3, 8, 4, 64, T, T, io=io)
+    keep = {n: torch.full((T, *v.shape[1:]), 7.0, dtype=v.dtype, device="cuda") for n, v in ref.items()}
+    got = _step(F, late, late, ddesc, adesc, torch.empty(F.delta_saved_size(ddesc), dtype=torch.uint8, device="cuda"), keep)
+    for n, v in ref.items():
+        assert torch.equal(got[n][skip:], v), n
+        assert (got[n][:skip] == 7.0).all(), n
+
+
+def test_offsets_that_fall(F):
+    """Wrong offsets give wrong results, but no access outside the tensors: the rows around them are left."""
+    x, t, _, _ = _layers(F, BF16, [73], 81)
+    t["off"] = torch.tensor([0, 900, 30, -5, 70, 10000], dtype=torch.int32, device="cuda")
+    ddesc, adesc = F.make_delta_desc(5, 2, 4, 64, 73), F.make_attn_desc(5, 8, 4, 64, 73, 73)
+    shapes = {"O": (4, 64), "Y": (8, 64), "lse": (8,), "dQ2": (8, 64), "dK2": (4, 64), "dO": (4, 64), "dQ": (2, 64),
+              "dK": (2, 64), "dV": (4, 64), "dg": (4,), "dbeta": (4,)}
+    wide = {n: torch.full((16 + 73 + 16, *s), 7.0, dtype=F32 if n == "lse" else BF16, device="cuda") for n, s in shapes.items()}
+    saved = torch.zeros(F.delta_saved_size(ddesc), dtype=torch.uint8, device="cuda")
+    _step(F, x, t, ddesc, adesc, saved, {n: v[16:16 + 73] for n, v in wide.items()})
+    torch.cuda.synchronize()
+    for n, v in wide.items():
+        assert (v[:16] == 7.0).all() and (v[-16:] == 7.0).all(), n
