@@ -365,14 +365,20 @@ def _run(fn, dev, desc, *args):
 
 
 def _seq_workspace(need, ws, dev):
+    """The workspace of a call, or None where it needs none.  The caller keeps the tensor until the call has
+    returned: memory freed earlier could be another thread's by the time the kernels are queued."""
     if ws is not None and (ws.device != dev or not ws.is_contiguous()):
         raise FlexError(FLEX_ERR_WORKSPACE, f"ws must be contiguous on {dev}")
     if ws is None or ws.numel() * ws.element_size() < need:
         if not need:
-            return None, 0
+            return None
         import torch
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws
+
+
+def _span(t):
+    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
 
 
 def make_attn_desc(B, Hq, Hkv, d, Tq, Tk, causal=True, io="bf16", scale=None, q_stride=0, k_stride=0,
@@ -409,9 +415,9 @@ def flex_attn_fwd(desc: flex_attn_desc, Q, K, V, q_off, k_off, k_len=None, O=Non
         O = torch.empty(rows, dtype=io, device=dev)
     if lse is None and want_lse:
         lse = torch.empty(rows[:2], dtype=f32, device=dev)
-    w = _seq_workspace(attn_workspace_size(desc, FLEX_PASS_FWD), ws, dev)
+    ws = _seq_workspace(attn_workspace_size(desc, FLEX_PASS_FWD), ws, dev)
     _run("flex_attn_fwd", dev, desc, Q.data_ptr(), K.data_ptr(), V.data_ptr(), q_off.data_ptr(), k_off.data_ptr(),
-         _at(k_len), O.data_ptr(), _at(lse), *w)
+         _at(k_len), O.data_ptr(), _at(lse), *_span(ws))
     return O, lse
 
 
@@ -426,8 +432,8 @@ def flex_attn_bwd(desc: flex_attn_desc, Q, K, V, q_off, k_off, O, lse, dO, dQ=No
     dQ = torch.empty(rows, dtype=io, device=dev) if dQ is None else dQ
     dK = torch.empty(krow, dtype=io, device=dev) if dK is None else dK
     dV = torch.empty(krow, dtype=io, device=dev) if dV is None else dV
-    w = _seq_workspace(attn_workspace_size(desc, FLEX_PASS_BWD), ws, dev)
-    _run("flex_attn_bwd", dev, desc, *(t.data_ptr() for t in (Q, K, V, q_off, k_off, O, lse, dO, dQ, dK, dV)), *w)
+    ws = _seq_workspace(attn_workspace_size(desc, FLEX_PASS_BWD), ws, dev)
+    _run("flex_attn_bwd", dev, desc, *(t.data_ptr() for t in (Q, K, V, q_off, k_off, O, lse, dO, dQ, dK, dV)), *_span(ws))
     return dict(dQ=dQ, dK=dK, dV=dV)
 
 
@@ -457,11 +463,9 @@ def _delta_inputs(what, desc, T, Q, K, V, g, beta, *more):
     return io, dev
 
 
-def _saved(what, desc, saved, dev):
-    n = saved.numel() * saved.element_size()
-    if n < delta_saved_size(desc) or not saved.is_contiguous() or saved.device != dev:
+def _check_saved(what, desc, saved, dev):
+    if _span(saved)[1] < delta_saved_size(desc) or not saved.is_contiguous() or saved.device != dev:
         raise FlexError(FLEX_ERR_WORKSPACE, f"{what}: saved must hold delta_saved_size bytes on {dev}")
-    return saved.data_ptr(), n
 
 
 def flex_delta_fwd(desc: flex_delta_desc, Q, K, V, g, beta, off, state0=None, O=None, state=None, saved=None,
@@ -480,11 +484,12 @@ def flex_delta_fwd(desc: flex_delta_desc, Q, K, V, g, beta, off, state0=None, O=
     if state is None and want_state:
         state = torch.empty(sshape, dtype=f32, device=dev)
     if saved is not None:
-        keep, w = _saved("flex_delta_fwd", desc, saved, dev), (None, 0)
+        _check_saved("flex_delta_fwd", desc, saved, dev)
+        ws = None
     else:
-        keep, w = (None, 0), _seq_workspace(delta_workspace_size(desc, FLEX_PASS_FWD), ws, dev)
+        ws = _seq_workspace(delta_workspace_size(desc, FLEX_PASS_FWD), ws, dev)
     _run("flex_delta_fwd", dev, desc, *(t.data_ptr() for t in (Q, K, V, g, beta, off)), _at(state0), O.data_ptr(),
-         _at(state), *keep, *w)
+         _at(state), *_span(saved), *_span(ws))
     return O, state
 
 
@@ -499,10 +504,10 @@ def flex_delta_bwd(desc: flex_delta_desc, Q, K, V, g, beta, off, dO, saved, dQ=N
     _, dev = _delta_inputs("flex_delta_bwd", desc, desc.T, Q, K, V, g, beta, ("off", off, (desc.B + 1,), torch.int32, 0),
                            ("dO", dO, rows, io, 0), *out)
     grads = {n: torch.empty(shape, dtype=io, device=dev) if t is None else t for n, t, shape, _, _ in out}
-    keep = _saved("flex_delta_bwd", desc, saved, dev)
-    w = _seq_workspace(delta_workspace_size(desc, FLEX_PASS_BWD), ws, dev)
-    _run("flex_delta_bwd", dev, desc, *(t.data_ptr() for t in (Q, K, V, g, beta, off)), *keep, dO.data_ptr(),
-         *(t.data_ptr() for t in grads.values()), *w)
+    _check_saved("flex_delta_bwd", desc, saved, dev)
+    ws = _seq_workspace(delta_workspace_size(desc, FLEX_PASS_BWD), ws, dev)
+    _run("flex_delta_bwd", dev, desc, *(t.data_ptr() for t in (Q, K, V, g, beta, off)), *_span(saved), dO.data_ptr(),
+         *(t.data_ptr() for t in grads.values()), *_span(ws))
     return grads
 
 
