@@ -324,12 +324,21 @@ def _size(fn, desc, *args):
     return n.value
 
 
-def _expect(what, dev, tensors):
-    """Each (name, tensor, shape, dtype, row stride or 0 for contiguous) as it must be; None where one
-    is left out."""
+def _device(what, Q):
+    if Q is None:
+        raise FlexError(FLEX_ERR_INVALID_ARG, f"{what}: the first tensor is missing")
+    return Q.device
+
+
+def _expect(what, dev, tensors, optional=()):
+    """Each (name, tensor, shape, dtype, row stride or 0 for contiguous) as it must be; the optional ones may
+    be None."""
     if dev.type != "cuda":
         raise FlexError(FLEX_ERR_INVALID_ARG, f"{what}: tensors must be on the GPU")
-    for name, t, shape, dtype, stride in tensors:
+    for name, t, _, _, _ in tensors:
+        if t is None:
+            raise FlexError(FLEX_ERR_INVALID_ARG, f"{what}: {name} is missing")
+    for name, t, shape, dtype, stride in (*tensors, *optional):
         if t is None:
             continue
         ok = t.shape == shape and t.dtype is dtype and t.device == dev
@@ -392,13 +401,13 @@ def attn_workspace_size(desc: flex_attn_desc, pass_: int) -> int:
     return _size("flex_attn_workspace_size", desc, pass_)
 
 
-def _attn_inputs(what, desc, Q, K, V, q_off, k_off, *more):
+def _attn_inputs(what, desc, Q, K, V, q_off, k_off, more, optional):
     import torch
-    io, dev, i32, off = _io(desc), Q.device, torch.int32, (desc.B + 1,)
+    io, dev, i32, off = _io(desc), _device(what, Q), torch.int32, (desc.B + 1,)
     kv = (desc.Tk, desc.Hkv, desc.d)
     _expect(what, dev, (("Q", Q, (desc.Tq, desc.Hq, desc.d), io, desc.q_stride), ("K", K, kv, io, desc.k_stride),
                         ("V", V, kv, io, desc.v_stride), ("q_off", q_off, off, i32, 0),
-                        ("k_off", k_off, off, i32, 0)) + more)
+                        ("k_off", k_off, off, i32, 0)) + more, optional)
     return io, dev
 
 
@@ -409,8 +418,9 @@ def flex_attn_fwd(desc: flex_attn_desc, Q, K, V, q_off, k_off, k_len=None, O=Non
     device.  Returns (O, lse)."""
     import torch
     rows, f32 = (desc.Tq, desc.Hq, desc.d), torch.float32
-    io, dev = _attn_inputs("flex_attn_fwd", desc, Q, K, V, q_off, k_off, ("k_len", k_len, (desc.B,), torch.int32, 0),
-                           ("O", O, rows, _io(desc), 0), ("lse", lse, rows[:2], f32, 0))
+    io, dev = _attn_inputs("flex_attn_fwd", desc, Q, K, V, q_off, k_off, (),
+                           (("k_len", k_len, (desc.B,), torch.int32, 0), ("O", O, rows, _io(desc), 0),
+                            ("lse", lse, rows[:2], f32, 0)))
     if O is None:
         O = torch.empty(rows, dtype=io, device=dev)
     if lse is None and want_lse:
@@ -426,9 +436,9 @@ def flex_attn_bwd(desc: flex_attn_desc, Q, K, V, q_off, k_off, O, lse, dO, dQ=No
     in the io dtype; rows of no sequence are not written."""
     import torch
     rows, krow, io = (desc.Tq, desc.Hq, desc.d), (desc.Tk, desc.Hkv, desc.d), _io(desc)
-    _, dev = _attn_inputs("flex_attn_bwd", desc, Q, K, V, q_off, k_off, ("O", O, rows, io, 0), ("dO", dO, rows, io, 0),
-                          ("lse", lse, rows[:2], torch.float32, 0), ("dQ", dQ, rows, io, 0), ("dK", dK, krow, io, 0),
-                          ("dV", dV, krow, io, 0))
+    _, dev = _attn_inputs("flex_attn_bwd", desc, Q, K, V, q_off, k_off,
+                          (("O", O, rows, io, 0), ("dO", dO, rows, io, 0), ("lse", lse, rows[:2], torch.float32, 0)),
+                          (("dQ", dQ, rows, io, 0), ("dK", dK, krow, io, 0), ("dV", dV, krow, io, 0)))
     dQ = torch.empty(rows, dtype=io, device=dev) if dQ is None else dQ
     dK = torch.empty(krow, dtype=io, device=dev) if dK is None else dK
     dV = torch.empty(krow, dtype=io, device=dev) if dV is None else dV
@@ -454,17 +464,17 @@ def delta_saved_size(desc: flex_delta_desc) -> int:
     return _size("flex_delta_saved_size", desc)
 
 
-def _delta_inputs(what, desc, T, Q, K, V, g, beta, *more):
+def _delta_inputs(what, desc, T, Q, K, V, g, beta, more, optional):
     import torch
-    io, dev, f32, qk = _io(desc), Q.device, torch.float32, (T, desc.Hk, desc.d)
+    io, dev, f32, qk = _io(desc), _device(what, Q), torch.float32, (T, desc.Hk, desc.d)
     _expect(what, dev, (("Q", Q, qk, io, desc.q_stride), ("K", K, qk, io, desc.k_stride),
                         ("V", V, (T, desc.H, desc.dv), io, desc.v_stride), ("g", g, (T, desc.H), f32, 0),
-                        ("beta", beta, (T, desc.H), f32, 0)) + more)
+                        ("beta", beta, (T, desc.H), f32, 0)) + more, optional)
     return io, dev
 
 
 def _check_saved(what, desc, saved, dev):
-    if _span(saved)[1] < delta_saved_size(desc) or not saved.is_contiguous() or saved.device != dev:
+    if saved is None or _span(saved)[1] < delta_saved_size(desc) or not saved.is_contiguous() or saved.device != dev:
         raise FlexError(FLEX_ERR_WORKSPACE, f"{what}: saved must hold delta_saved_size bytes on {dev}")
 
 
@@ -476,9 +486,9 @@ def flex_delta_fwd(desc: flex_delta_desc, Q, K, V, g, beta, off, state0=None, O=
     want_state."""
     import torch
     sshape, rows, f32 = (desc.B, desc.H, desc.d, desc.dv), (desc.T, desc.H, desc.dv), torch.float32
-    io, dev = _delta_inputs("flex_delta_fwd", desc, desc.T, Q, K, V, g, beta, ("off", off, (desc.B + 1,), torch.int32, 0),
-                            ("O", O, rows, _io(desc), 0), ("state0", state0, sshape, f32, 0),
-                            ("state", state, sshape, f32, 0))
+    io, dev = _delta_inputs("flex_delta_fwd", desc, desc.T, Q, K, V, g, beta, (("off", off, (desc.B + 1,), torch.int32, 0),),
+                            (("O", O, rows, _io(desc), 0), ("state0", state0, sshape, f32, 0),
+                             ("state", state, sshape, f32, 0)))
     if O is None:
         O = torch.empty(rows, dtype=io, device=dev)
     if state is None and want_state:
@@ -501,8 +511,8 @@ def flex_delta_bwd(desc: flex_delta_desc, Q, K, V, g, beta, off, dO, saved, dQ=N
     io, qk, rows, gates = _io(desc), (desc.T, desc.Hk, desc.d), (desc.T, desc.H, desc.dv), (desc.T, desc.H)
     out = (("dQ", dQ, qk, io, 0), ("dK", dK, qk, io, 0), ("dV", dV, rows, io, 0), ("dg", dg, gates, io, 0),
            ("dbeta", dbeta, gates, io, 0))
-    _, dev = _delta_inputs("flex_delta_bwd", desc, desc.T, Q, K, V, g, beta, ("off", off, (desc.B + 1,), torch.int32, 0),
-                           ("dO", dO, rows, io, 0), *out)
+    _, dev = _delta_inputs("flex_delta_bwd", desc, desc.T, Q, K, V, g, beta,
+                           (("off", off, (desc.B + 1,), torch.int32, 0), ("dO", dO, rows, io, 0)), out)
     grads = {n: torch.empty(shape, dtype=io, device=dev) if t is None else t for n, t, shape, _, _ in out}
     _check_saved("flex_delta_bwd", desc, saved, dev)
     ws = _seq_workspace(delta_workspace_size(desc, FLEX_PASS_BWD), ws, dev)
@@ -516,8 +526,9 @@ def flex_delta_step(desc: flex_delta_desc, q, k, v, g, beta, state, o=None):
     fp32 updated in place.  Returns o [B,H,dv]."""
     import torch
     rows = (desc.B, desc.H, desc.dv)
-    io, dev = _delta_inputs("flex_delta_step", desc, desc.B, q, k, v, g, beta, ("o", o, rows, _io(desc), 0),
-                            ("state", state, (desc.B, desc.H, desc.d, desc.dv), torch.float32, 0))
+    io, dev = _delta_inputs("flex_delta_step", desc, desc.B, q, k, v, g, beta,
+                            (("state", state, (desc.B, desc.H, desc.d, desc.dv), torch.float32, 0),),
+                            (("o", o, rows, _io(desc), 0),))
     if o is None:
         o = torch.empty(rows, dtype=io, device=dev)
     _run("flex_delta_step", dev, desc, *(t.data_ptr() for t in (q, k, v, g, beta, state, o)))

@@ -12,6 +12,7 @@ from tests.seq_util import BF16, offsets
 
 class Recorder:
     """Stands for the library: sizing calls answer 4096 bytes, the others call `entered` with their name."""
+    flex_status_string = staticmethod(lambda status: b"refused")
 
     def __init__(self, entered):
         self.entered = entered
@@ -101,3 +102,31 @@ def test_workspace_of_the_caller(calls, name):
     ws = torch.zeros(5000, dtype=torch.uint8)
     _run(name, ws)
     assert made == [] and seen[0][1][-3:-1] == (ws.data_ptr(), 5000)
+
+
+def _refused(f, status=F.FLEX_ERR_INVALID_ARG):
+    with pytest.raises(F.FlexError) as e:
+        f()
+    assert e.value.status == status
+
+
+def test_missing_tensors_are_refused(calls):
+    """A required tensor that is None is the binding's own error, and nothing is called."""
+    _, seen = calls
+    desc, q, k, off = _attn()
+    lse = torch.zeros(5, 2)
+    for entry, ok in ((F.flex_attn_fwd, [q, k, k, off, off]), (F.flex_attn_bwd, [q, k, k, off, off, q, lse, q])):
+        for i in range(len(ok)):
+            _refused(lambda: entry(desc, *ok[:i], None, *ok[i + 1:]))
+    desc, rows, dO, saved = _delta()
+    state = torch.zeros(1, 2, 64, 64)
+    one = [x[:1].contiguous() for x in rows[:5]]
+    for entry, d, ok in ((F.flex_delta_fwd, desc, [*rows]), (F.flex_delta_bwd, desc, [*rows, dO]),
+                         (F.flex_delta_step, F.make_delta_desc(1, 1, 2, 64, 1), [*one, state])):
+        more = [saved] if entry is F.flex_delta_bwd else []
+        for i in range(len(ok)):
+            _refused(lambda: entry(d, *ok[:i], None, *ok[i + 1:], *more))
+    _refused(lambda: F.flex_delta_bwd(desc, *rows, dO, None), F.FLEX_ERR_WORKSPACE)
+    assert seen == []
+    F.flex_delta_step(F.make_delta_desc(1, 1, 2, 64, 1), *one, state)   # what may be left out
+    assert [n for n, _, _ in seen] == ["flex_delta_step"]
