@@ -410,7 +410,7 @@ __device__ __forceinline__ void stage_linear(const char* L, const void* src, int
     if (N % NW == 0 || step < N) {
       const unsigned to = __builtin_amdgcn_readfirstlane(base + step * 1024);
       const int off = step * 1024 + l * 16;
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(d)
+      asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to), "v"(off), "s"(d)
                    : "memory");
     }
   }

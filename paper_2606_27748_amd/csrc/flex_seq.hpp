@@ -281,7 +281,8 @@ __device__ __forceinline__ void sync_tiles() {
 // and chunks' choice by each lane.  Rows outside the window become zeros.
 // The loads are assembly without outputs: the compiler, which would wait for the
 // builtin's before the next transposed read of any LDS, does not count them, so
-// wait_lds_loads / sync_tiles must come between them and the reads of the tile.
+// wait_lds_loads / sync_tiles must come between them and the reads of the tile.  The LDS address is m0's, an
+// operand, so that the compiler writes it and knows what it holds; one wait state lies between that and its use.
 template <class T, int D, int ROWS, int NW>
 __device__ __forceinline__ void stage_tile(const char* L, u32x4 rs, int stride_bytes, int w) {
   using RT = RowTile<T, D>;
@@ -298,7 +299,7 @@ __device__ __forceinline__ void stage_tile(const char* L, u32x4 rs, int stride_b
       const int r = step * PER + lr;
       const int off = r * stride_bytes + ((lc ^ RT::swz(r)) << 4);
       const unsigned to = __builtin_amdgcn_readfirstlane(base + step * 1024);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(rs)
+      asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to), "v"(off), "s"(rs)
                    : "memory");
     }
   }
@@ -308,7 +309,7 @@ __device__ __forceinline__ void stage_tile(const char* L, u32x4 rs, int stride_b
 __device__ __forceinline__ void stage_floats(const char* L, u32x4 rs) {
   const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) const char*)L);
   const int off = threadIdx.x % WAVE * 4;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(rs) : "memory");
+  asm volatile("s_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"{m0}"(to), "v"(off), "s"(rs) : "memory");
 }
 
 }  // namespace flex
