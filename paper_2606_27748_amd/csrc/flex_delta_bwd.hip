@@ -9,10 +9,12 @@
 //   dQ = e^G dO' S^T + (dP D) K
 //   dK = (dP D)^T Q + (M + M^T) K - b F + w U dS^T,     F = e^G dR S^T
 //   dbeta_i = dR_i.V_i - k_i.F_i + sum_j dA_ij D_ij k_i.k_j
-//   dG_i = q_i.(e^G dO' S^T)_i - b_i k_i.F_i - Z_i + sum_j (X_ij - X_ji),  dG_63 += sum_i Z_i + e^{G_63} <S, dS>
-//          with X = dP P + dA A (elementwise), Z_i = k_i.(w U dS^T)_i;  dg_t = sum_{i>=t} dG_i
-// X enters as a row sum and as a column sum of the same fp32 numbers, so that pairs on one
-// side of t cancel in dg_t exactly.
+//   dg_t = sum_{i>=t} (q_i.(e^G dO' S^T)_i - b_i k_i.F_i + sum_{j<i} X_ij - sum_{j>i} X_ji) + sum_{i<t} Z_i + e^{G_63} <S, dS>
+//          with X = dP P + dA A (elementwise), Z_i = k_i.(w U dS^T)_i
+// dg_t is what crosses t: reads from t on of states and writes before it.  X enters as a row sum and as a column
+// sum of the same fp32 numbers, so pairs on one side of t cancel to what fp32 sums of them leave, some 2^-24 of
+// their absolute values.  The diagonal of X and the Z from t on cross no t and are left out: they have no
+// decay in them, and where a head forgets at once (e^-6 a token) that remainder of theirs was 6e-5 of its dg.
 #include "flex_delta.hpp"
 #include "../../include/flex.h"
 
@@ -233,7 +235,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
   constexpr int BUFS = D * (int)sizeof(T) >= 256 && 2 * ROWS + 2 * BLOCK <= 156 * 1024 ? 2 : 1;
   __shared__ __attribute__((aligned(16))) char lds[2 * ROWS + BUFS * BLOCK];
   __shared__ double lG[DC];
-  __shared__ float col_x[4][DC], row_g[DC], sum_z[4], sum_s[4];
+  __shared__ float col_x[4][DC], row_g[DC], row_z[DC], sum_s[4];
   const char* LK = lds;
   const char* LQ = lds + ROWS;
 
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
     // the last block's place takes dP D and M, rows i
     char* LP = lds + 2 * ROWS + (BUFS == 2 ? ((it - 1) & 1) * BLOCK : 0);
     char* LM = LP + MAT;
-    // the rows' parts of dG and dbeta
+    // the rows' parts of dg and dbeta
     float dot_q = 0.f, dot_f = 0.f, dot_z = 0.f;
     const float ge = eg * a.scale;
 #pragma unroll
@@ -387,7 +389,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
           const float dad = tj < tok ? -da[j][e] * D_ij : 0.f;
           da[j][e] = dad * be;
           row_b = __builtin_fmaf(dad, kk[e], row_b);
-          x[e] = dp[j][e] * qk[e] + da[j][e] * kk[e];
+          x[e] = tj < tok ? dp[j][e] * qk[e] + da[j][e] * kk[e] : 0.f;
           row_x += x[e];
         }
       }
@@ -399,28 +401,29 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
     }
     row_x = group_sum(row_x);
     row_b = group_sum(row_b);
-    if (g == 0) row_g[tok] = dot_q - be * dot_f - dot_z + row_x;
+    if (g == 0) {
+      row_g[tok] = dot_q - be * dot_f + row_x;
+      row_z[tok] = dot_z;
+    }
     if (g == 0 && tok < n) {
       const size_t at = (size_t)(row0 + tok) * a.H + head;
       static_cast<S*>(a.dbeta)[at] = float_to_io<S>(rv - dot_f + row_b);
     }
-    const float z16 = lane_sum<16>(dot_z);
     ss = group_sum(lane_sum<16>(ss));
-    if (l == 0) {
-      sum_z[w] = z16;
-      sum_s[w] = ss;
-    }
+    if (l == 0) sum_s[w] = ss;
     sync_lds();   // the last block is no longer read; the next may be on its way
     if (w == 0) {
       const float gv = l < n ? a.g[(size_t)(row0 + l) * a.H + head] : 0.f;
       float x = row_g[l] - ((col_x[0][l] + col_x[1][l]) + (col_x[2][l] + col_x[3][l]));
-      if (l == DC - 1)
-        x += (sum_z[0] + sum_z[1]) + (sum_z[2] + sum_z[3]) + last * ((sum_s[0] + sum_s[1]) + (sum_s[2] + sum_s[3]));
+      float z = l > 0 ? row_z[l - 1] : 0.f;
+      if (l == DC - 1) x += last * ((sum_s[0] + sum_s[1]) + (sum_s[2] + sum_s[3]));
 #pragma unroll
-      for (int s = 1; s < WAVE; s *= 2) {
-        const float o = __shfl_down(x, s);
+      for (int s = 1; s < WAVE; s *= 2) {   // sums over i >= l, and over i < l
+        const float o = __shfl_down(x, s), p = __shfl_up(z, s);
         if (l + s < WAVE) x += o;
+        if (l >= s) z += p;
       }
+      x += z;
       // a decay of zero has no slope
       if (l < n) static_cast<S*>(a.dg)[(size_t)(row0 + l) * a.H + head] = float_to_io<S>(gv < -1e4f ? 0.f : x);
     }

@@ -1,4 +1,5 @@
-"""Gated delta rule, each head of each sequence by itself: heads with decays of all kinds, a short sequence beside a long one, gradient states carried over many chunks.
+"""Gated delta rule, each head of each sequence by itself: heads that forget at once beside heads that hardly
+forget, a short sequence beside a long one, gradient states carried over many chunks.
 
 Bounds, relative to the 2-norm of a head's result and of its terms (tests.delta_terms; a gradient whose terms
 cancel is off by roundings of the terms):
@@ -72,3 +73,10 @@ def test_every_head(F, lengths, d, dv, Hk, H, dtype):
 def test_many_chunks_of_slow_decay(F, d, dv, dtype):
     """Thirty-five chunks whose states, forward and reverse, hardly forget, behind a short sequence."""
     run_and_check(F, inputs([5, 2200], 1, 2, d, dv, dtype, 5, (0.0, [0.003, 0.03])), dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_heads_that_forget_at_once(F, dtype):
+    """Decays of e^-5 to e^-8 a token: the slope of a decay is some thousandth of the terms beside it that have no
+    part in it."""
+    run_and_check(F, inputs([150, 64, 20], 1, 2, 64, 64, dtype, 6, (5.0, [8.0, 6.0])), dtype)
