@@ -380,8 +380,8 @@ int32_t flex_delta_fwd(const flex_delta_desc* desc, const void* Q, const void* K
                        void* O, float* state, void* saved, size_t saved_bytes,
                        void* ws, size_t ws_bytes, void* stream);
 
-/* Backward of flex_delta_fwd from states of zero (state0 = NULL) and without a gradient of
- * the final states.
+/* Backward of flex_delta_fwd without gradients of the states: of the final ones none comes in, and
+ * of state0 none goes out (behind a forward with a state0 it counts as a constant).
  *   saved             written by the forward of the same descriptor and inputs
  *   dO [T,H,dv]       io_dtype
  *   dQ, dK [T,Hk,d], dV [T,H,dv], dg, dbeta [T,H]   io_dtype outputs: the rows of

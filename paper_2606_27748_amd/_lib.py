@@ -505,7 +505,7 @@ def flex_delta_fwd(desc: flex_delta_desc, Q, K, V, g, beta, off, state0=None, O=
 
 def flex_delta_bwd(desc: flex_delta_desc, Q, K, V, g, beta, off, dO, saved, dQ=None, dK=None, dV=None, dg=None,
                    dbeta=None, ws=None):
-    """Backward of flex_delta_fwd (state0 None) from what it kept in saved.  Returns dict(dQ,
+    """Backward of flex_delta_fwd from what it kept in saved, its state0 a constant.  Returns dict(dQ,
     dK, dV, dg, dbeta) in the io dtype; rows of no sequence are not written."""
     import torch
     io, qk, rows, gates = _io(desc), (desc.T, desc.Hk, desc.d), (desc.T, desc.H, desc.dv), (desc.T, desc.H)

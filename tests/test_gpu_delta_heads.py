@@ -1,5 +1,5 @@
 """Gated delta rule, each head of each sequence by itself: heads that forget at once beside heads that hardly
-forget, a short sequence beside a long one, gradient states carried over many chunks.
+forget, a short sequence beside a long one, gradient states carried over many chunks, a first state.
 
 Bounds, relative to the 2-norm of a head's result and of its terms (tests.delta_terms; a gradient whose terms
 cancel is off by roundings of the terms):
@@ -80,3 +80,9 @@ def test_heads_that_forget_at_once(F, dtype):
     """Decays of e^-5 to e^-8 a token: the slope of a decay is some thousandth of the terms beside it that have no
     part in it."""
     run_and_check(F, inputs([150, 64, 20], 1, 2, 64, 64, dtype, 6, (5.0, [8.0, 6.0])), dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_backward_behind_a_first_state(F, dtype):
+    """A forward from state0 that keeps what a backward needs: the gradients with state0 held constant."""
+    run_and_check(F, inputs([70, 1, 130], 1, 2, 64, 128, dtype, 7, (0.0, [0.05, 0.5])), dtype, start=True)
