@@ -344,8 +344,8 @@ int32_t flex_attn_bwd(const flex_attn_desc* desc, const void* Q, const void* K, 
  *     O_t = scale S_t^T q_t
  * from S_0 = state0, or zero.  Rows of K are meant to have unit length (and beta
  * 0 .. 2), which keeps the recurrence bounded; this is not checked.  g is a log
- * decay, usually <= 0; -inf (a = 0: the state is cleared) is allowed in the
- * forward and has gradient zero.  The prompt's forward and the backward work in
+ * decay, usually <= 0; -inf (a = 0: a state of finite numbers is cleared) is allowed in
+ * the forward and has gradient zero.  The prompt's forward and the backward work in
  * chunks of 64 tokens. */
 typedef struct {
   int32_t B, T;           /* sequences; rows of Q, K, V, g, beta, O                */
@@ -374,7 +374,10 @@ int32_t flex_delta_saved_size(const flex_delta_desc* desc, size_t* bytes);
  *   saved                       flex_delta_saved_size() bytes for a backward, or
  *                               NULL; with it ws is not used and may be NULL
  * States, decays and sums are fp32; with FLEX_BF16 they enter products as two
- * bf16 terms, so that a state is right to about 2^-17 of its terms. */
+ * bf16 terms, so that a state is right to about 2^-17 of its terms.
+ * From a token on whose row of K, V, g or beta is not finite, O and the state are not
+ * (of V: in its column); the tokens before it, other sequences and other columns keep
+ * their results.  What is not finite in a row of Q concerns that row of O alone. */
 int32_t flex_delta_fwd(const flex_delta_desc* desc, const void* Q, const void* K, const void* V,
                        const float* g, const float* beta, const int32_t* off, const float* state0,
                        void* O, float* state, void* saved, size_t saved_bytes,
@@ -387,7 +390,8 @@ int32_t flex_delta_fwd(const flex_delta_desc* desc, const void* Q, const void* K
  *   dQ, dK [T,Hk,d], dV [T,H,dv], dg, dbeta [T,H]   io_dtype outputs: the rows of
  *                     the sequences are overwritten
  * With FLEX_BF16 the gradients of states and rows are carried in fp32 (in products as two
- * bf16 terms); each product that a result sums has one operand rounded to bf16. */
+ * bf16 terms); each product that a result sums has one operand rounded to bf16.
+ * What is not finite in a row may reach every gradient of its sequence, and of no other. */
 int32_t flex_delta_bwd(const flex_delta_desc* desc, const void* Q, const void* K, const void* V,
                        const float* g, const float* beta, const int32_t* off,
                        const void* saved, size_t saved_bytes, const void* dO,

@@ -62,6 +62,7 @@ template <class T>
 __device__ __forceinline__ Split<T> split(const f32x4& a, const f32x4& b);
 template <>
 __device__ __forceinline__ Split<__bf16> split(const f32x4& a, const f32x4& b) {
+#pragma clang fp contract(off)   // the terms of the rounded value, the same wherever it comes from
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   unsigned hi[4], lo[4];
 #pragma unroll
@@ -320,6 +321,36 @@ struct LowTri {
     }
   }
 };
+
+// Rows of a chunk (result tiles) that are not finite.  The products with lower triangular matrices go over whole blocks,
+// and zero times NaN is not zero: a token's row would reach those before it.  Where a column has such a
+// row, it and those behind it are cut out of the product (0) and are NaN in the result, as the recurrence has it.
+__device__ __forceinline__ bool not_finite(const f32x4 (&u)[4]) {
+  f32x4 x = zero4();   // NaN from the first NaN or infinity on
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(u[m][e], 0.f, x[e]);
+  return (x[0] + x[1]) + (x[2] + x[3]) != 0.f;
+}
+// of this lane's column, the first such row; DC: none
+__device__ __forceinline__ int first_not_finite(const f32x4 (&u)[4], int g) {
+  int first = DC;
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (!(fabsf(u[m][e]) < INFINITY)) first = min(first, tile_row(m, 4 * g + e));
+  first = min(first, __shfl_xor(first, 16));
+  return min(first, __shfl_xor(first, 32));
+}
+__device__ __forceinline__ void cut(f32x4 (&u)[4], int g, int first, float value) {
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (tile_row(m, 4 * g + e) >= first) u[m][e] = value;
+}
 
 // Operands that one wave hands to another through LDS, as the lanes hold them: 16 bytes a
 // lane and instruction.

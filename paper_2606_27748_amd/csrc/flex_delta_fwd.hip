@@ -81,6 +81,7 @@ __global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
 
   // N(n, m), n <= m, and for n < m also A(m, n), which is N(n, m) as a left operand
   f32x4 N[4][4], A[4][4];
+  float bad = 0.f;   // NaN from the first element of A that is not finite on
 #pragma unroll
   for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -95,6 +96,8 @@ __global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
       }
       if (nn == m) {
         *reinterpret_cast<f32x4*>(Lt + (m * 16 + r16) * LD + 4 * g) = N[m][m];   // A(m,m)[i][j]
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad = __builtin_fmaf(N[m][m][e], 0.f, bad);
       } else {
         f32x4 d = zero4();
 #pragma unroll
@@ -103,10 +106,40 @@ __global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
         for (int e = 0; e < 4; ++e) {
           const int i = 16 * m + 4 * g + e;
           A[m][nn][e] = d[e] * (__shfl(bv, i) * decay(Lg[i] - Gi[nn]));
+          bad = __builtin_fmaf(A[m][nn][e], 0.f, bad);
         }
       }
     }
   lds_fence();
+  // From a token on whose row of A is not finite, A is taken as zero, so that T's rows before it stay what they
+  // are, and the decay as NaN, which makes the sweep's results from the token on what they then have to be.
+  if (__any(bad != 0.f)) {
+    int first = DC;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(Lt + (m * 16 + r16) * LD + 4 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (!(fabsf(x[e]) < INFINITY)) first = min(first, 16 * m + r16);
+#pragma unroll
+        for (int nn = 0; nn < m; ++nn)
+          if (!(fabsf(A[m][nn][e]) < INFINITY)) first = min(first, 16 * m + 4 * g + e);
+      }
+    }
+#pragma unroll
+    for (int s = 1; s < WAVE; s *= 2) first = min(first, __shfl_xor(first, s));
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      if (16 * m + r16 >= first) *reinterpret_cast<f32x4*>(Lt + (m * 16 + r16) * LD + 4 * g) = zero4();
+#pragma unroll
+      for (int nn = 0; nn < m; ++nn)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (16 * m + 4 * g + e >= first) A[m][nn][e] = 0.f;
+    }
+    if (l >= first) scal[l] = NAN;
+    lds_fence();
+  }
   // T(g,g), lane column r16: t_i = [i == column] - sum_{k<i} A_ik t_k
   float tc[16];
 #pragma unroll
@@ -271,21 +304,40 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
       f32x4 u[4];
 #pragma unroll
       for (int m = 0; m < 4; ++m) u[m] = zero4();
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
+      auto add_ks = [&](int s, const Split<T>& x, int r16, int g) {
         Frag<T> kr[4];
 #pragma unroll
         for (int m = 0; m < 4; ++m) kr[m] = KT::row8(L.k(), tile_row(m, r16), 32 * s + 8 * g);
-        mma_xs4(u, kr, sb[s]);
-      }
+        mma_xs4(u, kr, x);
+      };
+      auto form_r = [&](int g) {   // b (V - e^G K S)
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const f32x4 eg = L.scal(0, m, g), be = L.scal(2, m, g);
-        const auto vc = L.col(m, g, 16 * pair);
+        for (int m = 0; m < 4; ++m) {
+          const f32x4 eg = L.scal(0, m, g), be = L.scal(2, m, g);
+          const auto vc = L.col(m, g, 16 * pair);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) u[m][e] = be[e] * ((float)vc[e] - eg[e] * u[m][e]);
-      }
+          for (int e = 0; e < 4; ++e) u[m][e] = be[e] * ((float)vc[e] - eg[e] * u[m][e]);
+        }
+      };
+#pragma unroll
+      for (int s = 0; s < KS; ++s) add_ks(s, sb[s], r16, g);
+      form_r(g);
+      const bool bad = not_finite(u);   // looked at behind the product, which hides the wait for it
       LT::apply(u, L.t(), r16, g);
+      if (__any(bad)) {
+        int x = l;
+        asm volatile("" : "+v"(x)::"memory");   // all of it read again: no value and no address is kept for this
+        const int r16 = x % 16, g = x / 16;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) u[m] = zero4();
+#pragma unroll 1
+        for (int s = 0; s < KS; ++s) add_ks(s, FB::get(box + s * FB::BYTES, x), r16, g);
+        form_r(g);
+        const int first = first_not_finite(u, g);
+        cut(u, g, first, 0.f);
+        LT::apply(u, L.t(), r16, g);
+        cut(u, g, first, NAN);
+      }
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
         box_u[m * WAVE] = u[m];
@@ -339,11 +391,21 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
     for (int m = 0; m < 4; ++m) o[m] *= L.scal(0, m, g);
     sync_lds();
     const f32x4* box_u = reinterpret_cast<const f32x4*>(box + BOX_U) + l;
-    const Split<T> u0 = split<T>(box_u[0], box_u[WAVE]), u1 = split<T>(box_u[2 * WAVE], box_u[3 * WAVE]);
+    f32x4 u[4] = {box_u[0], box_u[WAVE], box_u[2 * WAVE], box_u[3 * WAVE]};
+    Split<T> u0 = split<T>(u[0], u[1]), u1 = split<T>(u[2], u[3]);
     if (SAVE) {
       S* uo = static_cast<S*>(a.ut) + blk * (size_t)(TERMS * DC) * a.dv;
       store_frag(uo, (col0 / 16 + pair) * 2, (size_t)DC * a.dv, u0);
       store_frag(uo, (col0 / 16 + pair) * 2 + 1, (size_t)DC * a.dv, u1);
+    }
+    if (__any(not_finite(u))) {
+      int x = g;
+      asm volatile("" : "+v"(x));
+      const int first = first_not_finite(u, x);
+      cut(u, x, first, 0.f);
+      cut(o, x, first, NAN);
+      u0 = split<T>(u[0], u[1]);
+      u1 = split<T>(u[2], u[3]);
     }
     LT::mul(o, L.p(), r16, g, u0, u1);
 #pragma unroll

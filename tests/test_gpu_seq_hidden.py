@@ -1,0 +1,79 @@
+"""Packed-sequence operators and rows that a query does not see: NaN and infinities in them change nothing."""
+import pytest
+import torch
+
+from tests.seq_util import BF16, F32
+from tests.test_gpu_delta import desc_of, dev
+from tests.test_gpu_delta_heads import inputs
+
+pytestmark = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def F():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    import paper_2606_27748_amd as F
+    F.load()
+    return F
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d,dv", [(64, 64), (128, 128), (128, 64)])
+@pytest.mark.parametrize("save", [False, True])
+def test_delta_rule_looks_at_no_later_row(F, save, d, dv, dtype):
+    """What is not finite in a token's row of K, V, g or beta: the tokens before it in the sequence (of the same chunk
+    too), other sequences and, for V, the other columns have the bits that they have without it; from the token on
+    the results are not finite.  In Q: the token's own row alone."""
+    x = inputs([70, 130, 20], 1, 2, d, dv, dtype, 41, (0.0, [0.05, 0.5]))
+    desc = desc_of(F, x, dtype)
+
+    def forward(y):
+        t = dev(y)
+        saved = torch.empty(F.delta_saved_size(desc), dtype=torch.uint8, device="cuda") if save else None
+        O, state = F.flex_delta_fwd(desc, *(t[n] for n in ("Q", "K", "V", "g", "beta", "off")), saved=saved, want_state=True)
+        return O.cpu(), state.cpu()
+
+    clean, clean_state = forward(x)
+    assert torch.isfinite(clean).all() and torch.isfinite(clean_state).all()
+    for name, at, value in (("V", (5, 0, 3), NAN), ("V", (63, 1, dv - 1), INF), ("V", (64 + 16, 1, 17), -INF),
+                            ("K", (0, 0, 9), NAN), ("K", (31, 0, d - 1), INF), ("K", (40, 0, 0), NAN), ("K", (110, 0, 1), NAN),
+                            ("g", (17, 1), NAN), ("g", (50, 0), INF), ("beta", (48, 0), NAN), ("beta", (2, 1), -INF),
+                            ("Q", (33, 0, 5), NAN)):
+        y = {n: v.clone() for n, v in x.items()}
+        tok, where = 70 + at[0], at[1:]
+        y[name][(tok, *where)] = value
+        O, state = forward(y)
+        heads = slice(None) if name in ("K", "Q") else where[0]
+        cols = where[1] if name == "V" else slice(None)
+        hit = torch.zeros(clean.shape, dtype=torch.bool)
+        hit[tok:tok + 1 if name == "Q" else 200, heads, cols] = True
+        same = (O == clean) | hit
+        assert same.all(), (name, at, value, (~same).nonzero()[:4].tolist())
+        assert not torch.isfinite(O[hit]).any(), (name, at, value)
+        kept = torch.ones(clean_state.shape, dtype=torch.bool)
+        if name != "Q":
+            kept[1, heads, :, cols] = False
+        assert torch.equal(state[kept], clean_state[kept]) and not torch.isfinite(state[~kept]).any(), (name, at, value)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_delta_gradients_of_other_sequences(F, dtype):
+    """What is not finite in one sequence: the gradients of the others have the bits that they have without it."""
+    x = inputs([70, 130, 20], 1, 2, 64, 64, dtype, 42, (0.0, [0.05, 0.5]))
+    desc, names = desc_of(F, x, dtype), ("Q", "K", "V", "g", "beta", "off")
+
+    def backward(y):
+        t = dev(y)
+        saved = torch.empty(F.delta_saved_size(desc), dtype=torch.uint8, device="cuda")
+        F.flex_delta_fwd(desc, *(t[n] for n in names), saved=saved)
+        return {n: v.cpu() for n, v in F.flex_delta_bwd(desc, *(t[n] for n in names), t["dO"], saved).items()}
+
+    clean = backward(x)
+    for name in ("Q", "K", "V", "g", "beta", "dO"):
+        y = {n: v.clone() for n, v in x.items()}
+        y[name][100] = NAN
+        got = backward(y)
+        for n, v in got.items():   # a gradient may not depend on the row at all, as dV on V
+            assert torch.equal(v[:70], clean[n][:70]) and torch.equal(v[200:], clean[n][200:]), (name, n)
+        assert any(not torch.isfinite(v[70:200].float()).all() for v in got.values()), name
