@@ -318,7 +318,8 @@ int32_t flex_attn_workspace_size(const flex_attn_desc* desc, int32_t pass, size_
  * heads of a group) per sequence on average the keys of a sequence are split over
  * several workgroups, joined in a fixed order.  Prompts and single tokens may come in
  * one call.
- * Key rows that a query does not see take no part, whatever they hold. */
+ * Key rows that a query does not see take no part, whatever they hold.  Causal calls with a
+ * NaN or an infinity in a V row that is seen take some three times as long. */
 int32_t flex_attn_fwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
                       const int32_t* q_off, const int32_t* k_off, const int32_t* k_len,
                       void* O, float* lse, void* ws, size_t ws_bytes, void* stream);

@@ -45,9 +45,6 @@ struct Soft {
   }
 };
 
-// A hidden key has the probability zero, and zero times a V row with NaN or infinities is NaN.  Where
-// a wave's sums are not finite, this forms them again over the keys that each query sees, one key
-// at a time (keys lo .. hi - 1 of the sequence, lane limits lim, final maximum m).
 template <class T, int D>
 __device__ __forceinline__ bool not_finite(const f32x16 (&o)[D / 32]) {
   float x = 0.f;   // NaN from the first NaN or infinity on
@@ -57,32 +54,77 @@ __device__ __forceinline__ bool not_finite(const f32x16 (&o)[D / 32]) {
     for (int e = 0; e < 16; ++e) x = __builtin_fmaf(o[d][e], 0.f, x);
   return x != 0.f;
 }
+// A hidden key has the probability zero, and zero times a V row with NaN or infinities is NaN.  Where
+// a wave's sums are not finite, this forms them again over the keys that each query sees (final
+// maximum m, lane limits lim): the blocks of 32 keys lo, lo + step .. below hi, those in which every query sees
+// every key (up to lim_lo) as products again, from memory, and one key at a time the others, 95 at most.  With a NaN
+// that all its queries see, a call takes three times as long so (8192 tokens, 8 heads of 64: 161 and 487 us; one key at
+// a time 4670).
 template <class T, int D>
 __device__ __forceinline__ void sum_seen(f32x16 (&o)[D / 32], const Frag<T> (&q)[D / 16],
-                                                   const typename Io<T>::type* K, const typename Io<T>::type* V, int ks,
-                                                   int vs, int lo, int hi, int lim, float m, float sl2) {
+                                         const typename Io<T>::type* K, const typename Io<T>::type* V, int ks, int vs,
+                                         int lo, int step, int hi, int lim_lo, int lim, float m, float sl2) {
   using S = typename Io<T>::type;
-  const int h = threadIdx.x % WAVE / 32;
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) o[d] = zero16();
-  for (int j = lo; j < hi; ++j) {
-    const S* k = K + (size_t)j * ks + 8 * h;
-    const S* v = V + (size_t)j * vs;
-    float s = 0.f;
+#pragma unroll 1
+  for (int j0 = lo; j0 < hi; j0 += step) {
+    int l = threadIdx.x % WAVE;
+    asm volatile("" : "+v"(l));   // no address of this rare path is kept in a register outside it
+    const int c = l % 32, h = l / 32;
+    if (j0 + 32 <= lim_lo) {
+      const S* k = K + (size_t)j0 * ks;
+      const S* v = V + (size_t)j0 * vs;
+      f32x16 s = zero16();
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      Frag<T> f;
-      load8(f, k + 16 * i, true);
+      for (int i = 0; i < D / 16; ++i) {
+        Frag<T> f;
+        load8(f, k + (unsigned)(c * ks + 8 * h + 16 * i), true);
+        mma32(s, f, q[i]);
+        asm volatile("" ::: "memory");
+      }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = __builtin_fmaf(f.get(e), q[i].get(e), s);
+      for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f((s[e] - m) * sl2);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const Frag<T> p = frag_of<T>(s, i);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) {
+          Frag<T> f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            f.set(e, io_to_float(v[(unsigned)((16 * i + 4 * h + 8 * (e / 4) + e % 4) * vs + 32 * d + c)]));
+          mma32(o[d], f, p);
+          asm volatile("" ::: "memory");
+        }
+      }
+      continue;
     }
-    s = half_sum(s);
-    const float p = (float)(T)__builtin_amdgcn_exp2f((s - m) * sl2);
-    if (j < lim) {
+#pragma unroll 1
+    for (int j = j0; j < min(j0 + 32, hi); ++j) {
+      const S* k = K + (size_t)j * ks + 8 * h;
+      const S* v = V + (size_t)j * vs + 4 * h;
+      float s = 0.f;
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d)
+      for (int i = 0; i < D / 16; ++i) {
+        Frag<T> f, x = q[i];
+        load8(f, k + 16 * i, true);
+        if constexpr (IsBf16<T>::value) asm volatile("" : "+v"(x.v)::"memory");   // unpacked here, not before the loops
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[d][e] = __builtin_fmaf(p, io_to_float(v[32 * d + res_row(e, h)]), o[d][e]);
+        for (int e = 0; e < 8; ++e) s = __builtin_fmaf(f.get(e), x.get(e), s);
+      }
+      s = half_sum(s);
+      const bool sees = j < lim;
+      const float p = sees ? (float)(T)__builtin_amdgcn_exp2f((s - m) * sl2) : 0.f;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float x = io_to_float(v[32 * d + 8 * (e / 4) + e % 4]);
+          o[d][e] = __builtin_fmaf(p, sees ? x : 0.f, o[d][e]);
+        }
+        asm volatile("" ::: "memory");
+      }
     }
   }
 }
@@ -110,7 +152,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, 
   const TileCoord tc = tile_coord(seq_slots(a.Tq, a.B, BM), a.Hq, true);
   const SeqTile t = find_tile<BM>(a.q_off, a.B, a.Tq, tc.slot);
   if (t.b < 0) return;
-  const int kvh = tc.head / (a.Hq / a.Hkv);
+  const int kvh = __builtin_amdgcn_readfirstlane(tc.head / (a.Hq / a.Hkv));   // in a scalar register, with the rows' addresses
   const SeqRange kr = seq_range(a.k_off, t.b, a.Tk, a.k_len);
   const int rows = min(BM, t.n - t.tile * BM), first = t.tile * BM + 32 * w, shift = kr.n - t.n;
   const int qi = first + c;
@@ -178,8 +220,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, 
         for (int d = 0; d < DT; ++d) mma32(o[d], RT::col(LV, 32 * b + 16 * k + 4 * h, 32 * d), p);
       }
   }
-  if (a.causal && __any(qi < t.n && not_finite<T, D>(o)))
-    sum_seen<T, D>(o, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, 0, min(lim_hi, kr.n), lim,
+  if (__builtin_expect(a.causal && __any(qi < t.n && not_finite<T, D>(o)), 0))
+    sum_seen<T, D>(o, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, 0, 32, lim_hi, lim_lo, lim,
                    sm.m, sl2);
   if (qi >= t.n) return;
   const float l_all = half_sum(sm.l);
@@ -303,20 +345,9 @@ __global__ __launch_bounds__(256) void k_attn_split(AttnArgs a) {
     }
     if (BUFS == 2) buf ^= 1;
   }
-  if (a.causal && __any(valid && not_finite<T, D>(o))) {   // this wave's blocks, one after the other
-    f32x16 x[DT];
-    f32x16 total[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d) total[d] = zero16();
-    for (int j0 = start; j0 < hi; j0 += 128) {
-      sum_seen<T, D>(x, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, j0, min(j0 + 32, hi), lim,
-                     sm.m, sl2);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) total[d] += x[d];
-    }
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = total[d];
-  }
+  if (__builtin_expect(a.causal && __any(valid && not_finite<T, D>(o)), 0))
+    sum_seen<T, D>(o, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, start, 128, hi, lim_lo, lim,
+                   sm.m, sl2);
   // join the four waves: statistics, then the scaled sums through LDS
   const float lw = half_sum(sm.l);
   __syncthreads();

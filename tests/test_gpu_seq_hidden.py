@@ -2,7 +2,8 @@
 import pytest
 import torch
 
-from tests.seq_util import BF16, F32
+from tests.seq_util import BF16, F32, attn_oracle, check, offsets, rows
+from tests.test_gpu_attn import TERMS
 from tests.test_gpu_delta import desc_of, dev
 from tests.test_gpu_delta_heads import inputs
 
@@ -77,3 +78,59 @@ def test_delta_gradients_of_other_sequences(F, dtype):
         for n, v in got.items():   # a gradient may not depend on the row at all, as dV on V
             assert torch.equal(v[:70], clean[n][:70]) and torch.equal(v[200:], clean[n][200:]), (name, n)
         assert any(not torch.isfinite(v[70:200].float()).all() for v in got.values()), name
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d,Hq,Hkv", [(32, 2, 2), (64, 4, 2), (128, 8, 2)])
+@pytest.mark.parametrize("nq,nk", [([330], [330]), ([5], [700]), ([40, 200], [300, 200])])
+def test_attention_forward_looks_at_no_hidden_row(F, nq, nk, d, Hq, Hkv, dtype):
+    """V with a NaN in one column of one row and an infinity in another's, K with a NaN row: a query that sees one
+    has its results not finite there, and every other value is what it is without them, within the bounds of the
+    other tests (a sum formed again rounds its products once more in fp32, far below a rounding of bf16)."""
+    g = torch.Generator().manual_seed(d + len(nq))
+    Q, K, V = rows(g, sum(nq), Hq, d, dtype), rows(g, sum(nk), Hkv, d, dtype), rows(g, sum(nk), Hkv, d, dtype)
+    qo, ko = offsets(nq), offsets(nk)
+    out, mag = attn_oracle(Q, K, V, qo, ko)
+    hit = torch.zeros(out["O"].shape, dtype=torch.bool)
+    grp = Hq // Hkv
+    for b in range(len(nq)):
+        first = lambda key: max(key - (nk[b] - nq[b]), 0) + int(qo[b])  # noqa: E731  the first query that sees it
+        end, k0 = int(qo[b + 1]), int(ko[b])
+        for key, head, col, value in ((nk[b] // 3, 0, 3, NAN), (nk[b] - 4, Hkv - 1, d - 1, INF), (nk[b] - 90, 0, 9, -INF)):
+            V[k0 + key, head, col] = value
+            hit[first(key):end, head * grp:(head + 1) * grp, col] = True
+        K[k0 + nk[b] - 2, 0] = NAN
+        hit[first(nk[b] - 2):end, :grp] = True
+    desc = F.make_attn_desc(len(nq), Hq, Hkv, d, sum(nq), sum(nk), io="bf16" if dtype == BF16 else "f32")
+    O, lse = F.flex_attn_fwd(desc, *(x.cuda() for x in (Q, K, V, qo, ko)))
+    O, lse = O.cpu(), lse.cpu().double()
+    check("O", O[~hit], out["O"][~hit], mag["O"][~hit], TERMS[dtype]["O"], dtype)
+    assert not torch.isfinite(O[hit]).any()
+    rest = ~hit.all(-1)
+    assert (lse - out["lse"])[rest].abs().max() <= 64 * 2.0 ** -24 * 16
+
+
+def test_a_visible_nan_costs_a_few_times_the_call(F):
+    """A NaN in the first row of V, which every query sees: its sums are formed again as products.  Three times
+    the call's time; one key at a time it was thirty times, so ten tells them apart."""
+    T, H, d = 8192, 8, 64
+    g = torch.Generator().manual_seed(3)
+    Q, K, V = (rows(g, T, H, d, BF16).cuda() for _ in range(3))
+    off, desc = offsets([T], "cuda"), F.make_attn_desc(1, H, H, d, T, T)
+
+    def us():
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        best = 1e9
+        for _ in range(5):
+            a.record()
+            F.flex_attn_fwd(desc, Q, K, V, off, off)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b) * 1e3)
+        return best
+
+    clean = us()
+    V[0, :, 0] = NAN
+    bad = us()
+    print(f"{clean:.0f} us, with a NaN {bad:.0f} us")
+    assert bad <= 10 * clean
