@@ -331,9 +331,10 @@ int32_t flex_attn_fwd(const flex_attn_desc* desc, const void* Q, const void* K, 
  *                     sequences are overwritten
  * With FLEX_BF16 the probabilities and the gradients of the logits are rounded to
  * bf16 for the products over them.  Rows of other sequences and behind the last
- * one take no part; within a sequence, NaN or infinities in a row of K, V or dO
- * may also reach the gradients of rows that the causal mask hides from it, in
- * the same block of 64. */
+ * one take no part, and within a sequence neither do rows of Q, O, lse and dO in the
+ * gradients of keys that they do not see, nor rows of K and V in those of queries that
+ * do not see them, whatever they hold.  Causal calls with gradients that are not finite take
+ * three to six times as long. */
 int32_t flex_attn_bwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
                       const int32_t* q_off, const int32_t* k_off, const void* O, const float* lse,
                       const void* dO, void* dQ, void* dK, void* dV,

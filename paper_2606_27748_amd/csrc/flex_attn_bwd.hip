@@ -1,10 +1,14 @@
 // Exact causal attention over packed sequences, backward.  The probabilities are
 // formed again from the logits and the forward's lse: dQ by query tiles, dK and dV by
 // key tiles over all the query heads of their group, each sum in one workgroup's
-// registers and a fixed order (no atomics: results are the same from run to run).
+// registers and a fixed order (no atomics: results are the same from run to run).  Sums under a causal mask that
+// are not finite are formed again over what is seen (rare_add): a NaN in every row of dO makes 2 x 8192
+// tokens, 16 heads of 128 on 4, 10.4 ms of 1.93, in one of two sequences 5.8.
 #include "flex_seq.hpp"
 #include "flex_seq_kernels.hpp"
 #include "../../include/flex.h"
+
+#include <type_traits>
 
 namespace flex {
 
@@ -63,7 +67,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, 
   const SeqTile t = find_tile<BM>(a.q_off, a.B, a.Tq, tc.slot);
   if (t.b < 0) return;
   const SeqRange kr = seq_range(a.k_off, t.b, a.Tk);
-  const int kvh = tc.head / (a.Hq / a.Hkv);
+  const int kvh = __builtin_amdgcn_readfirstlane(tc.head / (a.Hq / a.Hkv));   // in a scalar register, with the rows' addresses
   const int rows = min(BM, t.n - t.tile * BM), first = t.tile * BM + 32 * w, shift = kr.n - t.n;
   const int qi = first + c;
   const int lim = a.causal ? min(kr.n, qi + shift + 1) : kr.n;
@@ -165,6 +169,32 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, 
 #pragma unroll
           for (int d = 0; d < DT; ++d) mma32(dq[d], RT::col(LK, 32 * (b0 + b) + 16 * k + 4 * h, 32 * d), ds);
         }
+    }
+  }
+  if (a.causal && __any(qi < t.n && not_finite(dq))) {   // over what each query sees, again
+    const S* Ks = K + (size_t)kr.row0 * a.ks;
+    const S* Vs = V + (size_t)kr.row0 * a.vs;
+    auto qs = [&](int i) { return q[i]; };
+    auto gs = [&](int i) { return g[i]; };
+#pragma unroll
+    for (int d = 0; d < DT; ++d) dq[d] = zero16();
+#pragma unroll 1
+    for (int j0 = 0; j0 < lim_hi; j0 += 32) {
+      if (j0 + 32 <= lim_lo) {
+        const S* k = Ks + (size_t)j0 * a.ks;
+        f32x16 s = rare_products<T, D>(k, a.ks, qs);
+        const f32x16 p = rare_products<T, D>(Vs + (size_t)j0 * a.vs, a.vs, gs);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], sl2, -lse2)) * (p[e] - delta);
+        rare_add<T, D>(dq, k, a.ks, s);
+        continue;
+      }
+#pragma unroll 1
+      for (int j = j0; j < min(j0 + 32, lim_hi); ++j) {
+        const S* k = Ks + (size_t)j * a.ks;
+        const float s = rare_product<T, D>(k, qs), p = rare_product<T, D>(Vs + (size_t)j * a.vs, gs);
+        rare_add<T, D>(dq, k, __builtin_amdgcn_exp2f(__builtin_fmaf(s, sl2, -lse2)) * (p - delta), j < lim);
+      }
     }
   }
   if (qi >= t.n) return;
@@ -304,6 +334,47 @@ __global__ __launch_bounds__(256 * WQ) __attribute__((amdgpu_waves_per_eu(RowTil
           mma32(dk[d], RT::col(LQ, kb, 32 * d), df);
         }
       }
+  }
+  if (a.causal && __any(kj < t.n && (not_finite(dk) || not_finite(dv)))) {   // over the queries that see each key, again
+    auto ks = [&](int i) { return KL ? RT::row(LKeys, 32 * wk + RareLane().c, i, RareLane().h) : kf[KL ? 0 : i]; };
+    auto vs = [&](int i) { return KL ? RT::row(LVals, 32 * wk + RareLane().c, i, RareLane().h) : vf[KL ? 0 : i]; };
+    auto again = [&](f32x16 (&sum)[DT], auto is_dk) {   // one after the other: there are registers for one
+#pragma unroll
+      for (int d = 0; d < DT; ++d) sum[d] = zero16();
+#pragma unroll 1
+      for (int x = 0; x < grp * (last + 1 - q_wg / QT) * NB; ++x) {   // head, tile, block of this wave's rows in it
+        const int head = kvh * grp + x % grp, y = x / grp, q0 = (q_wg / QT + y / NB) * QT + WR * wq + 32 * (y % NB);
+        if (q0 + 32 <= q_w || q0 >= qr.n) continue;
+        const size_t at = (size_t)(qr.row0 + q0);
+        const S* Q = static_cast<const S*>(a.Q) + head * D + at * a.qs;
+        const S* G = static_cast<const S*>(a.dO) + (at * a.Hq + head) * D;
+        const float* ls = a.delta + (size_t)head * a.Tq + at;
+        const float* de = ls + (size_t)a.Hq * a.Tq;
+        if (q0 >= q_w + 31 && q0 + 32 <= qr.n) {
+          f32x16 s = rare_products<T, D>(Q, a.qs, ks);
+          const int h = RareLane().h;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], sl2, -ls[res_row(e, h)]));
+          if (is_dk.value) {
+            const f32x16 p = rare_products<T, D>(G, a.Hq * D, vs);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] *= p[e] - de[res_row(e, h)];
+          }
+          rare_add<T, D>(sum, is_dk.value ? Q : G, is_dk.value ? a.qs : a.Hq * D, s);
+          continue;
+        }
+#pragma unroll 1
+        for (int i = 0; i < min(32, qr.n - q0); ++i) {
+          const S* qrow = Q + (size_t)i * a.qs;
+          const S* grow = G + (size_t)i * a.Hq * D;
+          float s = __builtin_amdgcn_exp2f(__builtin_fmaf(rare_product<T, D>(qrow, ks), sl2, -ls[i]));
+          if (is_dk.value) s *= rare_product<T, D>(grow, vs) - de[i];
+          rare_add<T, D>(sum, is_dk.value ? qrow : grow, s, kj <= q0 + i + shift);
+        }
+      }
+    };
+    again(dv, std::false_type{});
+    again(dk, std::true_type{});
   }
   if (WQ > 1) {   // the second group's sums to the first, through LDS, dK and then dV
     float* J = reinterpret_cast<float*>(lds) + (32 * wk + c) * (D + 4);

@@ -45,86 +45,30 @@ struct Soft {
   }
 };
 
-template <class T, int D>
-__device__ __forceinline__ bool not_finite(const f32x16 (&o)[D / 32]) {
-  float x = 0.f;   // NaN from the first NaN or infinity on
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x = __builtin_fmaf(o[d][e], 0.f, x);
-  return x != 0.f;
-}
-// A hidden key has the probability zero, and zero times a V row with NaN or infinities is NaN.  Where
-// a wave's sums are not finite, this forms them again over the keys that each query sees (final
-// maximum m, lane limits lim): the blocks of 32 keys lo, lo + step .. below hi, those in which every query sees
-// every key (up to lim_lo) as products again, from memory, and one key at a time the others, 95 at most.  With a NaN
-// that all its queries see, a call takes three times as long so (8192 tokens, 8 heads of 64: 161 and 487 us; one key at
-// a time 4670).
+// The sums of a wave over the keys that each query sees, again (final maximum m, lane limits lim): blocks of 32 keys
+// lo, lo + step .. below hi as products where every query sees every key (up to lim_lo), and one key at a time in the
+// others, 95 keys at most.  With a NaN that all its queries see, a call takes three times as long so (8192 tokens,
+// 8 heads of 64: 161 and 487 us; one key at a time for all of them 4670).
 template <class T, int D>
 __device__ __forceinline__ void sum_seen(f32x16 (&o)[D / 32], const Frag<T> (&q)[D / 16],
                                          const typename Io<T>::type* K, const typename Io<T>::type* V, int ks, int vs,
                                          int lo, int step, int hi, int lim_lo, int lim, float m, float sl2) {
-  using S = typename Io<T>::type;
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) o[d] = zero16();
+  auto qs = [&](int i) { return q[i]; };
 #pragma unroll 1
   for (int j0 = lo; j0 < hi; j0 += step) {
-    int l = threadIdx.x % WAVE;
-    asm volatile("" : "+v"(l));   // no address of this rare path is kept in a register outside it
-    const int c = l % 32, h = l / 32;
     if (j0 + 32 <= lim_lo) {
-      const S* k = K + (size_t)j0 * ks;
-      const S* v = V + (size_t)j0 * vs;
-      f32x16 s = zero16();
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        Frag<T> f;
-        load8(f, k + (unsigned)(c * ks + 8 * h + 16 * i), true);
-        mma32(s, f, q[i]);
-        asm volatile("" ::: "memory");
-      }
+      f32x16 s = rare_products<T, D>(K + (size_t)j0 * ks, ks, qs);
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f((s[e] - m) * sl2);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const Frag<T> p = frag_of<T>(s, i);
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) {
-          Frag<T> f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            f.set(e, io_to_float(v[(unsigned)((16 * i + 4 * h + 8 * (e / 4) + e % 4) * vs + 32 * d + c)]));
-          mma32(o[d], f, p);
-          asm volatile("" ::: "memory");
-        }
-      }
+      rare_add<T, D>(o, V + (size_t)j0 * vs, vs, s);
       continue;
     }
 #pragma unroll 1
     for (int j = j0; j < min(j0 + 32, hi); ++j) {
-      const S* k = K + (size_t)j * ks + 8 * h;
-      const S* v = V + (size_t)j * vs + 4 * h;
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        Frag<T> f, x = q[i];
-        load8(f, k + 16 * i, true);
-        if constexpr (IsBf16<T>::value) asm volatile("" : "+v"(x.v)::"memory");   // unpacked here, not before the loops
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s = __builtin_fmaf(f.get(e), x.get(e), s);
-      }
-      s = half_sum(s);
-      const bool sees = j < lim;
-      const float p = sees ? (float)(T)__builtin_amdgcn_exp2f((s - m) * sl2) : 0.f;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float x = io_to_float(v[32 * d + 8 * (e / 4) + e % 4]);
-          o[d][e] = __builtin_fmaf(p, sees ? x : 0.f, o[d][e]);
-        }
-        asm volatile("" ::: "memory");
-      }
+      const float s = rare_product<T, D>(K + (size_t)j * ks, qs);
+      rare_add<T, D>(o, V + (size_t)j * vs, __builtin_amdgcn_exp2f((s - m) * sl2), j < lim);
     }
   }
 }
@@ -140,7 +84,7 @@ __device__ __forceinline__ void sum_seen(f32x16 (&o)[D / 32], const Frag<T> (&q)
 // Two waves per SIMD fill each other's gaps: the next tile's S ahead of this one's P V
 // measured the same at 128 and 6 % more at 64.
 template <class T, int D, int KT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, D>::ROW > 256 ? 1 : 2))) void k_attn_fwd(AttnArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, D>::ROW > 256 ? 1 : RowTile<T, D>::ROW > 128 ? 2 : 4))) void k_attn_fwd(AttnArgs a) {
   using S = typename Io<T>::type;
   using RT = RowTile<T, D>;
   constexpr int KS = D / 16, NB = KT / 32, DT = D / 32;
@@ -220,7 +164,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, 
         for (int d = 0; d < DT; ++d) mma32(o[d], RT::col(LV, 32 * b + 16 * k + 4 * h, 32 * d), p);
       }
   }
-  if (__builtin_expect(a.causal && __any(qi < t.n && not_finite<T, D>(o)), 0))
+  if (__builtin_expect(a.causal && __any(qi < t.n && not_finite(o)), 0))
     sum_seen<T, D>(o, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, 0, 32, lim_hi, lim_lo, lim,
                    sm.m, sl2);
   if (qi >= t.n) return;
@@ -345,7 +289,7 @@ __global__ __launch_bounds__(256) void k_attn_split(AttnArgs a) {
     }
     if (BUFS == 2) buf ^= 1;
   }
-  if (__builtin_expect(a.causal && __any(valid && not_finite<T, D>(o)), 0))
+  if (__builtin_expect(a.causal && __any(valid && not_finite(o)), 0))
     sum_seen<T, D>(o, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, start, 128, hi, lim_lo, lim,
                    sm.m, sl2);
   // join the four waves: statistics, then the scaled sums through LDS

@@ -238,6 +238,97 @@ __device__ __forceinline__ Frag<T> window_frag(__amdgpu_buffer_rsrc_t rs, int of
   return f;
 }
 
+// ---------------------------------------------------------------------------
+// Sums of rows that a wave forms once more, from memory.  A hidden row has the weight zero, and zero times a row
+// with NaN or infinities is NaN: where a wave's sums are not finite, they are formed again over what each of its
+// columns sees, as products (blocks of 32 rows that every column sees) and a row at a time (the others).  These
+// paths are rare, and nothing of them may cost the loops before them: the lane is opaque and the loads are
+// kept in order, so that no address and no operand of theirs lies in a register outside them.
+// ---------------------------------------------------------------------------
+struct RareLane {
+  int c, h;   // column, lane half
+  __device__ __forceinline__ RareLane() {
+    int l = threadIdx.x % WAVE;
+    asm volatile("" : "+v"(l));
+    c = l % 32;
+    h = l / 32;
+  }
+};
+template <int N>
+__device__ __forceinline__ bool not_finite(const f32x16 (&o)[N]) {
+  float x = 0.f;   // NaN from the first NaN or infinity on
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x = __builtin_fmaf(o[d][e], 0.f, x);
+  return x != 0.f;
+}
+// the products of 32 rows with the wave's columns, q(i) operand i of them
+template <class T, int D, class S, class Q>
+__device__ __forceinline__ f32x16 rare_products(const S* rows, int stride, Q q) {
+  const RareLane l;
+  const S* r = rows + (unsigned)(l.c * stride + 8 * l.h);
+  f32x16 s = zero16();
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    Frag<T> f;
+    load8(f, r + 16 * i, true);
+    mma32(s, f, q(i));
+    asm volatile("" ::: "memory");
+  }
+  return s;
+}
+// o += rows^T w over 32 rows, w as rare_products gives them, rounded to the io type
+template <class T, int D, class S>
+__device__ __forceinline__ void rare_add(f32x16 (&o)[D / 32], const S* rows, int stride, const f32x16& w) {
+  const RareLane l;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const Frag<T> p = frag_of<T>(w, i);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+      Frag<T> f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        f.set(e, io_to_float((rows + (16 * i + 8 * (e / 4) + e % 4) * stride + 32 * d)[(unsigned)(4 * l.h * stride + l.c)]));
+      mma32(o[d], f, p);
+      asm volatile("" ::: "memory");
+    }
+  }
+}
+// one row's products with the columns
+template <class T, int D, class S, class Q>
+__device__ __forceinline__ float rare_product(const S* row, Q q) {
+  const RareLane l;
+  const S* r = row + 8 * l.h;
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    Frag<T> f, x = q(i);
+    load8(f, r + 16 * i, true);
+    if constexpr (IsBf16<T>::value) asm volatile("" : "+v"(x.v)::"memory");   // unpacked here, not before the loops
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = __builtin_fmaf(f.get(e), x.get(e), s);
+  }
+  return half_sum(s);
+}
+// o += row w in the columns that see it, w rounded to the io type
+template <class T, int D, class S>
+__device__ __forceinline__ void rare_add(f32x16 (&o)[D / 32], const S* row, float w, bool sees) {
+  const RareLane l;
+  const S* r = row + 4 * l.h;
+  const float p = sees ? (float)(T)w : 0.f;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float x = io_to_float(r[32 * d + 8 * (e / 4) + e % 4]);
+      o[d][e] = __builtin_fmaf(p, sees ? x : 0.f, o[d][e]);
+      if (e % 8 == 7) asm volatile("" ::: "memory");
+    }
+  }
+}
+
 // four consecutive values in the io type
 __device__ __forceinline__ void store_io4(u16* p, f32x4 v) {
   const bf16x4 b = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};

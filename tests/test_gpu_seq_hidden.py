@@ -134,3 +134,41 @@ def test_a_visible_nan_costs_a_few_times_the_call(F):
     bad = us()
     print(f"{clean:.0f} us, with a NaN {bad:.0f} us")
     assert bad <= 10 * clean
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d,Hq,Hkv", [(32, 2, 2), (64, 4, 2), (128, 8, 2)])
+@pytest.mark.parametrize("nq,nk", [([330], [330]), ([40, 200], [301, 200]), ([150, 70], [100, 1100])])
+def test_attention_backward_looks_at_no_hidden_row(F, nq, nk, d, Hq, Hkv, dtype):
+    """A NaN row of Q, K, V or dO in the last sequence: the gradients that it has a part in are not finite (of a row of
+    K, those of each query that sees it and, through those, of every key), all others are what they are without it.
+    Rows of Q and dO take no part in the gradients of keys that they do not see, rows of K and V none in those of
+    queries that do not see them."""
+    g = torch.Generator().manual_seed(d + sum(nk))
+    Q, K, V = rows(g, sum(nq), Hq, d, dtype), rows(g, sum(nk), Hkv, d, dtype), rows(g, sum(nk), Hkv, d, dtype)
+    dO, qo, ko, grp = rows(g, sum(nq), Hq, d, dtype), offsets(nq), offsets(nk), Hq // Hkv
+    out, mag = attn_oracle(Q, K, V, qo, ko, dO=dO)
+    desc = F.make_attn_desc(len(nq), Hq, Hkv, d, sum(nq), sum(nk), io="bf16" if dtype == BF16 else "f32")
+    (q0, q1), (k0, k1), shift = qo[-2:].tolist(), ko[-2:].tolist(), nk[-1] - nq[-1]
+    for name, row in (("Q", nq[-1] - 37), ("Q", 11), ("dO", nq[-1] - 64), ("K", nk[-1] - 5), ("K", nk[-1] // 2 + 3),
+                      ("V", nk[-1] - 41)):
+        x = {"Q": Q, "K": K, "V": V, "dO": dO}
+        x[name] = x[name].clone()
+        x[name][(q0 if name in ("Q", "dO") else k0) + row, 0] = NAN   # head 0
+        t = [x[n].cuda() for n in ("Q", "K", "V")] + [qo.cuda(), ko.cuda()]
+        O, lse = F.flex_attn_fwd(desc, *t)
+        got = {n: v.cpu() for n, v in F.flex_attn_bwd(desc, *t, O, lse, x["dO"].cuda()).items()}
+        hit = {n: torch.zeros(out[n].shape, dtype=torch.bool) for n in got}
+        if name in ("Q", "dO"):
+            seen = min(max(row + shift + 1, 0), nk[-1])   # keys
+            if seen:
+                hit["dQ"][q0 + row, 0] = hit["dK"][k0:k0 + seen, 0] = hit["dV"][k0:k0 + seen, 0] = True
+        else:
+            first = max(row - shift, 0)   # query
+            hit["dQ"][q0 + first:q1, :grp] = hit["dK"][k0:k1, 0] = True
+            if name == "K":
+                hit["dV"][k0:k1, 0] = True
+        for n, v in got.items():
+            rest = ~hit[n]
+            check(f"{n} with {name} {row}", v[rest], out[n][rest], mag[n][rest], TERMS[dtype][n], dtype)
+            assert not torch.isfinite(v[hit[n]]).any(), (n, name, row)
