@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
   }
   const double Gc = __shfl(G, DC - 1);
   float* scal = reinterpret_cast<float*>(out + 2 * DELTA_MAT_BYTES);
-  scal[l] = expf((float)G);
+  float eg = expf((float)G);
   scal[DC + l] = expf((float)(Gc - G));
   scal[2 * DC + l] = bv;
   reinterpret_cast<double*>(out + DELTA_SWEEP_BYTES)[l] = G;
@@ -137,9 +137,10 @@ __global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
         for (int e = 0; e < 4; ++e)
           if (16 * m + 4 * g + e >= first) A[m][nn][e] = 0.f;
     }
-    if (l >= first) scal[l] = NAN;
+    if (l >= first) eg = NAN;
     lds_fence();
   }
+  scal[l] = eg;
   // T(g,g), lane column r16: t_i = [i == column] - sum_{k<i} A_ik t_k
   float tc[16];
 #pragma unroll
