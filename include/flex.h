@@ -271,7 +271,7 @@ int32_t flex_awd_loss(const flex_desc* desc, const void* Q, const void* K,
  * off [B+1] on the device with sequence b in rows off[b] .. off[b+1]-1
  * (non-decreasing, off[B] <= T; a sequence may be empty).  Offsets are clamped
  * to 0 .. T on the device, so wrong ones give wrong results but no access
- * outside the tensors; rows of no sequence are neither read nor written.  The
+ * outside the tensors; rows of no sequence take no part and are not written.  The
  * conventions at the top of this file hold, except:
  *   - input rows may be strided (slices of one projection's output): *_stride
  *     elements between consecutive rows, 0 for contiguous ones; at least
@@ -316,8 +316,10 @@ int32_t flex_attn_workspace_size(const flex_attn_desc* desc, int32_t pass, size_
  * Logits, statistics and sums are fp32; with FLEX_BF16 the probabilities are
  * rounded to bf16 for the product with V.  With at most 64 rows (queries times
  * heads of a group) per sequence on average the keys of a sequence are split over
- * several workgroups, joined in a fixed order.  Prompts and single tokens may come in
- * one call.
+ * several workgroups, joined in a fixed order; the parts go by the mean of the key rows.  Above
+ * that, a workgroup walks all keys of its 128 queries and head: a few hundred queries of
+ * few sequences against a long cache leave most of the card idle.  Prompts and single tokens may come in
+ * one call; which of the two ways all of it goes is decided by the mean.
  * Key rows that a query does not see take no part, whatever they hold.  Causal calls with a
  * NaN or an infinity in a V row that is seen take some three times as long. */
 int32_t flex_attn_fwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
@@ -392,7 +394,8 @@ int32_t flex_delta_fwd(const flex_delta_desc* desc, const void* Q, const void* K
  *   dQ, dK [T,Hk,d], dV [T,H,dv], dg, dbeta [T,H]   io_dtype outputs: the rows of
  *                     the sequences are overwritten
  * With FLEX_BF16 the gradients of states and rows are carried in fp32 (in products as two
- * bf16 terms); each product that a result sums has one operand rounded to bf16.
+ * bf16 terms); each product that a result sums has one operand rounded to bf16, that of a
+ * state with its gradient in dg both.  dg and dbeta are in io_dtype too, though g and beta are fp32.
  * What is not finite in a row may reach every gradient of its sequence, and of no other. */
 int32_t flex_delta_bwd(const flex_delta_desc* desc, const void* Q, const void* K, const void* V,
                        const float* g, const float* beta, const int32_t* off,

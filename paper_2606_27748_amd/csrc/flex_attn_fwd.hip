@@ -84,7 +84,9 @@ __device__ __forceinline__ void sum_seen(f32x16 (&o)[D / 32], const Frag<T> (&q)
 // Two waves per SIMD fill each other's gaps: the next tile's S ahead of this one's P V
 // measured the same at 128 and 6 % more at 64.
 template <class T, int D, int KT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, D>::ROW > 256 ? 1 : RowTile<T, D>::ROW > 128 ? 2 : 4))) void k_attn_fwd(AttnArgs a) {
+__global__ __launch_bounds__(256)
+    __attribute__((amdgpu_waves_per_eu(RowTile<T, D>::ROW > 256 ? 1 : RowTile<T, D>::ROW > 128 ? 2 : 4))) void k_attn_fwd(
+        AttnArgs a) {
   using S = typename Io<T>::type;
   using RT = RowTile<T, D>;
   constexpr int KS = D / 16, NB = KT / 32, DT = D / 32;

@@ -19,8 +19,10 @@
 //
 // Precision, bf16 rows: K, Q, V, dO are exact operands.  States, U, T and the like are
 // fp32 and enter products as two bf16 terms (16 bits), so a carried state is right to
-// about 2^-17 of its terms; a single rounding to bf16 is taken only where the result is
-// rounded to bf16 itself.
+// about 2^-17 of its terms.  What only the gradients read is kept as one bf16 term, half the
+// bytes that the sweeps write: S and dS of each chunk, and dP D and M for the rows that follow.  Those
+// roundings (2^-8) come before the sums of a gradient, of which some cancel (dg, dbeta, dK): they
+// scale with its terms, and in <S, dS> of dg both factors have one.
 #pragma once
 #include "flex_seq.hpp"
 #include "flex_seq_kernels.hpp"

@@ -407,6 +407,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {
     }
     if (g == 0 && tok < n) {
       const size_t at = (size_t)(row0 + tok) * a.H + head;
+      // in the io type like every gradient of this operator, though beta and g are fp32
       static_cast<S*>(a.dbeta)[at] = float_to_io<S>(rv - dot_f + row_b);
     }
     ss = group_sum(lane_sum<16>(ss));

@@ -125,8 +125,9 @@ __host__ __device__ inline int seq_slots(int T, int B, int M) { return T / M + B
 // ids go round-robin to the XCDs: where the heads divide among them, an XCD gets
 // whole heads, so that the workgroups of one head read its rows through one L2.
 // Within an XCD the slots come in order, or from the last one down (`down`: with a
-// causal mask the later query tiles are the longer ones, and the long ones first
-// leave the least to wait for at the end).
+// causal mask the later query tiles of a sequence are the longer ones, and the long ones
+// first leave the least to wait for at its end).  Among sequences the order is that of
+// the packing: where the longest is in front, its tiles come last.
 struct TileCoord {
   int slot, head;
 };

@@ -30,6 +30,12 @@ bool tensor_ok(const void* p, int64_t rows) { return rows == 0 || (p && aligned1
 
 // The calls of the split kernel, which takes 32 rows (queries times heads of a group) of a sequence
 // and reads its keys for each 32: those whose sequences have up to twice that many on average.
+// us of it and of the prompt kernel, 16 heads of 128 on 4: 64 sequences of 1000 keys, 32 rows 42 and 74, 64 rows 87
+// and 73, 128 rows 135 and 71; of 8192 keys 202 and 509, 473 and 517, 600 and 519; 8 sequences of 4000 keys 21 and
+// 79, 36 and 80, 53 and 82.  One sequence of 40000 keys does not give the prompt kernel workgroups enough, and
+// would gain far beyond the border: with 2 key heads 64 rows 27 and 705, 72 rows 35 and 705, 512 rows 154 and
+// 718.  Nor does the mean see a prompt of 4000 tokens with 255 single ones on 1000 keys each (279 and 360; 97 and 94
+// as two calls).
 bool few_rows(const flex_attn_desc* d) { return (int64_t)d->Tq * (d->Hq / d->Hkv) <= 64LL * d->B; }
 int64_t row_blocks(const flex_attn_desc* d) { return (int64_t)d->Tq * (d->Hq / d->Hkv) / 32 + d->B; }
 
@@ -59,7 +65,9 @@ int32_t check_attn(const flex_attn_desc* d) {
 // A workgroup of it fills a CU at d = 128: one part per CU where few heads and sequences share them,
 // and two where many do, whose lengths differ.  us with 256, 512 and 1024 workgroups: one
 // token against 40000 rows, 4 key heads, 20.6, 24.0 and 26; 64 tokens against 253385 rows in slots
-// of 8192, 2 key heads, 65.5, 63.0 and 66.
+// of 8192, 2 key heads, 65.5, 63.0 and 66.  With 256 and 512, 8192 rows a sequence, 4 key heads: 4 sequences 19.3 and
+// 21.9, 8 28.2 and 30.9, 12 43.9 and 43.9, 16 46.2 and 48.9, 24 95.7 and 85.7, 64 184 and 191.  The mean length decides:
+// one sequence of 40000 rows among 63 of 100 gets two parts (135; alone 16).
 int attn_parts(const flex_attn_desc* d) {
   if (!few_rows(d)) return 0;
   const int64_t wgs = (int64_t)d->B * d->Hkv, keys = d->Tk / d->B;

@@ -31,7 +31,7 @@ struct AttnArgs {
   float* part_ml;
   // backward
   const void* dO;
-  float* delta;           // [Tq][Hq] workspace: rows of dO . O
+  float* delta;           // [2][Hq][Tq] workspace: lse in units of log2, then rows of dO . O
   void* dQ;
   void* dK;
   void* dV;
