@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void k_attn_delta(AttnArgs a) {
 
 // dQ: the forward's tiles and orientation.  Per block of 32 keys S^T = K Q^T,
 // dP^T = V dO^T, dS^T = P^T (dP^T - delta), dQ^T += K^T dS^T.
-// Bound by the matrix cores (63 % busy): 775 us at 2 x 8192 tokens, 16 heads of 128 on 4 (1.06 PFLOP/s).
+// Bound by the matrix cores (63 % busy): 756 us at 2 x 8192 tokens, 16 heads of 128 on 4 (1.09 PFLOP/s).
 // delta = dO . O carries the rounding of O, which weighs in dQ and dK where a query sees few keys (its
 // error against dS goes with 1 / sqrt of their number: gradients of sequences of some hundred
 // rows are off by 3.2e-3 with it, against 2.4e-3 from the other roundings).  Query tiles that see
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, 
 // workgroups, all resident at once with one group, and waited for that one.  The rows of K and V
 // are in registers, or with KL in LDS: at d = 128 a wave then fits half a SIMD's registers
 // without spilling (a reload in the loop waits for the tile that is on its way, too).
-// 1258 us there (870 TFLOP/s, matrix cores 50 % busy): the rows of K and V are read from LDS again for each
+// 1221 us there (900 TFLOP/s, matrix cores 50 % busy): the rows of K and V are read from LDS again for each
 // product, and two waves per SIMD wait for a barrier every 64 rows.
 template <class T, int D, int QT, int WQ, bool KL>
 __global__ __launch_bounds__(256 * WQ) __attribute__((amdgpu_waves_per_eu(RowTile<T, D>::ROW > 256 ? 1 : 2))) void k_attn_dkv(

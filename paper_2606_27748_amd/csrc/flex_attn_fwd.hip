@@ -78,9 +78,9 @@ __device__ __forceinline__ void sum_seen(f32x16 (&o)[D / 32], const Frag<T> (&q)
 // Prompts.  One workgroup: 128 queries of one head, 32 per wave (in registers as
 // the right operand of S^T = K Q^T); K and V in tiles of KT rows, double-buffered in
 // LDS.  O^T = V^T P^T accumulates in registers, one lane per query.
-// Bound by the matrix cores and the exponentials beside them: at 16384 tokens, 16 heads of 128 on 2, 1073 us
-// (1.03 PFLOP/s of the seen half; the matrix cores are busy 55 % of the cycles), at 17973
-// ragged tokens, 16 heads of 64 on 4, 100 us (550 TFLOP/s: half the products per exponential).
+// Bound by the matrix cores and the exponentials beside them: at 16384 tokens, 16 heads of 128 on 2, 1061 us
+// (1.04 PFLOP/s of the seen half; the matrix cores are busy 55 % of the cycles), at 17973
+// ragged tokens, 16 heads of 64 on 4, 96 us (575 TFLOP/s: half the products per exponential).
 // Two waves per SIMD fill each other's gaps: the next tile's S ahead of this one's P V
 // measured the same at 128 and 6 % more at 64.
 template <class T, int D, int KT>

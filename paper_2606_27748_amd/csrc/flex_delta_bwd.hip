@@ -214,7 +214,7 @@ __global__ __launch_bounds__(NC * 128 + NL * 64) __attribute__((amdgpu_waves_per
 // the tokens 16 w .. + 15, a lane per token, and holds the rows of dQ^T and dK^T
 // ([d x 16 tokens]).  S, dS, U, dR, dO and V pass through LDS in blocks of VB value columns, the next
 // block on its way while one is worked on where two fit.
-// 312 us at 2 x 8192 tokens, 16 heads of 128 (the 960 MB it reads and writes take 185): one workgroup per CU, whose
+// 317 us at 2 x 8192 tokens, 16 heads of 128 (the 960 MB it reads and writes take 185): one workgroup per CU, whose
 // waves' registers and LDS leave no second to work while it waits.
 template <class T, int D, int VB>
 __global__ __launch_bounds__(256) void k_delta_grad(DeltaArgs a) {

@@ -20,7 +20,7 @@ __device__ __forceinline__ void mm16(f32x4& c, const f32x4& a, const f32x4& b) {
 // that the tiles of X = (I + N)^-1 = T^T come out as a lane per row i of T.  The diagonal
 // blocks are inverted by substitution, a lane per column, all four at once; the others
 // follow from X(n,m) = -X(n,n) sum_{n<k<=m} N(n,k) X(k,m) on the fp32 matrix cores.
-// Bound by the chain of substitution and block products of a wave, two waves per SIMD to cover it: 62 us
+// Bound by the chain of substitution and block products of a wave, two waves per SIMD to cover it: 63 us
 // for 2 x 8192 tokens, 16 heads of 128, where reading and writing its 250 MB takes 48.
 template <class T, int D>
 __global__ __launch_bounds__(256) void k_delta_prep(DeltaArgs a) {
