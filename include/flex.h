@@ -321,7 +321,7 @@ int32_t flex_attn_workspace_size(const flex_attn_desc* desc, int32_t pass, size_
  * few sequences against a long cache leave most of the card idle.  Prompts and single tokens may come in
  * one call; which of the two ways all of it goes is decided by the mean.
  * Key rows that a query does not see take no part, whatever they hold.  Causal calls with a
- * NaN or an infinity in a V row that is seen take some three times as long. */
+ * NaN or an infinity in a V row that is seen take some three to four times as long. */
 int32_t flex_attn_fwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
                       const int32_t* q_off, const int32_t* k_off, const int32_t* k_len,
                       void* O, float* lse, void* ws, size_t ws_bytes, void* stream);
@@ -336,7 +336,7 @@ int32_t flex_attn_fwd(const flex_attn_desc* desc, const void* Q, const void* K, 
  * one take no part, and within a sequence neither do rows of Q, O, lse and dO in the
  * gradients of keys that they do not see, nor rows of K and V in those of queries that
  * do not see them, whatever they hold.  Causal calls with gradients that are not finite take
- * three to six times as long. */
+ * some two to six times as long. */
 int32_t flex_attn_bwd(const flex_attn_desc* desc, const void* Q, const void* K, const void* V,
                       const int32_t* q_off, const int32_t* k_off, const void* O, const float* lse,
                       const void* dO, void* dQ, void* dK, void* dV,

@@ -3,7 +3,7 @@
 // key tiles over all the query heads of their group, each sum in one workgroup's
 // registers and a fixed order (no atomics: results are the same from run to run).  Sums under a causal mask that
 // are not finite are formed again over what is seen (rare_add): a NaN in every row of dO makes 2 x 8192
-// tokens, 16 heads of 128 on 4, 10.4 ms of 1.93, in one of two sequences 5.8.
+// tokens, 16 heads of 128 on 4, 8.7 ms of 2.0, in one row at the end of the first sequence 5.3.
 #include "flex_seq.hpp"
 #include "flex_seq_kernels.hpp"
 #include "../../include/flex.h"
@@ -189,6 +189,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RowTile<T, 
         rare_add<T, D>(dq, k, a.ks, s);
         continue;
       }
+      if (__all(qi >= t.n || none_finite(dq))) break;
 #pragma unroll 1
       for (int j = j0; j < min(j0 + 32, lim_hi); ++j) {
         const S* k = Ks + (size_t)j * a.ks;
@@ -342,8 +343,8 @@ __global__ __launch_bounds__(256 * WQ) __attribute__((amdgpu_waves_per_eu(RowTil
 #pragma unroll
       for (int d = 0; d < DT; ++d) sum[d] = zero16();
 #pragma unroll 1
-      for (int x = 0; x < grp * (last + 1 - q_wg / QT) * NB; ++x) {   // head, tile, block of this wave's rows in it
-        const int head = kvh * grp + x % grp, y = x / grp, q0 = (q_wg / QT + y / NB) * QT + WR * wq + 32 * (y % NB);
+      for (int x = 0; x < total * NB; ++x) {   // head, tile, block of this wave's rows in it, the diagonal last
+        const int head = kvh * grp + x % grp, y = x / grp, q0 = (last - y / NB) * QT + WR * wq + 32 * (NB - 1 - y % NB);
         if (q0 + 32 <= q_w || q0 >= qr.n) continue;
         const size_t at = (size_t)(qr.row0 + q0);
         const S* Q = static_cast<const S*>(a.Q) + head * D + at * a.qs;
@@ -363,6 +364,7 @@ __global__ __launch_bounds__(256 * WQ) __attribute__((amdgpu_waves_per_eu(RowTil
           rare_add<T, D>(sum, is_dk.value ? Q : G, is_dk.value ? a.qs : a.Hq * D, s);
           continue;
         }
+        if (__all(kj >= t.n || none_finite(sum))) continue;
 #pragma unroll 1
         for (int i = 0; i < min(32, qr.n - q0); ++i) {
           const S* qrow = Q + (size_t)i * a.qs;

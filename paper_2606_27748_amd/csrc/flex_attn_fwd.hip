@@ -47,12 +47,12 @@ struct Soft {
 
 // The sums of a wave over the keys that each query sees, again (final maximum m, lane limits lim): blocks of 32 keys
 // lo, lo + step .. below hi as products where every query sees every key (up to lim_lo), and one key at a time in the
-// others, 95 keys at most.  With a NaN that all its queries see, a call takes three times as long so (8192 tokens,
-// 8 heads of 64: 161 and 487 us; one key at a time for all of them 4670).
+// others, 95 keys at most, where that can change anything.  With a NaN that all its queries see, a call takes three times
+// as long so (8192 tokens, 8 heads of 64: 148 and 476 us; one key at a time for all of them 4670).
 template <class T, int D>
 __device__ __forceinline__ void sum_seen(f32x16 (&o)[D / 32], const Frag<T> (&q)[D / 16],
                                          const typename Io<T>::type* K, const typename Io<T>::type* V, int ks, int vs,
-                                         int lo, int step, int hi, int lim_lo, int lim, float m, float sl2) {
+                                         int lo, int step, int hi, int lim_lo, int lim, bool valid, float m, float sl2) {
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) o[d] = zero16();
   auto qs = [&](int i) { return q[i]; };
@@ -65,6 +65,7 @@ __device__ __forceinline__ void sum_seen(f32x16 (&o)[D / 32], const Frag<T> (&q)
       rare_add<T, D>(o, V + (size_t)j0 * vs, vs, s);
       continue;
     }
+    if (__all(!valid || none_finite(o))) break;
 #pragma unroll 1
     for (int j = j0; j < min(j0 + 32, hi); ++j) {
       const float s = rare_product<T, D>(K + (size_t)j * ks, qs);
@@ -168,7 +169,7 @@ __global__ __launch_bounds__(256)
   }
   if (__builtin_expect(a.causal && __any(qi < t.n && not_finite(o)), 0))
     sum_seen<T, D>(o, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, 0, 32, lim_hi, lim_lo, lim,
-                   sm.m, sl2);
+                   qi < t.n, sm.m, sl2);
   if (qi >= t.n) return;
   const float l_all = half_sum(sm.l);
   const float inv = l_all > 0.f ? 1.f / l_all : (l_all == 0.f ? 0.f : l_all);   // no key: zeros; NaN stays
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(256) void k_attn_split(AttnArgs a) {
   }
   if (__builtin_expect(a.causal && __any(valid && not_finite(o)), 0))
     sum_seen<T, D>(o, q, K + (size_t)kr.row0 * a.ks, V + (size_t)kr.row0 * a.vs, a.ks, a.vs, start, 128, hi, lim_lo, lim,
-                   sm.m, sl2);
+                   valid, sm.m, sl2);
   // join the four waves: statistics, then the scaled sums through LDS
   const float lw = half_sum(sm.l);
   __syncthreads();

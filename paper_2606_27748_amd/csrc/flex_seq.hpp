@@ -264,6 +264,16 @@ __device__ __forceinline__ bool not_finite(const f32x16 (&o)[N]) {
     for (int e = 0; e < 16; ++e) x = __builtin_fmaf(o[d][e], 0.f, x);
   return x != 0.f;
 }
+// Whether none of a lane's results is finite: no further row changes that.
+template <int N>
+__device__ __forceinline__ bool none_finite(const f32x16 (&o)[N]) {
+  float x = INFINITY;   // NaN is passed over
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x = fminf(x, fabsf(o[d][e]));
+  return !(x < INFINITY);
+}
 // the products of 32 rows with the wave's columns, q(i) operand i of them
 template <class T, int D, class S, class Q>
 __device__ __forceinline__ f32x16 rare_products(const S* rows, int stride, Q q) {

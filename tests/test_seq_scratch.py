@@ -14,7 +14,7 @@ ALLOWED = {
     "k_delta_rsweepIfLi64E": 12,
     "k_delta_rsweepIfLi128E": 436,
     "k_delta_gradIfLi128E": 384,
-    "k_attn_dkvIfLi64E": 152,
+    "k_attn_dkvIfLi64E": 148,
 }
 
 
