@@ -410,6 +410,140 @@ int32_t flex_delta_bwd(const flex_delta_desc* desc, const void* Q, const void* K
 int32_t flex_delta_step(const flex_delta_desc* desc, const void* q, const void* k, const void* v,
                         const float* g, const float* beta, float* state, void* o, void* stream);
 
+/* ---- Selective state-space layers ----------------------------------------
+ * A short causal convolution, a selective scan and a gated norm, over packed
+ * sequences as above (rows [T][...], int32 off [B+1] on the device, clamped).  The
+ * conventions of the packed sequences hold, and gradients' rows may be strided as the rows
+ * themselves (slices of the gradient of one projection's output): d*_stride.  Memory
+ * between strided rows is not written.  Outputs must not overlap inputs, but for
+ * states where it is said. */
+
+/* Short causal convolution of every channel with its own K taps, and SiLU behind it:
+ *     z_t = bias + sum_{k<K} W[:,k] x_{t-K+1+k},   y_t = z_t  or  z_t / (1 + exp(-z_t))
+ * Rows before a sequence's first are state0's, or zero. */
+typedef enum { FLEX_ACT_NONE = 0, FLEX_ACT_SILU = 1 } flex_act;
+typedef struct {
+  int32_t B, T;           /* sequences; rows of X, Y                               */
+  int32_t D;              /* channels: a multiple of 8                              */
+  int32_t K;              /* taps: 2, 3 or 4                                       */
+  int32_t act;            /* flex_act                                              */
+  int32_t io_dtype;       /* flex_dtype of X, Y, states, dY, dX                    */
+  int32_t x_stride, dx_stride;
+} flex_conv_desc;
+
+/* Bytes of workspace of the backward (the forward and the step take none). */
+int32_t flex_conv_workspace_size(const flex_conv_desc* desc, size_t* bytes);
+
+/* Forward over packed sequences.
+ *   X [T,D] io_dtype, W [D,K] fp32, bias [D] fp32 or NULL (zero), off [B+1] int32
+ *   state0 [B,K-1,D] io_dtype or NULL   the K-1 rows before each sequence, oldest first
+ *   Y [T,D] io_dtype
+ *   state [B,K-1,D] io_dtype or NULL    the last K-1 rows of each sequence (state0's among
+ *                               them where it is shorter; state0 itself is allowed)
+ * A row of Y depends on the K rows named above and on nothing else, whatever the others hold. */
+int32_t flex_conv_fwd(const flex_conv_desc* desc, const void* X, const float* W, const float* bias,
+                      const int32_t* off, const void* state0, void* Y, void* state, void* stream);
+
+/* Backward of flex_conv_fwd, state0 a constant.
+ *   dY [T,D] io_dtype
+ *   dX [T,D] io_dtype output: the rows of the sequences are overwritten
+ *   dW [D,K] fp32, dbias [D] fp32 or NULL   outputs, summed in a fixed order */
+int32_t flex_conv_bwd(const flex_conv_desc* desc, const void* X, const float* W, const float* bias,
+                      const int32_t* off, const void* state0, const void* dY, void* dX, float* dW, float* dbias,
+                      void* ws, size_t ws_bytes, void* stream);
+
+/* One token of every sequence (rows 0 .. B-1; T and the offsets are not used).
+ *   x [B,D], state [B,K-1,D] io_dtype updated in place, y [B,D] */
+int32_t flex_conv_step(const flex_conv_desc* desc, const void* x, const float* W, const float* bias,
+                       void* state, void* y, void* stream);
+
+/* Selective scan: a state per sequence and head that decays by a factor of the token's own
+ * and takes the token in with a step size of its own,
+ *     S_t = exp(g_t) S_{t-1} + dt_t B_t x_t^T,    y_t = S_t^T C_t + D x_t
+ * from S_0 = state0, or zero.  g is a log decay (usually <= 0: the step size times the head's
+ * negative rate); -inf is allowed (a state of finite numbers is cleared).  Heads share B and C in groups: head h
+ * takes group h / (H / G). */
+typedef struct {
+  int32_t B, T;           /* sequences; rows of X, Bt, Ct, dt, g, Y                */
+  int32_t G, H;           /* groups of B and C; heads (G divides H)                */
+  int32_t N, P;           /* rows of a state (size of B and C) and columns (of x): 64 or 128 each */
+  int32_t io_dtype;       /* flex_dtype of X, Bt, Ct, Y, dY and the gradients      */
+  int32_t x_stride, b_stride, c_stride;
+  int32_t dx_stride, db_stride, dc_stride;
+} flex_scan_desc;
+
+/* Bytes of workspace of a pass (FLEX_PASS_FWD, FLEX_PASS_BWD); 0 is possible, and then ws may be NULL. */
+int32_t flex_scan_workspace_size(const flex_scan_desc* desc, int32_t pass, size_t* bytes);
+
+/* Bytes of what a forward keeps for its backward. */
+int32_t flex_scan_saved_size(const flex_scan_desc* desc, size_t* bytes);
+
+/* Forward over packed sequences.
+ *   X [T,H,P], Bt, Ct [T,G,N]   io_dtype
+ *   dt, g [T,H] fp32, D [H] fp32 or NULL (zero), off [B+1] int32
+ *   state0 [B,H,N,P] fp32 or NULL   the states to continue from
+ *   Y [T,H,P] io_dtype
+ *   state [B,H,N,P] fp32 or NULL    the states after the last tokens (state0 itself is
+ *                               allowed); an empty sequence's is its state0, or zero
+ *   saved                       flex_scan_saved_size() bytes for a backward, or NULL
+ * States, decays and sums are fp32; with FLEX_BF16 a token's part of the state is formed from two
+ * bf16 terms (2^-17), and the matrix of a chunk of 64 tokens and the state it reads are rounded to bf16.
+ * From a token on whose row of X, Bt, dt or g is not finite, Y and the state are not (of X: in its
+ * column); the tokens before it, other sequences and other columns keep their results.  What is
+ * not finite in a row of Ct concerns that row of Y alone. */
+int32_t flex_scan_fwd(const flex_scan_desc* desc, const void* X, const void* Bt, const void* Ct, const float* dt,
+                      const float* g, const float* D, const int32_t* off, const float* state0, void* Y, float* state,
+                      void* saved, size_t saved_bytes, void* ws, size_t ws_bytes, void* stream);
+
+/* Backward of flex_scan_fwd without gradients of the states (of the final ones none comes in, state0 is a
+ * constant).
+ *   saved             written by the forward of the same descriptor and inputs
+ *   dY [T,H,P]        io_dtype
+ *   dX [T,H,P], dB, dC [T,G,N], ddt, dg [T,H]   io_dtype outputs: the rows of the sequences are
+ *                     overwritten.  dt's and g's are those of independent inputs.
+ *   dD [H] fp32       output, or NULL
+ * A group's dB and dC are sums over its heads, in fp32 and in a fixed order.  With FLEX_BF16 the products that a result
+ * sums have operands rounded to bf16 once (a state with its gradient in dg both).  What is not finite in a
+ * row may reach every gradient of its sequence, and dD; of other sequences none else. */
+int32_t flex_scan_bwd(const flex_scan_desc* desc, const void* X, const void* Bt, const void* Ct, const float* dt,
+                      const float* g, const float* D, const int32_t* off, const void* saved, size_t saved_bytes,
+                      const void* dY, void* dX, void* dB, void* dC, void* ddt, void* dg, float* dD,
+                      void* ws, size_t ws_bytes, void* stream);
+
+/* One token of every sequence (rows 0 .. B-1; T and the offsets are not used), fp32 throughout but for
+ * the io rows.
+ *   x [B,H,P], Bt, Ct [B,G,N], dt, g [B,H], D [H] or NULL, state [B,H,N,P] fp32 updated in
+ *   place, y [B,H,P] */
+int32_t flex_scan_step(const flex_scan_desc* desc, const void* x, const void* Bt, const void* Ct, const float* dt,
+                       const float* g, const float* D, float* state, void* y, void* stream);
+
+/* Gated norm of rows (behind a recurrence): over each group of `group` channels, with
+ * r(u) = 1 / sqrt(mean(u^2) + eps) and silu(z) = z / (1 + exp(-z)),
+ *     FLEX_GATE_NONE   y = x r(x) w
+ *     FLEX_GATE_FIRST  y = u r(u) w,  u = x silu(z)
+ *     FLEX_GATE_LAST   y = x r(x) w silu(z)
+ * Every row is for itself: there are no sequences. */
+typedef enum { FLEX_GATE_NONE = 0, FLEX_GATE_FIRST = 1, FLEX_GATE_LAST = 2 } flex_gate;
+typedef struct {
+  int32_t T, D;           /* rows; channels                                        */
+  int32_t group;          /* channels of a norm: a multiple of 8 up to 8192 that divides D */
+  int32_t gate;           /* flex_gate                                             */
+  int32_t io_dtype;       /* flex_dtype of X, Z, Y, dY, dX, dZ                     */
+  int32_t x_stride, z_stride, dx_stride, dz_stride;
+  float eps;              /* >= 0                                                  */
+} flex_norm_desc;
+
+/* Bytes of workspace of the backward (the forward takes none). */
+int32_t flex_norm_workspace_size(const flex_norm_desc* desc, size_t* bytes);
+
+/* Forward: X, Z [T,D] io_dtype (Z NULL without a gate), W [D] fp32, Y [T,D] io_dtype. */
+int32_t flex_norm_fwd(const flex_norm_desc* desc, const void* X, const void* Z, const float* W, void* Y, void* stream);
+
+/* Backward: dY [T,D]; dX, dZ [T,D] io_dtype outputs (dZ NULL without a gate), dW [D] fp32 output, summed in
+ * a fixed order. */
+int32_t flex_norm_bwd(const flex_norm_desc* desc, const void* X, const void* Z, const float* W, const void* dY,
+                      void* dX, void* dZ, float* dW, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- Kernel timing (profiling aid) --------------------------------------
  * Kernel classes of the library.  When timing is enabled for one class, every
  * launch of a kernel of that class is bracketed by two hipEvents recorded on
@@ -434,7 +568,15 @@ typedef enum {
   FLEX_KERNEL_ATTN_BWD = 14,    /* exact attention, all kernels of a backward */
   FLEX_KERNEL_DELTA_FWD = 15,   /* gated delta rule, all kernels of a forward  */
   FLEX_KERNEL_DELTA_BWD = 16,   /* gated delta rule, all kernels of a backward */
-  FLEX_KERNEL_DELTA_STEP = 17   /* gated delta rule, single-token step        */
+  FLEX_KERNEL_DELTA_STEP = 17,  /* gated delta rule, single-token step        */
+  FLEX_KERNEL_CONV_FWD = 18,    /* short convolution, all kernels of a forward  */
+  FLEX_KERNEL_CONV_BWD = 19,    /* short convolution, all kernels of a backward */
+  FLEX_KERNEL_CONV_STEP = 20,   /* short convolution, single-token step       */
+  FLEX_KERNEL_SCAN_FWD = 21,    /* selective scan, all kernels of a forward   */
+  FLEX_KERNEL_SCAN_BWD = 22,    /* selective scan, all kernels of a backward  */
+  FLEX_KERNEL_SCAN_STEP = 23,   /* selective scan, single-token step          */
+  FLEX_KERNEL_NORM_FWD = 24,    /* gated norm, forward                        */
+  FLEX_KERNEL_NORM_BWD = 25     /* gated norm, all kernels of a backward      */
 } flex_kernel;
 
 /* Select the kernel class to time (FLEX_KERNEL_NONE disables) and discard

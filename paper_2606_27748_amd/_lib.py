@@ -8,6 +8,7 @@ calls raise.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -24,11 +25,16 @@ EXPORTS = ("flex_abi_version", "flex_status_string", "flex_workspace_size",
            "flex_awd_loss", "flex_attn_workspace_size", "flex_attn_fwd", "flex_attn_bwd",
            "flex_delta_workspace_size", "flex_delta_saved_size", "flex_delta_fwd", "flex_delta_bwd",
            "flex_delta_step",
+           "flex_conv_workspace_size", "flex_conv_fwd", "flex_conv_bwd", "flex_conv_step",
+           "flex_scan_workspace_size", "flex_scan_saved_size", "flex_scan_fwd", "flex_scan_bwd", "flex_scan_step",
+           "flex_norm_workspace_size", "flex_norm_fwd", "flex_norm_bwd",
            "flex_timing_enable", "flex_timing_read")
 KERNELS = {"none": 0, "fwd_state": 1, "fwd_sweep": 2, "scan": 3, "bwd_prepass": 4,
            "bwd_dq": 5, "bwd_dkv": 6, "bwd_reduce": 7, "feature_map": 8, "decode_step": 9,
            "awd_fwd": 10, "awd_bwd_k": 11, "awd_wgrad": 12,
-           "attn_fwd": 13, "attn_bwd": 14, "delta_fwd": 15, "delta_bwd": 16, "delta_step": 17}
+           "attn_fwd": 13, "attn_bwd": 14, "delta_fwd": 15, "delta_bwd": 16, "delta_step": 17,
+           "conv_fwd": 18, "conv_bwd": 19, "conv_step": 20, "scan_fwd": 21, "scan_bwd": 22, "scan_step": 23,
+           "norm_fwd": 24, "norm_bwd": 25}
 
 
 class FlexError(RuntimeError):
@@ -54,6 +60,20 @@ class flex_attn_desc(ctypes.Structure):
 class flex_delta_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "Hk", "H", "d", "dv", "io_dtype", "q_stride", "k_stride",
                                               "v_stride")] + [("scale", ctypes.c_float)]
+
+
+class flex_conv_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "D", "K", "act", "io_dtype", "x_stride", "dx_stride")]
+
+
+class flex_scan_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "G", "H", "N", "P", "io_dtype", "x_stride", "b_stride", "c_stride",
+                                              "dx_stride", "db_stride", "dc_stride")]
+
+
+class flex_norm_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "D", "group", "gate", "io_dtype", "x_stride", "z_stride", "dx_stride",
+                                              "dz_stride")] + [("eps", ctypes.c_float)]
 
 
 _lib = None
@@ -115,6 +135,31 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.flex_delta_bwd.argtypes = [G] + [P] * 7 + [S] + [P] * 7 + [S, P]
     lib.flex_delta_step.restype = I
     lib.flex_delta_step.argtypes = [G] + [P] * 8
+    C, N, M = (ctypes.POINTER(x) for x in (flex_conv_desc, flex_scan_desc, flex_norm_desc))
+    lib.flex_conv_workspace_size.restype = I
+    lib.flex_conv_workspace_size.argtypes = [C, ctypes.POINTER(S)]
+    lib.flex_conv_fwd.restype = I
+    lib.flex_conv_fwd.argtypes = [C] + [P] * 8
+    lib.flex_conv_bwd.restype = I
+    lib.flex_conv_bwd.argtypes = [C] + [P] * 10 + [S, P]
+    lib.flex_conv_step.restype = I
+    lib.flex_conv_step.argtypes = [C] + [P] * 6
+    lib.flex_scan_workspace_size.restype = I
+    lib.flex_scan_workspace_size.argtypes = [N, I, ctypes.POINTER(S)]
+    lib.flex_scan_saved_size.restype = I
+    lib.flex_scan_saved_size.argtypes = [N, ctypes.POINTER(S)]
+    lib.flex_scan_fwd.restype = I
+    lib.flex_scan_fwd.argtypes = [N] + [P] * 11 + [S, P, S, P]
+    lib.flex_scan_bwd.restype = I
+    lib.flex_scan_bwd.argtypes = [N] + [P] * 8 + [S] + [P] * 8 + [S, P]
+    lib.flex_scan_step.restype = I
+    lib.flex_scan_step.argtypes = [N] + [P] * 9
+    lib.flex_norm_workspace_size.restype = I
+    lib.flex_norm_workspace_size.argtypes = [M, ctypes.POINTER(S)]
+    lib.flex_norm_fwd.restype = I
+    lib.flex_norm_fwd.argtypes = [M] + [P] * 5
+    lib.flex_norm_bwd.restype = I
+    lib.flex_norm_bwd.argtypes = [M] + [P] * 8 + [S, P]
     lib.flex_timing_enable.restype = I
     lib.flex_timing_enable.argtypes = [I]
     lib.flex_timing_read.restype = I
@@ -343,7 +388,7 @@ def _expect(what, dev, tensors, optional=()):
             continue
         ok = t.shape == shape and t.dtype is dtype and t.device == dev
         if ok and stride and shape[0] > 1:
-            ok = t.stride() == (stride, shape[2], 1)
+            ok = t.stride() == (stride, *shape[2:], 1)
         elif ok:
             ok = t.is_contiguous()
         if not ok:
@@ -533,6 +578,238 @@ def flex_delta_step(desc: flex_delta_desc, q, k, v, g, beta, state, o=None):
         o = torch.empty(rows, dtype=io, device=dev)
     _run("flex_delta_step", dev, desc, *(t.data_ptr() for t in (q, k, v, g, beta, state, o)))
     return o
+
+
+# ---------------------------------------------------------------------------
+# Selective state-space layers
+# ---------------------------------------------------------------------------
+_ACTS = {"none": 0, "silu": 1}
+_GATES = {"none": 0, "first": 1, "last": 2}
+
+
+def _make(out, dev):
+    """The tensors of (name, tensor or None, shape, dtype, row stride), new ones for None: contiguous, or with the
+    stride that the descriptor asks for, as the first columns of wider rows."""
+    import torch
+    made = {}
+    for n, t, shape, dtype, stride in out:
+        if t is None:
+            row = math.prod(shape[1:])
+            t = torch.empty(shape, dtype=dtype, device=dev)
+            if stride and stride != row and shape[0] > 1:
+                t = torch.empty(shape[0], stride, dtype=dtype, device=dev)[:, :row].unflatten(1, shape[1:])
+        made[n] = t
+    return made
+
+
+def make_conv_desc(B, T, D, K, act="silu", io="bf16", x_stride=0, dx_stride=0) -> flex_conv_desc:
+    """Short causal convolution of B sequences packed in T rows of D channels, K taps each, act "silu" or
+    "none" behind it; strides in elements between rows (0: contiguous)."""
+    return flex_conv_desc(B, T, D, K, _ACTS.get(act, -1), FLEX_BF16 if io == "bf16" else FLEX_F32, x_stride, dx_stride)
+
+
+def conv_workspace_size(desc: flex_conv_desc) -> int:
+    """Bytes of workspace of flex_conv_bwd."""
+    return _size("flex_conv_workspace_size", desc)
+
+
+def _conv_inputs(what, desc, T, X, W, bias, more, optional):
+    import torch
+    io, dev, f32 = _io(desc), _device(what, X), torch.float32
+    _expect(what, dev, (("X", X, (T, desc.D), io, desc.x_stride), ("W", W, (desc.D, desc.K), f32, 0)) + more,
+            (("bias", bias, (desc.D,), f32, 0),) + optional)
+    return io, dev
+
+
+def flex_conv_fwd(desc: flex_conv_desc, X, W, bias, off, state0=None, Y=None, state=None, want_state=False):
+    """Short causal convolution over packed sequences: X [T,D], W [D,K] and bias [D] (or None) fp32, int32
+    offsets [B+1] on the device, the K-1 rows before each sequence in state0 [B,K-1,D] (None: zeros).  Returns
+    (Y, state), the last K-1 rows of each sequence where a state was given or want_state."""
+    import torch
+    io, sshape = _io(desc), (desc.B, desc.K - 1, desc.D)
+    _, dev = _conv_inputs("flex_conv_fwd", desc, desc.T, X, W, bias, (("off", off, (desc.B + 1,), torch.int32, 0),),
+                          (("state0", state0, sshape, io, 0), ("Y", Y, (desc.T, desc.D), io, 0),
+                           ("state", state, sshape, io, 0)))
+    if Y is None:
+        Y = torch.empty(desc.T, desc.D, dtype=io, device=dev)
+    if state is None and want_state:
+        state = torch.empty(sshape, dtype=io, device=dev)
+    _run("flex_conv_fwd", dev, desc, X.data_ptr(), W.data_ptr(), _at(bias), off.data_ptr(), _at(state0), Y.data_ptr(),
+         _at(state))
+    return Y, state
+
+
+def flex_conv_bwd(desc: flex_conv_desc, X, W, bias, off, dY, state0=None, dX=None, dW=None, dbias=None, ws=None):
+    """Backward of flex_conv_fwd, its state0 a constant.  Returns dict(dX, dW, dbias): dX in the io dtype (rows of no
+    sequence are not written), dW [D,K] and dbias [D] (None without a bias) fp32."""
+    import torch
+    io, f32, rows = _io(desc), torch.float32, (desc.T, desc.D)
+    out = (("dX", dX, rows, io, desc.dx_stride), ("dW", dW, (desc.D, desc.K), f32, 0))
+    more = (("dbias", dbias, (desc.D,), f32, 0),)
+    _, dev = _conv_inputs("flex_conv_bwd", desc, desc.T, X, W, bias,
+                          (("off", off, (desc.B + 1,), torch.int32, 0), ("dY", dY, rows, io, 0)),
+                          (("state0", state0, (desc.B, desc.K - 1, desc.D), io, 0),) + out + more)
+    grads = _make(out + (more if bias is not None else ()), dev)
+    grads.setdefault("dbias", dbias)
+    ws = _seq_workspace(conv_workspace_size(desc), ws, dev)
+    _run("flex_conv_bwd", dev, desc, X.data_ptr(), W.data_ptr(), _at(bias), off.data_ptr(), _at(state0), dY.data_ptr(),
+         *(_at(t) for t in grads.values()), *_span(ws))
+    return grads
+
+
+def flex_conv_step(desc: flex_conv_desc, x, W, bias, state, y=None):
+    """One token of every sequence: x [B,D], state [B,K-1,D] (the rows before, oldest first) updated in
+    place.  Returns y [B,D]."""
+    import torch
+    io, rows = _io(desc), (desc.B, desc.D)
+    _, dev = _conv_inputs("flex_conv_step", desc, desc.B, x, W, bias, (("state", state, (desc.B, desc.K - 1, desc.D), io, 0),),
+                          (("y", y, rows, io, 0),))
+    if y is None:
+        y = torch.empty(rows, dtype=io, device=dev)
+    _run("flex_conv_step", dev, desc, x.data_ptr(), W.data_ptr(), _at(bias), state.data_ptr(), y.data_ptr())
+    return y
+
+
+def make_scan_desc(B, G, H, N, P, T, io="bf16", x_stride=0, b_stride=0, c_stride=0, dx_stride=0, db_stride=0,
+                   dc_stride=0) -> flex_scan_desc:
+    """Selective scan of B sequences packed in T rows: H heads of P columns on G groups of B and C of N elements;
+    strides in elements between rows (0: contiguous)."""
+    return flex_scan_desc(B, T, G, H, N, P, FLEX_BF16 if io == "bf16" else FLEX_F32, x_stride, b_stride, c_stride,
+                          dx_stride, db_stride, dc_stride)
+
+
+def scan_workspace_size(desc: flex_scan_desc, pass_: int) -> int:
+    return _size("flex_scan_workspace_size", desc, pass_)
+
+
+def scan_saved_size(desc: flex_scan_desc) -> int:
+    """Bytes of the buffer in which a forward keeps what its backward reads."""
+    return _size("flex_scan_saved_size", desc)
+
+
+def _scan_inputs(what, desc, T, X, Bt, Ct, dt, g, D, more, optional):
+    import torch
+    io, dev, f32, bc = _io(desc), _device(what, X), torch.float32, (T, desc.G, desc.N)
+    _expect(what, dev, (("X", X, (T, desc.H, desc.P), io, desc.x_stride), ("Bt", Bt, bc, io, desc.b_stride),
+                        ("Ct", Ct, bc, io, desc.c_stride), ("dt", dt, (T, desc.H), f32, 0),
+                        ("g", g, (T, desc.H), f32, 0)) + more, (("D", D, (desc.H,), f32, 0),) + optional)
+    return io, dev
+
+
+def _scan_saved(what, desc, saved, dev):
+    if saved is None or _span(saved)[1] < scan_saved_size(desc) or not saved.is_contiguous() or saved.device != dev:
+        raise FlexError(FLEX_ERR_WORKSPACE, f"{what}: saved must hold scan_saved_size bytes on {dev}")
+
+
+def flex_scan_fwd(desc: flex_scan_desc, X, Bt, Ct, dt, g, D, off, state0=None, Y=None, state=None, saved=None, ws=None,
+                  want_state=False):
+    """Selective scan over packed sequences: X [T,H,P], Bt and Ct [T,G,N], dt and g (log decay) [T,H] fp32, D [H]
+    fp32 or None, int32 offsets [B+1] on the device.  saved: a buffer of scan_saved_size bytes for
+    flex_scan_bwd.  Returns (Y, state), state [B,H,N,P] fp32 where one was given or want_state."""
+    import torch
+    sshape, rows, f32 = (desc.B, desc.H, desc.N, desc.P), (desc.T, desc.H, desc.P), torch.float32
+    io, dev = _scan_inputs("flex_scan_fwd", desc, desc.T, X, Bt, Ct, dt, g, D, (("off", off, (desc.B + 1,), torch.int32, 0),),
+                           (("Y", Y, rows, _io(desc), 0), ("state0", state0, sshape, f32, 0),
+                            ("state", state, sshape, f32, 0)))
+    if Y is None:
+        Y = torch.empty(rows, dtype=io, device=dev)
+    if state is None and want_state:
+        state = torch.empty(sshape, dtype=f32, device=dev)
+    if saved is not None:
+        _scan_saved("flex_scan_fwd", desc, saved, dev)
+    ws = _seq_workspace(scan_workspace_size(desc, FLEX_PASS_FWD), ws, dev)
+    _run("flex_scan_fwd", dev, desc, *(t.data_ptr() for t in (X, Bt, Ct, dt, g)), _at(D), off.data_ptr(), _at(state0),
+         Y.data_ptr(), _at(state), *_span(saved), *_span(ws))
+    return Y, state
+
+
+def flex_scan_bwd(desc: flex_scan_desc, X, Bt, Ct, dt, g, D, off, dY, saved, dX=None, dB=None, dC=None, ddt=None, dg=None,
+                  dD=None, ws=None):
+    """Backward of flex_scan_fwd from what it kept in saved, its state0 a constant.  Returns dict(dX, dB, dC,
+    ddt, dg) in the io dtype (rows of no sequence are not written) and dD [H] fp32 (None without a D)."""
+    import torch
+    io, rows, bc, gates = _io(desc), (desc.T, desc.H, desc.P), (desc.T, desc.G, desc.N), (desc.T, desc.H)
+    out = (("dX", dX, rows, io, desc.dx_stride), ("dB", dB, bc, io, desc.db_stride), ("dC", dC, bc, io, desc.dc_stride),
+           ("ddt", ddt, gates, io, 0), ("dg", dg, gates, io, 0))
+    more = (("dD", dD, (desc.H,), torch.float32, 0),)
+    _, dev = _scan_inputs("flex_scan_bwd", desc, desc.T, X, Bt, Ct, dt, g, D,
+                          (("off", off, (desc.B + 1,), torch.int32, 0), ("dY", dY, rows, io, 0)), out + more)
+    grads = _make(out + (more if D is not None else ()), dev)
+    grads.setdefault("dD", dD)
+    _scan_saved("flex_scan_bwd", desc, saved, dev)
+    ws = _seq_workspace(scan_workspace_size(desc, FLEX_PASS_BWD), ws, dev)
+    _run("flex_scan_bwd", dev, desc, *(t.data_ptr() for t in (X, Bt, Ct, dt, g)), _at(D), off.data_ptr(), *_span(saved),
+         dY.data_ptr(), *(_at(t) for t in grads.values()), *_span(ws))
+    return grads
+
+
+def flex_scan_step(desc: flex_scan_desc, x, Bt, Ct, dt, g, D, state, y=None):
+    """One token of every sequence: x [B,H,P], Bt and Ct [B,G,N], dt and g [B,H], state [B,H,N,P] fp32 updated
+    in place.  Returns y [B,H,P]."""
+    import torch
+    rows = (desc.B, desc.H, desc.P)
+    io, dev = _scan_inputs("flex_scan_step", desc, desc.B, x, Bt, Ct, dt, g, D,
+                           (("state", state, (desc.B, desc.H, desc.N, desc.P), torch.float32, 0),),
+                           (("y", y, rows, _io(desc), 0),))
+    if y is None:
+        y = torch.empty(rows, dtype=io, device=dev)
+    _run("flex_scan_step", dev, desc, *(t.data_ptr() for t in (x, Bt, Ct, dt, g)), _at(D), state.data_ptr(), y.data_ptr())
+    return y
+
+
+def make_norm_desc(T, D, group, gate="first", io="bf16", eps=1e-5, x_stride=0, z_stride=0, dx_stride=0,
+                   dz_stride=0) -> flex_norm_desc:
+    """Gated norm of T rows of D channels in groups of `group`; gate "first" (before the norm), "last" or "none";
+    strides in elements between rows (0: contiguous)."""
+    return flex_norm_desc(T, D, group, _GATES.get(gate, -1), FLEX_BF16 if io == "bf16" else FLEX_F32, x_stride, z_stride, dx_stride,
+                          dz_stride, float(eps))
+
+
+def norm_workspace_size(desc: flex_norm_desc) -> int:
+    """Bytes of workspace of flex_norm_bwd."""
+    return _size("flex_norm_workspace_size", desc)
+
+
+def _norm_inputs(what, desc, X, Z, W, more, optional):
+    import torch
+    io, dev, rows = _io(desc), _device(what, X), (desc.T, desc.D)
+    gate = (("Z", Z, rows, io, desc.z_stride),)
+    if desc.gate == 0 and Z is not None:
+        raise FlexError(FLEX_ERR_INVALID_ARG, f"{what}: Z without a gate")
+    _expect(what, dev, (("X", X, rows, io, desc.x_stride), ("W", W, (desc.D,), torch.float32, 0))
+            + (gate if desc.gate else ()) + more, optional)
+    return io, dev
+
+
+def flex_norm_fwd(desc: flex_norm_desc, X, Z, W, Y=None):
+    """Gated norm of rows: X, Z [T,D] (Z None without a gate), W [D] fp32.  Returns Y [T,D]."""
+    import torch
+    rows = (desc.T, desc.D)
+    io, dev = _norm_inputs("flex_norm_fwd", desc, X, Z, W, (), (("Y", Y, rows, _io(desc), 0),))
+    if Y is None:
+        Y = torch.empty(rows, dtype=io, device=dev)
+    _run("flex_norm_fwd", dev, desc, X.data_ptr(), _at(Z), W.data_ptr(), Y.data_ptr())
+    return Y
+
+
+def flex_norm_bwd(desc: flex_norm_desc, X, Z, W, dY, dX=None, dZ=None, dW=None, ws=None):
+    """Backward of flex_norm_fwd.  Returns dict(dX, dZ, dW): dX and dZ (None without a gate) in the io dtype, dW
+    [D] fp32."""
+    import torch
+    io, rows = _io(desc), (desc.T, desc.D)
+    out = (("dX", dX, rows, io, desc.dx_stride), ("dZ", dZ, rows, io, desc.dz_stride),
+           ("dW", dW, (desc.D,), torch.float32, 0))
+    _, dev = _norm_inputs("flex_norm_bwd", desc, X, Z, W, (("dY", dY, rows, io, 0),), out)
+    if desc.gate == 0:
+        if dZ is not None:
+            raise FlexError(FLEX_ERR_INVALID_ARG, "flex_norm_bwd: dZ without a gate")
+        out = (out[0], out[2])
+    made = _make(out, dev)
+    grads = {n: made.get(n) for n in ("dX", "dZ", "dW")}
+    ws = _seq_workspace(norm_workspace_size(desc), ws, dev)
+    _run("flex_norm_bwd", dev, desc, X.data_ptr(), _at(Z), W.data_ptr(), dY.data_ptr(), *(_at(t) for t in grads.values()),
+         *_span(ws))
+    return grads
 
 
 def flex_timing_enable(kernel: str) -> None:

@@ -1,0 +1,292 @@
+// Gated norm of rows, forward and backward.  With gate s = silu(z), r = 1 / sqrt(mean(u^2) + eps), n = u r:
+//   gate first  u = x s,  y = n w        gate last  u = x,  y = n w s        none  u = x,  y = n w
+//   dn = dy w (times s, gate last),  du = r (dn - n mean(dn n)),  dW = sum_rows dy n (times s, gate last)
+//   first  dx = du s, ds = du x          last  dx = du, ds = dy n w          dz = ds silu'(z)
+//
+// A team of lanes has a group: 8 channels a lane and piece, the pieces of a group TEAM * 8 channels
+// apart.  Teams stay on their channels, with their part of W (and the sum of dW) in registers, and go
+// from row to row, the next row on its way while one is worked on.  One pass over the data: bound by
+// memory.
+#include <type_traits>
+#include "flex_rows.hpp"
+#include "flex_layer_kernels.hpp"
+#include "../../include/flex.h"
+
+namespace flex {
+
+namespace {
+struct Eight {
+  float v[8];
+};
+template <class S>
+struct Raw8 {
+  Piece<S> p[8 / Piece<S>::N];
+  __device__ __forceinline__ void load(const S* q, bool in) {
+#pragma unroll
+    for (int i = 0; i < 8 / Piece<S>::N; ++i)
+      if (in) p[i].load(q + i * Piece<S>::N);
+      else p[i].zero();
+  }
+  __device__ __forceinline__ void get(Eight& x) const {
+#pragma unroll
+    for (int i = 0; i < 8 / Piece<S>::N; ++i) p[i].get(x.v + i * Piece<S>::N);
+  }
+  static __device__ __forceinline__ void store(S* q, const Eight& x) {
+#pragma unroll
+    for (int i = 0; i < 8 / Piece<S>::N; ++i) Piece<S>::store(q + i * Piece<S>::N, x.v + i * Piece<S>::N);
+  }
+};
+
+// Sums over a team, in every lane of it: aligned lanes of a wave, `team` a power of two, or a
+// workgroup of four waves (each passes through `box`, of which two are used in turn: one barrier a sum).
+template <bool WG, int N>
+__device__ __forceinline__ void team_sum(float (&x)[N], int team, float (*box)[4], int turn) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (WG || team > 1) x[i] = dpp_add(x[i], 0);
+    if (WG || team > 2) x[i] = dpp_add(x[i], 1);
+    if (WG || team > 4) x[i] = dpp_add(x[i], 2);
+    if (WG || team > 8) x[i] = dpp_add(x[i], 3);
+    if (WG || team > 16) {
+      const unsigned v = __float_as_uint(x[i]);
+      const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+      x[i] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    if (WG || team > 32) x[i] = half_sum(x[i]);
+  }
+  if (WG) {
+    const int w = threadIdx.x / WAVE;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (threadIdx.x % WAVE == 0) box[turn * N + i][w] = x[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = (box[turn * N + i][0] + box[turn * N + i][1]) + (box[turn * N + i][2] + box[turn * N + i][3]);
+  }
+}
+}  // namespace
+
+// Where a lane works: rows row0, row0 + step, ... and pieces at channels c + i * team * 8 of them
+struct NormPlace {
+  int row0, step, c, end, team;
+  template <bool WG>
+  __device__ __forceinline__ static NormPlace of(const NormArgs& a, int team) {
+    NormPlace p;
+    const int groups = a.D / a.group;
+    p.team = WG ? 256 : team;
+    const unsigned id = blockIdx.x * 256u + threadIdx.x, t = WG ? blockIdx.x : id / (unsigned)team;
+    p.row0 = t / (unsigned)groups;
+    const int base = t % (unsigned)groups * a.group;
+    p.c = base + (WG ? (int)threadIdx.x : (int)(id % (unsigned)team)) * 8;
+    p.end = base + a.group;
+    p.step = a.parts;
+    return p;
+  }
+};
+
+template <class S, int GATE, int PIECES, bool WG>
+__global__ __launch_bounds__(256) void k_norm_fwd(NormArgs a, int team, float inv) {
+  __shared__ float box[2][4];
+  const NormPlace p = NormPlace::of<WG>(a, team);
+  if (p.row0 >= a.parts) return;   // never a part of a team
+  Eight w[PIECES];
+  Raw8<S> nx[PIECES], nz[PIECES];
+  bool in[PIECES];
+  auto fetch = [&](int row) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int c = p.c + i * p.team * 8;
+      nx[i].load(static_cast<const S*>(a.X) + (size_t)row * a.xs + c, in[i]);
+      if (GATE != FLEX_GATE_NONE) nz[i].load(static_cast<const S*>(a.Z) + (size_t)row * a.zs + c, in[i]);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) in[i] = p.c + i * p.team * 8 < p.end;
+  fetch(p.row0);
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    Raw8<float> r;
+    r.load(a.W + p.c + i * p.team * 8, in[i]);
+    r.get(w[i]);
+  }
+  int turn = 0;
+  for (int row = p.row0; row < a.T; row += p.step, turn ^= 1) {
+    Eight u[PIECES], s[PIECES];
+    float sum[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      nx[i].get(u[i]);
+      if (GATE != FLEX_GATE_NONE) {
+        nz[i].get(s[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[i].v[e] *= sigmoid(s[i].v[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (GATE == FLEX_GATE_FIRST) u[i].v[e] *= s[i].v[e];
+        sum[0] = __builtin_fmaf(u[i].v[e], u[i].v[e], sum[0]);
+      }
+    }
+    if (row + p.step < a.T) fetch(row + p.step);
+    team_sum<WG>(sum, team, box, turn);
+    const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[0], inv, a.eps));
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        u[i].v[e] = u[i].v[e] * r * w[i].v[e];
+        if (GATE == FLEX_GATE_LAST) u[i].v[e] *= s[i].v[e];
+      }
+      if (in[i]) Raw8<S>::store(static_cast<S*>(a.Y) + (size_t)row * a.D + p.c + i * p.team * 8, u[i]);
+    }
+  }
+}
+
+template <class S, int GATE, int PIECES, bool WG>
+__global__ __launch_bounds__(256) void k_norm_bwd(NormArgs a, int team, float inv) {
+  __shared__ float box[4][4];
+  const NormPlace p = NormPlace::of<WG>(a, team);
+  if (p.row0 >= a.parts) return;
+  Eight w[PIECES], dw[PIECES];
+  Raw8<S> nx[PIECES], nz[PIECES], ng[PIECES];
+  bool in[PIECES];
+  auto fetch = [&](int row) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int c = p.c + i * p.team * 8;
+      nx[i].load(static_cast<const S*>(a.X) + (size_t)row * a.xs + c, in[i]);
+      if (GATE != FLEX_GATE_NONE) nz[i].load(static_cast<const S*>(a.Z) + (size_t)row * a.zs + c, in[i]);
+      ng[i].load(static_cast<const S*>(a.dY) + (size_t)row * a.D + c, in[i]);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    in[i] = p.c + i * p.team * 8 < p.end;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[i].v[e] = 0.f;
+  }
+  if (p.row0 < a.T) fetch(p.row0);
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    Raw8<float> r;
+    r.load(a.W + p.c + i * p.team * 8, in[i]);
+    r.get(w[i]);
+  }
+  int turn = 0;
+  for (int row = p.row0; row < a.T; row += p.step, turn ^= 1) {
+    Eight x[PIECES], z[PIECES], sig[PIECES], g[PIECES];
+    float sum[2] = {0.f, 0.f};   // of u^2, of dn u
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      nx[i].get(x[i]);
+      ng[i].get(g[i]);
+      if (GATE != FLEX_GATE_NONE) nz[i].get(z[i]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (GATE != FLEX_GATE_NONE) sig[i].v[e] = sigmoid(z[i].v[e]);
+        const float s = GATE != FLEX_GATE_NONE ? z[i].v[e] * sig[i].v[e] : 1.f;
+        const float u = GATE == FLEX_GATE_FIRST ? x[i].v[e] * s : x[i].v[e];
+        float dn = g[i].v[e] * w[i].v[e];
+        if (GATE == FLEX_GATE_LAST) dn *= s;
+        sum[0] = __builtin_fmaf(u, u, sum[0]);
+        sum[1] = __builtin_fmaf(dn, u, sum[1]);
+      }
+    }
+    if (row + p.step < a.T) fetch(row + p.step);
+    team_sum<WG>(sum, team, box, turn);
+    const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[0], inv, a.eps));
+    const float m = sum[1] * r * inv;   // mean(dn n)
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      Eight dz;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float s = GATE != FLEX_GATE_NONE ? z[i].v[e] * sig[i].v[e] : 1.f;
+        const float ds = GATE != FLEX_GATE_NONE ? dsilu(z[i].v[e], sig[i].v[e]) : 0.f;
+        const float n = (GATE == FLEX_GATE_FIRST ? x[i].v[e] * s : x[i].v[e]) * r;
+        const float gn = g[i].v[e] * n;
+        float dn = g[i].v[e] * w[i].v[e];
+        if (GATE == FLEX_GATE_LAST) dn *= s;
+        const float du = r * (dn - n * m);
+        dw[i].v[e] += GATE == FLEX_GATE_LAST ? gn * s : gn;
+        dz.v[e] = (GATE == FLEX_GATE_FIRST ? du * x[i].v[e] : gn * w[i].v[e]) * ds;
+        x[i].v[e] = GATE == FLEX_GATE_FIRST ? du * s : du;
+      }
+      const int c = p.c + i * p.team * 8;
+      if (in[i]) {
+        Raw8<S>::store(static_cast<S*>(a.dX) + (size_t)row * a.dxs + c, x[i]);
+        if (GATE != FLEX_GATE_NONE) Raw8<S>::store(static_cast<S*>(a.dZ) + (size_t)row * a.dzs + c, dz);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i)
+    if (in[i]) Raw8<float>::store(a.part + (size_t)p.row0 * a.D + p.c + i * p.team * 8, dw[i]);
+}
+
+// Sums of the parts, 64 channels to a workgroup, each of its 16 waves a sixteenth of the parts.
+__global__ __launch_bounds__(1024) void k_norm_sum(NormArgs a) {
+  __shared__ double sums[16][WAVE];
+  const int l = threadIdx.x % WAVE, w = threadIdx.x / WAVE, c = blockIdx.x * WAVE + l;
+  const float* p = a.part + (c < a.D ? c : 0);
+  const int per = (a.parts + 15) / 16, p0 = w * per, p1 = min(p0 + per, a.parts);
+  double s = 0.0;
+#pragma unroll 8
+  for (int i = p0; i < p1; ++i) s += (double)p[(size_t)i * a.D];
+  sums[w][l] = s;
+  __syncthreads();
+  if (w > 0 || c >= a.D) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) s += sums[i][l];
+  a.dW[c] = (float)s;
+}
+
+namespace {
+// Lanes of a team: as many as a group has pieces of 8 channels, a power of two up to a wave, then a wave of
+// up to four pieces a lane, then a workgroup.
+template <bool BWD, class S, int GATE>
+void run(const NormArgs& a, hipStream_t st) {
+  const int units = a.group / 8, groups = a.D / a.group;
+  const float inv = 1.f / (float)a.group;
+  int team = 1;
+  while (team < units && team < WAVE) team *= 2;
+  const int64_t teams = (int64_t)a.parts * groups;
+  const unsigned grid = (unsigned)((teams * team + 255) / 256), wide = (unsigned)teams;
+  auto go = [&](auto pieces, auto wg) {
+    constexpr int P = decltype(pieces)::value;
+    constexpr bool W = decltype(wg)::value;
+    if constexpr (BWD)
+      k_norm_bwd<S, GATE, P, W><<<W ? wide : grid, 256, 0, st>>>(a, team, inv);
+    else
+      k_norm_fwd<S, GATE, P, W><<<W ? wide : grid, 256, 0, st>>>(a, team, inv);
+  };
+  using std::integral_constant;
+  if (units <= 64) go(integral_constant<int, 1>{}, integral_constant<bool, false>{});
+  else if (units <= 128) go(integral_constant<int, 2>{}, integral_constant<bool, false>{});
+  else if (units <= 256) go(integral_constant<int, 4>{}, integral_constant<bool, false>{});
+  else if (units <= 512) go(integral_constant<int, 2>{}, integral_constant<bool, true>{});
+  else go(integral_constant<int, 4>{}, integral_constant<bool, true>{});
+}
+template <bool BWD, class S>
+void by_gate(const NormArgs& a, hipStream_t st) {
+  if (a.gate == FLEX_GATE_NONE) run<BWD, S, FLEX_GATE_NONE>(a, st);
+  if (a.gate == FLEX_GATE_FIRST) run<BWD, S, FLEX_GATE_FIRST>(a, st);
+  if (a.gate == FLEX_GATE_LAST) run<BWD, S, FLEX_GATE_LAST>(a, st);
+}
+}  // namespace
+
+hipError_t launch_norm_fwd(const NormArgs& a, bool bf16, hipStream_t st) {
+  timing_mark(FLEX_KERNEL_NORM_FWD, st, true);
+  bf16 ? by_gate<false, u16>(a, st) : by_gate<false, float>(a, st);
+  timing_mark(FLEX_KERNEL_NORM_FWD, st, false);
+  return hipGetLastError();
+}
+hipError_t launch_norm_bwd(const NormArgs& a, bool bf16, hipStream_t st) {
+  timing_mark(FLEX_KERNEL_NORM_BWD, st, true);
+  bf16 ? by_gate<true, u16>(a, st) : by_gate<true, float>(a, st);
+  k_norm_sum<<<(a.D + WAVE - 1) / WAVE, 1024, 0, st>>>(a);
+  timing_mark(FLEX_KERNEL_NORM_BWD, st, false);
+  return hipGetLastError();
+}
+
+}  // namespace flex

@@ -1,0 +1,142 @@
+// Device building blocks of the selective scan's kernels.
+//
+//   S_t = e^{g_t} S_{t-1} + dt_t B_t x_t^T,   y_t = S_t^T C_t + D x_t
+//
+// In chunks of 64 tokens, L the inclusive sum of g within the chunk and S [N x P] the state at its start:
+//   P_ij = e^{L_i - L_j} (C_i.B_j) dt_j (j <= i)     y = P x + e^L (C S) + D x
+//   S <- e^{L_63} S + B^T (w x),                     w_j = e^{L_63 - L_j} dt_j
+//
+// A wave has 32 columns of a head's state in registers, as 32 x 32 results with the rows n and a lane per
+// column.  Both matrix operands have the same layout (a row or column per lane, eight contraction indices in
+// its slots), so a result whose rows are the next product's contraction is that product's operand as it is, on
+// either side: S -> C S, C B^T -> P, without a pass through LDS.
+// Rows of a result are dealt so that the eight a lane holds of a step of 16 are consecutive (perm32): element e
+// of lane half h of a 32-row tile is row 16 (e / 8) + 8 h + e % 8.  A row operand is then read 16 bytes at once,
+// and a lane's results are stored 16 bytes at once.
+#pragma once
+#include <type_traits>
+#include "flex_seq.hpp"
+#include "flex_rows.hpp"
+#include "flex_layer_kernels.hpp"
+
+namespace flex {
+
+constexpr int SC = SCAN_CHUNK;
+
+// the row (or column) of 32 that lane r % 32 of an operand stands for, so that results come as above
+__device__ __forceinline__ constexpr int perm32(int r) { return (r & 16) | ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 | (r & 3); }
+// row of a tile that element e of lane half h of a result of permuted rows is
+__device__ __forceinline__ constexpr int perm_row(int e, int h) { return 16 * (e / 8) + 8 * h + e % 8; }
+
+template <class T, int D>
+struct ScanTile : RowTile<T, D> {
+  using R = RowTile<T, D>;
+  // Columns m0 + perm32(l % 32), slots 0..3 the rows r0 .. r0+3, slots 4..7 r1 .. r1+3
+  static __device__ __forceinline__ Frag<T> colp(const char* L, int r0, int r1, int m0) {
+    const int l = threadIdx.x % WAVE;
+    Frag<T> f;
+    if constexpr (IsBf16<T>::value) {
+      // the lane's part of the read: row i / 4, of the 16 columns the quarter that place i % 4 takes
+      const int i = l % 16, q = (i & 1) << 1 | (i >> 1 & 1);
+      const int m = m0 + 16 * ((l / 16) & 1) + 4 * q, c = m / 8, o = (m % 8) * 2;
+      const tr_v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(L + R::at(r0 + i / 4, c) + o));
+      const tr_v4i16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(L + R::at(r1 + i / 4, c) + o));
+      f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      const int m = m0 + perm32(l % 32), c = m / 4, o = (m % 4) * 4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        f.v[j] = *reinterpret_cast<const float*>(L + R::at(r0 + j, c) + o);
+        f.v[4 + j] = *reinterpret_cast<const float*>(L + R::at(r1 + j, c) + o);
+      }
+    }
+    return f;
+  }
+};
+
+// Stages 64 rows of a window by `nw` waves of which this is w, 16 rows at a time.
+template <class T, int D>
+__device__ __forceinline__ void stage_rows(const char* L, const typename Io<T>::type* base, size_t row0, int stride, int n, int w,
+                                           int nw) {
+  for (int k = w; k < 4; k += nw)
+    stage_tile<T, D, 16, 1>(L + k * 16 * D * (int)sizeof(T), row_words(base, row0 + 16 * k, stride, n - 16 * k, D),
+                            stride * (int)sizeof(T), 0);
+}
+
+// Inclusive sum over the lanes of a wave.
+__device__ __forceinline__ double wave_scan(double x) {
+  auto step = [&](auto ctrl, auto rows) {
+    const uint64_t v = __builtin_bit_cast(uint64_t, x);
+    const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(v >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    x += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+  };
+  using std::integral_constant;
+  step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});   // from 1, 2, 4, 8 lanes before within 16
+  step(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});   // lane 15 of the 16 before
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});   // lane 31
+  return x;
+}
+__device__ __forceinline__ double last_lane(double x) {
+  const uint64_t v = __builtin_bit_cast(uint64_t, x);
+  const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)v, WAVE - 1), hi = __builtin_amdgcn_readlane((int)(unsigned)(v >> 32), WAVE - 1);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// A chunk's decays, lane = token.  Sums of g in 64 bits, in units of log2 as two floats, so that differences of
+// them are as exact as floats are; a decay of zero (g = -inf) is kept as a finite sum whose exponential is
+// zero, so that the differences are defined.
+constexpr float SCAN_MIN_G = -1e4f;
+struct Decay {
+  double L, end;    // the token's, and the chunk's, in units of log2
+  float hi, lo;     // the token's
+  __device__ __forceinline__ explicit Decay(float g) {
+    if (g < SCAN_MIN_G) g = SCAN_MIN_G;
+    L = wave_scan((double)g * 1.4426950408889634);
+    end = last_lane(L);
+    hi = (float)L;
+    lo = (float)(L - (double)hi);
+  }
+  __device__ __forceinline__ float from_start() const { return __builtin_amdgcn_exp2f(hi); }
+  __device__ __forceinline__ float to_end() const { return __builtin_amdgcn_exp2f((float)(end - L)); }
+};
+// e^{L_i - L_j}
+__device__ __forceinline__ float decay(float hi_i, float lo_i, float hi_j, float lo_j) {
+  return __builtin_amdgcn_exp2f((hi_i - hi_j) + (lo_i - lo_j));
+}
+
+// The work of a workgroup of a sweep: a segment of a sequence (tokens t0 .. of it) and a set of heads of one group.
+// Consecutive workgroups go round-robin to the XCDs: an XCD gets all sets of a segment, which read the same
+// rows of B and C.
+struct SegTile {
+  int b, row0, n;     // sequence (-1: none), first row and length of it
+  int index, count;   // which of how many segments
+  int slot, set;
+};
+__device__ __forceinline__ SegTile find_segment(const int32_t* __restrict__ off, int B, int T, int seg, int sets) {
+  const int id = blockIdx.x, k = id / NUM_XCD;
+  SegTile t;
+  t.slot = k / sets * NUM_XCD + id % NUM_XCD;
+  t.set = k % sets;
+  t.b = -1;
+  t.row0 = t.n = t.index = t.count = 0;
+  if (t.slot >= seq_slots(T, B, seg)) return t;
+  const int slot = t.slot;
+  const int cnt = leading(B, [=](int b) { return clamp_off(off[b], T) / seg + b <= slot; });
+  if (cnt == 0) return t;
+  const SeqRange r = seq_range(off, cnt - 1, T);
+  t.row0 = r.row0;
+  t.n = r.n;
+  t.index = slot - (r.row0 / seg + cnt - 1);
+  t.count = max(1, (r.n + seg - 1) / seg);   // a sequence without tokens has one, for its state
+  if (t.index >= 0 && t.index < t.count) t.b = __builtin_amdgcn_readfirstlane(cnt - 1);
+  t.index = __builtin_amdgcn_readfirstlane(t.index);
+  t.count = __builtin_amdgcn_readfirstlane(t.count);
+  return t;
+}
+inline int seg_grid(int T, int B, int seg, int sets) { return (seq_slots(T, B, seg) + NUM_XCD - 1) / NUM_XCD * NUM_XCD * sets; }
+
+}  // namespace flex

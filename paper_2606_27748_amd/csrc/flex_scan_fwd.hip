@@ -1,0 +1,472 @@
+// Selective scan, forward: the sweep over the chunks (k_scan_sweep), what joins the segments of a
+// sequence (k_scan_join), the single-token step (k_scan_step), and the sweeps that carry a state alone,
+// forwards or, for the backward, in reverse.
+#include <type_traits>
+#include "flex_scan.hpp"
+#include "../../include/flex.h"
+
+namespace flex {
+
+namespace {
+enum {
+  CARRY,       // what a segment leaves, forwards: no rows out
+  SWEEP,       // y
+  SWEEP_SAVE,  // y, and the state at each chunk's start
+  REV_CARRY,   // what a segment leaves of the state's gradient, in reverse
+  REV_SAVE     // the gradient of the state at each chunk's end
+};
+constexpr bool is_rev(int mode) { return mode >= REV_CARRY; }
+constexpr bool is_carry(int mode) { return mode == CARRY || mode == REV_CARRY; }
+constexpr bool has_y(int mode) { return mode == SWEEP || mode == SWEEP_SAVE; }
+
+// c += a x for operands a that are exact and fp32 values x, as three bf16 terms (24 bits) or as they are.
+// Two terms leave 2^-18 of each product: 1.5e-6 of a state, where fp32 sums leave 1e-7.
+__device__ __forceinline__ void split3(Frag<__bf16> (&t)[3], const float (&x)[8]) {
+#pragma clang fp contract(off)
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const __bf16 a = (__bf16)x[j];
+    const float r = x[j] - (float)a;
+    const __bf16 b = (__bf16)r;
+    t[0].v[j] = a;
+    t[1].v[j] = b;
+    t[2].v[j] = (__bf16)(r - (float)b);
+  }
+}
+__device__ __forceinline__ void split3(Frag<float> (&t)[1], const float (&x)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) t[0].v[j] = x[j];
+}
+}  // namespace
+
+// Workgroups: a segment and a set of heads of one group; a wave has 32 columns of one head's state.  The rows of B
+// (and C) pass through LDS for all of them, its own columns of x for each wave, the next chunk on its way while one is
+// worked on where two fit.  In reverse the state is its gradient dS, the rows C, x is dy and the weights are e^L:
+//   dS <- e^{L_63} dS + C^T (e^L dy)
+template <class T, int N, int MODE>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_sweep(ScanArgs a) {
+  using S = typename Io<T>::type;
+  using RT = ScanTile<T, N>;
+  using XT = ScanTile<T, 32>;
+  constexpr bool REV = is_rev(MODE), Y = has_y(MODE);
+  constexpr int NS = N / 16, NT = N / 32, TERMS = IsBf16<T>::value ? 3 : 1;
+  constexpr int ROWS = SC * N * (int)sizeof(T), XROWS = SC * 32 * (int)sizeof(T);
+  constexpr int BUF = (Y ? 2 : 1) * ROWS + 8 * XROWS, SCAL = Y ? 5 * SC : SC;
+  constexpr int BUFS = 2 * BUF + 8 * SCAL * 4 <= 160 * 1024 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) char lds[BUFS * BUF];
+  __shared__ __attribute__((aligned(16))) float scal[8][SCAL];
+  const int l = threadIdx.x % WAVE, c = l % 32, h = l / 32;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
+  const SegTile sg = find_segment(a.off, a.B, a.T, a.seg, a.H / a.heads);
+  if (sg.b < 0) return;
+  const bool last_seg = sg.index == sg.count - 1;
+  if (MODE == CARRY && last_seg) return;
+  if (MODE == REV_CARRY && sg.index == 0) return;
+  const int per = a.P / 32, head = sg.set * a.heads + w / per, p0 = w % per * 32, grp = head / (a.H / a.G);
+  const int t0 = sg.index * a.seg, n = min(sg.n - t0, a.seg), row0 = sg.row0 + t0;
+  const int nchunks = (n + SC - 1) / SC, slot0 = sg.row0 / SC + sg.b + t0 / SC;
+  const int pc = p0 + perm32(c);   // this lane's column of the state
+
+  const S* rb = static_cast<const S*>(REV ? a.Ct : a.Bt) + (size_t)grp * N;
+  const S* rc = static_cast<const S*>(a.Ct) + (size_t)grp * N;
+  const S* rx = REV ? static_cast<const S*>(a.dY) + (size_t)head * a.P + p0 : static_cast<const S*>(a.X) + (size_t)head * a.P + p0;
+  const int bs = REV ? a.cs : a.bs, xs = REV ? a.H * a.P : a.xs;
+  auto buf = [&](int k) { return lds + (BUFS == 2 ? (k & 1) * BUF : 0); };
+  auto stage = [&](int k, int chunk) {
+    const int r = row0 + chunk * SC, m = min(SC, n - chunk * SC);
+    const char* L = buf(k);
+    stage_rows<T, N>(L, rb, r, bs, m, w, nw);
+    if (Y) stage_rows<T, N>(L + ROWS, rc, r, a.cs, m, nw - 1 - w, nw);
+    stage_tile<T, 32, SC, 1>(L + (Y ? 2 : 1) * ROWS + w * XROWS, row_words(rx, r, xs, m, 32), xs * (int)sizeof(S), 0);
+  };
+  float gn = 0.f, dn = 0.f;   // of the next chunk, lane = token
+  auto fetch = [&](int chunk) {
+    const int t = chunk * SC + l;
+    gn = dn = 0.f;
+    if (t < n) {
+      const size_t at = (size_t)(row0 + t) * a.H + head;
+      gn = a.g[at];
+      if (!REV) dn = a.dt[at];
+    }
+  };
+
+  f32x16 st[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) st[i] = zero16();
+  // tile i's elements 4 q .. + 3 of every lane, in a row
+  float* carry = a.carry ? a.carry + ((size_t)sg.slot * a.H + head) * N * a.P + (size_t)p0 * N + l * 4 : nullptr;
+  const bool from_state0 = !REV && a.state0 && sg.index == 0 && (MODE == CARRY || sg.count == 1);
+  if (from_state0) {
+    const float* s0 = a.state0 + ((size_t)sg.b * a.H + head) * N * a.P + pc;
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) st[i][e] = s0[(size_t)(32 * i + perm_row(e, h)) * a.P];
+  } else if (!is_carry(MODE) && carry && (REV ? !last_seg : sg.index > 0 || (a.state0 && sg.count > 1))) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(carry + (i * 4 + q) * WAVE * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st[i][4 * q + e] = v[e];
+      }
+  }
+  auto keep = [&](void* base, int chunk, const Frag<T> (&f)[NS]) {   // as [P][N]
+    S* p = static_cast<S*>(base) + (((size_t)(slot0 + chunk) * a.H + head) * a.P + pc) * N + 8 * h;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      if constexpr (IsBf16<T>::value) {
+        *reinterpret_cast<bf16x8*>(p + 16 * s) = f[s].v;
+      } else {
+        *reinterpret_cast<f32x4*>(p + 16 * s) = f32x4{f[s].v[0], f[s].v[1], f[s].v[2], f[s].v[3]};
+        *reinterpret_cast<f32x4*>(p + 16 * s + 4) = f32x4{f[s].v[4], f[s].v[5], f[s].v[6], f[s].v[7]};
+      }
+    }
+  };
+  auto state_frags = [&](Frag<T> (&f)[NS]) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) f[s] = frag_of<T>(st[s / 2], s % 2);
+  };
+
+  float* sc = scal[w];
+  double total = 0.0;
+  const float Dh = Y && a.D ? a.D[head] : 0.f;
+  if (nchunks > 0) {
+    const int first = REV ? nchunks - 1 : 0;
+    stage(0, first);
+    fetch(first);
+  }
+  for (int k = 0; k < nchunks; ++k) {
+    const int chunk = REV ? nchunks - 1 - k : k, next = REV ? chunk - 1 : chunk + 1;
+    const char* L = buf(k);
+    sync_tiles();   // the chunk is in LDS, and the buffer of the one before is free
+    const Decay d(gn);
+    if (Y) {
+      sc[l] = d.hi;
+      sc[SC + l] = d.lo;
+      sc[2 * SC + l] = dn;
+      sc[3 * SC + l] = d.from_start();
+      sc[4 * SC + l] = d.to_end() * dn;
+    } else {
+      sc[l] = REV ? d.from_start() : d.to_end() * dn;
+    }
+    const float last = __builtin_amdgcn_exp2f((float)d.end);
+    if (is_carry(MODE)) total += d.end;
+    if (BUFS == 2 && k + 1 < nchunks) stage(k + 1, next);
+    if (k + 1 < nchunks) fetch(next);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the wave's own writes above
+
+    const char* LX = L + (Y ? 2 : 1) * ROWS + w * XROWS;
+    Frag<T> xf[4];   // columns of x, slots the tokens 16 q + 4 h + i and 8 further
+#pragma unroll
+    for (int q = 0; q < 4; ++q) xf[q] = XT::colp(LX, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 0);
+
+    if constexpr (MODE == REV_SAVE) {
+      Frag<T> sb[NS];
+      state_frags(sb);
+      keep(a.dst, chunk, sb);
+    }
+    if constexpr (Y) {
+      const char* LC = L + ROWS;
+      f32x16 y[2] = {zero16(), zero16()}, cb[3] = {zero16(), zero16(), zero16()};
+      {
+        Frag<T> sb[NS];
+        state_frags(sb);
+        if constexpr (MODE == SWEEP_SAVE) keep(a.st, chunk, sb);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          const Frag<T> c0 = RT::row(LC, c, s, h), c1 = RT::row(LC, 32 + c, s, h);
+          const Frag<T> b0 = RT::row(L, c, s, h), b1 = RT::row(L, 32 + c, s, h);
+          mma32(y[0], sb[s], c0);
+          mma32(cb[0], b0, c0);
+          mma32(y[1], sb[s], c1);
+          mma32(cb[1], b0, c1);
+          mma32(cb[2], b1, c1);
+        }
+      }
+      // x with a value that is not finite: its column's products go over the rows before it only, and the rows from it on are NaN
+      float bad = 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bad = __builtin_fmaf(xf[q].get(j), 0.f, bad);
+      const bool any_bad = __any(bad != 0.f);
+      int fb = SC;
+      Frag<T> xc[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) xc[q] = xf[q];
+      if (any_bad) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (!(fabsf(xf[q].get(j)) < INFINITY)) fb = min(fb, 16 * q + 4 * h + 8 * (j / 4) + j % 4);
+        fb = min(fb, __shfl_xor(fb, 32));
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (16 * q + 4 * h + 8 * (j / 4) + j % 4 >= fb) xc[q].set(j, 0.f);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float hi = sc[32 * i + c], lo = sc[SC + 32 * i + c], eg = sc[3 * SC + 32 * i + c];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) y[i][e] *= eg;
+#pragma unroll
+        for (int j = 0; j <= i; ++j) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int t = 32 * j + 8 * q + 4 * h;
+            const f32x4 hj = *reinterpret_cast<const f32x4*>(sc + t), lj = *reinterpret_cast<const f32x4*>(sc + SC + t);
+            const f32x4 dj = *reinterpret_cast<const f32x4*>(sc + 2 * SC + t);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = cb[i + j][4 * q + e];
+              cb[i + j][4 * q + e] = j < i || t + e <= 32 * i + c ? v * (decay(hi, lo, hj[e], lj[e]) * dj[e]) : 0.f;
+            }
+          }
+#pragma unroll
+          for (int s = 0; s < 2; ++s) mma32(y[i], xc[2 * j + s], frag_of<T>(cb[i + j], s));
+        }
+      }
+      if (any_bad) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int f = __shfl(fb, 8 * (e / 4) + 4 * h + e % 4);
+          if (c >= f) y[0][e] = NAN;
+          if (32 + c >= f) y[1][e] = NAN;
+        }
+      }
+      const int m = min(SC, n - chunk * SC), ys = a.H * a.P;
+      const auto ry = row_window(static_cast<S*>(a.Y) + (size_t)head * a.P + p0, row0 + chunk * SC, ys, m, 32);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const Frag<T> xr = XT::row(LX, 32 * i + c, s, h);
+          const int at = ((32 * i + c) * ys + 16 * s + 8 * h) * (int)sizeof(S);
+          float v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf(Dh, xr.get(j), y[i][8 * s + j]);
+          if constexpr (IsBf16<T>::value) {
+            Frag<T> o;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o.set(j, v[j]);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o.v), ry, at, 0, 0);
+          } else {
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}), ry, at, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]}), ry, at + 16, 0, 0);
+          }
+        }
+    }
+    // S <- e^{L_63} S + B^T (w x)
+    Frag<T> wx[4][TERMS];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float* ws = sc + (Y ? 4 * SC : 0) + 16 * q + 4 * h;
+      const f32x4 w0 = *reinterpret_cast<const f32x4*>(ws), w1 = *reinterpret_cast<const f32x4*>(ws + 8);
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = xf[q].get(j) * (j < 4 ? w0[j % 4] : w1[j % 4]);
+      split3(wx[q], v);
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      f32x16 u = zero16();
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const Frag<T> bf = RT::colp(L, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 32 * i);
+#pragma unroll
+        for (int t = TERMS - 1; t >= 0; --t) mma32(u, bf, wx[q][t]);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) st[i][e] = __builtin_fmaf(st[i][e], last, u[e]);
+    }
+    if (BUFS == 1) {
+      sync_lds();
+      if (k + 1 < nchunks) stage(k + 1, next);
+    }
+  }
+  if (is_carry(MODE)) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(carry + (i * 4 + q) * WAVE * 4) =
+            f32x4{st[i][4 * q], st[i][4 * q + 1], st[i][4 * q + 2], st[i][4 * q + 3]};
+    if (l == 0 && p0 == 0) a.tot[(size_t)sg.slot * a.H + head] = __builtin_amdgcn_exp2f((float)total);
+  }
+  if (Y && a.state && last_seg) {
+    float* so = a.state + ((size_t)sg.b * a.H + head) * N * a.P + pc;
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) so[(size_t)(32 * i + perm_row(e, h)) * a.P] = st[i][e];
+  }
+}
+
+// What each segment leaves becomes what it starts from, a sequence's segments in order (in reverse: from the last
+// one), a thread for four elements of a state.  The first segment left the whole state, state0 in it.
+template <bool REV>
+__global__ __launch_bounds__(256) void k_scan_join(ScanArgs a) {
+  const int size = a.N * a.P / 4, blocks = (a.H * size + 255) / 256;
+  const int b = blockIdx.x / blocks, id = blockIdx.x % blocks * 256 + threadIdx.x;
+  if (id >= a.H * size) return;
+  const int head = id / size, at = id % size;
+  const SeqRange r = seq_range(a.off, b, a.T);
+  const int count = (r.n + a.seg - 1) / a.seg, slot0 = r.row0 / a.seg + b;
+  if (count < 2) return;
+  f32x4* p = reinterpret_cast<f32x4*>(a.carry) + ((size_t)slot0 * a.H + head) * size + at;
+  const float* tot = a.tot + (size_t)slot0 * a.H + head;
+  const size_t step = (size_t)a.H * size;
+  constexpr int U = 8;
+  if (REV) {
+    f32x4 s = p[(count - 1) * step];
+    for (int k0 = count - 2; k0 >= 0; k0 -= U) {
+      f32x4 v[U];
+      float d[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = max(k0 - u, 1);
+        v[u] = p[k * step];
+        d[u] = tot[(size_t)k * a.H];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (k0 - u >= 0) {
+          p[(k0 - u) * step] = s;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[e] = __builtin_fmaf(s[e], d[u], v[u][e]);
+        }
+    }
+    return;
+  }
+  f32x4 s = p[0];
+  if (a.state0) {   // the place of element e of lane l of tile i, 4 q + e % 4 of it
+    const int l = at % WAVE, q = at / WAVE % 4, i = at / (WAVE * 4) % (a.N / 32), p0 = at / (WAVE * 4 * (a.N / 32)) * 32;
+    const float* s0 = a.state0 + ((size_t)b * a.H + head) * a.N * a.P + (size_t)(32 * i + perm_row(4 * q, l / 32)) * a.P + p0 + perm32(l % 32);
+    p[0] = f32x4{s0[0], s0[a.P], s0[2 * a.P], s0[3 * a.P]};
+  }
+  for (int k0 = 1; k0 < count; k0 += U) {
+    f32x4 v[U];
+    float d[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = min(k0 + u, count - 2);   // the last one's is not needed
+      v[u] = p[k * step];
+      d[u] = tot[(size_t)k * a.H];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < count) {
+        p[(k0 + u) * step] = s;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = __builtin_fmaf(s[e], d[u], v[u][e]);
+      }
+  }
+}
+
+// One token of every sequence and head, fp32 throughout.  A workgroup has a state: each thread four
+// columns of N / ROWS rows, in registers between the read and the write.  Bound by the state's read and write.
+template <class S, int N, int P>
+__global__ __launch_bounds__(256) void k_scan_step(ScanArgs a) {
+  constexpr int C4 = P / 4, RG = 256 / C4, ROWS = N / RG;
+  __shared__ float lb[N], lc[N];
+  __shared__ __attribute__((aligned(16))) float py[RG][P + 4];
+  const int t = threadIdx.x, c = t % C4, rg = t / C4;
+  const int bh = blockIdx.x, b = bh / a.H, head = bh % a.H, grp = head / (a.H / a.G);
+  float* sp = a.state + ((size_t)bh * N + rg * ROWS) * P + 4 * c;
+  f32x4 s[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) s[i] = *reinterpret_cast<const f32x4*>(sp + (size_t)i * P);
+  if (t < N) {
+    lb[t] = io_to_float(static_cast<const S*>(a.Bt)[(size_t)b * a.bs + grp * N + t]);
+    lc[t] = io_to_float(static_cast<const S*>(a.Ct)[(size_t)b * a.cs + grp * N + t]);
+  }
+  const float dec = expf(a.g[bh]), dt = a.dt[bh], D = a.D ? a.D[head] : 0.f;
+  f32x4 x;
+  {
+    const S* xp = static_cast<const S*>(a.X) + (size_t)b * a.xs + (size_t)head * P + 4 * c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = io_to_float(xp[e]);
+  }
+  const f32x4 u = x * dt;
+  __syncthreads();
+  f32x4 y = zero4();
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    s[i] = s[i] * dec + u * lb[rg * ROWS + i];
+    y += s[i] * lc[rg * ROWS + i];
+    *reinterpret_cast<f32x4*>(sp + (size_t)i * P) = s[i];
+  }
+  *reinterpret_cast<f32x4*>(&py[rg][4 * c]) = y;
+  __syncthreads();
+  if (rg > 0) return;
+#pragma unroll
+  for (int i = 1; i < RG; ++i) y += *reinterpret_cast<const f32x4*>(&py[i][4 * c]);
+  store_io4(static_cast<S*>(a.Y) + (size_t)bh * P + 4 * c, y + x * D);
+}
+
+namespace {
+template <class T, int N, int MODE>
+void sweep(const ScanArgs& a, hipStream_t st) {
+  k_scan_sweep<T, N, MODE><<<seg_grid(a.T, a.B, a.seg, a.H / a.heads), a.heads * a.P * 2, 0, st>>>(a);
+}
+template <bool REV>
+void join(const ScanArgs& a, hipStream_t st) {
+  k_scan_join<REV><<<a.B * ((a.H * (a.N * a.P / 4) + 255) / 256), 256, 0, st>>>(a);
+}
+template <class T, int N>
+void run_fwd(const ScanArgs& a, hipStream_t st) {
+  if (a.carry) {
+    sweep<T, N, CARRY>(a, st);
+    join<false>(a, st);
+  }
+  if (a.st)
+    sweep<T, N, SWEEP_SAVE>(a, st);
+  else
+    sweep<T, N, SWEEP>(a, st);
+}
+template <class T, int N>
+void run_states(const ScanArgs& a, hipStream_t st) {
+  if (a.carry) {
+    sweep<T, N, REV_CARRY>(a, st);
+    join<true>(a, st);
+  }
+  sweep<T, N, REV_SAVE>(a, st);
+}
+template <class S>
+void run_step(const ScanArgs& a, hipStream_t st) {
+  const int n = a.B * a.H;
+  if (a.N == 64 && a.P == 64) k_scan_step<S, 64, 64><<<n, 256, 0, st>>>(a);
+  if (a.N == 64 && a.P == 128) k_scan_step<S, 64, 128><<<n, 256, 0, st>>>(a);
+  if (a.N == 128 && a.P == 64) k_scan_step<S, 128, 64><<<n, 256, 0, st>>>(a);
+  if (a.N == 128 && a.P == 128) k_scan_step<S, 128, 128><<<n, 256, 0, st>>>(a);
+}
+}  // namespace
+
+hipError_t launch_scan_fwd(const ScanArgs& a, bool bf16, hipStream_t st) {
+  timing_mark(FLEX_KERNEL_SCAN_FWD, st, true);
+  if (bf16)
+    a.N == 64 ? run_fwd<__bf16, 64>(a, st) : run_fwd<__bf16, 128>(a, st);
+  else
+    a.N == 64 ? run_fwd<float, 64>(a, st) : run_fwd<float, 128>(a, st);
+  timing_mark(FLEX_KERNEL_SCAN_FWD, st, false);
+  return hipGetLastError();
+}
+void launch_scan_states(const ScanArgs& a, bool bf16, hipStream_t st) {
+  if (bf16)
+    a.N == 64 ? run_states<__bf16, 64>(a, st) : run_states<__bf16, 128>(a, st);
+  else
+    a.N == 64 ? run_states<float, 64>(a, st) : run_states<float, 128>(a, st);
+}
+hipError_t launch_scan_step(const ScanArgs& a, bool bf16, hipStream_t st) {
+  timing_mark(FLEX_KERNEL_SCAN_STEP, st, true);
+  bf16 ? run_step<u16>(a, st) : run_step<float>(a, st);
+  timing_mark(FLEX_KERNEL_SCAN_STEP, st, false);
+  return hipGetLastError();
+}
+
+}  // namespace flex
