@@ -87,9 +87,11 @@ __device__ __forceinline__ double last_lane(double x) {
 }
 
 // A chunk's decays, lane = token.  Sums of g in 64 bits, in units of log2 as two floats, so that differences of
-// them are as exact as floats are; a decay of zero (g = -inf) is kept as a finite sum whose exponential is
-// zero, so that the differences are defined.
-constexpr float SCAN_MIN_G = -1e4f;
+// them are as exact as floats are.  Bf16 rows take the first float alone: a difference is then off by 2^-24 of the
+// larger sum, e^{L_i - L_j} by less than a rounding to bf16 up to sums of 2^16.  A decay of zero (g = -inf) is kept as a
+// finite sum whose exponential is zero and that no growth within a chunk makes up for, so that the differences are
+// defined.
+constexpr float SCAN_MIN_G = -1e3f;
 struct Decay {
   double L, end;    // the token's, and the chunk's, in units of log2
   float hi, lo;     // the token's
@@ -104,8 +106,9 @@ struct Decay {
   __device__ __forceinline__ float to_end() const { return __builtin_amdgcn_exp2f((float)(end - L)); }
 };
 // e^{L_i - L_j}
+template <bool ONE>
 __device__ __forceinline__ float decay(float hi_i, float lo_i, float hi_j, float lo_j) {
-  return __builtin_amdgcn_exp2f((hi_i - hi_j) + (lo_i - lo_j));
+  return __builtin_amdgcn_exp2f(ONE ? hi_i - hi_j : (hi_i - hi_j) + (lo_i - lo_j));
 }
 
 // The work of a workgroup of a sweep: a segment of a sequence (tokens t0 .. of it) and a set of heads of one group.

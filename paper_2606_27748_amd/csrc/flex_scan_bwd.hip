@@ -27,6 +27,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   using S = typename Io<T>::type;
   using RT = ScanTile<T, N>;
   using XT = ScanTile<T, 64>;
+  constexpr bool BF = IsBf16<T>::value;
   constexpr int NT = N / 64, ROWS = SC * N * (int)sizeof(T), XROWS = SC * 64 * (int)sizeof(T);
   // fp32 states of 128 rows leave room for one of S and dS at a time
   constexpr bool ONE = 4 * ROWS + 2 * XROWS > 144 * 1024;
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
             const f32x4 hi = *reinterpret_cast<const f32x4*>(&sc[0][ti]), lo = *reinterpret_cast<const f32x4*>(&sc[1][ti]);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              q[4 * b + e] = ti + e >= tok ? cb[i][4 * b + e] * decay(hi[e], lo[e], hj, lj) : 0.f;
+              q[4 * b + e] = ti + e >= tok ? cb[i][4 * b + e] * decay<BF>(hi[e], lo[e], hj, lj) : 0.f;
           }
 #pragma unroll
           for (int s = 0; s < 2; ++s)
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         for (int e = 0; e < 4; ++e) {
           const int x = 4 * b + e, i = ti + e;
           if (i == tok) dd = m0[x];
-          const float m = i >= tok ? m0[x] * decay(hi[e], lo[e], hj, lj) * dt : 0.f;
+          const float m = i >= tok ? m0[x] * decay<BF>(hi[e], lo[e], hj, lj) * dt : 0.f;
           W[x] += m;
           z[x] = i > tok ? m * (hf == 0 ? cb[0][x] : cb[1][x]) : 0.f;
           cz += z[x];

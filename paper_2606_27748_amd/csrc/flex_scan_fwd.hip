@@ -9,15 +9,10 @@ namespace flex {
 
 namespace {
 enum {
-  CARRY,       // what a segment leaves, forwards: no rows out
   SWEEP,       // y
   SWEEP_SAVE,  // y, and the state at each chunk's start
-  REV_CARRY,   // what a segment leaves of the state's gradient, in reverse
-  REV_SAVE     // the gradient of the state at each chunk's end
+  REV_SAVE     // in reverse, the gradient of the state at each chunk's end
 };
-constexpr bool is_rev(int mode) { return mode >= REV_CARRY; }
-constexpr bool is_carry(int mode) { return mode == CARRY || mode == REV_CARRY; }
-constexpr bool has_y(int mode) { return mode == SWEEP || mode == SWEEP_SAVE; }
 
 // c += a x for operands a that are exact and fp32 values x, as three bf16 terms (24 bits) or as they are.
 // Two terms leave 2^-18 of each product: 1.5e-6 of a state, where fp32 sums leave 1e-7.
@@ -37,39 +32,169 @@ __device__ __forceinline__ void split3(Frag<float> (&t)[1], const float (&x)[8])
 #pragma unroll
   for (int j = 0; j < 8; ++j) t[0].v[j] = x[j];
 }
+
+// u += rows^T (w x) over a chunk: x as its columns' operands, w of the tokens in LDS
+template <class T, int N>
+__device__ __forceinline__ void add_rows(f32x16 (&u)[N / 32], const char* rows, const Frag<T> (&xf)[4], const float* w, int h) {
+  constexpr int TERMS = IsBf16<T>::value ? 3 : 1;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float* ws = w + 16 * q + 4 * h;
+    const f32x4 w0 = *reinterpret_cast<const f32x4*>(ws), w1 = *reinterpret_cast<const f32x4*>(ws + 8);
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = xf[q].get(j) * (j < 4 ? w0[j % 4] : w1[j % 4]);
+    Frag<T> wx[TERMS], bf[N / 32];
+    split3(wx, v);
+#pragma unroll
+    for (int i = 0; i < N / 32; ++i) bf[i] = ScanTile<T, N>::colp(rows, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 32 * i);
+#pragma unroll
+    for (int t = TERMS - 1; t >= 0; --t)
+#pragma unroll
+      for (int i = 0; i < N / 32; ++i) mma32(u[i], bf[i], wx[t]);
+  }
+}
+
+__device__ __forceinline__ bool not_finite(const Frag<__bf16> (&x)[4]) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  u16x2 top = {0, 0};
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const u32x4 v = __builtin_bit_cast(u32x4, x[q].v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[j] & 0x7fff7fffu));
+  }
+  return top[0] >= 0x7f80 || top[1] >= 0x7f80;
+}
+__device__ __forceinline__ bool not_finite(const Frag<float> (&x)[4]) {
+  float s = 0.f;   // NaN from the first NaN or infinity on
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = __builtin_fmaf(x[q].get(j), 0.f, s);
+  return s != 0.f;
+}
 }  // namespace
 
-// Workgroups: a segment and a set of heads of one group; a wave has 32 columns of one head's state.  The rows of B
-// (and C) pass through LDS for all of them, its own columns of x for each wave, the next chunk on its way while one is
-// worked on where two fit.  In reverse the state is its gradient dS, the rows C, x is dy and the weights are e^L:
+// What a segment of a sequence leaves on its own, S = sum_j e^{L_end - L_j} dt_j B_j x_j^T with L from the segment's
+// start (REV: dS = sum_i e^{L_i} C_i dy_i^T), and its decay.  A workgroup has a segment and a set of heads of one group,
+// a wave 32 columns of one head's state; the rows of B pass through LDS for all of them.  Forwards the chunks are
+// taken from the last one, so that their weights are known and the sum has no decay in it.
+// The segment that nothing starts from is left out, and of the first one state0 is a part.
+template <class T, int N, bool REV>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_carry(ScanArgs a) {
+  using S = typename Io<T>::type;
+  using RT = ScanTile<T, N>;
+  using XT = ScanTile<T, 32>;
+  constexpr int NT = N / 32, TERMS = IsBf16<T>::value ? 3 : 1;
+  constexpr int ROWS = SC * N * (int)sizeof(T), XROWS = SC * 32 * (int)sizeof(T), BUF = ROWS + 8 * XROWS;
+  constexpr int BUFS = 2 * BUF <= 156 * 1024 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) char lds[BUFS * BUF];
+  __shared__ __attribute__((aligned(16))) float scal[8][SC];
+  const int l = threadIdx.x % WAVE, c = l % 32, h = l / 32;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
+  const SegTile sg = find_segment(a.off, a.B, a.T, a.seg, a.H / a.heads);
+  if (sg.b < 0 || (REV ? sg.index == 0 : sg.index == sg.count - 1)) return;
+  const int per = a.P / 32, head = sg.set * a.heads + w / per, p0 = w % per * 32, grp = head / (a.H / a.G);
+  const int t0 = sg.index * a.seg, n = min(sg.n - t0, a.seg), row0 = sg.row0 + t0, nchunks = (n + SC - 1) / SC;
+  const S* rb = static_cast<const S*>(REV ? a.Ct : a.Bt) + (size_t)grp * N;
+  const S* rx = static_cast<const S*>(REV ? a.dY : a.X) + (size_t)head * a.P + p0;
+  const int bs = REV ? a.cs : a.bs, xs = REV ? a.H * a.P : a.xs;
+  auto buf = [&](int k) { return lds + (BUFS == 2 ? (k & 1) * BUF : 0); };
+  auto stage = [&](int k, int chunk) {
+    const int r = row0 + chunk * SC, m = min(SC, n - chunk * SC);
+    stage_rows<T, N>(buf(k), rb, r, bs, m, w, nw);
+    stage_tile<T, 32, SC, 1>(buf(k) + ROWS + w * XROWS, row_words(rx, r, xs, m, 32), xs * (int)sizeof(S), 0);
+  };
+  float gn = 0.f, dn = 0.f;   // of the next chunk, lane = token
+  auto fetch = [&](int chunk) {
+    const int t = chunk * SC + l;
+    gn = dn = 0.f;
+    if (t < n) {
+      const size_t at = (size_t)(row0 + t) * a.H + head;
+      gn = a.g[at];
+      if (!REV) dn = a.dt[at];
+    }
+  };
+  f32x16 st[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) st[i] = zero16();
+  float* sc = scal[w];
+  double total = 0.0;
+  stage(0, REV ? 0 : nchunks - 1);   // a segment that another follows has chunks, and so has one behind another
+  fetch(REV ? 0 : nchunks - 1);
+  for (int k = 0; k < nchunks; ++k) {
+    const int next = REV ? k + 1 : nchunks - 2 - k;
+    const char* L = buf(k);
+    sync_tiles();   // the chunk is in LDS, and the buffer of the one before is free
+    if (BUFS == 2 && k + 1 < nchunks) stage(k + 1, next);
+    const Decay d(gn);
+    sc[l] = REV ? __builtin_amdgcn_exp2f((float)(d.L + total)) : __builtin_amdgcn_exp2f((float)(d.end - d.L + total)) * dn;
+    total += d.end;
+    if (k + 1 < nchunks) fetch(next);
+    const char* LX = L + ROWS + w * XROWS;
+    Frag<T> xf[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) xf[q] = XT::colp(LX, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 0);
+    f32x16 u[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) u[i] = zero16();
+    add_rows<T, N>(u, L, xf, sc, h);
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) st[i][e] += u[i][e];
+    if (BUFS == 1) {
+      sync_lds();
+      if (k + 1 < nchunks) stage(k + 1, next);
+    }
+  }
+  const float whole = __builtin_amdgcn_exp2f((float)total);
+  if (!REV && a.state0 && sg.index == 0) {
+    const float* s0 = a.state0 + ((size_t)sg.b * a.H + head) * N * a.P + p0 + perm32(c);
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) st[i][e] = __builtin_fmaf(whole, s0[(size_t)(32 * i + perm_row(e, h)) * a.P], st[i][e]);
+  }
+  float* carry = a.carry + ((size_t)sg.slot * a.H + head) * N * a.P + (size_t)p0 * N + l * 4;
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<f32x4*>(carry + (i * 4 + q) * WAVE * 4) =
+          f32x4{st[i][4 * q], st[i][4 * q + 1], st[i][4 * q + 2], st[i][4 * q + 3]};
+  if (l == 0 && p0 == 0) a.tot[(size_t)sg.slot * a.H + head] = whole;
+}
+
+// The sweep over a segment's chunks: workgroups, waves and LDS as above, with the rows of C too.  In reverse the
+// state is its gradient dS, the rows are C's, x is dy and the weights are e^L:
 //   dS <- e^{L_63} dS + C^T (e^L dy)
 template <class T, int N, int MODE>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_sweep(ScanArgs a) {
   using S = typename Io<T>::type;
   using RT = ScanTile<T, N>;
   using XT = ScanTile<T, 32>;
-  constexpr bool REV = is_rev(MODE), Y = has_y(MODE);
-  constexpr int NS = N / 16, NT = N / 32, TERMS = IsBf16<T>::value ? 3 : 1;
+  constexpr bool REV = MODE == REV_SAVE, Y = !REV, BF = IsBf16<T>::value;
+  constexpr int NS = N / 16, NT = N / 32;
   constexpr int ROWS = SC * N * (int)sizeof(T), XROWS = SC * 32 * (int)sizeof(T);
   constexpr int BUF = (Y ? 2 : 1) * ROWS + 8 * XROWS, SCAL = Y ? 5 * SC : SC;
   constexpr int BUFS = 2 * BUF + 8 * SCAL * 4 <= 160 * 1024 ? 2 : 1;
   __shared__ __attribute__((aligned(16))) char lds[BUFS * BUF];
   __shared__ __attribute__((aligned(16))) float scal[8][SCAL];
-  const int l = threadIdx.x % WAVE, c = l % 32, h = l / 32;
+  const int l = threadIdx.x % WAVE;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
   const SegTile sg = find_segment(a.off, a.B, a.T, a.seg, a.H / a.heads);
   if (sg.b < 0) return;
   const bool last_seg = sg.index == sg.count - 1;
-  if (MODE == CARRY && last_seg) return;
-  if (MODE == REV_CARRY && sg.index == 0) return;
   const int per = a.P / 32, head = sg.set * a.heads + w / per, p0 = w % per * 32, grp = head / (a.H / a.G);
   const int t0 = sg.index * a.seg, n = min(sg.n - t0, a.seg), row0 = sg.row0 + t0;
   const int nchunks = (n + SC - 1) / SC, slot0 = sg.row0 / SC + sg.b + t0 / SC;
-  const int pc = p0 + perm32(c);   // this lane's column of the state
+  const int pc = p0 + perm32(l % 32);   // this lane's column of the state
 
   const S* rb = static_cast<const S*>(REV ? a.Ct : a.Bt) + (size_t)grp * N;
   const S* rc = static_cast<const S*>(a.Ct) + (size_t)grp * N;
-  const S* rx = REV ? static_cast<const S*>(a.dY) + (size_t)head * a.P + p0 : static_cast<const S*>(a.X) + (size_t)head * a.P + p0;
+  const S* rx = static_cast<const S*>(REV ? a.dY : a.X) + (size_t)head * a.P + p0;
   const int bs = REV ? a.cs : a.bs, xs = REV ? a.H * a.P : a.xs;
   auto buf = [&](int k) { return lds + (BUFS == 2 ? (k & 1) * BUF : 0); };
   auto stage = [&](int k, int chunk) {
@@ -94,15 +219,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 #pragma unroll
   for (int i = 0; i < NT; ++i) st[i] = zero16();
   // tile i's elements 4 q .. + 3 of every lane, in a row
-  float* carry = a.carry ? a.carry + ((size_t)sg.slot * a.H + head) * N * a.P + (size_t)p0 * N + l * 4 : nullptr;
-  const bool from_state0 = !REV && a.state0 && sg.index == 0 && (MODE == CARRY || sg.count == 1);
-  if (from_state0) {
+  const float* carry = a.carry ? a.carry + ((size_t)sg.slot * a.H + head) * N * a.P + (size_t)p0 * N + l * 4 : nullptr;
+  if (!REV && a.state0 && sg.count == 1) {
     const float* s0 = a.state0 + ((size_t)sg.b * a.H + head) * N * a.P + pc;
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) st[i][e] = s0[(size_t)(32 * i + perm_row(e, h)) * a.P];
-  } else if (!is_carry(MODE) && carry && (REV ? !last_seg : sg.index > 0 || (a.state0 && sg.count > 1))) {
+      for (int e = 0; e < 16; ++e) st[i][e] = s0[(size_t)(32 * i + perm_row(e, l / 32)) * a.P];
+  } else if (carry && (REV ? !last_seg : sg.index > 0 || (a.state0 && sg.count > 1))) {
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -113,10 +237,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
       }
   }
   auto keep = [&](void* base, int chunk, const Frag<T> (&f)[NS]) {   // as [P][N]
-    S* p = static_cast<S*>(base) + (((size_t)(slot0 + chunk) * a.H + head) * a.P + pc) * N + 8 * h;
+    S* p = static_cast<S*>(base) + (((size_t)(slot0 + chunk) * a.H + head) * a.P + pc) * N + 8 * (l / 32);
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      if constexpr (IsBf16<T>::value) {
+      if constexpr (BF) {
         *reinterpret_cast<bf16x8*>(p + 16 * s) = f[s].v;
       } else {
         *reinterpret_cast<f32x4*>(p + 16 * s) = f32x4{f[s].v[0], f[s].v[1], f[s].v[2], f[s].v[3]};
@@ -128,34 +252,37 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 #pragma unroll
     for (int s = 0; s < NS; ++s) f[s] = frag_of<T>(st[s / 2], s % 2);
   };
+  // stores of a step, behind its loads
+  constexpr int LATER = BUFS == 1 ? 0 : Y ? (BF ? 4 : 8) : (BF ? NS : 2 * NS);
 
   float* sc = scal[w];
-  double total = 0.0;
   const float Dh = Y && a.D ? a.D[head] : 0.f;
   if (nchunks > 0) {
     const int first = REV ? nchunks - 1 : 0;
     stage(0, first);
     fetch(first);
+    wait_lds_loads();
   }
   for (int k = 0; k < nchunks; ++k) {
     const int chunk = REV ? nchunks - 1 - k : k, next = REV ? chunk - 1 : chunk + 1;
     const char* L = buf(k);
-    sync_tiles();   // the chunk is in LDS, and the buffer of the one before is free
+    int x = l;   // places in LDS are formed anew: kept over the loop they would take the registers that it is short of
+    asm volatile("" : "+v"(x));
+    const int c = x % 32, h = x / 32;
+    sync_tiles_but<LATER>();   // the chunk is in LDS, and the buffer of the one before is free
+    if (BUFS == 2 && k + 1 < nchunks) stage(k + 1, next);
     const Decay d(gn);
     if (Y) {
       sc[l] = d.hi;
-      sc[SC + l] = d.lo;
+      if (!BF) sc[SC + l] = d.lo;
       sc[2 * SC + l] = dn;
       sc[3 * SC + l] = d.from_start();
       sc[4 * SC + l] = d.to_end() * dn;
     } else {
-      sc[l] = REV ? d.from_start() : d.to_end() * dn;
+      sc[l] = d.from_start();
     }
     const float last = __builtin_amdgcn_exp2f((float)d.end);
-    if (is_carry(MODE)) total += d.end;
-    if (BUFS == 2 && k + 1 < nchunks) stage(k + 1, next);
     if (k + 1 < nchunks) fetch(next);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the wave's own writes above
 
     const char* LX = L + (Y ? 2 : 1) * ROWS + w * XROWS;
     Frag<T> xf[4];   // columns of x, slots the tokens 16 q + 4 h + i and 8 further
@@ -169,88 +296,71 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     }
     if constexpr (Y) {
       const char* LC = L + ROWS;
-      f32x16 y[2] = {zero16(), zero16()}, cb[3] = {zero16(), zero16(), zero16()};
-      {
-        Frag<T> sb[NS];
-        state_frags(sb);
-        if constexpr (MODE == SWEEP_SAVE) keep(a.st, chunk, sb);
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          const Frag<T> c0 = RT::row(LC, c, s, h), c1 = RT::row(LC, 32 + c, s, h);
-          const Frag<T> b0 = RT::row(L, c, s, h), b1 = RT::row(L, 32 + c, s, h);
-          mma32(y[0], sb[s], c0);
-          mma32(cb[0], b0, c0);
-          mma32(y[1], sb[s], c1);
-          mma32(cb[1], b0, c1);
-          mma32(cb[2], b1, c1);
-        }
-      }
-      // x with a value that is not finite: its column's products go over the rows before it only, and the rows from it on are NaN
-      float bad = 0.f;
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) bad = __builtin_fmaf(xf[q].get(j), 0.f, bad);
-      const bool any_bad = __any(bad != 0.f);
+      Frag<T> sb[NS];
+      state_frags(sb);
+      if constexpr (MODE == SWEEP_SAVE) keep(a.st, chunk, sb);
+      // x with a value that is not finite: its column's products go over the rows before it only, and the rows from it
+      // on are NaN
       int fb = SC;
-      Frag<T> xc[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) xc[q] = xf[q];
+      const bool any_bad = __any(not_finite(xf));
       if (any_bad) {
+        auto token = [&](int q, int j) { return 16 * q + 4 * h + 8 * (j / 4) + j % 4; };
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (!(fabsf(xf[q].get(j)) < INFINITY)) fb = min(fb, 16 * q + 4 * h + 8 * (j / 4) + j % 4);
+            if (!(fabsf(xf[q].get(j)) < INFINITY)) fb = min(fb, token(q, j));
         fb = min(fb, __shfl_xor(fb, 32));
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (16 * q + 4 * h + 8 * (j / 4) + j % 4 >= fb) xc[q].set(j, 0.f);
+            if (token(q, j) >= fb) xf[q].set(j, 0.f);
       }
+      const int m = min(SC, n - chunk * SC), ys = a.H * a.P;
+      const auto ry = row_window(static_cast<S*>(a.Y) + (size_t)head * a.P + p0, row0 + chunk * SC, ys, m, 32);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float hi = sc[32 * i + c], lo = sc[SC + 32 * i + c], eg = sc[3 * SC + 32 * i + c];
+        f32x16 y = zero16(), cb[2] = {zero16(), zero16()};
 #pragma unroll
-        for (int e = 0; e < 16; ++e) y[i][e] *= eg;
+        for (int s = 0; s < NS; ++s) {
+          const Frag<T> cr = RT::row(LC, 32 * i + c, s, h);
+          mma32(y, sb[s], cr);
+#pragma unroll
+          for (int j = 0; j <= i; ++j) mma32(cb[j], RT::row(L, 32 * j + c, s, h), cr);
+        }
+        const float hi = sc[32 * i + c], lo = BF ? 0.f : sc[SC + 32 * i + c], eg = sc[3 * SC + 32 * i + c];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) y[e] *= eg;
 #pragma unroll
         for (int j = 0; j <= i; ++j) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const int t = 32 * j + 8 * q + 4 * h;
-            const f32x4 hj = *reinterpret_cast<const f32x4*>(sc + t), lj = *reinterpret_cast<const f32x4*>(sc + SC + t);
-            const f32x4 dj = *reinterpret_cast<const f32x4*>(sc + 2 * SC + t);
+            const f32x4 hj = *reinterpret_cast<const f32x4*>(sc + t), dj = *reinterpret_cast<const f32x4*>(sc + 2 * SC + t);
+            const f32x4 lj = BF ? zero4() : *reinterpret_cast<const f32x4*>(sc + SC + t);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float v = cb[i + j][4 * q + e];
-              cb[i + j][4 * q + e] = j < i || t + e <= 32 * i + c ? v * (decay(hi, lo, hj[e], lj[e]) * dj[e]) : 0.f;
+              const float v = cb[j][4 * q + e] * (decay<BF>(hi, lo, hj[e], lj[e]) * dj[e]);
+              cb[j][4 * q + e] = j < i || t + e <= 32 * i + c ? v : 0.f;
             }
           }
 #pragma unroll
-          for (int s = 0; s < 2; ++s) mma32(y[i], xc[2 * j + s], frag_of<T>(cb[i + j], s));
+          for (int s = 0; s < 2; ++s) mma32(y, xf[2 * j + s], frag_of<T>(cb[j], s));
         }
-      }
-      if (any_bad) {
+        if (any_bad) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int f = __shfl(fb, 8 * (e / 4) + 4 * h + e % 4);
-          if (c >= f) y[0][e] = NAN;
-          if (32 + c >= f) y[1][e] = NAN;
+          for (int e = 0; e < 16; ++e)
+            if (32 * i + c >= __shfl(fb, 8 * (e / 4) + 4 * h + e % 4)) y[e] = NAN;
         }
-      }
-      const int m = min(SC, n - chunk * SC), ys = a.H * a.P;
-      const auto ry = row_window(static_cast<S*>(a.Y) + (size_t)head * a.P + p0, row0 + chunk * SC, ys, m, 32);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           const Frag<T> xr = XT::row(LX, 32 * i + c, s, h);
           const int at = ((32 * i + c) * ys + 16 * s + 8 * h) * (int)sizeof(S);
           float v[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf(Dh, xr.get(j), y[i][8 * s + j]);
-          if constexpr (IsBf16<T>::value) {
+          for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf(Dh, xr.get(j), y[8 * s + j]);
+          if constexpr (BF) {
             Frag<T> o;
 #pragma unroll
             for (int j = 0; j < 8; ++j) o.set(j, v[j]);
@@ -260,50 +370,31 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]}), ry, at + 16, 0, 0);
           }
         }
-    }
-    // S <- e^{L_63} S + B^T (w x)
-    Frag<T> wx[4][TERMS];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float* ws = sc + (Y ? 4 * SC : 0) + 16 * q + 4 * h;
-      const f32x4 w0 = *reinterpret_cast<const f32x4*>(ws), w1 = *reinterpret_cast<const f32x4*>(ws + 8);
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = xf[q].get(j) * (j < 4 ? w0[j % 4] : w1[j % 4]);
-      split3(wx[q], v);
-    }
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      f32x16 u = zero16();
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const Frag<T> bf = RT::colp(L, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 32 * i);
-#pragma unroll
-        for (int t = TERMS - 1; t >= 0; --t) mma32(u, bf, wx[q][t]);
+        asm volatile("" ::: "memory");   // the second half's operands are not read before the first half is done
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) st[i][e] = __builtin_fmaf(st[i][e], last, u[e]);
+      for (int q = 0; q < 4; ++q) xf[q] = XT::colp(LX, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 0);
     }
+    // S <- e^{L_63} S + B^T (w x)
+    f32x16 u[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) u[i] = zero16();
+    add_rows<T, N>(u, L, xf, sc + (Y ? 4 * SC : 0), h);
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) st[i][e] = __builtin_fmaf(st[i][e], last, u[i][e]);
     if (BUFS == 1) {
       sync_lds();
       if (k + 1 < nchunks) stage(k + 1, next);
     }
-  }
-  if (is_carry(MODE)) {
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4*>(carry + (i * 4 + q) * WAVE * 4) =
-            f32x4{st[i][4 * q], st[i][4 * q + 1], st[i][4 * q + 2], st[i][4 * q + 3]};
-    if (l == 0 && p0 == 0) a.tot[(size_t)sg.slot * a.H + head] = __builtin_amdgcn_exp2f((float)total);
   }
   if (Y && a.state && last_seg) {
     float* so = a.state + ((size_t)sg.b * a.H + head) * N * a.P + pc;
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) so[(size_t)(32 * i + perm_row(e, h)) * a.P] = st[i][e];
+      for (int e = 0; e < 16; ++e) so[(size_t)(32 * i + perm_row(e, l / 32)) * a.P] = st[i][e];
   }
 }
 
@@ -414,6 +505,10 @@ template <class T, int N, int MODE>
 void sweep(const ScanArgs& a, hipStream_t st) {
   k_scan_sweep<T, N, MODE><<<seg_grid(a.T, a.B, a.seg, a.H / a.heads), a.heads * a.P * 2, 0, st>>>(a);
 }
+template <class T, int N, bool REV>
+void carry(const ScanArgs& a, hipStream_t st) {
+  k_scan_carry<T, N, REV><<<seg_grid(a.T, a.B, a.seg, a.H / a.heads), a.heads * a.P * 2, 0, st>>>(a);
+}
 template <bool REV>
 void join(const ScanArgs& a, hipStream_t st) {
   k_scan_join<REV><<<a.B * ((a.H * (a.N * a.P / 4) + 255) / 256), 256, 0, st>>>(a);
@@ -421,7 +516,7 @@ void join(const ScanArgs& a, hipStream_t st) {
 template <class T, int N>
 void run_fwd(const ScanArgs& a, hipStream_t st) {
   if (a.carry) {
-    sweep<T, N, CARRY>(a, st);
+    carry<T, N, false>(a, st);
     join<false>(a, st);
   }
   if (a.st)
@@ -432,7 +527,7 @@ void run_fwd(const ScanArgs& a, hipStream_t st) {
 template <class T, int N>
 void run_states(const ScanArgs& a, hipStream_t st) {
   if (a.carry) {
-    sweep<T, N, REV_CARRY>(a, st);
+    carry<T, N, true>(a, st);
     join<true>(a, st);
   }
   sweep<T, N, REV_SAVE>(a, st);
