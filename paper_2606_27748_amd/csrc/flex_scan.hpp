@@ -31,9 +31,8 @@ __device__ __forceinline__ constexpr int perm_row(int e, int h) { return 16 * (e
 template <class T, int D>
 struct ScanTile : RowTile<T, D> {
   using R = RowTile<T, D>;
-  // Columns m0 + perm32(l % 32), slots 0..3 the rows r0 .. r0+3, slots 4..7 r1 .. r1+3
-  static __device__ __forceinline__ Frag<T> colp(const char* L, int r0, int r1, int m0) {
-    const int l = threadIdx.x % WAVE;
+  // Columns m0 + perm32(l % 32) for lane l, slots 0..3 the rows r0 .. r0+3, slots 4..7 r1 .. r1+3
+  static __device__ __forceinline__ Frag<T> colp(const char* L, int r0, int r1, int m0, int l = threadIdx.x % WAVE) {
     Frag<T> f;
     if constexpr (IsBf16<T>::value) {
       // the lane's part of the read: row i / 4, of the 16 columns the quarter that place i % 4 takes
@@ -49,6 +48,62 @@ struct ScanTile : RowTile<T, D> {
         f.v[j] = *reinterpret_cast<const float*>(L + R::at(r0 + j, c) + o);
         f.v[4 + j] = *reinterpret_cast<const float*>(L + R::at(r1 + j, c) + o);
       }
+    }
+    return f;
+  }
+};
+
+// States [32 columns p][N] as the sweeps' lanes hold them: of step s the 64 lanes' eight elements, 16 bytes a lane in a
+// row (fp32: twice), so that a store of them is 1 KB in a row.  Lanes of the upper half lie four places
+// off, for the banks of a transposed read.
+template <class T, int N>
+struct StateRows {
+  using S = typename Io<T>::type;
+  static constexpr int E = 16 / sizeof(T), FRAG = WAVE * 8 * (int)sizeof(T), BLOCK = N / 16 * FRAG;   // bytes of 32 columns
+  static __device__ __forceinline__ int place(int r, int h) { return h * 32 + (r ^ (4 * h)); }
+  static __device__ __forceinline__ void store(S* base, int s, const Frag<T>& f) {
+    const int l = threadIdx.x % WAVE;
+    S* p = base + s * (FRAG / (int)sizeof(S)) + place(l % 32, l / 32) * E;
+    if constexpr (IsBf16<T>::value) {
+      *reinterpret_cast<bf16x8*>(p) = f.v;
+    } else {
+      *reinterpret_cast<f32x4*>(p) = f32x4{f.v[0], f.v[1], f.v[2], f.v[3]};
+      *reinterpret_cast<f32x4*>(p + WAVE * E) = f32x4{f.v[4], f.v[5], f.v[6], f.v[7]};
+    }
+  }
+  // bytes to column p of (several blocks of) 32, elements n .. of 16 bytes
+  static __device__ __forceinline__ int at(int p, int n) {
+    return p / 32 * BLOCK + n / 16 * FRAG + n % 8 / E * (WAVE * 16) + place(perm32(p % 32), n / 8 % 2) * 16 + n % E * (int)sizeof(T);
+  }
+  // the operand with lane l % 32 column p0 + perm32(l % 32) and the slots 16 s + 8 h ..
+  static __device__ __forceinline__ Frag<T> row(const char* L, int p0, int s) {
+    const int l = threadIdx.x % WAVE;
+    const char* q = L + p0 / 32 * BLOCK + s * FRAG + place(l % 32, l / 32) * 16;
+    Frag<T> f;
+    if constexpr (IsBf16<T>::value) {
+      f.v = *reinterpret_cast<const bf16x8*>(q);
+    } else {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(q), b = *reinterpret_cast<const f32x4*>(q + WAVE * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        f.v[j] = a[j];
+        f.v[4 + j] = b[j];
+      }
+    }
+    return f;
+  }
+  // the operand with lane l % 32 element n0 + perm32(l % 32) and the slots columns p .. p + 7
+  static __device__ __forceinline__ Frag<T> colp(const char* L, int p, int n0) {
+    const int l = threadIdx.x % WAVE;
+    Frag<T> f;
+    if constexpr (IsBf16<T>::value) {
+      const int i = l % 16, q = (i & 1) << 1 | (i >> 1 & 1), n = n0 + 16 * ((l / 16) & 1) + 4 * q;
+      const tr_v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(L + at(p + i / 4, n)));
+      const tr_v4i16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(L + at(p + 4 + i / 4, n)));
+      f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f.v[j] = *reinterpret_cast<const float*>(L + at(p + j, n0 + perm32(l % 32)));
     }
     return f;
   }
@@ -80,9 +135,9 @@ __device__ __forceinline__ double wave_scan(double x) {
   step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});   // lane 31
   return x;
 }
-__device__ __forceinline__ double last_lane(double x) {
+__device__ __forceinline__ double lane_of(double x, int lane) {
   const uint64_t v = __builtin_bit_cast(uint64_t, x);
-  const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)v, WAVE - 1), hi = __builtin_amdgcn_readlane((int)(unsigned)(v >> 32), WAVE - 1);
+  const unsigned lo = __builtin_amdgcn_readlane((int)(unsigned)v, lane), hi = __builtin_amdgcn_readlane((int)(unsigned)(v >> 32), lane);
   return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
@@ -98,7 +153,7 @@ struct Decay {
   __device__ __forceinline__ explicit Decay(float g) {
     if (g < SCAN_MIN_G) g = SCAN_MIN_G;
     L = wave_scan((double)g * 1.4426950408889634);
-    end = last_lane(L);
+    end = lane_of(L, WAVE - 1);
     hi = (float)L;
     lo = (float)(L - (double)hi);
   }
@@ -112,21 +167,20 @@ __device__ __forceinline__ float decay(float hi_i, float lo_i, float hi_j, float
 }
 
 // The work of a workgroup of a sweep: a segment of a sequence (tokens t0 .. of it) and a set of heads of one group.
-// Consecutive workgroups go round-robin to the XCDs: an XCD gets all sets of a segment, which read the same
-// rows of B and C.
+// Consecutive workgroups go round-robin to the XCDs, and so do the sets of a segment: each XCD has a share of
+// every segment.  (An XCD with all sets of its segments reads the rows of B and C once, but the last round of
+// segments leaves some XCDs without work.)
 struct SegTile {
   int b, row0, n;     // sequence (-1: none), first row and length of it
   int index, count;   // which of how many segments
   int slot, set;
 };
 __device__ __forceinline__ SegTile find_segment(const int32_t* __restrict__ off, int B, int T, int seg, int sets) {
-  const int id = blockIdx.x, k = id / NUM_XCD;
   SegTile t;
-  t.slot = k / sets * NUM_XCD + id % NUM_XCD;
-  t.set = k % sets;
+  t.slot = blockIdx.x / sets;
+  t.set = blockIdx.x % sets;
   t.b = -1;
   t.row0 = t.n = t.index = t.count = 0;
-  if (t.slot >= seq_slots(T, B, seg)) return t;
   const int slot = t.slot;
   const int cnt = leading(B, [=](int b) { return clamp_off(off[b], T) / seg + b <= slot; });
   if (cnt == 0) return t;
@@ -140,6 +194,4 @@ __device__ __forceinline__ SegTile find_segment(const int32_t* __restrict__ off,
   t.count = __builtin_amdgcn_readfirstlane(t.count);
   return t;
 }
-inline int seg_grid(int T, int B, int seg, int sets) { return (seq_slots(T, B, seg) + NUM_XCD - 1) / NUM_XCD * NUM_XCD * sets; }
-
 }  // namespace flex

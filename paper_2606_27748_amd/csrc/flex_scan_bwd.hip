@@ -27,6 +27,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   using S = typename Io<T>::type;
   using RT = ScanTile<T, N>;
   using XT = ScanTile<T, 64>;
+  using ST = StateRows<T, N>;
   constexpr bool BF = IsBf16<T>::value;
   constexpr int NT = N / 64, ROWS = SC * N * (int)sizeof(T), XROWS = SC * 64 * (int)sizeof(T);
   // fp32 states of 128 rows leave room for one of S and dS at a time
@@ -82,8 +83,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
       sync_lds();   // what was staged before is no longer read
       stage_rows<T, 64>(LX, static_cast<const S*>(a.X) + xcol, row0, a.xs, n, w, 4);
       stage_rows<T, 64>(LY, static_cast<const S*>(a.dY) + xcol, row0, a.H * a.P, n, w, 4);
-      stage_tile<T, N, 64, 4>(LS, row_words(static_cast<const S*>(a.st) + sat, 0, N, 64, N), N * (int)sizeof(S), w);
-      if (!ONE) stage_tile<T, N, 64, 4>(LD, row_words(static_cast<const S*>(a.dst) + sat, 0, N, 64, N), N * (int)sizeof(S), w);
+      stage_linear<ROWS / 1024, 4>(LS, static_cast<const S*>(a.st) + sat, w);
+      if (!ONE) stage_linear<ROWS / 1024, 4>(LD, static_cast<const S*>(a.dst) + sat, w);
       if (pb == 0) {   // every wave forms the decays, the first one writes them
         float g = 0.f, dt = 0.f;
         if (l < n) {
@@ -115,7 +116,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         const int n0 = hf * (N / 2) + 32 * i;
 #pragma unroll
         for (int s = 0; s < 4; ++s)
-          mma32(u, RT::colp(LS, 16 * s + 8 * h, 16 * s + 8 * h + 4, n0), XT::row(LY, tok, s, h));
+          mma32(u, ST::colp(LS, 16 * s + 8 * h, n0), XT::row(LY, tok, s, h));
         float r = 0.f;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
       }
       if (ONE) {
         sync_lds();
-        stage_tile<T, N, 64, 4>(LD, row_words(static_cast<const S*>(a.dst) + sat, 0, N, 64, N), N * (int)sizeof(S), w);
+        stage_linear<ROWS / 1024, 4>(LD, static_cast<const S*>(a.dst) + sat, w);
         const float* s0 = reinterpret_cast<const float*>(static_cast<const S*>(a.st) + sat);
         const float* d0 = reinterpret_cast<const float*>(static_cast<const S*>(a.dst) + sat);
         for (int i = threadIdx.x; i < 64 * N; i += 256) ss = __builtin_fmaf(s0[i], d0[i], ss);
@@ -155,14 +156,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         const int n0 = hf * (N / 2) + 32 * i;
 #pragma unroll
         for (int s = 0; s < 4; ++s)
-          mma32(u, RT::colp(LD, 16 * s + 8 * h, 16 * s + 8 * h + 4, n0), XT::row(LX, tok, s, h));
+          mma32(u, ST::colp(LD, 16 * s + 8 * h, n0), XT::row(LX, tok, s, h));
 #pragma unroll
         for (int e = 0; e < 16; ++e) dB[i][e] = __builtin_fmaf(u[e], dtv, dB[i][e]);
       }
       // dx of the half hf of the block's columns
       f32x16 xa = zero16(), xv = zero16();
 #pragma unroll
-      for (int s = 0; s < N / 16; ++s) mma32(xv, RT::row(LD, 32 * hf + perm32(c), s, h), RT::row(LB, tok, s, h));
+      for (int s = 0; s < N / 16; ++s) mma32(xv, ST::row(LD, 32 * hf, s), RT::row(LB, tok, s, h));
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         if (i >= tj) {

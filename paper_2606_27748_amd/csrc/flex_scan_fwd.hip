@@ -18,24 +18,31 @@ enum {
 // Two terms leave 2^-18 of each product: 1.5e-6 of a state, where fp32 sums leave 1e-7.
 __device__ __forceinline__ void split3(Frag<__bf16> (&t)[3], const float (&x)[8]) {
 #pragma clang fp contract(off)
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  u32x4 w[3];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const __bf16 a = (__bf16)x[j];
-    const float r = x[j] - (float)a;
-    const __bf16 b = (__bf16)r;
-    t[0].v[j] = a;
-    t[1].v[j] = b;
-    t[2].v[j] = (__bf16)(r - (float)b);
+  for (int j = 0; j < 4; ++j) {   // pairs: one conversion instruction each
+    f32x2 v = {x[2 * j], x[2 * j + 1]};
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const unsigned u = __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
+      w[k][j] = u;
+      v[0] -= __uint_as_float(u << 16);
+      v[1] -= __uint_as_float(u & 0xffff0000u);
+    }
   }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) t[k].v = __builtin_bit_cast(bf16x8, w[k]);
 }
 __device__ __forceinline__ void split3(Frag<float> (&t)[1], const float (&x)[8]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) t[0].v[j] = x[j];
 }
 
-// u += rows^T (w x) over a chunk: x as its columns' operands, w of the tokens in LDS
+// u = rows^T (w x) over a chunk: x as its columns' operands, w of the tokens in LDS
 template <class T, int N>
-__device__ __forceinline__ void add_rows(f32x16 (&u)[N / 32], const char* rows, const Frag<T> (&xf)[4], const float* w, int h) {
+__device__ __forceinline__ void form_rows(f32x16 (&u)[N / 32], const char* rows, const Frag<T> (&xf)[4], const float* w, int l) {
+  const int h = l / 32;
   constexpr int TERMS = IsBf16<T>::value ? 3 : 1;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
@@ -47,11 +54,14 @@ __device__ __forceinline__ void add_rows(f32x16 (&u)[N / 32], const char* rows, 
     Frag<T> wx[TERMS], bf[N / 32];
     split3(wx, v);
 #pragma unroll
-    for (int i = 0; i < N / 32; ++i) bf[i] = ScanTile<T, N>::colp(rows, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 32 * i);
+    for (int i = 0; i < N / 32; ++i) bf[i] = ScanTile<T, N>::colp(rows, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 32 * i, l);
 #pragma unroll
     for (int t = TERMS - 1; t >= 0; --t)
 #pragma unroll
-      for (int i = 0; i < N / 32; ++i) mma32(u[i], bf[i], wx[t]);
+      for (int i = 0; i < N / 32; ++i) {
+        if (q == 0 && t == TERMS - 1) u[i] = zero16();
+        mma32(u[i], bf[i], wx[t]);
+      }
   }
 }
 
@@ -86,12 +96,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   using S = typename Io<T>::type;
   using RT = ScanTile<T, N>;
   using XT = ScanTile<T, 32>;
-  constexpr int NT = N / 32, TERMS = IsBf16<T>::value ? 3 : 1;
+  constexpr int NT = N / 32;
   constexpr int ROWS = SC * N * (int)sizeof(T), XROWS = SC * 32 * (int)sizeof(T), BUF = ROWS + 8 * XROWS;
   constexpr int BUFS = 2 * BUF <= 156 * 1024 ? 2 : 1;
   __shared__ __attribute__((aligned(16))) char lds[BUFS * BUF];
   __shared__ __attribute__((aligned(16))) float scal[8][SC];
-  const int l = threadIdx.x % WAVE, c = l % 32, h = l / 32;
+  const int l = threadIdx.x % WAVE;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), nw = blockDim.x / WAVE;
   const SegTile sg = find_segment(a.off, a.B, a.T, a.seg, a.H / a.heads);
   if (sg.b < 0 || (REV ? sg.index == 0 : sg.index == sg.count - 1)) return;
@@ -125,6 +135,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   fetch(REV ? 0 : nchunks - 1);
   for (int k = 0; k < nchunks; ++k) {
     const int next = REV ? k + 1 : nchunks - 2 - k;
+    int x = l;   // places in LDS are formed anew: kept over the loop they would take the registers that it is short of
+    asm volatile("" : "+v"(x));
+    const int h = x / 32;
     const char* L = buf(k);
     sync_tiles();   // the chunk is in LDS, and the buffer of the one before is free
     if (BUFS == 2 && k + 1 < nchunks) stage(k + 1, next);
@@ -135,11 +148,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     const char* LX = L + ROWS + w * XROWS;
     Frag<T> xf[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) xf[q] = XT::colp(LX, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 0);
+    for (int q = 0; q < 4; ++q) xf[q] = XT::colp(LX, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 0, x);
     f32x16 u[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) u[i] = zero16();
-    add_rows<T, N>(u, L, xf, sc, h);
+    form_rows<T, N>(u, L, xf, sc, x);
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -151,11 +162,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   }
   const float whole = __builtin_amdgcn_exp2f((float)total);
   if (!REV && a.state0 && sg.index == 0) {
-    const float* s0 = a.state0 + ((size_t)sg.b * a.H + head) * N * a.P + p0 + perm32(c);
+    const float* s0 = a.state0 + ((size_t)sg.b * a.H + head) * N * a.P + p0 + perm32(l % 32);
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) st[i][e] = __builtin_fmaf(whole, s0[(size_t)(32 * i + perm_row(e, h)) * a.P], st[i][e]);
+      for (int e = 0; e < 16; ++e) st[i][e] = __builtin_fmaf(whole, s0[(size_t)(32 * i + perm_row(e, l / 32)) * a.P], st[i][e]);
   }
   float* carry = a.carry + ((size_t)sg.slot * a.H + head) * N * a.P + (size_t)p0 * N + l * 4;
 #pragma unroll
@@ -236,17 +247,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         for (int e = 0; e < 4; ++e) st[i][4 * q + e] = v[e];
       }
   }
-  auto keep = [&](void* base, int chunk, const Frag<T> (&f)[NS]) {   // as [P][N]
-    S* p = static_cast<S*>(base) + (((size_t)(slot0 + chunk) * a.H + head) * a.P + pc) * N + 8 * (l / 32);
+  auto keep = [&](void* base, int chunk, const Frag<T> (&f)[NS]) {
+    S* p = static_cast<S*>(base) + (((size_t)(slot0 + chunk) * a.H + head) * a.P + p0) * N;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      if constexpr (BF) {
-        *reinterpret_cast<bf16x8*>(p + 16 * s) = f[s].v;
-      } else {
-        *reinterpret_cast<f32x4*>(p + 16 * s) = f32x4{f[s].v[0], f[s].v[1], f[s].v[2], f[s].v[3]};
-        *reinterpret_cast<f32x4*>(p + 16 * s + 4) = f32x4{f[s].v[4], f[s].v[5], f[s].v[6], f[s].v[7]};
-      }
-    }
+    for (int s = 0; s < NS; ++s) StateRows<T, N>::store(p, s, f[s]);
   };
   auto state_frags = [&](Frag<T> (&f)[NS]) {
 #pragma unroll
@@ -266,18 +270,31 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   for (int k = 0; k < nchunks; ++k) {
     const int chunk = REV ? nchunks - 1 - k : k, next = REV ? chunk - 1 : chunk + 1;
     const char* L = buf(k);
-    int x = l;   // places in LDS are formed anew: kept over the loop they would take the registers that it is short of
+    int x = l;   // as above
     asm volatile("" : "+v"(x));
     const int c = x % 32, h = x / 32;
     sync_tiles_but<LATER>();   // the chunk is in LDS, and the buffer of the one before is free
     if (BUFS == 2 && k + 1 < nchunks) stage(k + 1, next);
     const Decay d(gn);
+    float both = 1.f;      // from the middle of the first half to that of the second
+    bool product = false;
     if (Y) {
-      sc[l] = d.hi;
-      if (!BF) sc[SC + l] = d.lo;
-      sc[2 * SC + l] = dn;
-      sc[3 * SC + l] = d.from_start();
-      sc[4 * SC + l] = d.to_end() * dn;
+      sc[l] = d.from_start();
+      sc[SC + l] = d.to_end() * dn;
+      // e^{L_i - L_j} as a product of what lies between a token and its half's middle, where that is far from any
+      // overflow; fp32 rows take the exponential of each difference, whose argument has a smaller error
+      const double m0 = lane_of(d.L, 15), m1 = lane_of(d.L, 47);
+      const float from = (float)(d.L - (l < 32 ? m0 : m1));
+      product = BF && __all(fabsf(from) < 50.f);
+      if (product) {
+        both = __builtin_amdgcn_exp2f((float)(m1 - m0));
+        sc[2 * SC + l] = __builtin_amdgcn_exp2f(from);
+        sc[3 * SC + l] = __builtin_amdgcn_exp2f(-from) * dn;
+      } else {
+        sc[2 * SC + l] = d.hi;
+        sc[3 * SC + l] = d.lo;
+        sc[4 * SC + l] = dn;
+      }
     } else {
       sc[l] = d.from_start();
     }
@@ -285,20 +302,29 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     if (k + 1 < nchunks) fetch(next);
 
     const char* LX = L + (Y ? 2 : 1) * ROWS + w * XROWS;
-    Frag<T> xf[4];   // columns of x, slots the tokens 16 q + 4 h + i and 8 further
+    // columns of x, slots the tokens 16 q + 4 h + i and 8 further
+    auto columns = [&](Frag<T> (&xf)[4]) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) xf[q] = XT::colp(LX, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 0);
-
-    if constexpr (MODE == REV_SAVE) {
-      Frag<T> sb[NS];
-      state_frags(sb);
-      keep(a.dst, chunk, sb);
-    }
-    if constexpr (Y) {
+      for (int q = 0; q < 4; ++q) xf[q] = XT::colp(LX, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 0, x);
+    };
+    auto advance = [&]() {   // S <- e^{L_63} S + B^T (w x)
+      Frag<T> xf[4];
+      columns(xf);
+      f32x16 u[NT];
+      form_rows<T, N>(u, L, xf, sc + (Y ? SC : 0), x);
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st[i][e] = __builtin_fmaf(st[i][e], last, u[i][e]);
+    };
+    Frag<T> sb[NS];
+    state_frags(sb);
+    if constexpr (MODE == REV_SAVE) keep(a.dst, chunk, sb);
+    if constexpr (MODE == SWEEP_SAVE) keep(a.st, chunk, sb);
+    auto read_out = [&]() {
       const char* LC = L + ROWS;
-      Frag<T> sb[NS];
-      state_frags(sb);
-      if constexpr (MODE == SWEEP_SAVE) keep(a.st, chunk, sb);
+      Frag<T> xf[4];
+      columns(xf);
       // x with a value that is not finite: its column's products go over the rows before it only, and the rows from it
       // on are NaN
       int fb = SC;
@@ -329,19 +355,29 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 #pragma unroll
           for (int j = 0; j <= i; ++j) mma32(cb[j], RT::row(L, 32 * j + c, s, h), cr);
         }
-        const float hi = sc[32 * i + c], lo = BF ? 0.f : sc[SC + 32 * i + c], eg = sc[3 * SC + 32 * i + c];
+        const float eg = sc[32 * i + c], ai = sc[2 * SC + 32 * i + c], lo = sc[3 * SC + 32 * i + c];
 #pragma unroll
         for (int e = 0; e < 16; ++e) y[e] *= eg;
 #pragma unroll
         for (int j = 0; j <= i; ++j) {
+          const float aij = j < i ? ai * both : ai;
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const int t = 32 * j + 8 * q + 4 * h;
-            const f32x4 hj = *reinterpret_cast<const f32x4*>(sc + t), dj = *reinterpret_cast<const f32x4*>(sc + 2 * SC + t);
-            const f32x4 lj = BF ? zero4() : *reinterpret_cast<const f32x4*>(sc + SC + t);
+            const f32x4 hj = *reinterpret_cast<const f32x4*>(sc + (product ? 3 * SC : 2 * SC) + t);
+            f32x4 f;
+            if (product) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) f[e] = aij * hj[e];
+            } else {
+              const f32x4 dj = *reinterpret_cast<const f32x4*>(sc + 4 * SC + t);
+              const f32x4 lj = BF ? zero4() : *reinterpret_cast<const f32x4*>(sc + 3 * SC + t);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) f[e] = decay<BF>(ai, lo, hj[e], lj[e]) * dj[e];
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float v = cb[j][4 * q + e] * (decay<BF>(hi, lo, hj[e], lj[e]) * dj[e]);
+              const float v = cb[j][4 * q + e] * f[e];
               cb[j][4 * q + e] = j < i || t + e <= 32 * i + c ? v : 0.f;
             }
           }
@@ -372,18 +408,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         }
         asm volatile("" ::: "memory");   // the second half's operands are not read before the first half is done
       }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) xf[q] = XT::colp(LX, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 0);
+    };
+    if constexpr (!Y) {
+      advance();
+    } else {
+      read_out();
+      advance();
     }
-    // S <- e^{L_63} S + B^T (w x)
-    f32x16 u[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) u[i] = zero16();
-    add_rows<T, N>(u, L, xf, sc + (Y ? 4 * SC : 0), h);
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) st[i][e] = __builtin_fmaf(st[i][e], last, u[i][e]);
     if (BUFS == 1) {
       sync_lds();
       if (k + 1 < nchunks) stage(k + 1, next);
@@ -503,11 +534,11 @@ __global__ __launch_bounds__(256) void k_scan_step(ScanArgs a) {
 namespace {
 template <class T, int N, int MODE>
 void sweep(const ScanArgs& a, hipStream_t st) {
-  k_scan_sweep<T, N, MODE><<<seg_grid(a.T, a.B, a.seg, a.H / a.heads), a.heads * a.P * 2, 0, st>>>(a);
+  k_scan_sweep<T, N, MODE><<<seq_slots(a.T, a.B, a.seg) * (a.H / a.heads), a.heads * a.P * 2, 0, st>>>(a);
 }
 template <class T, int N, bool REV>
 void carry(const ScanArgs& a, hipStream_t st) {
-  k_scan_carry<T, N, REV><<<seg_grid(a.T, a.B, a.seg, a.H / a.heads), a.heads * a.P * 2, 0, st>>>(a);
+  k_scan_carry<T, N, REV><<<seq_slots(a.T, a.B, a.seg) * (a.H / a.heads), a.heads * a.P * 2, 0, st>>>(a);
 }
 template <bool REV>
 void join(const ScanArgs& a, hipStream_t st) {

@@ -407,6 +407,29 @@ __device__ __forceinline__ void stage_tile(const char* L, u32x4 rs, int stride_b
   }
 }
 
+// Linear copy of 1024 N bytes to LDS, one instruction per 1024 bytes, by NW waves.
+template <int N, int NW>
+__device__ __forceinline__ void stage_linear(const char* L, const void* src, int w) {
+  u32x4 d;
+  const uint64_t p = reinterpret_cast<uint64_t>(src);
+  d[0] = __builtin_amdgcn_readfirstlane((unsigned)p);
+  d[1] = __builtin_amdgcn_readfirstlane((unsigned)(p >> 32) & 0xffff);
+  d[2] = N * 1024;
+  d[3] = BUF_FLAGS;
+  const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) const char*)L;
+  const int l = threadIdx.x % WAVE;
+#pragma unroll
+  for (int n = 0; n < (N + NW - 1) / NW; ++n) {
+    const int step = n * NW + w;
+    if (N % NW == 0 || step < N) {
+      const unsigned to = __builtin_amdgcn_readfirstlane(base + step * 1024);
+      const int off = step * 1024 + l * 16;
+      asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to), "v"(off), "s"(d)
+                   : "memory");
+    }
+  }
+}
+
 // 64 consecutive floats of a window to LDS, by one wave; zeros behind it.
 __device__ __forceinline__ void stage_floats(const char* L, u32x4 rs) {
   const unsigned to = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(__attribute__((address_space(3))) const char*)L);
