@@ -145,12 +145,12 @@ size_t scan_tot_bytes(const flex_scan_desc* d) {
 size_t scan_saved_bytes(const flex_scan_desc* d) {
   return (size_t)scan_slots(d, SCAN_CHUNK) * scan_state(d) * esize(d->io_dtype);
 }
-// Parts of a group's heads in the gradients, each a workgroup's: as many as give the card four workgroups per CU.
+// Parts of a group's heads in the gradients, each a workgroup's: as many as give the card two workgroups per CU.
 int scan_parts(const flex_scan_desc* d) {
   const int r = d->H / d->G;
   const int64_t wgs = scan_slots(d, SCAN_CHUNK) * d->G;
   int n = 1;
-  while (n < r && (r % (2 * n) == 0) && wgs * n < 1024) n *= 2;
+  while (n < r && (r % (2 * n) == 0) && wgs * n < 512) n *= 2;
   return n;
 }
 size_t scan_part_bytes(const flex_scan_desc* d) {

@@ -76,8 +76,7 @@ struct StateRows {
     return p / 32 * BLOCK + n / 16 * FRAG + n % 8 / E * (WAVE * 16) + place(perm32(p % 32), n / 8 % 2) * 16 + n % E * (int)sizeof(T);
   }
   // the operand with lane l % 32 column p0 + perm32(l % 32) and the slots 16 s + 8 h ..
-  static __device__ __forceinline__ Frag<T> row(const char* L, int p0, int s) {
-    const int l = threadIdx.x % WAVE;
+  static __device__ __forceinline__ Frag<T> row(const char* L, int p0, int s, int l) {
     const char* q = L + p0 / 32 * BLOCK + s * FRAG + place(l % 32, l / 32) * 16;
     Frag<T> f;
     if constexpr (IsBf16<T>::value) {
@@ -93,8 +92,7 @@ struct StateRows {
     return f;
   }
   // the operand with lane l % 32 element n0 + perm32(l % 32) and the slots columns p .. p + 7
-  static __device__ __forceinline__ Frag<T> colp(const char* L, int p, int n0) {
-    const int l = threadIdx.x % WAVE;
+  static __device__ __forceinline__ Frag<T> colp(const char* L, int p, int n0, int l) {
     Frag<T> f;
     if constexpr (IsBf16<T>::value) {
       const int i = l % 16, q = (i & 1) << 1 | (i >> 1 & 1), n = n0 + 16 * ((l / 16) & 1) + 4 * q;

@@ -19,31 +19,39 @@ namespace flex {
 
 void launch_scan_states(const ScanArgs& a, bool bf16, hipStream_t st);
 
-// One workgroup per chunk, group and part of its heads, over them in order and over their columns in blocks of 64.
-// Wave w has the tokens j of tile w % 2, a lane per token, and of what it forms for them the half w / 2: of the rows n
-// of dB and dC, of the columns p of dx, and of M the tokens i of tile w / 2.
+// One workgroup per chunk, group and part of its heads, over them in order and over their columns in blocks of 64; the
+// next block's x, dy, S and dS on their way to LDS while one is worked on, where two fit.  Of eight waves each has
+// the rows of dB and dC of 32 tokens and 32 elements n (N = 64: the upper four); the lower four form dx of 32
+// tokens and columns each, three of the others the tiles of M and the sums of Z; the last one forms the
+// decays of the next head and puts out dg and ddt of the one before.  A lane is a token j throughout (of M too).
 template <class T, int N>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_grad(ScanArgs a) {
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_grad(ScanArgs a) {
   using S = typename Io<T>::type;
   using RT = ScanTile<T, N>;
   using XT = ScanTile<T, 64>;
   using ST = StateRows<T, N>;
   constexpr bool BF = IsBf16<T>::value;
-  constexpr int NT = N / 64, ROWS = SC * N * (int)sizeof(T), XROWS = SC * 64 * (int)sizeof(T);
+  constexpr int ROWS = SC * N * (int)sizeof(T), XROWS = SC * 64 * (int)sizeof(T);
   // fp32 states of 128 rows leave room for one of S and dS at a time
   constexpr bool ONE = 4 * ROWS + 2 * XROWS > 144 * 1024;
-  __shared__ __attribute__((aligned(16))) char lds[(ONE ? 3 : 4) * ROWS + 2 * XROWS];
-  __shared__ __attribute__((aligned(16))) float sc[5][SC];       // L (hi, lo), dt, e^L, v
-  __shared__ float dot_r[2][SC], dot_v[2][SC], dot_i[2][SC], col_z[2][SC], row_z[2][2][SC], sums[2][4];
+  constexpr int BLOCK = 2 * XROWS + (ONE ? 1 : 2) * ROWS, BUFS = 2 * ROWS + 2 * BLOCK <= 144 * 1024 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) char lds[2 * ROWS + BUFS * BLOCK];
+  // of a head, two in turn: decays as factors from a half's middle (or L, hi and lo), dt, e^L, v; whether they are
+  // factors, that from one middle to the other, the whole decay
+  __shared__ __attribute__((aligned(16))) float scal[2][5 * SC + 4];
+  // what the waves leave for dg and ddt
+  struct Dots {
+    float r[4][SC], v[2][SC], i[2][SC], col[2][SC], row[2][2][SC], d[2], s[8];
+  };
+  __shared__ Dots dots[2];
   char* LB = lds;
   char* LC = lds + ROWS;
-  char* LX = lds + 2 * ROWS;
-  char* LY = LX + XROWS;
-  char* LS = LY + XROWS;
-  char* LD = ONE ? LS : LS + ROWS;
 
   const int l = threadIdx.x % WAVE, c = l % 32, h = l / 32;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), tj = w % 2, hf = w / 2;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), tj = w % 2;
+  const int n0 = N == 128 ? 32 * (w / 2) : 32 * (w / 2 - 2);   // the wave's rows of dB and dC
+  const bool has_n = N == 128 || w >= 4;
+  const int ti = w == 4 ? 0 : 1;                                // the tile of i of waves 4, 5 and 6
   const int id = blockIdx.x, sets = a.G * a.parts, k = id / NUM_XCD;
   const int slot = k / sets * NUM_XCD + id % NUM_XCD, grp = k % sets / a.parts, part = k % sets % a.parts;
   const int slots = seq_slots(a.T, a.B, SC);
@@ -51,272 +59,332 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   const int hpg = a.H / a.G, hpp = hpg / a.parts, head0 = grp * hpg + part * hpp;
   const SeqTile t = find_tile<SC>(a.off, a.B, a.T, slot);
   if (t.b < 0) {
-    for (int i = threadIdx.x; i < hpp; i += 256) a.part_d[(size_t)slot * a.H + head0 + i] = 0.f;
+    for (int i = threadIdx.x; i < hpp; i += 512) a.part_d[(size_t)slot * a.H + head0 + i] = 0.f;
     return;
   }
   const int n = min(SC, t.n - t.tile * SC), row0 = t.row0 + t.tile * SC;
   const int tok = 32 * tj + c;   // this lane's token
-  stage_rows<T, N>(LB, static_cast<const S*>(a.Bt) + (size_t)grp * N, row0, a.bs, n, w, 4);
-  stage_rows<T, N>(LC, static_cast<const S*>(a.Ct) + (size_t)grp * N, row0, a.cs, n, w, 4);
-
-  f32x16 dB[NT], dC[NT], W = zero16(), cb[2];   // cb: C_i.B_j, tiles of i, lane j
-#pragma unroll
-  for (int i = 0; i < NT; ++i) dB[i] = dC[i] = zero16();
-  sync_tiles();
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    cb[i] = zero16();
-    if (i >= tj) {
-#pragma unroll
-      for (int s = 0; s < N / 16; ++s) mma32(cb[i], RT::row(LC, 32 * i + c, s, h), RT::row(LB, tok, s, h));
+  const int nb = a.P / 64, items = hpp * nb;
+  auto block = [&](int it) { return lds + 2 * ROWS + (BUFS == 2 ? (it & 1) * BLOCK : 0); };
+  auto state_at = [&](int it) { return (((size_t)slot * a.H + head0 + it / nb) * a.P + it % nb * 64) * N; };
+  auto stage = [&](int it) {
+    const size_t xcol = (size_t)(head0 + it / nb) * a.P + it % nb * 64;
+    const char* L = block(it);
+    if (w < 4)
+      stage_rows<T, 64>(L, static_cast<const S*>(a.X) + xcol, row0, a.xs, n, w, 4);
+    else
+      stage_rows<T, 64>(L + XROWS, static_cast<const S*>(a.dY) + xcol, row0, a.H * a.P, n, w - 4, 4);
+    stage_linear<ROWS / 1024, 8>(L + 2 * XROWS, static_cast<const S*>(a.st) + state_at(it), w);
+    if (!ONE) stage_linear<ROWS / 1024, 8>(L + 2 * XROWS + ROWS, static_cast<const S*>(a.dst) + state_at(it), w);
+  };
+  float gn = 0.f, dn = 0.f;   // of the next head, lane = token
+  auto fetch = [&](int hd) {
+    if (l < n) {
+      const size_t at = (size_t)(row0 + l) * a.H + head0 + hd;
+      gn = a.g[at];
+      dn = a.dt[at];
     }
-  }
-  const int nb = a.P / 64;
-  for (int hd = 0; hd < hpp; ++hd) {
-    const int head = head0 + hd;
-    f32x16 m0 = zero16();   // dy_i.x_j of the tile hf of i
-    float di = 0.f, dv = 0.f, dr = 0.f, ss = 0.f;
-    const float Dh = a.D ? a.D[head] : 0.f;
-    float last = 0.f;
-    for (int pb = 0; pb < nb; ++pb) {
-      const size_t xcol = (size_t)head * a.P + pb * 64, sat = (((size_t)slot * a.H + head) * a.P + pb * 64) * N;
-      sync_lds();   // what was staged before is no longer read
-      stage_rows<T, 64>(LX, static_cast<const S*>(a.X) + xcol, row0, a.xs, n, w, 4);
-      stage_rows<T, 64>(LY, static_cast<const S*>(a.dY) + xcol, row0, a.H * a.P, n, w, 4);
-      stage_linear<ROWS / 1024, 4>(LS, static_cast<const S*>(a.st) + sat, w);
-      if (!ONE) stage_linear<ROWS / 1024, 4>(LD, static_cast<const S*>(a.dst) + sat, w);
-      if (pb == 0) {   // every wave forms the decays, the first one writes them
-        float g = 0.f, dt = 0.f;
-        if (l < n) {
-          const size_t at = (size_t)(row0 + l) * a.H + head;
-          g = a.g[at];
-          dt = a.dt[at];
-        }
-        const Decay d(g);
-        last = __builtin_amdgcn_exp2f((float)d.end);
-        if (w == 0) {
-          sc[0][l] = d.hi;
-          sc[1][l] = d.lo;
-          sc[2][l] = dt;
-          sc[3][l] = d.from_start();
-          sc[4][l] = d.to_end();
-        }
-      }
-      sync_tiles();
-      const float hj = sc[0][tok], lj = sc[1][tok], dt = sc[2][tok], eg = sc[3][tok], vj = sc[4][tok];
+  };
+  auto decays = [&](int hd) {
+    float* sc = scal[hd & 1];
+    const Decay d(gn);
+    const double m0 = lane_of(d.L, 15), m1 = lane_of(d.L, 47);
+    const float from = (float)(d.L - (l < 32 ? m0 : m1));
+    const bool product = BF && __all(fabsf(from) < 50.f);
+    sc[l] = product ? __builtin_amdgcn_exp2f(from) : d.hi;
+    sc[SC + l] = product ? __builtin_amdgcn_exp2f(-from) : d.lo;
+    sc[2 * SC + l] = dn;
+    sc[3 * SC + l] = d.from_start();
+    sc[4 * SC + l] = d.to_end();
+    if (l == 0) {
+      sc[5 * SC] = product ? 1.f : 0.f;
+      sc[5 * SC + 1] = __builtin_amdgcn_exp2f((float)(m1 - m0));
+      sc[5 * SC + 2] = __builtin_amdgcn_exp2f((float)d.end);
+    }
+  };
+  // dg, ddt and the chunk's part of dD of a head, by one wave; lane = token
+  auto put_out = [&](int hd) {
+    const float* sc = scal[hd & 1];
+    const Dots& o = dots[hd & 1];
+    const size_t at = (size_t)(row0 + l) * a.H + head0 + hd;
+    const float g = l < n ? a.g[at] : 0.f;
+    // rows of tile 0 have the tile of j 0 alone
+    const float rz = (o.row[0][0][l] + o.row[0][1][l]) + (l >= 32 ? o.row[1][0][l] + o.row[1][1][l] : 0.f);
+    const float cz = l < 32 ? o.col[0][l] + o.col[1][l] : o.col[1][l];
+    float x = (N == 128 ? (o.r[0][l] + o.r[1][l]) + (o.r[2][l] + o.r[3][l]) : o.r[0][l] + o.r[1][l]) * sc[3 * SC + l] + rz - cz;
+    const float v = o.v[0][l] + o.v[1][l];
+    float z = __shfl_up(v * sc[2 * SC + l], 1);
+    if (l == 0) z = 0.f;
+    if (l == SC - 1) x += sc[5 * SC + 2] * (((o.s[0] + o.s[1]) + (o.s[2] + o.s[3])) + ((o.s[4] + o.s[5]) + (o.s[6] + o.s[7])));
+#pragma unroll
+    for (int s = 1; s < WAVE; s *= 2) {   // sums over i >= l, and over i < l
+      const float p = __shfl_down(x, s), q = __shfl_up(z, s);
+      if (l + s < WAVE) x += p;
+      if (l >= s) z += q;
+    }
+    if (l < n) {
+      // in the io type like every gradient of this operator, though dt and g are fp32; a decay of zero has no slope
+      static_cast<S*>(a.dg)[at] = float_to_io<S>(g < SCAN_MIN_G ? 0.f : x + z);
+      static_cast<S*>(a.ddt)[at] = float_to_io<S>((o.i[0][l] + o.i[1][l]) + v);
+    }
+    if (l == 0) a.part_d[(size_t)slot * a.H + head0 + hd] = o.d[0] + o.d[1];
+  };
 
-      // M's products, and e^L S dy
-      if (hf >= tj) {
+  stage_rows<T, N>(w < 4 ? LB : LC, (w < 4 ? static_cast<const S*>(a.Bt) : static_cast<const S*>(a.Ct)) + (size_t)grp * N, row0,
+                   w < 4 ? a.bs : a.cs, n, w % 4, 4);
+  if (w == 7) {
+    fetch(0);
+    decays(0);
+    if (hpp > 1) fetch(1);
+  }
+  // ka, kb: of the lower waves C_i.B_j of the tiles 0 and 1 of i, of the upper ones that of the tile ti, and dy_i.x_j of it
+  f32x16 dB = zero16(), dC = zero16(), W = zero16(), ka = zero16(), kb = zero16();
+  stage(0);
+  sync_tiles();
+  auto products = [&](f32x16& to, int tile) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) mma32(m0, XT::row(LY, 32 * hf + c, s, h), XT::row(LX, tok, s, h));
+    for (int s = 0; s < N / 16; ++s) mma32(to, RT::row(LC, 32 * tile + c, s, h), RT::row(LB, tok, s, h));
+  };
+  if (w >= 4) {
+    products(ka, ti);
+  } else {
+    if (tj == 0) products(ka, 0);
+    products(kb, 1);
+  }
+  // the operands of a phase are not read before the one before it is done: registers
+  auto phase = [&]() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  float di = 0.f, dv = 0.f, dr = 0.f, ss = 0.f;
+  for (int it = 0; it < items; ++it) {
+    const int hd = it / nb, head = head0 + hd, pb = it % nb;
+    if (BUFS == 1 && it > 0) {
+      sync_lds();   // what was staged before is no longer read
+      stage(it);
+    }
+    if (BUFS == 1 || it > 0) sync_tiles();
+    if (BUFS == 2 && it + 1 < items) stage(it + 1);
+    int x = l;   // places in LDS are formed anew: kept over the loop they would take the registers that it is short of
+    asm volatile("" : "+v"(x));
+    const int c = x % 32, h = x / 32, tok = 32 * tj + c;
+    const char* LX = block(it);
+    const char* LY = LX + XROWS;
+    const char* LS = LY + XROWS;
+    const char* LD = ONE ? LS : LS + ROWS;
+    const float* sc = scal[hd & 1];
+    Dots& o = dots[hd & 1];
+    if (w == 7 && pb == 0) {
+      if (hd > 0) put_out(hd - 1);
+      if (hd + 1 < hpp) {   // its place was the head's before, which is put out
+        decays(hd + 1);
+        if (hd + 2 < hpp) fetch(hd + 2);
+      }
+    }
+    const float eg = sc[3 * SC + tok], dt = sc[2 * SC + tok], vj = sc[4 * SC + tok];
+    if (pb == 0) {
+      if (w >= 4) kb = zero16();
+      di = dv = dr = ss = 0.f;
+    }
+    if (has_n) {   // e^L S dy
+      f32x16 u = zero16();
+#pragma unroll
+      for (int s = 0; s < 4; ++s) mma32(u, ST::colp(LS, 16 * s + 8 * h, n0, x), XT::row(LY, tok, s, h));
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const Frag<T> cr = RT::row(LC, tok, n0 / 16 + s, h);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dr = __builtin_fmaf(cr.get(j), u[8 * s + j], dr);
       }
 #pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        f32x16 u = zero16();
-        const int n0 = hf * (N / 2) + 32 * i;
+      for (int e = 0; e < 16; ++e) dC[e] = __builtin_fmaf(u[e], eg, dC[e]);
+    }
+    phase();
+    if (ONE) {
+      sync_lds();
+      stage_linear<ROWS / 1024, 8>(LD, static_cast<const S*>(a.dst) + state_at(it), w);
+      const float* s0 = reinterpret_cast<const float*>(static_cast<const S*>(a.st) + state_at(it));
+      const float* d0 = reinterpret_cast<const float*>(static_cast<const S*>(a.dst) + state_at(it));
+      for (int i = threadIdx.x; i < 64 * N; i += 512) ss = __builtin_fmaf(s0[i], d0[i], ss);
+      sync_tiles();
+    } else {
+      for (int i = w * WAVE + x; i < ROWS / 16; i += 512) {   // <S, dS>: the same place in both
+        if constexpr (BF) {
+          const bf16x8 u = *reinterpret_cast<const bf16x8*>(LS + 16 * i), v = *reinterpret_cast<const bf16x8*>(LD + 16 * i);
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-          mma32(u, ST::colp(LS, 16 * s + 8 * h, n0), XT::row(LY, tok, s, h));
-        float r = 0.f;
+          for (int j = 0; j < 8; ++j) ss = __builtin_fmaf((float)u[j], (float)v[j], ss);
+        } else {
+          const f32x4 u = *reinterpret_cast<const f32x4*>(LS + 16 * i), v = *reinterpret_cast<const f32x4*>(LD + 16 * i);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const Frag<T> cr = RT::row(LC, tok, n0 / 16 + s, h);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) r = __builtin_fmaf(cr.get(j), u[8 * s + j], r);
+          for (int j = 0; j < 4; ++j) ss = __builtin_fmaf(u[j], v[j], ss);
         }
-        dr += r;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) dC[i][e] = __builtin_fmaf(u[e], eg, dC[i][e]);
       }
-      if (ONE) {
-        sync_lds();
-        stage_linear<ROWS / 1024, 4>(LD, static_cast<const S*>(a.dst) + sat, w);
-        const float* s0 = reinterpret_cast<const float*>(static_cast<const S*>(a.st) + sat);
-        const float* d0 = reinterpret_cast<const float*>(static_cast<const S*>(a.dst) + sat);
-        for (int i = threadIdx.x; i < 64 * N; i += 256) ss = __builtin_fmaf(s0[i], d0[i], ss);
-        sync_tiles();
-      } else {
-        for (int i = threadIdx.x; i < ROWS / 16; i += 256) {   // <S, dS>: the same place in both tiles
-          if constexpr (IsBf16<T>::value) {
-            const bf16x8 x = *reinterpret_cast<const bf16x8*>(LS + 16 * i), y = *reinterpret_cast<const bf16x8*>(LD + 16 * i);
+    }
+    phase();
+    if (has_n) {   // dt v dS x
+      f32x16 u = zero16();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) ss = __builtin_fmaf((float)x[j], (float)y[j], ss);
-          } else {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(LS + 16 * i), y = *reinterpret_cast<const f32x4*>(LD + 16 * i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) ss = __builtin_fmaf(x[j], y[j], ss);
-          }
-        }
-      }
-      // dt v dS x
+      for (int s = 0; s < 4; ++s) mma32(u, ST::colp(LD, 16 * s + 8 * h, n0, x), XT::row(LX, tok, s, h));
       const float dtv = dt * vj;
 #pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        f32x16 u = zero16();
-        const int n0 = hf * (N / 2) + 32 * i;
+      for (int e = 0; e < 16; ++e) dB[e] = __builtin_fmaf(u[e], dtv, dB[e]);
+    }
+    phase();
+    // e^{L_i - L_j} of a tile of i, its element 4 q + e
+    const bool product = sc[5 * SC] != 0.f;
+    const float hj = sc[(product ? SC : 0) + tok], lj = sc[SC + tok];
+    auto decay_to = [&](f32x4& f, int tile, int q, float bj) {
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(sc + 32 * tile + 8 * q + 4 * h);
+      if (product) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-          mma32(u, ST::colp(LD, 16 * s + 8 * h, n0), XT::row(LX, tok, s, h));
+        for (int e = 0; e < 4; ++e) f[e] = hi[e] * bj;
+      } else {
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(sc + SC + 32 * tile + 8 * q + 4 * h);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) dB[i][e] = __builtin_fmaf(u[e], dtv, dB[i][e]);
+        for (int e = 0; e < 4; ++e) f[e] = decay<BF>(hi[e], lo[e], hj, lj);
       }
-      // dx of the half hf of the block's columns
+    };
+    if (w < 4) {   // dx of 32 of the block's columns
+      const int p0 = 32 * (w / 2);
       f32x16 xa = zero16(), xv = zero16();
 #pragma unroll
-      for (int s = 0; s < N / 16; ++s) mma32(xv, ST::row(LD, 32 * hf, s), RT::row(LB, tok, s, h));
+      for (int s = 0; s < N / 16; ++s) mma32(xv, ST::row(LD, p0, s, x), RT::row(LB, tok, s, h));
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         if (i >= tj) {
           f32x16 q;
+          const float bj = i > tj ? hj * sc[5 * SC + 1] : hj;
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
-            const int ti = 32 * i + 8 * b + 4 * h;
-            const f32x4 hi = *reinterpret_cast<const f32x4*>(&sc[0][ti]), lo = *reinterpret_cast<const f32x4*>(&sc[1][ti]);
+            f32x4 f;
+            decay_to(f, i, b, bj);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              q[4 * b + e] = ti + e >= tok ? cb[i][4 * b + e] * decay<BF>(hi[e], lo[e], hj, lj) : 0.f;
+            for (int e = 0; e < 4; ++e) q[4 * b + e] = i > tj || 8 * b + 4 * h + e >= c ? (i == 0 ? ka[4 * b + e] : kb[4 * b + e]) * f[e] : 0.f;
           }
 #pragma unroll
           for (int s = 0; s < 2; ++s)
-            mma32(xa, XT::colp(LY, 32 * i + 16 * s + 4 * h, 32 * i + 16 * s + 8 + 4 * h, 32 * hf), frag_of<T>(q, s));
+            mma32(xa, XT::colp(LY, 32 * i + 16 * s + 4 * h, 32 * i + 16 * s + 8 + 4 * h, p0, x), frag_of<T>(q, s));
         }
-      const auto rx = row_window(static_cast<S*>(a.dX) + xcol + 32 * hf, row0, a.dxs, n, 32);
+      phase();
+      const float Dh = a.D ? a.D[head] : 0.f;
+      const auto rx = row_window(static_cast<S*>(a.dX) + (size_t)head * a.P + pb * 64 + p0, row0, a.dxs, n, 32);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const Frag<T> xr = XT::row(LX, tok, 2 * hf + s, h), yr = XT::row(LY, tok, 2 * hf + s, h);
+        const Frag<T> xr = XT::row(LX, tok, p0 / 16 + s, h), yr = XT::row(LY, tok, p0 / 16 + s, h);
         const int at = (tok * a.dxs + 16 * s + 8 * h) * (int)sizeof(S);
-        float o[8];
+        float v8[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float p = xa[8 * s + j], v = vj * xv[8 * s + j];
           di = __builtin_fmaf(p, xr.get(j), di);
           dv = __builtin_fmaf(v, xr.get(j), dv);
-          o[j] = __builtin_fmaf(dt, p + v, Dh * yr.get(j));
+          v8[j] = __builtin_fmaf(dt, p + v, Dh * yr.get(j));
         }
-        if constexpr (IsBf16<T>::value) {
+        if constexpr (BF) {
           Frag<T> f;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f.set(j, o[j]);
+          for (int j = 0; j < 8; ++j) f.set(j, v8[j]);
           __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f.v), rx, at, 0, 0);
         } else {
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{o[0], o[1], o[2], o[3]}), rx, at, 0, 0);
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{o[4], o[5], o[6], o[7]}), rx, at + 16, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v8[0], v8[1], v8[2], v8[3]}), rx, at, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v8[4], v8[5], v8[6], v8[7]}), rx, at + 16, 0, 0);
         }
       }
-    }
-    // M, W and the sums of Z; the diagonal of dy x^T
-    const float hj = sc[0][tok], lj = sc[1][tok], dt = sc[2][tok], eg = sc[3][tok];
-    float dd = 0.f, cz = 0.f;
-    if (hf >= tj) {
-      f32x16 z;
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int ti = 32 * hf + 8 * b + 4 * h;
-        const f32x4 hi = *reinterpret_cast<const f32x4*>(&sc[0][ti]), lo = *reinterpret_cast<const f32x4*>(&sc[1][ti]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int x = 4 * b + e, i = ti + e;
-          if (i == tok) dd = m0[x];
-          const float m = i >= tok ? m0[x] * decay<BF>(hi[e], lo[e], hj, lj) * dt : 0.f;
-          W[x] += m;
-          z[x] = i > tok ? m * (hf == 0 ? cb[0][x] : cb[1][x]) : 0.f;
-          cz += z[x];
+      if (pb == nb - 1) {
+        di = half_sum(di);
+        dv = half_sum(dv);
+        if (h == 0) {
+          o.i[w / 2][tok] = di;
+          o.v[w / 2][tok] = dv;
         }
       }
+    } else if (w < 7) {   // M, and the sums of Z
 #pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        const float r = lane_sum<16>(z[x]);
-        if (l % 16 == 0) row_z[tj][(l / 16) & 1][32 * hf + res_row(x, h)] = r;
-      }
-    }
-    dd = group_sum_swap(lane_sum<16>(dd));
-    ss = group_sum_swap(lane_sum<16>(ss));
-    cz = half_sum(cz);
-    di = half_sum(di);
-    dv = half_sum(dv);
-    dr = half_sum(dr);
-    if (h == 0) {
-      col_z[hf][tok] = hf >= tj ? cz : 0.f;
-      dot_i[hf][tok] = di;
-      dot_v[hf][tok] = dv;
-      dot_r[hf][tok] = dr * eg;
-    }
-    if (l == 0) {
-      sums[0][w] = dd;
-      sums[1][w] = ss;
-    }
-    sync_lds();
-    if (w == 0) {
-      const float g = l < n ? a.g[(size_t)(row0 + l) * a.H + head] : 0.f, dtl = sc[2][l];
-      // rows of tile 0 have the tile of j 0 alone
-      const float rz = (row_z[0][0][l] + row_z[0][1][l]) + (l >= 32 ? row_z[1][0][l] + row_z[1][1][l] : 0.f);
-      float x = (dot_r[0][l] + dot_r[1][l]) + rz - (col_z[0][l] + col_z[1][l]);
-      const float v = dot_v[0][l] + dot_v[1][l];
-      float z = __shfl_up(v * dtl, 1);
-      if (l == 0) z = 0.f;
-      if (l == SC - 1) x += last * ((sums[1][0] + sums[1][1]) + (sums[1][2] + sums[1][3]));
+      for (int s = 0; s < 4; ++s) mma32(kb, XT::row(LY, 32 * ti + c, s, h), XT::row(LX, tok, s, h));
+      if (pb == nb - 1) {
+        float dd = 0.f, cz = 0.f;
+        f32x16 z;
+        const float bj = ti > tj ? hj * sc[5 * SC + 1] : hj;
 #pragma unroll
-      for (int s = 1; s < WAVE; s *= 2) {   // sums over i >= l, and over i < l
-        const float o = __shfl_down(x, s), p = __shfl_up(z, s);
-        if (l + s < WAVE) x += o;
-        if (l >= s) z += p;
+        for (int b = 0; b < 4; ++b) {
+          f32x4 f;
+          decay_to(f, ti, b, bj);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int y = 4 * b + e, i = 8 * b + 4 * h + e;   // of the tile
+            if (ti == tj && i == c) dd = kb[y];
+            const float m = ti > tj || i >= c ? kb[y] * f[e] * dt : 0.f;
+            W[y] += m;
+            z[y] = ti > tj || i > c ? m * ka[y] : 0.f;
+            cz += z[y];
+          }
+        }
+#pragma unroll
+        for (int y = 0; y < 16; ++y) {
+          const float r = lane_sum<16>(z[y]);
+          if (l % 16 == 0) o.row[tj][(l / 16) & 1][32 * ti + res_row(y, h)] = r;
+        }
+        cz = half_sum(cz);
+        if (h == 0) o.col[ti][tok] = cz;
+        dd = group_sum_swap(lane_sum<16>(dd));
+        if (l == 0 && ti == tj) o.d[ti] = dd;
       }
-      if (l < n) {
-        const size_t at = (size_t)(row0 + l) * a.H + head;
-        // in the io type like every gradient of this operator, though dt and g are fp32; a decay of zero has no slope
-        static_cast<S*>(a.dg)[at] = float_to_io<S>(g < SCAN_MIN_G ? 0.f : x + z);
-        static_cast<S*>(a.ddt)[at] = float_to_io<S>((dot_i[0][l] + dot_i[1][l]) + v);
+    }
+    if (pb == nb - 1) {
+      if (has_n) {
+        dr = half_sum(dr);
+        if (h == 0) o.r[n0 / 32][tok] = dr;
       }
-      if (l == 0) a.part_d[(size_t)slot * a.H + head] = (sums[0][0] + sums[0][1]) + (sums[0][2] + sums[0][3]);
+      ss = group_sum_swap(lane_sum<16>(ss));
+      if (l == 0) o.s[w] = ss;
     }
   }
+  sync_lds();
+  if (w == 7) put_out(hpp - 1);
   // dB += W^T C, dC += W B, through W as rows i in LDS, as two bf16 terms: the heads' M may cancel in it
-  sync_lds();
-  constexpr int TERMS = IsBf16<T>::value ? 2 : 1;
+  constexpr int TERMS = BF ? 2 : 1;
+  char* LW = lds + 2 * ROWS;
+  if (w >= 4) {
+    const int ri = w < 7 ? ti : 0;
 #pragma unroll
-  for (int x = 0; x < 16; ++x) {
-    const int i = 32 * hf + res_row(x, h);
-    float v = hf >= tj ? W[x] : 0.f;
+    for (int y = 0; y < 16; ++y) {
+      const int i = 32 * ri + res_row(y, h);
+      float v = w < 7 ? W[y] : 0.f;
 #pragma unroll
-    for (int t = 0; t < TERMS; ++t) {
-      const S u = float_to_io<S>(v);
-      *reinterpret_cast<S*>(LX + t * XROWS + XT::at(i, tok / XT::E) + tok % XT::E * (int)sizeof(S)) = u;
-      v -= io_to_float(u);
+      for (int k = 0; k < TERMS; ++k) {
+        const S u = float_to_io<S>(v);
+        *reinterpret_cast<S*>(LW + k * XROWS + XT::at(i, tok / XT::E) + tok % XT::E * (int)sizeof(S)) = u;
+        v -= io_to_float(u);
+      }
     }
   }
   sync_lds();
+  if (!has_n) return;
 #pragma unroll
   for (int s = 0; s < 4; ++s)
 #pragma unroll
-    for (int t = TERMS - 1; t >= 0; --t) {
-      const char* LW = LX + t * XROWS;
-      const Frag<T> wr = XT::row(LW, tok, s, h), wc = XT::col(LW, 16 * s + 4 * h, 32 * tj);
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        const int n0 = hf * (N / 2) + 32 * i;
-        if (s / 2 <= tj) mma32(dC[i], RT::colp(LB, 16 * s + 8 * h, 16 * s + 8 * h + 4, n0), wr);
-        if (s / 2 >= tj) mma32(dB[i], RT::colp(LC, 16 * s + 4 * h, 16 * s + 8 + 4 * h, n0), wc);
-      }
+    for (int k = TERMS - 1; k >= 0; --k) {
+      const char* L = LW + k * XROWS;
+      if (s / 2 <= tj) mma32(dC, RT::colp(LB, 16 * s + 8 * h, 16 * s + 8 * h + 4, n0), XT::row(L, tok, s, h));
+      if (s / 2 >= tj) mma32(dB, RT::colp(LC, 16 * s + 4 * h, 16 * s + 8 + 4 * h, n0), XT::col(L, 16 * s + 4 * h, 32 * tj));
     }
-  auto store = [&](const f32x16 (&x)[NT], float* parts, void* out, int stride) {
+  auto store = [&](const f32x16& x, float* parts, void* out, int stride) {
     if (tok >= n) return;
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int n0 = hf * (N / 2) + 32 * i + 16 * s + 8 * h;
-        const f32x4 u = {x[i][8 * s], x[i][8 * s + 1], x[i][8 * s + 2], x[i][8 * s + 3]};
-        const f32x4 v = {x[i][8 * s + 4], x[i][8 * s + 5], x[i][8 * s + 6], x[i][8 * s + 7]};
-        if (parts) {
-          float* p = parts + ((((size_t)part * slots + slot) * SC + tok) * a.G + grp) * N + n0;
-          *reinterpret_cast<f32x4*>(p) = u;
-          *reinterpret_cast<f32x4*>(p + 4) = v;
-        } else {
-          S* p = static_cast<S*>(out) + (size_t)(row0 + tok) * stride + (size_t)grp * N + n0;
-          store_io4(p, u);
-          store_io4(p + 4, v);
-        }
+    for (int s = 0; s < 2; ++s) {
+      const int col = n0 + 16 * s + 8 * h;
+      const f32x4 u = {x[8 * s], x[8 * s + 1], x[8 * s + 2], x[8 * s + 3]};
+      const f32x4 v = {x[8 * s + 4], x[8 * s + 5], x[8 * s + 6], x[8 * s + 7]};
+      if (parts) {
+        float* p = parts + ((((size_t)part * slots + slot) * SC + tok) * a.G + grp) * N + col;
+        *reinterpret_cast<f32x4*>(p) = u;
+        *reinterpret_cast<f32x4*>(p + 4) = v;
+      } else {
+        S* p = static_cast<S*>(out) + (size_t)(row0 + tok) * stride + (size_t)grp * N + col;
+        store_io4(p, u);
+        store_io4(p + 4, v);
       }
+    }
   };
   store(dB, a.part_b, a.dB, a.dbs);
   store(dC, a.part_c, a.dC, a.dcs);
@@ -361,7 +429,7 @@ namespace {
 template <class T, int N>
 void grad(const ScanArgs& a, hipStream_t st) {
   const int slots = seq_slots(a.T, a.B, SC);
-  k_scan_grad<T, N><<<(slots + NUM_XCD - 1) / NUM_XCD * NUM_XCD * a.G * a.parts, 256, 0, st>>>(a);
+  k_scan_grad<T, N><<<(slots + NUM_XCD - 1) / NUM_XCD * NUM_XCD * a.G * a.parts, 512, 0, st>>>(a);
   if (a.part_b) k_scan_parts<typename Io<T>::type><<<slots, 256, 0, st>>>(a);
 }
 }  // namespace
