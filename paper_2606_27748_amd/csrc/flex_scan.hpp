@@ -110,10 +110,10 @@ struct StateRows {
 // Stages 64 rows of a window by `nw` waves of which this is w, 16 rows at a time.
 template <class T, int D>
 __device__ __forceinline__ void stage_rows(const char* L, const typename Io<T>::type* base, size_t row0, int stride, int n, int w,
-                                           int nw) {
+                                           int nw, int l = threadIdx.x % WAVE) {
   for (int k = w; k < 4; k += nw)
     stage_tile<T, D, 16, 1>(L + k * 16 * D * (int)sizeof(T), row_words(base, row0 + 16 * k, stride, n - 16 * k, D),
-                            stride * (int)sizeof(T), 0);
+                            stride * (int)sizeof(T), 0, l);
 }
 
 // Inclusive sum over the lanes of a wave.

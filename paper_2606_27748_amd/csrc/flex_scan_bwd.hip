@@ -65,20 +65,28 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   const int n = min(SC, t.n - t.tile * SC), row0 = t.row0 + t.tile * SC;
   const int tok = 32 * tj + c;   // this lane's token
   const int nb = a.P / 64, items = hpp * nb;
+  // the lane, for places that are formed anew: kept over the loop they would take the registers that it is short of
+  auto again = [&]() {
+    int x = l;
+    asm volatile("" : "+v"(x));
+    return x;
+  };
   auto block = [&](int it) { return lds + 2 * ROWS + (BUFS == 2 ? (it & 1) * BLOCK : 0); };
   auto state_at = [&](int it) { return (((size_t)slot * a.H + head0 + it / nb) * a.P + it % nb * 64) * N; };
   auto stage = [&](int it) {
+    const int x = again();
     const size_t xcol = (size_t)(head0 + it / nb) * a.P + it % nb * 64;
     const char* L = block(it);
     if (w < 4)
-      stage_rows<T, 64>(L, static_cast<const S*>(a.X) + xcol, row0, a.xs, n, w, 4);
+      stage_rows<T, 64>(L, static_cast<const S*>(a.X) + xcol, row0, a.xs, n, w, 4, x);
     else
-      stage_rows<T, 64>(L + XROWS, static_cast<const S*>(a.dY) + xcol, row0, a.H * a.P, n, w - 4, 4);
-    stage_linear<ROWS / 1024, 8>(L + 2 * XROWS, static_cast<const S*>(a.st) + state_at(it), w);
-    if (!ONE) stage_linear<ROWS / 1024, 8>(L + 2 * XROWS + ROWS, static_cast<const S*>(a.dst) + state_at(it), w);
+      stage_rows<T, 64>(L + XROWS, static_cast<const S*>(a.dY) + xcol, row0, a.H * a.P, n, w - 4, 4, x);
+    stage_linear<ROWS / 1024, 8>(L + 2 * XROWS, static_cast<const S*>(a.st) + state_at(it), w, x);
+    if (!ONE) stage_linear<ROWS / 1024, 8>(L + 2 * XROWS + ROWS, static_cast<const S*>(a.dst) + state_at(it), w, x);
   };
   float gn = 0.f, dn = 0.f;   // of the next head, lane = token
   auto fetch = [&](int hd) {
+    const int l = again();
     if (l < n) {
       const size_t at = (size_t)(row0 + l) * a.H + head0 + hd;
       gn = a.g[at];
@@ -86,6 +94,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     }
   };
   auto decays = [&](int hd) {
+    const int l = again();
     float* sc = scal[hd & 1];
     const Decay d(gn);
     const double m0 = lane_of(d.L, 15), m1 = lane_of(d.L, 47);
@@ -104,6 +113,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   };
   // dg, ddt and the chunk's part of dD of a head, by one wave; lane = token
   auto put_out = [&](int hd) {
+    const int l = again();
     const float* sc = scal[hd & 1];
     const Dots& o = dots[hd & 1];
     const size_t at = (size_t)(row0 + l) * a.H + head0 + hd;
@@ -165,8 +175,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     }
     if (BUFS == 1 || it > 0) sync_tiles();
     if (BUFS == 2 && it + 1 < items) stage(it + 1);
-    int x = l;   // places in LDS are formed anew: kept over the loop they would take the registers that it is short of
-    asm volatile("" : "+v"(x));
+    const int x = again();
     const int c = x % 32, h = x / 32, tok = 32 * tj + c;
     const char* LX = block(it);
     const char* LY = LX + XROWS;
