@@ -116,6 +116,18 @@ __device__ __forceinline__ void stage_rows(const char* L, const typename Io<T>::
                             stride * (int)sizeof(T), 0, l);
 }
 
+// the value of lane l ^ M, M 1 or 2
+template <int M>
+__device__ __forceinline__ float lane_xor(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), M == 1 ? 0xB1 : 0x4E, 0xF, 0xF, false));
+}
+// sum over the lanes of a row of 16 with the same place in four, in each of them
+__device__ __forceinline__ float row_sum4(float x) {
+  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x124, 0xF, 0xF, false));   // rotated by 4
+  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x128, 0xF, 0xF, false));   // and by 8
+  return x;
+}
+
 // Inclusive sum over the lanes of a wave.
 __device__ __forceinline__ double wave_scan(double x) {
   auto step = [&](auto ctrl, auto rows) {

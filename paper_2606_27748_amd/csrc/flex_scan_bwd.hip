@@ -38,7 +38,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   __shared__ __attribute__((aligned(16))) char lds[2 * ROWS + BUFS * BLOCK];
   // of a head, two in turn: decays as factors from a half's middle (or L, hi and lo), dt, e^L, v; whether they are
   // factors, that from one middle to the other, the whole decay
-  __shared__ __attribute__((aligned(16))) float scal[2][5 * SC + 4];
+  __shared__ __attribute__((aligned(16))) float scal[2][6 * SC + 4];
   // what the waves leave for dg and ddt
   struct Dots {
     float r[4][SC], v[2][SC], i[2][SC], col[2][SC], row[2][2][SC], d[2], s[8];
@@ -52,6 +52,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   const int n0 = N == 128 ? 32 * (w / 2) : 32 * (w / 2 - 2);   // the wave's rows of dB and dC
   const bool has_n = N == 128 || w >= 4;
   const int ti = w == 4 ? 0 : 1;                                // the tile of i of waves 4, 5 and 6
+  // the tokens that waves 0 to 3 form dx of: those of two tiles of i are not on the SIMDs of M's tiles on the diagonal
+  const int tx = w < 2 ? 1 : 0;
   const int id = blockIdx.x, sets = a.G * a.parts, k = id / NUM_XCD;
   const int slot = k / sets * NUM_XCD + id % NUM_XCD, grp = k % sets / a.parts, part = k % sets % a.parts;
   const int slots = seq_slots(a.T, a.B, SC);
@@ -105,10 +107,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     sc[2 * SC + l] = dn;
     sc[3 * SC + l] = d.from_start();
     sc[4 * SC + l] = d.to_end();
+    sc[5 * SC + l] = gn < SCAN_MIN_G ? 0.f : 1.f;   // a decay of zero has no slope
     if (l == 0) {
-      sc[5 * SC] = product ? 1.f : 0.f;
-      sc[5 * SC + 1] = __builtin_amdgcn_exp2f((float)(m1 - m0));
-      sc[5 * SC + 2] = __builtin_amdgcn_exp2f((float)d.end);
+      sc[6 * SC] = product ? 1.f : 0.f;
+      sc[6 * SC + 1] = __builtin_amdgcn_exp2f((float)(m1 - m0));
+      sc[6 * SC + 2] = __builtin_amdgcn_exp2f((float)d.end);
     }
   };
   // dg, ddt and the chunk's part of dD of a head, by one wave; lane = token
@@ -117,24 +120,19 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     const float* sc = scal[hd & 1];
     const Dots& o = dots[hd & 1];
     const size_t at = (size_t)(row0 + l) * a.H + head0 + hd;
-    const float g = l < n ? a.g[at] : 0.f;
     // rows of tile 0 have the tile of j 0 alone
     const float rz = (o.row[0][0][l] + o.row[0][1][l]) + (l >= 32 ? o.row[1][0][l] + o.row[1][1][l] : 0.f);
     const float cz = l < 32 ? o.col[0][l] + o.col[1][l] : o.col[1][l];
     float x = (N == 128 ? (o.r[0][l] + o.r[1][l]) + (o.r[2][l] + o.r[3][l]) : o.r[0][l] + o.r[1][l]) * sc[3 * SC + l] + rz - cz;
     const float v = o.v[0][l] + o.v[1][l];
-    float z = __shfl_up(v * sc[2 * SC + l], 1);
-    if (l == 0) z = 0.f;
-    if (l == SC - 1) x += sc[5 * SC + 2] * (((o.s[0] + o.s[1]) + (o.s[2] + o.s[3])) + ((o.s[4] + o.s[5]) + (o.s[6] + o.s[7])));
-#pragma unroll
-    for (int s = 1; s < WAVE; s *= 2) {   // sums over i >= l, and over i < l
-      const float p = __shfl_down(x, s), q = __shfl_up(z, s);
-      if (l + s < WAVE) x += p;
-      if (l >= s) z += q;
-    }
+    if (l == SC - 1) x += sc[6 * SC + 2] * (((o.s[0] + o.s[1]) + (o.s[2] + o.s[3])) + ((o.s[4] + o.s[5]) + (o.s[6] + o.s[7])));
+    // sums over i >= l, and over i < l: what is left of a whole in 64 bits
+    const float z = v * sc[2 * SC + l];
+    const double xs = wave_scan((double)x), zs = wave_scan((double)z);
+    const float slope = (float)((lane_of(xs, WAVE - 1) - xs + (double)x) + (zs - (double)z));
     if (l < n) {
-      // in the io type like every gradient of this operator, though dt and g are fp32; a decay of zero has no slope
-      static_cast<S*>(a.dg)[at] = float_to_io<S>(g < SCAN_MIN_G ? 0.f : x + z);
+      // in the io type like every gradient of this operator, though dt and g are fp32
+      static_cast<S*>(a.dg)[at] = float_to_io<S>(sc[5 * SC + l] != 0.f ? slope : 0.f);
       static_cast<S*>(a.ddt)[at] = float_to_io<S>((o.i[0][l] + o.i[1][l]) + v);
     }
     if (l == 0) a.part_d[(size_t)slot * a.H + head0 + hd] = o.d[0] + o.d[1];
@@ -151,21 +149,16 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   f32x16 dB = zero16(), dC = zero16(), W = zero16(), ka = zero16(), kb = zero16();
   stage(0);
   sync_tiles();
-  auto products = [&](f32x16& to, int tile) {
+  auto products = [&](f32x16& to, int i, int j) {
 #pragma unroll
-    for (int s = 0; s < N / 16; ++s) mma32(to, RT::row(LC, 32 * tile + c, s, h), RT::row(LB, tok, s, h));
+    for (int s = 0; s < N / 16; ++s) mma32(to, RT::row(LC, 32 * i + c, s, h), RT::row(LB, 32 * j + c, s, h));
   };
   if (w >= 4) {
-    products(ka, ti);
+    products(ka, ti, tj);
   } else {
-    if (tj == 0) products(ka, 0);
-    products(kb, 1);
+    if (tx == 0) products(ka, 0, tx);
+    products(kb, 1, tx);
   }
-  // the operands of a phase are not read before the one before it is done: registers
-  auto phase = [&]() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-  };
   float di = 0.f, dv = 0.f, dr = 0.f, ss = 0.f;
   for (int it = 0; it < items; ++it) {
     const int hd = it / nb, head = head0 + hd, pb = it % nb;
@@ -190,7 +183,6 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         if (hd + 2 < hpp) fetch(hd + 2);
       }
     }
-    const float eg = sc[3 * SC + tok], dt = sc[2 * SC + tok], vj = sc[4 * SC + tok];
     if (pb == 0) {
       if (w >= 4) kb = zero16();
       di = dv = dr = ss = 0.f;
@@ -206,9 +198,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         for (int j = 0; j < 8; ++j) dr = __builtin_fmaf(cr.get(j), u[8 * s + j], dr);
       }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) dC[e] = __builtin_fmaf(u[e], eg, dC[e]);
+      for (int e = 0; e < 16; ++e) dC[e] = __builtin_fmaf(u[e], sc[3 * SC + tok], dC[e]);
     }
-    phase();
     if (ONE) {
       sync_lds();
       stage_linear<ROWS / 1024, 8>(LD, static_cast<const S*>(a.dst) + state_at(it), w);
@@ -229,53 +220,51 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         }
       }
     }
-    phase();
     if (has_n) {   // dt v dS x
       f32x16 u = zero16();
 #pragma unroll
       for (int s = 0; s < 4; ++s) mma32(u, ST::colp(LD, 16 * s + 8 * h, n0, x), XT::row(LX, tok, s, h));
-      const float dtv = dt * vj;
+      const float dtv = sc[2 * SC + tok] * sc[4 * SC + tok];
 #pragma unroll
       for (int e = 0; e < 16; ++e) dB[e] = __builtin_fmaf(u[e], dtv, dB[e]);
     }
-    phase();
-    // e^{L_i - L_j} of a tile of i, its element 4 q + e
-    const bool product = sc[5 * SC] != 0.f;
-    const float hj = sc[(product ? SC : 0) + tok], lj = sc[SC + tok];
-    auto decay_to = [&](f32x4& f, int tile, int q, float bj) {
+    // e^{L_i - L_j} from a token (its own factor, or L) to a tile of i, its elements 4 q ..
+    const bool product = sc[6 * SC] != 0.f;
+    auto decay_to = [&](f32x4& f, int tile, int q, float hj, float lj) {
       const f32x4 hi = *reinterpret_cast<const f32x4*>(sc + 32 * tile + 8 * q + 4 * h);
       if (product) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = hi[e] * bj;
+        for (int e = 0; e < 4; ++e) f[e] = hi[e] * hj;
       } else {
         const f32x4 lo = *reinterpret_cast<const f32x4*>(sc + SC + 32 * tile + 8 * q + 4 * h);
 #pragma unroll
         for (int e = 0; e < 4; ++e) f[e] = decay<BF>(hi[e], lo[e], hj, lj);
       }
     };
+    auto own = [&](int at, bool next) { return sc[(product ? SC : 0) + at] * (product && next ? sc[6 * SC + 1] : 1.f); };
     if (w < 4) {   // dx of 32 of the block's columns
-      const int p0 = 32 * (w / 2);
+      const int p0 = 32 * (w % 2), tok = 32 * tx + c;
+      const float dt = sc[2 * SC + tok], vj = sc[4 * SC + tok], lj = sc[SC + tok];
       f32x16 xa = zero16(), xv = zero16();
 #pragma unroll
       for (int s = 0; s < N / 16; ++s) mma32(xv, ST::row(LD, p0, s, x), RT::row(LB, tok, s, h));
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        if (i >= tj) {
+        if (i >= tx) {
           f32x16 q;
-          const float bj = i > tj ? hj * sc[5 * SC + 1] : hj;
+          const float hj = own(tok, i > tx);
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
             f32x4 f;
-            decay_to(f, i, b, bj);
+            decay_to(f, i, b, hj, lj);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) q[4 * b + e] = i > tj || 8 * b + 4 * h + e >= c ? (i == 0 ? ka[4 * b + e] : kb[4 * b + e]) * f[e] : 0.f;
+            for (int e = 0; e < 4; ++e) q[4 * b + e] = i > tx || 8 * b + 4 * h + e >= c ? (i == 0 ? ka[4 * b + e] : kb[4 * b + e]) * f[e] : 0.f;
           }
 #pragma unroll
           for (int s = 0; s < 2; ++s)
             mma32(xa, XT::colp(LY, 32 * i + 16 * s + 4 * h, 32 * i + 16 * s + 8 + 4 * h, p0, x), frag_of<T>(q, s));
         }
-      phase();
-      const float Dh = a.D ? a.D[head] : 0.f;
+        const float Dh = a.D ? a.D[head] : 0.f;
       const auto rx = row_window(static_cast<S*>(a.dX) + (size_t)head * a.P + pb * 64 + p0, row0, a.dxs, n, 32);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -303,21 +292,20 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         di = half_sum(di);
         dv = half_sum(dv);
         if (h == 0) {
-          o.i[w / 2][tok] = di;
-          o.v[w / 2][tok] = dv;
+          o.i[w % 2][tok] = di;
+          o.v[w % 2][tok] = dv;
         }
       }
     } else if (w < 7) {   // M, and the sums of Z
 #pragma unroll
       for (int s = 0; s < 4; ++s) mma32(kb, XT::row(LY, 32 * ti + c, s, h), XT::row(LX, tok, s, h));
       if (pb == nb - 1) {
-        float dd = 0.f, cz = 0.f;
-        f32x16 z;
-        const float bj = ti > tj ? hj * sc[5 * SC + 1] : hj;
+        const float dt = sc[2 * SC + tok], hj = own(tok, ti > tj), lj = sc[SC + tok];
+        float dd = 0.f, cz = 0.f, z[16];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           f32x4 f;
-          decay_to(f, ti, b, bj);
+          decay_to(f, ti, b, hj, lj);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int y = 4 * b + e, i = 8 * b + 4 * h + e;   // of the tile
@@ -328,10 +316,15 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
             cz += z[y];
           }
         }
+        // sums over a row of 16 lanes of each element: a lane keeps the elements of its place in four, then four each
+        float s8[8], s4[4];
 #pragma unroll
-        for (int y = 0; y < 16; ++y) {
-          const float r = lane_sum<16>(z[y]);
-          if (l % 16 == 0) o.row[tj][(l / 16) & 1][32 * ti + res_row(y, h)] = r;
+        for (int y = 0; y < 8; ++y) s8[y] = (x & 1 ? z[2 * y + 1] : z[2 * y]) + lane_xor<1>(x & 1 ? z[2 * y] : z[2 * y + 1]);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          s4[y] = (x & 2 ? s8[2 * y + 1] : s8[2 * y]) + lane_xor<2>(x & 2 ? s8[2 * y] : s8[2 * y + 1]);
+          s4[y] = row_sum4(s4[y]);
+          if (x % 16 < 4) o.row[tj][(x / 16) & 1][32 * ti + 8 * y + 4 * h + x % 4] = s4[y];
         }
         cz = half_sum(cz);
         if (h == 0) o.col[ti][tok] = cz;
