@@ -212,7 +212,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         if constexpr (BF) {
           const bf16x8 u = *reinterpret_cast<const bf16x8*>(LS + 16 * i), v = *reinterpret_cast<const bf16x8*>(LD + 16 * i);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) ss = __builtin_fmaf((float)u[j], (float)v[j], ss);
+          for (int j = 0; j < 8; j += 2)
+            ss = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{u[j], u[j + 1]}, bf16x2{v[j], v[j + 1]}, ss, false);
         } else {
           const f32x4 u = *reinterpret_cast<const f32x4*>(LS + 16 * i), v = *reinterpret_cast<const f32x4*>(LD + 16 * i);
 #pragma unroll
@@ -392,14 +393,15 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   store(dC, a.part_c, a.dC, a.dcs);
 }
 
-// dB and dC from the parts of the heads, in order: a workgroup has rows of a chunk, a thread four values.
+// dB and dC from the parts of the heads, in order: a workgroup has PART_ROWS rows of a chunk, a thread four values.
+constexpr int PART_ROWS = 8;
 template <class S>
 __global__ __launch_bounds__(256) void k_scan_parts(ScanArgs a) {
-  const int slots = seq_slots(a.T, a.B, SC), slot = blockIdx.x;
+  const int slots = seq_slots(a.T, a.B, SC), slot = blockIdx.x / (SC / PART_ROWS), r0 = blockIdx.x % (SC / PART_ROWS) * PART_ROWS;
   const SeqTile t = find_tile<SC>(a.off, a.B, a.T, slot);
   if (t.b < 0) return;
   const int n = min(SC, t.n - t.tile * SC), row0 = t.row0 + t.tile * SC, width = a.G * a.N;
-  for (int i = threadIdx.x * 4; i < n * width; i += 1024) {
+  for (int i = r0 * width + threadIdx.x * 4; i < min(n, r0 + PART_ROWS) * width; i += 1024) {
     const int r = i / width, col = i % width;
     f32x4 b = zero4(), c = zero4();
     for (int p = 0; p < a.parts; ++p) {
@@ -432,7 +434,7 @@ template <class T, int N>
 void grad(const ScanArgs& a, hipStream_t st) {
   const int slots = seq_slots(a.T, a.B, SC);
   k_scan_grad<T, N><<<(slots + NUM_XCD - 1) / NUM_XCD * NUM_XCD * a.G * a.parts, 512, 0, st>>>(a);
-  if (a.part_b) k_scan_parts<typename Io<T>::type><<<slots, 256, 0, st>>>(a);
+  if (a.part_b) k_scan_parts<typename Io<T>::type><<<slots * (SC / PART_ROWS), 256, 0, st>>>(a);
 }
 }  // namespace
 
