@@ -116,6 +116,11 @@ __device__ __forceinline__ void stage_rows(const char* L, const typename Io<T>::
                             stride * (int)sizeof(T), 0, l);
 }
 
+// x where bit e of a lane's mask is set, else 0: a comparison into vcc and a selection by it take three times as long
+__device__ __forceinline__ float keep_if(float x, unsigned mask, int e) {
+  return __uint_as_float(__float_as_uint(x) & (unsigned)((int)(mask << (31 - e)) >> 31));
+}
+
 // the value of lane l ^ M, M 1 or 2
 template <int M>
 __device__ __forceinline__ float lane_xor(float x) {
@@ -174,6 +179,41 @@ struct Decay {
 template <bool ONE>
 __device__ __forceinline__ float decay(float hi_i, float lo_i, float hi_j, float lo_j) {
   return __builtin_amdgcn_exp2f(ONE ? hi_i - hi_j : (hi_i - hi_j) + (lo_i - lo_j));
+}
+
+// Stores 32 tokens of 32 columns from results of permuted rows (a lane per token, element e the column perm_row(e, h)):
+// o(s, j) the lane's values 8 s + j.  Of bf16 rows the lanes trade places first, so that a store
+// has whole rows of 64 bytes and not halves of twice as many.
+template <class T, class F>
+__device__ __forceinline__ void store_rows(__amdgpu_buffer_rsrc_t rs, int tok0, int stride, F o) {
+  const int l = threadIdx.x % WAVE;
+  if constexpr (IsBf16<T>::value) {
+    u32x4 v[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      Frag<T> f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f.set(j, o(s, j));
+      v[s] = __builtin_bit_cast(u32x4, f.v);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {   // lanes 16 .. 31 (48 .. 63) of the first with 0 .. 15 (32 .. 47) of the second
+      const auto p = __builtin_amdgcn_permlane16_swap(v[0][k], v[1][k], false, false);
+      v[0][k] = p[0];
+      v[1][k] = p[1];
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      __builtin_amdgcn_raw_buffer_store_b128(v[k], rs, (tok0 + 16 * k + l % 16) * stride * 2 + (l / 16 % 2) * 32 + l / 32 * 16, 0, 0);
+  } else {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        __builtin_amdgcn_raw_buffer_store_b128(
+            __builtin_bit_cast(u32x4, f32x4{o(s, 4 * k), o(s, 4 * k + 1), o(s, 4 * k + 2), o(s, 4 * k + 3)}), rs,
+            (tok0 + l % 32) * stride * 4 + 64 * s + 32 * (l / 32) + 16 * k, 0, 0);
+  }
 }
 
 // The work of a workgroup of a sweep: a segment of a sequence (tokens t0 .. of it) and a set of heads of one group.

@@ -159,6 +159,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     if (tx == 0) products(ka, 0, tx);
     products(kb, 1, tx);
   }
+  unsigned from_on = 0, behind = 0;   // of a tile on the diagonal, the elements i from this lane's j on, and behind it
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    from_on |= res_row(e, h) >= c ? 1u << e : 0u;
+    behind |= res_row(e, h) > c ? 1u << e : 0u;
+  }
   float di = 0.f, dv = 0.f, dr = 0.f, ss = 0.f;
   for (int it = 0; it < items; ++it) {
     const int hd = it / nb, head = head0 + hd, pb = it % nb;
@@ -175,7 +181,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     const char* LS = LY + XROWS;
     const char* LD = ONE ? LS : LS + ROWS;
     const float* sc = scal[hd & 1];
-    Dots& o = dots[hd & 1];
+    Dots& left = dots[hd & 1];
     if (w == 7 && pb == 0) {
       if (hd > 0) put_out(hd - 1);
       if (hd + 1 < hpp) {   // its place was the head's before, which is put out
@@ -254,12 +260,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         if (i >= tx) {
           f32x16 q;
           const float hj = own(tok, i > tx);
+          const unsigned seen = i > tx ? ~0u : from_on;
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
             f32x4 f;
             decay_to(f, i, b, hj, lj);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) q[4 * b + e] = i > tx || 8 * b + 4 * h + e >= c ? (i == 0 ? ka[4 * b + e] : kb[4 * b + e]) * f[e] : 0.f;
+            for (int e = 0; e < 4; ++e) q[4 * b + e] = keep_if((i == 0 ? ka[4 * b + e] : kb[4 * b + e]) * f[e], seen, 4 * b + e);
           }
 #pragma unroll
           for (int s = 0; s < 2; ++s)
@@ -267,34 +274,25 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         }
         const float Dh = a.D ? a.D[head] : 0.f;
       const auto rx = row_window(static_cast<S*>(a.dX) + (size_t)head * a.P + pb * 64 + p0, row0, a.dxs, n, 32);
+      float o[2][8];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const Frag<T> xr = XT::row(LX, tok, p0 / 16 + s, h), yr = XT::row(LY, tok, p0 / 16 + s, h);
-        const int at = (tok * a.dxs + 16 * s + 8 * h) * (int)sizeof(S);
-        float v8[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float p = xa[8 * s + j], v = vj * xv[8 * s + j];
           di = __builtin_fmaf(p, xr.get(j), di);
           dv = __builtin_fmaf(v, xr.get(j), dv);
-          v8[j] = __builtin_fmaf(dt, p + v, Dh * yr.get(j));
-        }
-        if constexpr (BF) {
-          Frag<T> f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f.set(j, v8[j]);
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f.v), rx, at, 0, 0);
-        } else {
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v8[0], v8[1], v8[2], v8[3]}), rx, at, 0, 0);
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v8[4], v8[5], v8[6], v8[7]}), rx, at + 16, 0, 0);
+          o[s][j] = __builtin_fmaf(dt, p + v, Dh * yr.get(j));
         }
       }
+      store_rows<T>(rx, 32 * tx, a.dxs, [&](int s, int j) { return o[s][j]; });
       if (pb == nb - 1) {
         di = half_sum(di);
         dv = half_sum(dv);
         if (h == 0) {
-          o.i[w % 2][tok] = di;
-          o.v[w % 2][tok] = dv;
+          left.i[w % 2][tok] = di;
+          left.v[w % 2][tok] = dv;
         }
       }
     } else if (w < 7) {   // M, and the sums of Z
@@ -302,6 +300,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
       for (int s = 0; s < 4; ++s) mma32(kb, XT::row(LY, 32 * ti + c, s, h), XT::row(LX, tok, s, h));
       if (pb == nb - 1) {
         const float dt = sc[2 * SC + tok], hj = own(tok, ti > tj), lj = sc[SC + tok];
+        const unsigned seen = ti > tj ? ~0u : from_on, at_tok = ti > tj ? 0u : from_on & ~behind;
         float dd = 0.f, cz = 0.f, z[16];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
@@ -309,11 +308,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
           decay_to(f, ti, b, hj, lj);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int y = 4 * b + e, i = 8 * b + 4 * h + e;   // of the tile
-            if (ti == tj && i == c) dd = kb[y];
-            const float m = ti > tj || i >= c ? kb[y] * f[e] * dt : 0.f;
+            const int y = 4 * b + e;
+            dd += keep_if(kb[y], at_tok, y);
+            const float m = keep_if(kb[y] * f[e] * dt, seen, y);
             W[y] += m;
-            z[y] = ti > tj || i > c ? m * ka[y] : 0.f;
+            z[y] = keep_if(m * ka[y], seen & ~at_tok, y);
             cz += z[y];
           }
         }
@@ -325,21 +324,21 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         for (int y = 0; y < 4; ++y) {
           s4[y] = (x & 2 ? s8[2 * y + 1] : s8[2 * y]) + lane_xor<2>(x & 2 ? s8[2 * y] : s8[2 * y + 1]);
           s4[y] = row_sum4(s4[y]);
-          if (x % 16 < 4) o.row[tj][(x / 16) & 1][32 * ti + 8 * y + 4 * h + x % 4] = s4[y];
+          if (x % 16 < 4) left.row[tj][(x / 16) & 1][32 * ti + 8 * y + 4 * h + x % 4] = s4[y];
         }
         cz = half_sum(cz);
-        if (h == 0) o.col[ti][tok] = cz;
+        if (h == 0) left.col[ti][tok] = cz;
         dd = group_sum_swap(lane_sum<16>(dd));
-        if (l == 0 && ti == tj) o.d[ti] = dd;
+        if (l == 0 && ti == tj) left.d[ti] = dd;
       }
     }
     if (pb == nb - 1) {
       if (has_n) {
         dr = half_sum(dr);
-        if (h == 0) o.r[n0 / 32][tok] = dr;
+        if (h == 0) left.r[n0 / 32][tok] = dr;
       }
       ss = group_sum_swap(lane_sum<16>(ss));
-      if (l == 0) o.s[w] = ss;
+      if (l == 0) left.s[w] = ss;
     }
   }
   sync_lds();

@@ -16,19 +16,19 @@ enum {
 
 // c += a x for operands a that are exact and fp32 values x, as three bf16 terms (24 bits) or as they are.
 // Two terms leave 2^-18 of each product: 1.5e-6 of a state, where fp32 sums leave 1e-7.
+// By cutting bits off: each term takes the eight leading ones that are left, the third what remains.
 __device__ __forceinline__ void split3(Frag<__bf16> (&t)[3], const float (&x)[8]) {
 #pragma clang fp contract(off)
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
   u32x4 w[3];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {   // pairs: one conversion instruction each
-    f32x2 v = {x[2 * j], x[2 * j + 1]};
+  for (int j = 0; j < 4; ++j) {
+    unsigned u = __float_as_uint(x[2 * j]), v = __float_as_uint(x[2 * j + 1]);
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-      const unsigned u = __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
-      w[k][j] = u;
-      v[0] -= __uint_as_float(u << 16);
-      v[1] -= __uint_as_float(u & 0xffff0000u);
+      w[k][j] = __builtin_amdgcn_perm(v, u, 0x07060302);   // the upper halves
+      if (k == 2) break;
+      u = __float_as_uint(__uint_as_float(u) - __uint_as_float(u & 0xffff0000u));
+      v = __float_as_uint(__uint_as_float(v) - __uint_as_float(v & 0xffff0000u));
     }
   }
 #pragma unroll
@@ -252,6 +252,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 #pragma unroll
     for (int s = 0; s < NS; ++s) StateRows<T, N>::store(p, s, f[s]);
   };
+  unsigned up_to = 0;   // of a tile on the diagonal, the elements j up to this lane's i
+#pragma unroll
+  for (int e = 0; e < 16; ++e) up_to |= res_row(e, l / 32) <= l % 32 ? 1u << e : 0u;
   auto state_frags = [&](Frag<T> (&f)[NS]) {
 #pragma unroll
     for (int s = 0; s < NS; ++s) f[s] = frag_of<T>(st[s / 2], s % 2);
@@ -378,7 +381,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float v = cb[j][4 * q + e] * f[e];
-              cb[j][4 * q + e] = j < i || t + e <= 32 * i + c ? v : 0.f;
+              cb[j][4 * q + e] = j < i ? v : keep_if(v, up_to, 4 * q + e);
             }
           }
 #pragma unroll
@@ -389,23 +392,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
           for (int e = 0; e < 16; ++e)
             if (32 * i + c >= __shfl(fb, 8 * (e / 4) + 4 * h + e % 4)) y[e] = NAN;
         }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const Frag<T> xr = XT::row(LX, 32 * i + c, s, h);
-          const int at = ((32 * i + c) * ys + 16 * s + 8 * h) * (int)sizeof(S);
-          float v[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf(Dh, xr.get(j), y[8 * s + j]);
-          if constexpr (BF) {
-            Frag<T> o;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o.set(j, v[j]);
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o.v), ry, at, 0, 0);
-          } else {
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]}), ry, at, 0, 0);
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]}), ry, at + 16, 0, 0);
-          }
-        }
+        const Frag<T> xr[2] = {XT::row(LX, 32 * i + c, 0, h), XT::row(LX, 32 * i + c, 1, h)};
+        store_rows<T>(ry, 32 * i, ys, [&](int s, int j) { return __builtin_fmaf(Dh, xr[s].get(j), y[8 * s + j]); });
         asm volatile("" ::: "memory");   // the second half's operands are not read before the first half is done
       }
     };
