@@ -235,23 +235,29 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 #pragma unroll
       for (int e = 0; e < 16; ++e) dB[e] = __builtin_fmaf(u[e], dtv, dB[e]);
     }
-    // e^{L_i - L_j} from a token (its own factor, or L) to a tile of i, its elements 4 q ..
+    // use(q, f) with the decays f = e^{L_i - L_j} of the elements 4 q .. of a tile of i, from the token j = at
     const bool product = sc[6 * SC] != 0.f;
-    auto decay_to = [&](f32x4& f, int tile, int q, float hj, float lj) {
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(sc + 32 * tile + 8 * q + 4 * h);
+    auto decays_to = [&](int tile, int at, bool next, auto use) {
+      const float* si = sc + 32 * tile + 4 * h;
       if (product) {
+        const float bj = sc[SC + at] * (next ? sc[6 * SC + 1] : 1.f);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = hi[e] * hj;
+        for (int q = 0; q < 4; ++q) use(q, *reinterpret_cast<const f32x4*>(si + 8 * q) * bj);
       } else {
-        const f32x4 lo = *reinterpret_cast<const f32x4*>(sc + SC + 32 * tile + 8 * q + 4 * h);
+        const float hj = sc[at], lj = sc[SC + at];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = decay<BF>(hi[e], lo[e], hj, lj);
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 hi = *reinterpret_cast<const f32x4*>(si + 8 * q), lo = *reinterpret_cast<const f32x4*>(si + SC + 8 * q);
+          f32x4 f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[e] = decay<BF>(hi[e], lo[e], hj, lj);
+          use(q, f);
+        }
       }
     };
-    auto own = [&](int at, bool next) { return sc[(product ? SC : 0) + at] * (product && next ? sc[6 * SC + 1] : 1.f); };
     if (w < 4) {   // dx of 32 of the block's columns
       const int p0 = 32 * (w % 2), tok = 32 * tx + c;
-      const float dt = sc[2 * SC + tok], vj = sc[4 * SC + tok], lj = sc[SC + tok];
+      const float dt = sc[2 * SC + tok], vj = sc[4 * SC + tok];
       f32x16 xa = zero16(), xv = zero16();
 #pragma unroll
       for (int s = 0; s < N / 16; ++s) mma32(xv, ST::row(LD, p0, s, x), RT::row(LB, tok, s, h));
@@ -259,15 +265,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
       for (int i = 0; i < 2; ++i)
         if (i >= tx) {
           f32x16 q;
-          const float hj = own(tok, i > tx);
           const unsigned seen = i > tx ? ~0u : from_on;
-#pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            f32x4 f;
-            decay_to(f, i, b, hj, lj);
+          decays_to(i, tok, i > tx, [&](int b, const f32x4& f) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) q[4 * b + e] = keep_if((i == 0 ? ka[4 * b + e] : kb[4 * b + e]) * f[e], seen, 4 * b + e);
-          }
+          });
 #pragma unroll
           for (int s = 0; s < 2; ++s)
             mma32(xa, XT::colp(LY, 32 * i + 16 * s + 4 * h, 32 * i + 16 * s + 8 + 4 * h, p0, x), frag_of<T>(q, s));
@@ -299,13 +301,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 #pragma unroll
       for (int s = 0; s < 4; ++s) mma32(kb, XT::row(LY, 32 * ti + c, s, h), XT::row(LX, tok, s, h));
       if (pb == nb - 1) {
-        const float dt = sc[2 * SC + tok], hj = own(tok, ti > tj), lj = sc[SC + tok];
+        const float dt = sc[2 * SC + tok];
         const unsigned seen = ti > tj ? ~0u : from_on, at_tok = ti > tj ? 0u : from_on & ~behind;
         float dd = 0.f, cz = 0.f, z[16];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          f32x4 f;
-          decay_to(f, ti, b, hj, lj);
+        decays_to(ti, tok, ti > tj, [&](int b, const f32x4& f) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int y = 4 * b + e;
@@ -315,7 +314,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
             z[y] = keep_if(m * ka[y], seen & ~at_tok, y);
             cz += z[y];
           }
-        }
+        });
         // sums over a row of 16 lanes of each element: a lane keeps the elements of its place in four, then four each
         float s8[8], s4[4];
 #pragma unroll

@@ -284,8 +284,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     if (Y) {
       sc[l] = d.from_start();
       sc[SC + l] = d.to_end() * dn;
-      // e^{L_i - L_j} as a product of what lies between a token and its half's middle, where that is far from any
-      // overflow; fp32 rows take the exponential of each difference, whose argument has a smaller error
+      // e^{L_i - L_j} as a product of what lies between each token and its half's middle, and between the middles, where
+      // the former are within 2^50: the latter then is a float's where e^{L_i - L_j} of any two tokens is above
+      // 2^-26.  Fp32 rows take the exponential of each difference, whose argument has a smaller error.
       const double m0 = lane_of(d.L, 15), m1 = lane_of(d.L, 47);
       const float from = (float)(d.L - (l < 32 ? m0 : m1));
       product = BF && __all(fabsf(from) < 50.f);
@@ -358,35 +359,44 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 #pragma unroll
           for (int j = 0; j <= i; ++j) mma32(cb[j], RT::row(L, 32 * j + c, s, h), cr);
         }
-        const float eg = sc[32 * i + c], ai = sc[2 * SC + 32 * i + c], lo = sc[3 * SC + 32 * i + c];
+        const float eg = sc[32 * i + c];
 #pragma unroll
         for (int e = 0; e < 16; ++e) y[e] *= eg;
+        // P from C B^T, factor(j, q) the decays (times dt) of the elements 4 q .. of the tile of j
+        auto matrix = [&](auto factor) {
 #pragma unroll
-        for (int j = 0; j <= i; ++j) {
-          const float aij = j < i ? ai * both : ai;
+          for (int j = 0; j <= i; ++j)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
+            for (int q = 0; q < 4; ++q) {
+              const f32x4 f = factor(j, q);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float v = cb[j][4 * q + e] * f[e];
+                cb[j][4 * q + e] = j < i ? v : keep_if(v, up_to, 4 * q + e);
+              }
+            }
+        };
+        const float ai = sc[2 * SC + 32 * i + c];
+        if (product) {
+          matrix([&](int j, int q) {
+            return *reinterpret_cast<const f32x4*>(sc + 3 * SC + 32 * j + 8 * q + 4 * h) * (j < i ? ai * both : ai);
+          });
+        } else {
+          const float lo = BF ? 0.f : sc[3 * SC + 32 * i + c];
+          matrix([&](int j, int q) {
             const int t = 32 * j + 8 * q + 4 * h;
-            const f32x4 hj = *reinterpret_cast<const f32x4*>(sc + (product ? 3 * SC : 2 * SC) + t);
+            const f32x4 hj = *reinterpret_cast<const f32x4*>(sc + 2 * SC + t), dj = *reinterpret_cast<const f32x4*>(sc + 4 * SC + t);
+            const f32x4 lj = BF ? zero4() : *reinterpret_cast<const f32x4*>(sc + 3 * SC + t);
             f32x4 f;
-            if (product) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) f[e] = aij * hj[e];
-            } else {
-              const f32x4 dj = *reinterpret_cast<const f32x4*>(sc + 4 * SC + t);
-              const f32x4 lj = BF ? zero4() : *reinterpret_cast<const f32x4*>(sc + 3 * SC + t);
+            for (int e = 0; e < 4; ++e) f[e] = decay<BF>(ai, lo, hj[e], lj[e]) * dj[e];
+            return f;
+          });
+        }
 #pragma unroll
-              for (int e = 0; e < 4; ++e) f[e] = decay<BF>(ai, lo, hj[e], lj[e]) * dj[e];
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float v = cb[j][4 * q + e] * f[e];
-              cb[j][4 * q + e] = j < i ? v : keep_if(v, up_to, 4 * q + e);
-            }
-          }
+        for (int j = 0; j <= i; ++j)
 #pragma unroll
           for (int s = 0; s < 2; ++s) mma32(y, xf[2 * j + s], frag_of<T>(cb[j], s));
-        }
         if (any_bad) {
 #pragma unroll
           for (int e = 0; e < 16; ++e)

@@ -167,6 +167,29 @@ def test_heads_that_forget_at_once(F, dtype):
             near((n, h), grads[n][:, h], ref[n][:, h], NORM[dtype]["grad"])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rate", [1.0, 1.7, 2.4, 3.0, 4.5])
+def test_decays_of_a_chunk_over_many_powers_of_two(F, rate, dtype):
+    """Decays whose sums over a chunk run from 2^-92 to 2^-415, even and with a quiet stretch across its middle, each
+    token by itself against its neighbours: what lies between two tokens is the same however far both have come."""
+    x = scan_inputs([64, 200], 1, 2, 64, 64, dtype, 16)
+    x["g"] = -rate * (0.9 + 0.2 * torch.rand(x["g"].shape, generator=torch.Generator().manual_seed(2)))
+    x["g"][[30, 31, 32, 33, 95, 96]] = -0.01
+    ref = scan_oracle(x, False, grads=True)
+    t, args, desc, _ = run_fwd(F, x, dtype, False)
+    saved = torch.empty(F.scan_saved_size(desc), dtype=torch.uint8, device="cuda")
+    Y, state = F.flex_scan_fwd(desc, *args, saved=saved, want_state=True)
+    near("state", state, ref["state"], NORM[dtype]["state"])
+    grads = F.flex_scan_bwd(desc, *args, t["dY"], saved)
+    for i in range(0, len(x["X"]), 8):
+        at = slice(i, i + 8)
+        near(("Y", i), Y[at], ref["Y"][at], NORM[dtype]["Y"])
+        for n in ("dX", "dB", "dC"):
+            near((n, i), grads[n][at], ref[n][at], NORM[dtype]["grad"])
+    for n in ("ddt", "dg"):
+        near(n, grads[n], ref[n], NORM[dtype]["grad"])
+
+
 def test_backward_against_differences(F):
     """<gradient, r> against the change of sum(dY Y) along r, by the float64 recurrence: within the gradient's
     tolerance times both norms, and the difference's own error, step^2 = 1e-10 of derivatives of the gradient's size."""
