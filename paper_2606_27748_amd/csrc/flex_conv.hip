@@ -14,9 +14,8 @@ namespace flex {
 
 namespace {
 // a lane's channels' taps and bias
-template <class S, int K>
+template <int E, int K>
 struct Taps {
-  static constexpr int E = Piece<S>::N;
   float w[E * K], bias[E];
   __device__ __forceinline__ void load(const ConvArgs& a, int c) {
 #pragma unroll
@@ -37,12 +36,12 @@ struct Taps {
 };
 
 // the K-1 rows before row t of a sequence
-template <class S, int K>
-__device__ __forceinline__ void window(float (&win)[K - 1][Piece<S>::N], const ConvArgs& a, const RowSeq& q, int t, int c) {
+template <class S, int K, int E>
+__device__ __forceinline__ void window(float (&win)[K - 1][E], const ConvArgs& a, const RowSeq& q, int t, int c) {
 #pragma unroll
   for (int k = 0; k < K - 1; ++k) {
     const int r = t - (K - 1) + k;
-    Piece<S> p;
+    Piece<S, E * (int)sizeof(S)> p;
     p.zero();
     if (r >= q.first)
       p.load(static_cast<const S*>(a.X) + (size_t)r * a.xs + c);
@@ -78,7 +77,7 @@ __device__ __forceinline__ void last_rows(const ConvArgs& a, int b, int c) {
   }
 #pragma unroll
   for (int k = 0; k < K - 1; ++k)
-    *reinterpret_cast<uint4*>(static_cast<S*>(a.state) + ((size_t)b * (K - 1) + k) * a.D + c) = p[k].raw;
+    p[k].save(static_cast<S*>(a.state) + ((size_t)b * (K - 1) + k) * a.D + c);
 }
 }  // namespace
 
@@ -100,7 +99,7 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a, int spans, int til
   Piece<S> next[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) next[u].load(X + (size_t)min(r0 + u, r1 - 1) * a.xs);
-  Taps<S, K> taps;
+  Taps<E, K> taps;
   taps.load(a, cc);
   RowSeq q = find_row(a.off, a.B, a.T, r0);
   float win[K - 1][E] = {};
@@ -112,6 +111,29 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a, int spans, int til
     if (t0 + U < r1) {
 #pragma unroll
       for (int u = 0; u < U; ++u) next[u].load(X + (size_t)min(t0 + U + u, r1 - 1) * a.xs);
+    }
+    if (q.b >= 0 && t0 + U <= min(q.end, r1)) {   // rows of one sequence: no row's window is moved, but named
+      float x[U][E];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float z[E], before[K - 1][E];
+        cur[u].get(x[u]);
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+          for (int i = 0; i < E; ++i) before[k][i] = u + k < K - 1 ? win[u + k < K - 1 ? u + k : 0][i] : x[u + k < K - 1 ? 0 : u + k - (K - 1)][i];
+        taps.conv(z, before, x[u]);
+        if (SILU) {
+#pragma unroll
+          for (int i = 0; i < E; ++i) z[i] *= sigmoid(z[i]);
+        }
+        if (in) Piece<S>::store(static_cast<S*>(a.Y) + (size_t)(t0 + u) * a.D + c, z);
+      }
+#pragma unroll
+      for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+        for (int i = 0; i < E; ++i) win[k][i] = x[U - (K - 1) + k][i];
+      continue;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -139,10 +161,12 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a, int spans, int til
 
 // As the forward, over CONV_BWD_ROWS rows and the K-1 behind them, whose dz the last rows' dx take: at row
 // t, dz_t is formed and dx of row t - (K-1) is complete.  A workgroup's waves have consecutive rows and
-// leave one row of partial sums of dW and dbias.
+// leave one row of partial sums of dW and dbias.  Four channels a lane: with eight, their windows and sums leave a SIMD
+// one wave (143 us for 2 x 8192 rows of 4352 channels).
 template <class S, int K, bool SILU>
 __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
-  constexpr int E = Piece<S>::N, U = 4;
+  constexpr int E = 4, U = 4;
+  using P = Piece<S, E * (int)sizeof(S)>;
   __shared__ float sums[CONV_BWD_WAVES - 1][(K + 1) * E][WAVE];
   const int l = threadIdx.x % WAVE, w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
   const int part = blockIdx.x / spans, c = (blockIdx.x % spans * WAVE + l) * E;
@@ -153,7 +177,7 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
   const S* G = static_cast<const S*>(a.dY) + cc;
   float dw[K][E] = {}, db[E] = {};
   if (r0 < r1) {
-    Taps<S, K> taps;
+    Taps<E, K> taps;
     taps.load(a, cc);
     for (int t0 = r0; t0 < r1;) {   // a sequence's rows at a time
       const RowSeq q = find_row(a.off, a.B, a.T, t0);
@@ -164,7 +188,7 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
       const int e = min(q.end, r1), stop = e + K - 1;   // dx of rows t0 .. e-1
       float win[K - 1][E], dzw[K - 1][E] = {};
       window<S, K>(win, a, q, t0, cc);
-      Piece<S> nx[U], ng[U];
+      P nx[U], ng[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const size_t r = min(t0 + u, q.end - 1);
@@ -172,7 +196,7 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
         ng[u].load(G + r * a.D);
       }
       for (int tb = t0; tb < stop; tb += U) {
-        Piece<S> px[U], pg[U];
+        P px[U], pg[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           px[u] = nx[u];
@@ -185,6 +209,48 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
             nx[u].load(X + r * a.xs);
             ng[u].load(G + r * a.D);
           }
+        }
+        if (tb > t0 && tb + U <= e) {   // every row's dz counts here, and every row's dx is one of the tile's
+          static_assert(U >= K - 1, "dx of the rows before the batch");
+          float x[U][E], dz[U][E];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            px[u].get(x[u]);
+            pg[u].get(dz[u]);
+            float before[K - 1][E], z[E], dx[E];
+#pragma unroll
+            for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+              for (int i = 0; i < E; ++i) before[k][i] = u + k < K - 1 ? win[u + k < K - 1 ? u + k : 0][i] : x[u + k < K - 1 ? 0 : u + k - (K - 1)][i];
+            if (SILU) {
+              taps.conv(z, before, x[u]);
+#pragma unroll
+              for (int i = 0; i < E; ++i) dz[u][i] *= dsilu(z[i], sigmoid(z[i]));
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+#pragma unroll
+              for (int k = 0; k < K - 1; ++k) dw[k][i] = __builtin_fmaf(dz[u][i], before[k][i], dw[k][i]);
+              dw[K - 1][i] = __builtin_fmaf(dz[u][i], x[u][i], dw[K - 1][i]);
+              db[i] += dz[u][i];
+              float v = taps.w[i * K] * dz[u][i];
+#pragma unroll
+              for (int k = 1; k < K; ++k) {
+                const int j = u + K - 1 - k;   // of the K - 1 rows before the batch, then of it
+                v = __builtin_fmaf(taps.w[i * K + k], j < K - 1 ? dzw[j < K - 1 ? j : 0][i] : dz[j < K - 1 ? 0 : j - (K - 1)][i], v);
+              }
+              dx[i] = v;
+            }
+            if (in) P::store(static_cast<S*>(a.dX) + (size_t)(tb + u - (K - 1)) * a.dxs + c, dx);
+          }
+#pragma unroll
+          for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+              win[k][i] = x[U - (K - 1) + k][i];
+              dzw[k][i] = dz[U - (K - 1) + k][i];
+            }
+          continue;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -221,7 +287,7 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
                 for (int k = 1; k < K; ++k) v = __builtin_fmaf(taps.w[i * K + k], dzw[K - 1 - k][i], v);
                 dx[i] = v;
               }
-              if (in) Piece<S>::store(static_cast<S*>(a.dX) + (size_t)s * a.dxs + c, dx);
+              if (in) P::store(static_cast<S*>(a.dX) + (size_t)s * a.dxs + c, dx);
             }
             shift<K, E>(dzw, dz);
           }
@@ -285,7 +351,7 @@ __global__ __launch_bounds__(256) void k_conv_step(ConvArgs a, int units) {
   px.load(static_cast<const S*>(a.X) + (size_t)b * a.xs + c);
 #pragma unroll
   for (int k = 0; k < K - 1; ++k) ps[k].load(st + (size_t)k * a.D);
-  Taps<S, K> taps;
+  Taps<E, K> taps;
   taps.load(a, c);
   float x[E], win[K - 1][E], z[E];
   px.get(x);
@@ -298,7 +364,7 @@ __global__ __launch_bounds__(256) void k_conv_step(ConvArgs a, int units) {
   }
   Piece<S>::store(static_cast<S*>(a.Y) + (size_t)b * a.D + c, z);
 #pragma unroll
-  for (int k = 0; k < K - 1; ++k) *reinterpret_cast<uint4*>(st + (size_t)k * a.D) = k + 1 < K - 1 ? ps[k + 1 < K - 1 ? k + 1 : 0].raw : px.raw;
+  for (int k = 0; k < K - 1; ++k) (k + 1 < K - 1 ? ps[k + 1 < K - 1 ? k + 1 : 0] : px).save(st + (size_t)k * a.D);
 }
 
 namespace {
@@ -314,7 +380,7 @@ void run_fwd(const ConvArgs& a, hipStream_t st) {
 }
 template <class S, int K, bool SILU>
 void run_bwd(const ConvArgs& a, hipStream_t st) {
-  const int units = a.D / Piece<S>::N, spans = (units + WAVE - 1) / WAVE;
+  const int spans = (a.D / 4 + WAVE - 1) / WAVE;
   if (a.parts > 0) k_conv_bwd<S, K, SILU><<<a.parts * spans, 256, 0, st>>>(a, spans);
   const int cols = (a.D + WAVE - 1) / WAVE;
   k_conv_sum<<<cols * (K + 1), 1024, 0, st>>>(a, cols);

@@ -5,33 +5,38 @@
 
 namespace flex {
 
-// 16 bytes of a row
-template <class S> struct Piece {
-  static constexpr int N = 16 / sizeof(S);
-  uint4 raw;
-  __device__ __forceinline__ void load(const S* p) { raw = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void zero() { raw = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void get(float* x) const {
-    const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
+// 16 bytes of a row (or 8)
+template <class S, int BYTES = 16> struct Piece {
+  static constexpr int N = BYTES / sizeof(S), WORDS = BYTES / 4;
+  typedef unsigned Words __attribute__((ext_vector_type(WORDS)));
+  Words raw;
+  __device__ __forceinline__ void load(const S* p) { raw = *reinterpret_cast<const Words*>(p); }
+  __device__ __forceinline__ void save(S* p) const { *reinterpret_cast<Words*>(p) = raw; }
+  __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < WORDS; ++i) raw[i] = 0;
+  }
+  __device__ __forceinline__ void get(float* x) const {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
       if constexpr (sizeof(S) == 2) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        x[2 * i] = __uint_as_float(raw[i] << 16);
+        x[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
       } else {
-        x[i] = __uint_as_float(w[i]);
+        x[i] = __uint_as_float(raw[i]);
       }
     }
   }
   __device__ __forceinline__ static void store(S* p, const float* x) {
-    if constexpr (sizeof(S) == 2) {
-      bf16x8 b;
+    Piece v;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) b[i] = (__bf16)x[i];
-      *reinterpret_cast<bf16x8*>(p) = b;
-    } else {
-      *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
+    for (int i = 0; i < WORDS; ++i) {
+      if constexpr (sizeof(S) == 2)
+        v.raw[i] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});
+      else
+        v.raw[i] = __float_as_uint(x[i]);
     }
+    v.save(p);
   }
 };
 
