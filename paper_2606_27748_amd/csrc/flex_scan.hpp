@@ -108,12 +108,12 @@ struct StateRows {
 };
 
 // Stages 64 rows of a window by `nw` waves of which this is w, 16 rows at a time.
-template <class T, int D>
+template <class T, int D, class Lane = ThisLane>
 __device__ __forceinline__ void stage_rows(const char* L, const typename Io<T>::type* base, size_t row0, int stride, int n, int w,
-                                           int nw, int l = threadIdx.x % WAVE) {
+                                           int nw, Lane lane = {}) {
   for (int k = w; k < 4; k += nw)
     stage_tile<T, D, 16, 1>(L + k * 16 * D * (int)sizeof(T), row_words(base, row0 + 16 * k, stride, n - 16 * k, D),
-                            stride * (int)sizeof(T), 0, l);
+                            stride * (int)sizeof(T), 0, lane);
 }
 
 // x where bit e of a lane's mask is set, else 0: a comparison into vcc and a selection by it take three times as long

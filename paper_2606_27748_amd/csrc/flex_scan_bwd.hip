@@ -76,7 +76,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   auto block = [&](int it) { return lds + 2 * ROWS + (BUFS == 2 ? (it & 1) * BLOCK : 0); };
   auto state_at = [&](int it) { return (((size_t)slot * a.H + head0 + it / nb) * a.P + it % nb * 64) * N; };
   auto stage = [&](int it) {
-    const int x = again();
+    const LaneOf x{again()};
     const size_t xcol = (size_t)(head0 + it / nb) * a.P + it % nb * 64;
     const char* L = block(it);
     if (w < 4)
