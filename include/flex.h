@@ -486,11 +486,11 @@ int32_t flex_scan_saved_size(const flex_scan_desc* desc, size_t* bytes);
  *   state [B,H,N,P] fp32 or NULL    the states after the last tokens (state0 itself is
  *                               allowed); an empty sequence's is its state0, or zero
  *   saved                       flex_scan_saved_size() bytes for a backward, or NULL
- * States, decays and sums are fp32; with FLEX_BF16 a token's part of the state is formed from two
- * bf16 terms (2^-17), and the matrix of a chunk of 64 tokens and the state it reads are rounded to bf16.
- * From a token on whose row of X, Bt, dt or g is not finite, Y and the state are not (of X: in its
- * column); the tokens before it, other sequences and other columns keep their results.  What is
- * not finite in a row of Ct concerns that row of Y alone. */
+ * States, decays and sums are fp32; with FLEX_BF16 a token's part of the state is formed from three
+ * bf16 terms (24 bits), and the matrix of a chunk of 64 tokens and the state it reads are rounded to bf16.
+ * A g below -1000 counts as a decay of zero.  From a token on whose row of X, Bt, dt or g is not finite (but for a g of
+ * -inf), Y and the state are not (of X: in its column); the tokens before it, other sequences and other columns
+ * keep their results.  What is not finite in a row of Ct concerns that row of Y alone. */
 int32_t flex_scan_fwd(const flex_scan_desc* desc, const void* X, const void* Bt, const void* Ct, const float* dt,
                       const float* g, const float* D, const int32_t* off, const float* state0, void* Y, float* state,
                       void* saved, size_t saved_bytes, void* ws, size_t ws_bytes, void* stream);

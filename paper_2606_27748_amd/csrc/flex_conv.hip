@@ -3,9 +3,10 @@
 //   z_t = bias + sum_{k<K} W[:,k] x_{t-K+1+k},  y = z or z sigmoid(z)
 //   dz = dy act'(z),  dx_t = sum_k W[:,k] dz_{t+K-1-k},  dW[:,k] = sum_t dz_t x_{t-K+1+k},  dbias = sum_t dz_t
 //
-// A lane has 16 bytes of a row's channels with their taps in registers and walks down the rows, the
+// A lane has some of a row's channels with their taps in registers and walks down the rows, the
 // K-1 rows before the present one in registers too: every row is read once, but for the K-1 that
-// a tile shares with its neighbour.  Bound by memory.
+// a tile shares with its neighbour.  Rows go through windows that hold a tile: a lane behind the last channel
+// reads zeros and writes nothing, without a branch, and a row's place is a scalar.
 #include "flex_rows.hpp"
 #include "flex_layer_kernels.hpp"
 #include "../../include/flex.h"
@@ -13,13 +14,16 @@
 namespace flex {
 
 namespace {
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+constexpr int OUTSIDE = 0x7fffff00;   // of any window of rows: a lane there reads zeros and writes nothing
+
 // a lane's channels' taps and bias
 template <int E, int K>
 struct Taps {
   float w[E * K], bias[E];
   __device__ __forceinline__ void load(const ConvArgs& a, int c) {
 #pragma unroll
-    for (int i = 0; i < E * K / 4; ++i) *reinterpret_cast<f32x4*>(w + 4 * i) = reinterpret_cast<const f32x4*>(a.W + (size_t)c * K)[i];
+    for (int i = 0; i < E * K / 2; ++i) *reinterpret_cast<f32x2*>(w + 2 * i) = reinterpret_cast<const f32x2*>(a.W + (size_t)c * K)[i];
 #pragma unroll
     for (int i = 0; i < E; ++i) bias[i] = a.bias ? a.bias[c + i] : 0.f;
   }
@@ -82,6 +86,8 @@ __device__ __forceinline__ void last_rows(const ConvArgs& a, int b, int c) {
 }  // namespace
 
 // Waves 0 .. tiles-1 of a span of channels have CONV_ROWS rows each, the B behind them a sequence's last rows.
+// 16 bytes a lane, the next eight rows on their way.  Bound by memory: 35907 rows of 4352 channels in 16 prompts,
+// bf16, 625 MB in 122 us (5.1 TB/s, a large copy's rate).
 template <class S, int K, bool SILU>
 __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a, int spans, int tiles, int first_b) {
   constexpr int E = Piece<S>::N, U = 8;
@@ -95,10 +101,12 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a, int spans, int til
     return;
   }
   const int r0 = tile * CONV_ROWS, r1 = min(r0 + CONV_ROWS, a.T);
-  const S* X = static_cast<const S*>(a.X) + cc;
+  const int at = in ? c * (int)sizeof(S) : OUTSIDE, xb = a.xs * (int)sizeof(S), yb = a.D * (int)sizeof(S);
+  const auto X = row_window(static_cast<const S*>(a.X), r0, a.xs, r1 - r0, a.D);
+  const auto Y = row_window(static_cast<S*>(a.Y), r0, a.D, r1 - r0, a.D);
   Piece<S> next[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) next[u].load(X + (size_t)min(r0 + u, r1 - 1) * a.xs);
+  for (int u = 0; u < U; ++u) next[u].load(X, at, (min(r0 + u, r1 - 1) - r0) * xb);
   Taps<E, K> taps;
   taps.load(a, cc);
   RowSeq q = find_row(a.off, a.B, a.T, r0);
@@ -110,7 +118,7 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a, int spans, int til
     for (int u = 0; u < U; ++u) cur[u] = next[u];
     if (t0 + U < r1) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) next[u].load(X + (size_t)min(t0 + U + u, r1 - 1) * a.xs);
+      for (int u = 0; u < U; ++u) next[u].load(X, at, (min(t0 + U + u, r1 - 1) - r0) * xb);
     }
     if (q.b >= 0 && t0 + U <= min(q.end, r1)) {   // rows of one sequence: no row's window is moved, but named
       float x[U][E];
@@ -127,7 +135,7 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a, int spans, int til
 #pragma unroll
           for (int i = 0; i < E; ++i) z[i] *= sigmoid(z[i]);
         }
-        if (in) Piece<S>::store(static_cast<S*>(a.Y) + (size_t)(t0 + u) * a.D + c, z);
+        Piece<S>::of(z).save(Y, at, (t0 + u - r0) * yb);
       }
 #pragma unroll
       for (int k = 0; k < K - 1; ++k)
@@ -152,7 +160,7 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a, int spans, int til
 #pragma unroll
             for (int i = 0; i < E; ++i) z[i] *= sigmoid(z[i]);
           }
-          if (in) Piece<S>::store(static_cast<S*>(a.Y) + (size_t)t * a.D + c, z);
+          Piece<S>::of(z).save(Y, at, (t - r0) * yb);
         }
       }
     }
@@ -161,11 +169,12 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a, int spans, int til
 
 // As the forward, over CONV_BWD_ROWS rows and the K-1 behind them, whose dz the last rows' dx take: at row
 // t, dz_t is formed and dx of row t - (K-1) is complete.  A workgroup's waves have consecutive rows and
-// leave one row of partial sums of dW and dbias.  Four channels a lane: with eight, their windows and sums leave a SIMD
-// one wave (143 us for 2 x 8192 rows of 4352 channels).
+// leave one row of partial sums of dW and dbias.  29 instructions an element, two of them exponential and reciprocal,
+// keep the SIMDs busy 65 % of the time: bound by them and by memory.  Two channels a lane leave five
+// waves a SIMD: 2 x 8192 rows of 4352 channels, bf16, 91 us (342 MB, 3.8 TB/s); with four channels 106, with eight 143.
 template <class S, int K, bool SILU>
 __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
-  constexpr int E = 4, U = 4;
+  constexpr int E = CONV_BWD_CH, U = 4;
   using P = Piece<S, E * (int)sizeof(S)>;
   __shared__ float sums[CONV_BWD_WAVES - 1][(K + 1) * E][WAVE];
   const int l = threadIdx.x % WAVE, w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
@@ -173,8 +182,12 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
   const bool in = c < a.D;
   const int cc = in ? c : 0;
   const int r0 = (part * CONV_BWD_WAVES + w) * CONV_BWD_ROWS, r1 = min(r0 + CONV_BWD_ROWS, a.T);
-  const S* X = static_cast<const S*>(a.X) + cc;
-  const S* G = static_cast<const S*>(a.dY) + cc;
+  const int at = in ? c * (int)sizeof(S) : OUTSIDE;
+  const int xb = a.xs * (int)sizeof(S), gb = a.D * (int)sizeof(S), dxb = a.dxs * (int)sizeof(S);
+  const int rows = max(min(r0 + CONV_BWD_ROWS + K - 1, a.T) - r0, 0);
+  const auto X = row_window(static_cast<const S*>(a.X), r0, a.xs, rows, a.D);
+  const auto G = row_window(static_cast<const S*>(a.dY), r0, a.D, rows, a.D);
+  const auto DX = row_window(static_cast<S*>(a.dX), r0, a.dxs, r1 - r0, a.D);
   float dw[K][E] = {}, db[E] = {};
   if (r0 < r1) {
     Taps<E, K> taps;
@@ -185,15 +198,15 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
         t0 = q.end;
         continue;
       }
-      const int e = min(q.end, r1), stop = e + K - 1;   // dx of rows t0 .. e-1
+      const int e = min(q.end, r1), stop = e + K - 1, last = min(q.end, r0 + rows) - 1;   // dx of rows t0 .. e-1
       float win[K - 1][E], dzw[K - 1][E] = {};
       window<S, K>(win, a, q, t0, cc);
       P nx[U], ng[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const size_t r = min(t0 + u, q.end - 1);
-        nx[u].load(X + r * a.xs);
-        ng[u].load(G + r * a.D);
+        const int r = min(t0 + u, last) - r0;
+        nx[u].load(X, at, r * xb);
+        ng[u].load(G, at, r * gb);
       }
       for (int tb = t0; tb < stop; tb += U) {
         P px[U], pg[U];
@@ -205,9 +218,9 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
         if (tb + U < stop) {
 #pragma unroll
           for (int u = 0; u < U; ++u) {
-            const size_t r = min(tb + U + u, q.end - 1);
-            nx[u].load(X + r * a.xs);
-            ng[u].load(G + r * a.D);
+            const int r = min(tb + U + u, last) - r0;
+            nx[u].load(X, at, r * xb);
+            ng[u].load(G, at, r * gb);
           }
         }
         if (tb > t0 && tb + U <= e) {   // every row's dz counts here, and every row's dx is one of the tile's
@@ -241,7 +254,7 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
               }
               dx[i] = v;
             }
-            if (in) P::store(static_cast<S*>(a.dX) + (size_t)(tb + u - (K - 1)) * a.dxs + c, dx);
+            P::of(dx).save(DX, at, (tb + u - (K - 1) - r0) * dxb);
           }
 #pragma unroll
           for (int k = 0; k < K - 1; ++k)
@@ -287,7 +300,7 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
                 for (int k = 1; k < K; ++k) v = __builtin_fmaf(taps.w[i * K + k], dzw[K - 1 - k][i], v);
                 dx[i] = v;
               }
-              if (in) P::store(static_cast<S*>(a.dX) + (size_t)s * a.dxs + c, dx);
+              P::of(dx).save(DX, at, (s - r0) * dxb);
             }
             shift<K, E>(dzw, dz);
           }
@@ -380,7 +393,7 @@ void run_fwd(const ConvArgs& a, hipStream_t st) {
 }
 template <class S, int K, bool SILU>
 void run_bwd(const ConvArgs& a, hipStream_t st) {
-  const int spans = (a.D / 4 + WAVE - 1) / WAVE;
+  const int spans = (a.D / CONV_BWD_CH + WAVE - 1) / WAVE;
   if (a.parts > 0) k_conv_bwd<S, K, SILU><<<a.parts * spans, 256, 0, st>>>(a, spans);
   const int cols = (a.D + WAVE - 1) / WAVE;
   k_conv_sum<<<cols * (K + 1), 1024, 0, st>>>(a, cols);

@@ -39,10 +39,12 @@ int32_t check_conv(const flex_conv_desc* d, bool step) {
   if (d->D % 8 != 0 || d->D > kMaxStride || d->K < 2 || d->K > 4) return FLEX_ERR_UNSUPPORTED;
   const int e = esize(d->io_dtype);
   if (!stride_ok(d->x_stride, d->D, e) || !stride_ok(d->dx_stride, d->D, e)) return FLEX_ERR_INVALID_ARG;
-  // the threads of a launch: a wave per tile of rows (and sequence, for the last rows) and 64 pieces; a step's
+  // the threads of a launch: a wave per tile of rows (and sequence, for the last rows) and 64 lanes' channels; a step's
   // thread per piece; indexes of rows fit 31 bits
-  const int64_t units = d->D / (16 / e), spans = ceil_div(d->D / 4, 64);
-  const int64_t waves = step ? ceil_div((int64_t)d->B * units, 64) : (ceil_div(d->T, CONV_ROWS) + d->B + 4) * spans;
+  const int64_t units = d->D / (16 / e), spans = ceil_div(units, 64);
+  const int64_t back = ceil_div(d->T, CONV_BWD_ROWS * CONV_BWD_WAVES) * CONV_BWD_WAVES * ceil_div(d->D / CONV_BWD_CH, 64);
+  int64_t waves = step ? ceil_div((int64_t)d->B * units, 64) : (ceil_div(d->T, CONV_ROWS) + d->B + 4) * spans;
+  if (!step && back > waves) waves = back;
   if ((waves + 4) * 64 > kMaxThreads || (int64_t)d->T + CONV_BWD_ROWS * CONV_BWD_WAVES >= (1LL << 31)) return FLEX_ERR_INVALID_ARG;
   return FLEX_OK;
 }

@@ -11,11 +11,12 @@ namespace flex {
 void timing_mark(int kernel_class, hipStream_t st, bool begin);
 
 // Short convolution.  Strides are between consecutive rows, in elements.  A wave takes
-// CONV_ROWS rows (of the packed rows, whatever their sequences) of 64 pieces of 8 (bf16: 16 bytes a
-// lane) or 4 (fp32) channels.
+// rows of the packed ones, whatever their sequences, and a lane of it 16 bytes of channels (forward) or
+// CONV_BWD_CH channels.
 constexpr int CONV_ROWS = 32;        // of a wave in the forward
 constexpr int CONV_BWD_ROWS = 64;    // of a wave in the backward
 constexpr int CONV_BWD_WAVES = 4;    // of a workgroup, one after the other: one row of partial sums
+constexpr int CONV_BWD_CH = 2;
 struct ConvArgs {
   const void* X;
   const float* W;
@@ -74,12 +75,13 @@ struct ScanArgs {
   int heads;              // of a workgroup's sweep, all of one group
   // Sequences go in segments of `seg` tokens (a multiple of the chunk), one after the other
   // where carry is NULL (no sequence is longer than one), else at once, from
-  //   carry [segment slots][H][N * P]   what each segment leaves of its own, then the state it starts from
+  //   carry [segment slots][H][N * P]   what each segment leaves of its own, then the state it starts from (as the lanes
+  //                                     hold it)
   //   tot   [segment slots][H]          its decay
   int seg;
   float* carry;
   float* tot;
-  void* st;               // states at the chunks' starts [chunk slots][H][P][N], io type; NULL: not kept
+  void* st;               // states at the chunks' starts [chunk slots][H][N * P] as the lanes hold them, io type; NULL: not kept
   // backward
   const void* dY;
   void* dst;              // gradients of the states at the chunks' ends, as st

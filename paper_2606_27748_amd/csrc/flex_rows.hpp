@@ -12,6 +12,19 @@ template <class S, int BYTES = 16> struct Piece {
   Words raw;
   __device__ __forceinline__ void load(const S* p) { raw = *reinterpret_cast<const Words*>(p); }
   __device__ __forceinline__ void save(S* p) const { *reinterpret_cast<Words*>(p) = raw; }
+  // of a window of rows, at a lane's place in a row (nothing outside the window) and a row's place in it, in bytes
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, int at, int row) {
+    if constexpr (WORDS == 1) raw[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, at, row, 0);
+    if constexpr (WORDS == 2) raw = __builtin_bit_cast(Words, __builtin_amdgcn_raw_buffer_load_b64(rs, at, row, 0));
+    if constexpr (WORDS == 4) raw = __builtin_bit_cast(Words, __builtin_amdgcn_raw_buffer_load_b128(rs, at, row, 0));
+  }
+  // A store of 16 bytes has its row in the lane's offset: with a scalar one the first word has been seen to be what the
+  // next instruction put into its register (once in some 10^5 stores), and the compiler leaves no room between them.
+  __device__ __forceinline__ void save(__amdgpu_buffer_rsrc_t rs, int at, int row) const {
+    if constexpr (WORDS == 1) __builtin_amdgcn_raw_buffer_store_b32(raw[0], rs, at, row, 0);
+    if constexpr (WORDS == 2) __builtin_amdgcn_raw_buffer_store_b64(raw, rs, at, row, 0);
+    if constexpr (WORDS == 4) __builtin_amdgcn_raw_buffer_store_b128(raw, rs, (int)((unsigned)at + (unsigned)row), 0, 0);
+  }
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) raw[i] = 0;
@@ -27,7 +40,7 @@ template <class S, int BYTES = 16> struct Piece {
       }
     }
   }
-  __device__ __forceinline__ static void store(S* p, const float* x) {
+  __device__ __forceinline__ static Piece of(const float* x) {
     Piece v;
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) {
@@ -36,8 +49,9 @@ template <class S, int BYTES = 16> struct Piece {
       else
         v.raw[i] = __float_as_uint(x[i]);
     }
-    v.save(p);
+    return v;
   }
+  __device__ __forceinline__ static void store(S* p, const float* x) { of(x).save(p); }
 };
 
 constexpr float LOG2E = 1.4426950408889634f;

@@ -72,6 +72,32 @@ def test_backward(F, lengths, D, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("K", [2, 4])
+def test_every_value_of_a_large_call(F, K, dtype):
+    """Small whole numbers and quarters, whose products and sums every type here holds: millions of values without one off.
+    |x|, |dy| <= 8, |w| <= 1/2 and |bias| <= 2 in quarters: |z|, |dx| <= 18, 72 quarters; dW and dbias below 64 T = 2^20."""
+    T, D = 16384, 1032
+    gen = torch.Generator().manual_seed(K)
+    whole = lambda n, *shape: torch.randint(-n, n + 1, shape, generator=gen).float()
+    X, dY, W, bias = on(whole(8, T, D)), on(whole(8, T, D)), on(whole(2, D, K) / 4), on(whole(8, D) / 4)
+    ends = [0, 5000, 5001, 16384]
+    off = on(torch.tensor(ends, dtype=torch.int32))
+    Y, dX, dW = bias.expand(T, D).clone(), torch.zeros_like(X), torch.zeros_like(W)
+    for a, b in zip(ends, ends[1:]):
+        for k in range(K):
+            back = K - 1 - k
+            if b - a > back:
+                Y[a + back:b] += W[:, k] * X[a:b - back]
+                dX[a:b - back] += W[:, k] * dY[a + back:b]
+                dW[:, k] += (dY[a + back:b] * X[a:b - back]).sum(0)
+    desc = F.make_conv_desc(3, T, D, K, act="none", io=io_of(dtype))
+    args = (desc, X.to(dtype), W, bias, off)
+    assert torch.equal(F.flex_conv_fwd(*args)[0].float(), Y)
+    got = F.flex_conv_bwd(*args, dY.to(dtype))
+    assert torch.equal(got["dX"].float(), dX) and torch.equal(got["dW"], dW) and torch.equal(got["dbias"], dY.sum(0))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("D,K,B", [(8, 4, 1), (520, 3, 5), (1032, 4, 33), (64, 2, 2)])
 def test_step_continues_a_prompt(F, D, K, B, dtype):
     """Prompts of n tokens, then steps: the same rows as longer prompts give."""
