@@ -86,7 +86,7 @@ __device__ __forceinline__ void last_rows(const ConvArgs& a, int b, int c) {
 }  // namespace
 
 // Waves 0 .. tiles-1 of a span of channels have CONV_ROWS rows each, the B behind them a sequence's last rows.
-// 16 bytes a lane, the next eight rows on their way.  Bound by memory: 35907 rows of 4352 channels in 16 prompts,
+// 16 bytes a lane, the next eight rows on their way.  Bound by memory: 35947 rows of 4352 channels in 16 prompts,
 // bf16, 625 MB in 122 us (5.1 TB/s, a large copy's rate).
 template <class S, int K, bool SILU>
 __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a, int spans, int tiles, int first_b) {

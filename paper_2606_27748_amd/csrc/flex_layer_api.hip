@@ -76,12 +76,22 @@ int32_t check_norm(const flex_norm_desc* d) {
   if ((int64_t)d->T + kNormWaves * 64 >= (1LL << 31)) return FLEX_ERR_INVALID_ARG;   // row indexes fit 31 bits
   return FLEX_OK;
 }
-// Rows that are walked at once, and rows of partial sums of dW: as many as give the card kNormWaves waves.
+// Rows that are walked at once: as many as give the card kNormWaves waves.
+int norm_rows(const flex_norm_desc* d) {
+  const int64_t n = kNormWaves * 64 / (d->D / 8);
+  return (int)(n < 1 ? 1 : n > d->T ? (d->T > 0 ? d->T : 1) : n);
+}
+// Rows of a workgroup of the backward at a time, which leaves one row of partial sums of dW: of rows that up to a wave's lanes
+// have. Wider ones leave a row of sums for each that is walked.
+int norm_wg_rows(const flex_norm_desc* d) {
+  const int64_t lanes = (int64_t)norm_team(d->group) * (d->D / d->group);
+  return lanes <= 64 ? (int)(256 / lanes) : 1;
+}
 int norm_parts(const flex_norm_desc* d) {
-  const int64_t lanes = d->D / 8;
-  int64_t n = kNormWaves * 64 / (lanes < 64 ? 64 : lanes);
-  if (n > d->T) n = d->T;
-  return n < 1 ? 1 : (int)n;
+  const int r = norm_wg_rows(d);
+  if (r == 1) return norm_rows(d);
+  const int64_t wgs = ceil_div(d->T, r);
+  return (int)(wgs < 1 ? 1 : wgs > kNormWaves / 4 ? kNormWaves / 4 : wgs);
 }
 size_t norm_ws_bytes(const flex_norm_desc* d) { return (size_t)norm_parts(d) * d->D * sizeof(float); }
 NormArgs norm_args(const flex_norm_desc* d, const void* X, const void* Z, const float* W) {
@@ -93,7 +103,7 @@ NormArgs norm_args(const flex_norm_desc* d, const void* X, const void* Z, const 
   a.zs = stride_of(d->z_stride, d->D);
   a.dxs = stride_of(d->dx_stride, d->D);
   a.dzs = stride_of(d->dz_stride, d->D);
-  a.parts = norm_parts(d);
+  a.rows = norm_rows(d);
   return a;
 }
 
@@ -129,7 +139,7 @@ int32_t check_scan(const flex_scan_desc* d, bool step) {
 // Tokens of a segment.  A sweep's workgroup takes a CU, its sequences are walked in order, and a
 // segment that is not its sequence's last has its rows read twice: segments so long that the card has one
 // workgroup per CU of them, 64 to 4096 tokens (a prompt of 32768 tokens, 16 heads of 128: 213 us; with twice as many
-// 237).  Many sequences, whose ends leave workgroups of any length, have twice as many (16 prompts of 18000 tokens, 64 heads
+// 237).  Many sequences, whose ends leave workgroups of any length, have twice as many (16 prompts of 17152 tokens, 64 heads
 // of 64: 295 us; with one per CU 315).
 int scan_seg(const flex_scan_desc* d) {
   const int64_t sets = d->H / scan_heads(d), wgs = d->B * sets < 128 ? 256 : 512;
@@ -283,6 +293,9 @@ int32_t flex_norm_bwd(const flex_norm_desc* desc, const void* X, const void* Z, 
   NormArgs a = norm_args(desc, X, Z, W);
   a.dY = dY; a.dX = dX; a.dZ = dZ; a.dW = dW;
   a.part = static_cast<float*>(ws);
+  a.parts = norm_parts(desc);
+  a.wg_rows = norm_wg_rows(desc);
+  if (a.wg_rows > 1) a.rows = a.parts * a.wg_rows;
   return done(launch_norm_bwd(a, desc->io_dtype == FLEX_BF16, (hipStream_t)stream));
 }
 

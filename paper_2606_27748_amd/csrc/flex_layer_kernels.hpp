@@ -40,6 +40,12 @@ hipError_t launch_conv_step(const ConvArgs& a, bool bf16, hipStream_t st);
 
 // Gated norm.  A team of lanes takes a group of a row at a time.
 constexpr int NORM_MAX = 8192;   // channels of a group
+// lanes of a group: as many as it has pieces of 8 channels, a power of two up to a wave
+inline int norm_team(int group) {
+  int team = 1;
+  while (team < group / 8 && team < 64) team *= 2;
+  return team;
+}
 struct NormArgs {
   const void* X;
   const void* Z;
@@ -47,6 +53,7 @@ struct NormArgs {
   void* Y;
   int T, D, group, gate, xs, zs;
   float eps;
+  int rows;               // that are walked at once
   // backward
   const void* dY;
   void* dX;
@@ -54,6 +61,7 @@ struct NormArgs {
   float* part;            // [parts][D] workspace
   float* dW;
   int dxs, dzs, parts;
+  int wg_rows;            // rows of a workgroup at a time: more than one of narrow ones
 };
 hipError_t launch_norm_fwd(const NormArgs& a, bool bf16, hipStream_t st);
 hipError_t launch_norm_bwd(const NormArgs& a, bool bf16, hipStream_t st);

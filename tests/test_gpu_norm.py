@@ -68,6 +68,20 @@ def test_many_rows(F, dtype):
     assert all(torch.equal(got[n], again[n]) for n in got)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,group,D", [(70001, 8, 8), (40003, 24, 72), (50000, 64, 64), (20000, 56, 504), (9000, 512, 512), (12000, 40, 360)])
+def test_many_narrow_rows(F, T, group, D, dtype):
+    """Rows of which a workgroup has several, more of them than are walked at once."""
+    x = make(T, D, dtype, 5, 8)
+    t, desc = {k: on(v) for k, v in x.items()}, desc_of(F, x, group, "last", dtype)
+    ref, err = norm_oracle(x, group, "last", 1e-5)
+    Y = F.flex_norm_fwd(desc, t["X"], t["Z"], t["W"])
+    within("Y", Y, ref["Y"], err["Y"] + STEP[dtype] * ref["Y"].abs())
+    got = F.flex_norm_bwd(desc, t["X"], t["Z"], t["W"], t["dY"])
+    for n in ("dX", "dZ", "dW"):
+        within(n, got[n], ref[n], err[n] + STEP[F32 if n == "dW" else dtype] * ref[n].abs())
+
+
 def test_rows_are_for_themselves(F):
     """A row of NaN or zeros changes no other row's results."""
     x = make(33, 256, BF16, 6)
