@@ -31,6 +31,17 @@ __device__ __forceinline__ constexpr int perm_row(int e, int h) { return 16 * (e
 template <class T, int D>
 struct ScanTile : RowTile<T, D> {
   using R = RowTile<T, D>;
+  // RowTile::row: the places of the steps differ by bits that are turned over
+  static __device__ __forceinline__ Frag<T> row(const char* L, int r, int s, int h) {
+    Frag<T> f;
+    if constexpr (IsBf16<T>::value) {
+      const int lane = (h ^ R::swz(r)) << 4;
+      f.v = *reinterpret_cast<const bf16x8*>(L + r * R::ROW + (lane ^ (s << 5)));
+      return f;
+    } else {
+      return R::row(L, r, s, h);
+    }
+  }
   // Columns m0 + perm32(l % 32) for lane l, slots 0..3 the rows r0 .. r0+3, slots 4..7 r1 .. r1+3
   static __device__ __forceinline__ Frag<T> colp(const char* L, int r0, int r1, int m0, int l = threadIdx.x % WAVE) {
     Frag<T> f;
@@ -91,6 +102,21 @@ struct StateRows {
     }
     return f;
   }
+  // the same of the slots columns 16 s + 8 h .., h = l / 32, n0 a multiple of 32: one place of the lane's for all s and n0
+  static __device__ __forceinline__ Frag<T> steps(const char* L, int s, int n0, int l) {
+    if constexpr (IsBf16<T>::value) {
+      Frag<T> f;
+      // at(16 s + 8 h + 4 k + i / 4, n0 + 16 b + 4 q), as the sum of what the lane has and what s, k and n0 have
+      const int i = l % 16, b = l / 16 % 2, h = l / 32, hh = i & 1;
+      const char* p = L + n0 / 16 * FRAG + s / 2 * BLOCK + s % 2 * 256 + (b * FRAG + hh * 512 + (h ^ hh) * 64 + i / 4 * 16 + (i / 2 & 1) * 8);
+      const tr_v4i16 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)p);
+      const tr_v4i16 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(p + 128));
+      f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7));
+      return f;
+    } else {
+      return colp(L, 16 * s + 8 * (l / 32), n0, l);
+    }
+  }
   // the operand with lane l % 32 element n0 + perm32(l % 32) and the slots columns p .. p + 7
   static __device__ __forceinline__ Frag<T> colp(const char* L, int p, int n0, int l) {
     Frag<T> f;
@@ -116,10 +142,22 @@ __device__ __forceinline__ void stage_rows(const char* L, const typename Io<T>::
                             stride * (int)sizeof(T), 0, lane);
 }
 
-// x where bit e of a lane's mask is set, else 0: a comparison into vcc and a selection by it take three times as long
-__device__ __forceinline__ float keep_if(float x, unsigned mask, int e) {
-  return __uint_as_float(__float_as_uint(x) & (unsigned)((int)(mask << (31 - e)) >> 31));
-}
+// Lanes (column l % 32) for which element e of a tile is a row from their column on, or behind it
+struct DiagonalMasks {
+  uint64_t from[16] = {}, behind[16] = {};
+  constexpr DiagonalMasks() {
+    for (int e = 0; e < 16; ++e)
+      for (int l = 0; l < 64; ++l) {
+        const int row = 8 * (e / 4) + 4 * (l / 32) + e % 4;
+        from[e] |= (uint64_t)(row >= l % 32) << l;
+        behind[e] |= (uint64_t)(row > l % 32) << l;
+      }
+  }
+};
+constexpr DiagonalMasks DIAGONAL;
+// x in the lanes of a mask, else 0.  A mask that is a constant costs a scalar instruction: as conditions that the compiler
+// keeps over a loop, 32 masks do not fit the scalar registers.
+__device__ __forceinline__ float keep_lanes(float x, uint64_t lanes) { return __builtin_amdgcn_inverse_ballot_w64(lanes) ? x : 0.f; }
 
 // the value of lane l ^ M, M 1 or 2
 template <int M>

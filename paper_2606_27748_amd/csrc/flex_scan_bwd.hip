@@ -44,7 +44,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   __shared__ __attribute__((aligned(16))) float scal[2][6 * SC + 4];
   // what the waves leave for dg and ddt
   struct Dots {
-    float r[4][SC], v[2][SC], i[2][SC], col[2][SC], row[2][2][SC], d[2], s[8];
+    float r[4][SC], v[2][SC], i[2][SC], col[2][SC], row[2][2][SC], d[4], s[8];
   };
   __shared__ Dots dots[2];
   char* LB = lds;
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
       static_cast<S*>(a.dg)[at] = float_to_io<S>(sc[5 * SC + l] != 0.f ? slope : 0.f);
       static_cast<S*>(a.ddt)[at] = float_to_io<S>((o.i[0][l] + o.i[1][l]) + v);
     }
-    if (l == 0) a.part_d[(size_t)slot * a.H + head0 + hd] = o.d[0] + o.d[1];
+    if (l == 0) a.part_d[(size_t)slot * a.H + head0 + hd] = (o.d[0] + o.d[1]) + (o.d[2] + o.d[3]);
   };
 
   stage_rows<T, N>(w < 4 ? LB : LC, (w < 4 ? static_cast<const S*>(a.Bt) : static_cast<const S*>(a.Ct)) + (size_t)grp * N, row0,
@@ -162,13 +162,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     if (tx == 0) products(ka, 0, tx);
     products(kb, 1, tx);
   }
-  unsigned from_on = 0, behind = 0;   // of a tile on the diagonal, the elements i from this lane's j on, and behind it
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    from_on |= res_row(e, h) >= c ? 1u << e : 0u;
-    behind |= res_row(e, h) > c ? 1u << e : 0u;
-  }
-  float di = 0.f, dv = 0.f, dr = 0.f, ss = 0.f;
+  float di = 0.f, dv = 0.f, dd = 0.f, dr = 0.f, ss = 0.f;
   for (int it = 0; it < items; ++it) {
     const int hd = it / nb, head = head0 + hd, pb = it % nb;
     if (BUFS == 1 && it > 0) {
@@ -194,12 +188,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     }
     if (pb == 0) {
       if (w >= 4) kb = zero16();
-      di = dv = dr = ss = 0.f;
+      di = dv = dd = dr = ss = 0.f;
     }
     if (has_n) {   // e^L S dy
       f32x16 u = zero16();
 #pragma unroll
-      for (int s = 0; s < 4; ++s) mma32(u, ST::colp(LS, 16 * s + 8 * h, n0, x), XT::row(LY, tok, s, h));
+      for (int s = 0; s < 4; ++s) mma32(u, ST::steps(LS, s, n0, x), XT::row(LY, tok, s, h));
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const Frag<T> cr = RT::row(LC, tok, n0 / 16 + s, h);
@@ -233,17 +227,17 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     if (has_n) {   // dt v dS x
       f32x16 u = zero16();
 #pragma unroll
-      for (int s = 0; s < 4; ++s) mma32(u, ST::colp(LD, 16 * s + 8 * h, n0, x), XT::row(LX, tok, s, h));
+      for (int s = 0; s < 4; ++s) mma32(u, ST::steps(LD, s, n0, x), XT::row(LX, tok, s, h));
       const float dtv = sc[2 * SC + tok] * sc[4 * SC + tok];
 #pragma unroll
       for (int e = 0; e < 16; ++e) dB[e] = __builtin_fmaf(u[e], dtv, dB[e]);
     }
-    // use(q, f) with the decays f = e^{L_i - L_j} of the elements 4 q .. of a tile of i, from the token j = at
+    // use(q, f) with the decays f = e^{L_i - L_j} of the elements 4 q .. of a tile of i, from the token j = at, times by
     const bool product = sc[6 * SC] != 0.f;
-    auto decays_to = [&](int tile, int at, bool next, auto use) {
+    auto decays_to = [&](int tile, int at, bool next, float by, auto use) {
       const float* si = sc + 32 * tile + 4 * h;
       if (product) {
-        const float bj = sc[SC + at] * (next ? sc[6 * SC + 1] : 1.f);
+        const float bj = sc[SC + at] * by * (next ? sc[6 * SC + 1] : 1.f);
 #pragma unroll
         for (int q = 0; q < 4; ++q) use(q, *reinterpret_cast<const f32x4*>(si + 8 * q) * bj);
       } else {
@@ -253,11 +247,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
           const f32x4 hi = *reinterpret_cast<const f32x4*>(si + 8 * q), lo = *reinterpret_cast<const f32x4*>(si + SC + 8 * q);
           f32x4 f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) f[e] = decay<BF>(hi[e], lo[e], hj, lj);
+          for (int e = 0; e < 4; ++e) f[e] = decay<BF>(hi[e], lo[e], hj, lj) * by;
           use(q, f);
         }
       }
     };
+    uint64_t whole = ~0ull;   // every lane: formed anew, so that no mask of a whole tile or the diagonal is kept over the loop
+    asm volatile("" : "+s"(whole));
     if (w < 4) {   // dx of 32 of the block's columns
       const int p0 = 32 * (w % 2), tok = 32 * tx + c;
       const float dt = sc[2 * SC + tok], vj = sc[4 * SC + tok];
@@ -268,10 +264,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
       for (int i = 0; i < 2; ++i)
         if (i >= tx) {
           f32x16 q;
-          const unsigned seen = i > tx ? ~0u : from_on;
-          decays_to(i, tok, i > tx, [&](int b, const f32x4& f) {
+          const uint64_t all = i > tx ? whole : 0;
+          decays_to(i, tok, i > tx, 1.f, [&](int b, const f32x4& f) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) q[4 * b + e] = keep_if((i == 0 ? ka[4 * b + e] : kb[4 * b + e]) * f[e], seen, 4 * b + e);
+            for (int e = 0; e < 4; ++e)
+              q[4 * b + e] = keep_lanes((i == 0 ? ka[4 * b + e] : kb[4 * b + e]) * f[e], DIAGONAL.from[4 * b + e] | all);
           });
 #pragma unroll
           for (int s = 0; s < 2; ++s)
@@ -288,6 +285,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
           const float p = xa[8 * s + j], v = vj * xv[8 * s + j];
           di = __builtin_fmaf(p, xr.get(j), di);
           dv = __builtin_fmaf(v, xr.get(j), dv);
+          dd = __builtin_fmaf(yr.get(j), xr.get(j), dd);
           o[s][j] = __builtin_fmaf(dt, p + v, Dh * yr.get(j));
         }
       }
@@ -299,22 +297,23 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
           left.i[w % 2][tok] = di;
           left.v[w % 2][tok] = dv;
         }
+        dd = group_sum_swap(lane_sum<16>(dd));
+        if (l == 0) left.d[w] = dd;
       }
     } else if (w < 7) {   // M, and the sums of Z
 #pragma unroll
       for (int s = 0; s < 4; ++s) mma32(kb, XT::row(LY, 32 * ti + c, s, h), XT::row(LX, tok, s, h));
       if (pb == nb - 1) {
         const float dt = sc[2 * SC + tok];
-        const unsigned seen = ti > tj ? ~0u : from_on, at_tok = ti > tj ? 0u : from_on & ~behind;
-        float dd = 0.f, cz = 0.f, z[16];
-        decays_to(ti, tok, ti > tj, [&](int b, const f32x4& f) {
+        const uint64_t all = ti > tj ? whole : 0;
+        float cz = 0.f, z[16];
+        decays_to(ti, tok, ti > tj, dt, [&](int b, const f32x4& f) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int y = 4 * b + e;
-            dd += keep_if(kb[y], at_tok, y);
-            const float m = keep_if(kb[y] * f[e] * dt, seen, y);
+            const float m = keep_lanes(kb[y] * f[e], DIAGONAL.from[y] | all);
             W[y] += m;
-            z[y] = keep_if(m * ka[y], seen & ~at_tok, y);
+            z[y] = keep_lanes(m * ka[y], DIAGONAL.behind[y] | all);
             cz += z[y];
           }
         });
@@ -330,8 +329,6 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         }
         cz = half_sum(cz);
         if (h == 0) left.col[ti][tok] = cz;
-        dd = group_sum_swap(lane_sum<16>(dd));
-        if (l == 0 && ti == tj) left.d[ti] = dd;
       }
     }
     if (pb == nb - 1) {

@@ -259,9 +259,6 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 #pragma unroll
     for (int s = 0; s < NS; ++s) StateRows<T, N>::store(p, s, f[s]);
   };
-  unsigned up_to = 0;   // of a tile on the diagonal, the elements j up to this lane's i
-#pragma unroll
-  for (int e = 0; e < 16; ++e) up_to |= res_row(e, l / 32) <= l % 32 ? 1u << e : 0u;
   auto state_frags = [&](Frag<T> (&f)[NS]) {
 #pragma unroll
     for (int s = 0; s < NS; ++s) f[s] = frag_of<T>(st[s / 2], s % 2);
@@ -379,7 +376,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 const float v = cb[j][4 * q + e] * f[e];
-                cb[j][4 * q + e] = j < i ? v : keep_if(v, up_to, 4 * q + e);
+                cb[j][4 * q + e] = j < i ? v : keep_lanes(v, ~DIAGONAL.behind[4 * q + e]);   // j <= i, a lane per i
               }
             }
         };
