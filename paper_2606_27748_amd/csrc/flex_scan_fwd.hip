@@ -39,7 +39,7 @@ __device__ __forceinline__ void split3(Frag<float> (&t)[1], const float (&x)[8])
   for (int j = 0; j < 8; ++j) t[0].v[j] = x[j];
 }
 
-// u = rows^T (w x) over a chunk: x as its columns' operands, w of the tokens in LDS
+// u += rows^T (w x) over a chunk: x as its columns' operands, w of the tokens in LDS
 template <class T, int N>
 __device__ __forceinline__ void form_rows(f32x16 (&u)[N / 32], const char* rows, const Frag<T> (&xf)[4], const float* w, int l) {
   const int h = l / 32;
@@ -59,7 +59,6 @@ __device__ __forceinline__ void form_rows(f32x16 (&u)[N / 32], const char* rows,
     for (int t = TERMS - 1; t >= 0; --t)
 #pragma unroll
       for (int i = 0; i < N / 32; ++i) {
-        if (q == 0 && t == TERMS - 1) u[i] = zero16();
         mma32(u[i], bf[i], wx[t]);
       }
   }
@@ -151,12 +150,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     Frag<T> xf[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) xf[q] = XT::colp(LX, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 0, x);
-    f32x16 u[NT];
-    form_rows<T, N>(u, L, xf, sc, x);
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) st[i][e] += u[i][e];
+    form_rows<T, N>(st, L, xf, sc, x);
     if (BUFS == 1) {
       sync_lds();
       if (k + 1 < nchunks) stage(k + 1, next);
@@ -318,12 +312,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     auto advance = [&]() {   // S <- e^{L_63} S + B^T (w x)
       Frag<T> xf[4];
       columns(xf);
-      f32x16 u[NT];
-      form_rows<T, N>(u, L, xf, sc + (Y ? SC : 0), x);
 #pragma unroll
       for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) st[i][e] = __builtin_fmaf(st[i][e], last, u[i][e]);
+        for (int e = 0; e < 16; ++e) st[i][e] *= last;
+      form_rows<T, N>(st, L, xf, sc + (Y ? SC : 0), x);
     };
     Frag<T> sb[NS];
     state_frags(sb);
