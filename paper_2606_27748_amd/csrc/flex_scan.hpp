@@ -175,8 +175,9 @@ __device__ __forceinline__ float row_sum4(float x) {
 __device__ __forceinline__ double wave_scan(double x) {
   auto step = [&](auto ctrl, auto rows) {
     const uint64_t v = __builtin_bit_cast(uint64_t, x);
-    const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
-    const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(v >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    constexpr bool whole = decltype(rows)::value == 0xf;   // lanes without a source have a zero, without an instruction for it
+    const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, whole);
+    const unsigned hi = __builtin_amdgcn_update_dpp(0, (int)(unsigned)(v >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xf, whole);
     x += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
   };
   using std::integral_constant;

@@ -64,24 +64,23 @@ __device__ __forceinline__ void form_rows(f32x16 (&u)[N / 32], const char* rows,
   }
 }
 
+// NaN from the first NaN or infinity on, else zero
 __device__ __forceinline__ bool not_finite(const Frag<__bf16> (&x)[4]) {
-  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-  u16x2 top = {0, 0};
+  float s[2] = {0.f, 0.f};
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const u32x4 v = __builtin_bit_cast(u32x4, x[q].v);
+  for (int q = 0; q < 4; ++q)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[j] & 0x7fff7fffu));
-  }
-  return top[0] >= 0x7f80 || top[1] >= 0x7f80;
+    for (int j = 0; j < 8; j += 2)
+      s[q % 2] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{x[q].v[j], x[q].v[j + 1]}, bf16x2{(__bf16)0.f, (__bf16)0.f}, s[q % 2], false);
+  return !(s[0] + s[1] == 0.f);
 }
 __device__ __forceinline__ bool not_finite(const Frag<float> (&x)[4]) {
-  float s = 0.f;   // NaN from the first NaN or infinity on
+  float s = 0.f;
 #pragma unroll
   for (int q = 0; q < 4; ++q)
 #pragma unroll
     for (int j = 0; j < 8; ++j) s = __builtin_fmaf(x[q].get(j), 0.f, s);
-  return s != 0.f;
+  return !(s == 0.f);
 }
 }  // namespace
 
