@@ -81,11 +81,11 @@ int norm_rows(const flex_norm_desc* d) {
   const int64_t n = kNormWaves * 64 / (d->D / 8);
   return (int)(n < 1 ? 1 : n > d->T ? (d->T > 0 ? d->T : 1) : n);
 }
-// Rows of a workgroup of the backward at a time, which leaves one row of partial sums of dW: of rows that up to a wave's lanes
-// have. Wider ones leave a row of sums for each that is walked.
+// Rows of a workgroup of the backward at a time, which leaves one row of partial sums of dW: of rows that up to a wave's
+// lanes have, a piece each.  Wider ones leave a row of sums for each that is walked.
 int norm_wg_rows(const flex_norm_desc* d) {
   const int64_t lanes = (int64_t)norm_team(d->group) * (d->D / d->group);
-  return lanes <= 64 ? (int)(256 / lanes) : 1;
+  return lanes <= 64 && d->group <= 64 * 8 ? (int)(256 / lanes) : 1;
 }
 int norm_parts(const flex_norm_desc* d) {
   const int r = norm_wg_rows(d);

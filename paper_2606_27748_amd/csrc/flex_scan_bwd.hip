@@ -24,9 +24,9 @@ void launch_scan_states(const ScanArgs& a, bool bf16, hipStream_t st);
 // the rows of dB and dC of 32 tokens and 32 elements n (N = 64: the upper four); the lower four form dx of 32
 // tokens and columns each, three of the others the tiles of M and the sums of Z; the last one forms the
 // decays of the next head and puts out dg and ddt of the one before.  A lane is a token j throughout (of M too).
-// Bound by what each wave does one after the other between two barriers, some 9700 clocks a head of 64 columns and chunk (the tiles
-// of M are the longest), with two waves a SIMD: the registers hold no more, nor does LDS a second workgroup.  16384 tokens, 64
-// heads of 64, N = 128, bf16: 337 us (0.95 GB, S and dS more than half of it).
+// Bound by what each wave does one after the other between two barriers, vector instructions above all (4.5 us a head of 64 columns
+// and chunk), with two waves a SIMD: the registers hold no more, nor does LDS a second workgroup.  16384 tokens, 64
+// heads of 64, N = 128, bf16: 290 us (0.95 GB, S and dS more than half of it).
 template <class T, int N>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_grad(ScanArgs a) {
   using S = typename Io<T>::type;
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     asm volatile("" : "+s"(whole));
     if (w < 4) {   // dx of 32 of the block's columns
       const int p0 = 32 * (w % 2), tok = 32 * tx + c;
-      const float dt = sc[2 * SC + tok], vj = sc[4 * SC + tok];
+      const float dt = sc[2 * SC + tok], vj = sc[4 * SC + tok], dtv = dt * vj;
       f32x16 xa = zero16(), xv = zero16();
 #pragma unroll
       for (int s = 0; s < N / 16; ++s) mma32(xv, ST::row(LD, p0, s, x), RT::row(LB, tok, s, h));
@@ -282,11 +282,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         const Frag<T> xr = XT::row(LX, tok, p0 / 16 + s, h), yr = XT::row(LY, tok, p0 / 16 + s, h);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float p = xa[8 * s + j], v = vj * xv[8 * s + j];
+          const float p = xa[8 * s + j], v = xv[8 * s + j];
           di = __builtin_fmaf(p, xr.get(j), di);
           dv = __builtin_fmaf(v, xr.get(j), dv);
           dd = __builtin_fmaf(yr.get(j), xr.get(j), dd);
-          o[s][j] = __builtin_fmaf(dt, p + v, Dh * yr.get(j));
+          o[s][j] = __builtin_fmaf(dt, p, __builtin_fmaf(dtv, v, Dh * yr.get(j)));
         }
       }
       store_rows<T>(rx, 32 * tx, a.dxs, [&](int s, int j) { return o[s][j]; });
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         dv = half_sum(dv);
         if (h == 0) {
           left.i[w % 2][tok] = di;
-          left.v[w % 2][tok] = dv;
+          left.v[w % 2][tok] = dv * vj;
         }
         dd = group_sum_swap(lane_sum<16>(dd));
         if (l == 0) left.d[w] = dd;

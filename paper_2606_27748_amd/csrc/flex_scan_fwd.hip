@@ -90,7 +90,7 @@ __device__ __forceinline__ bool not_finite(const Frag<float> (&x)[4]) {
 // taken from the last one, so that their weights are known and the sum has no decay in it.
 // The segment that nothing starts from is left out, and of the first one state0 is a part.
 // Bound by the vector instructions that form the weighted rows' terms, between the products of two waves a SIMD: 17152 tokens in 16
-// prompts, 64 heads of 64, N = 128, bf16: 75 us (141 MB of x).  With one buffer and two workgroups a CU 99.
+// prompts, 64 heads of 64, N = 128, bf16: 73 us (141 MB of x).  With one buffer and two workgroups a CU 99.
 template <class T, int N, bool REV>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_carry(ScanArgs a) {
   using S = typename Io<T>::type;
@@ -179,8 +179,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 // 32 columns a wave and eight waves: two a SIMD, with S, C B^T and the terms of a chunk in 256 registers each, and the rows of B and C
 // are read from memory once for eight of them.  A wave's chunk is 94 matrix instructions (N = 128, 3000 clocks) and some
 // 9000 clocks of vector instructions: decays, three terms of each weighted row, roundings.  Both waves of a SIMD are at the
-// same place of a chunk and hardly overlap; a wave of 64 columns by itself on a SIMD takes as long (200 us to these 195), C B^T
-// formed once for all heads beforehand costs more than it saves (162 and 47).  The prompts above: 195 us (281 MB of x and y).
+// same place of a chunk and hardly overlap; a wave of 64 columns by itself on a SIMD takes as long (3 % more), C B^T
+// formed once for all heads beforehand costs more than it saves (162 and 47 us for 195).  The prompts above: 188 us (281 MB of x and y).
 template <class T, int N, int MODE>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_sweep(ScanArgs a) {
   using S = typename Io<T>::type;

@@ -92,6 +92,20 @@ def test_sizes():
     assert _size("flex_scan_workspace_size", d, F.FLEX_PASS_AWD)[0] == BAD
 
 
+@pytest.mark.parametrize("T", [0, 1, 300, 100000])
+def test_norm_sums_of_every_width(T):
+    """A row of partial sums for each row that is walked, or for each workgroup of rows that a wave's lanes hold, a piece of 8
+    channels each."""
+    for group, D in ((8, 8), (24, 24), (24, 72), (512, 512), (520, 520), (1048, 1048), (1024, 1024), (2056, 2056), (8192, 8192), (40, 360)):
+        team = 1
+        while team < group // 8 and team < 64:
+            team *= 2
+        rows = max(1, min(T, 4096 * 64 // (D // 8)))
+        if group <= 512 and team * (D // group) <= 64:
+            rows = max(1, min(-(-T // (256 // (team * (D // group)))), 1024))
+        assert _size("flex_norm_workspace_size", F.make_norm_desc(T, D, group)) == (OK, rows * D * 4), (group, D)
+
+
 @pytest.mark.skipif(not NO_GPU, reason="fake pointers are only passed where no GPU is visible")
 def test_calls_are_refused():
     lib, big = F.load(), 1 << 40
