@@ -138,9 +138,9 @@ int32_t check_scan(const flex_scan_desc* d, bool step) {
 
 // Tokens of a segment.  A sweep's workgroup takes a CU, its sequences are walked in order, and a
 // segment that is not its sequence's last has its rows read twice: segments so long that the card has one
-// workgroup per CU of them, 64 to 4096 tokens (a prompt of 32768 tokens, 16 heads of 128: 213 us; with twice as many
-// 237).  Many sequences, whose ends leave workgroups of any length, have twice as many (16 prompts of 17152 tokens, 64 heads
-// of 64: 295 us; with one per CU 315).
+// workgroup per CU of them, 64 to 4096 tokens (a prompt of 32768 tokens, 16 heads of 128: 207 us; with twice as many
+// 235).  Many sequences, whose ends leave workgroups of any length, have twice as many (16 prompts of 17152 tokens, 64 heads
+// of 64: 274 us; with one per CU 277).
 int scan_seg(const flex_scan_desc* d) {
   const int64_t sets = d->H / scan_heads(d), wgs = d->B * sets < 128 ? 256 : 512;
   int64_t n = ceil_div((int64_t)d->T * sets, wgs * SCAN_CHUNK) * SCAN_CHUNK;

@@ -134,12 +134,12 @@ struct StateRows {
 };
 
 // Stages 64 rows of a window by `nw` waves of which this is w, 16 rows at a time.
-template <class T, int D, class Lane = ThisLane>
+template <class T, int D>
 __device__ __forceinline__ void stage_rows(const char* L, const typename Io<T>::type* base, size_t row0, int stride, int n, int w,
-                                           int nw, Lane lane = {}) {
+                                           int nw) {
   for (int k = w; k < 4; k += nw)
     stage_tile<T, D, 16, 1>(L + k * 16 * D * (int)sizeof(T), row_words(base, row0 + 16 * k, stride, n - 16 * k, D),
-                            stride * (int)sizeof(T), 0, lane);
+                            stride * (int)sizeof(T), 0);
 }
 
 // Lanes (column l % 32) for which element e of a tile is a row from their column on, or behind it

@@ -24,9 +24,9 @@ void launch_scan_states(const ScanArgs& a, bool bf16, hipStream_t st);
 // the rows of dB and dC of 32 tokens and 32 elements n (N = 64: the upper four); the lower four form dx of 32
 // tokens and columns each, three of the others the tiles of M and the sums of Z; the last one forms the
 // decays of the next head and puts out dg and ddt of the one before.  A lane is a token j throughout (of M too).
-// Bound by what each wave does one after the other between two barriers, vector instructions above all (4.5 us a head of 64 columns
+// Bound by what each wave does one after the other between two barriers, vector instructions above all (4.3 us a head of 64 columns
 // and chunk), with two waves a SIMD: the registers hold no more, nor does LDS a second workgroup.  16384 tokens, 64
-// heads of 64, N = 128, bf16: 290 us (0.95 GB, S and dS more than half of it).
+// heads of 64, N = 128, bf16: 275 us (0.95 GB, S and dS more than half of it).
 template <class T, int N>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_grad(ScanArgs a) {
   using S = typename Io<T>::type;
@@ -79,15 +79,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   auto block = [&](int it) { return lds + 2 * ROWS + (BUFS == 2 ? (it & 1) * BLOCK : 0); };
   auto state_at = [&](int it) { return (((size_t)slot * a.H + head0 + it / nb) * a.P + it % nb * 64) * N; };
   auto stage = [&](int it) {
-    const LaneOf x{again()};
     const size_t xcol = (size_t)(head0 + it / nb) * a.P + it % nb * 64;
     const char* L = block(it);
     if (w < 4)
-      stage_rows<T, 64>(L, static_cast<const S*>(a.X) + xcol, row0, a.xs, n, w, 4, x);
+      stage_rows<T, 64>(L, static_cast<const S*>(a.X) + xcol, row0, a.xs, n, w, 4);
     else
-      stage_rows<T, 64>(L + XROWS, static_cast<const S*>(a.dY) + xcol, row0, a.H * a.P, n, w - 4, 4, x);
-    stage_linear<ROWS / 1024, 8>(L + 2 * XROWS, static_cast<const S*>(a.st) + state_at(it), w, x);
-    if (!ONE) stage_linear<ROWS / 1024, 8>(L + 2 * XROWS + ROWS, static_cast<const S*>(a.dst) + state_at(it), w, x);
+      stage_rows<T, 64>(L + XROWS, static_cast<const S*>(a.dY) + xcol, row0, a.H * a.P, n, w - 4, 4);
+    stage_linear<ROWS / 1024, 8>(L + 2 * XROWS, static_cast<const S*>(a.st) + state_at(it), w);
+    if (!ONE) stage_linear<ROWS / 1024, 8>(L + 2 * XROWS + ROWS, static_cast<const S*>(a.dst) + state_at(it), w);
   };
   float gn = 0.f, dn = 0.f;   // of the next head, lane = token
   auto fetch = [&](int hd) {
@@ -171,8 +170,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     }
     if (BUFS == 1 || it > 0) sync_tiles();
     if (BUFS == 2 && it + 1 < items) stage(it + 1);
-    const int x = again();
-    const int c = x % 32, h = x / 32, tok = 32 * tj + c;
+    // fp32 rows of N = 128 have no registers for places that are kept over the loop
+    const int x = BF ? l : again(), c = x % 32, h = x / 32, tok = 32 * tj + c;
     const char* LX = block(it);
     const char* LY = LX + XROWS;
     const char* LS = LY + XROWS;

@@ -385,21 +385,13 @@ __device__ __forceinline__ void sync_tiles() {
 // builtin's before the next transposed read of any LDS, does not count them, so
 // wait_lds_loads / sync_tiles must come between them and the reads of the tile.  The LDS address is m0's, an
 // operand, so that the compiler writes it and knows what it holds; one wait state lies between that and its use.
-// lane() is the lane, where a caller wants it formed in its own way.
-struct ThisLane {
-  __device__ __forceinline__ int operator()() const { return threadIdx.x % WAVE; }
-};
-struct LaneOf {
-  int l;
-  __device__ __forceinline__ int operator()() const { return l; }
-};
-template <class T, int D, int ROWS, int NW, class Lane = ThisLane>
-__device__ __forceinline__ void stage_tile(const char* L, u32x4 rs, int stride_bytes, int w, Lane lane = {}) {
+template <class T, int D, int ROWS, int NW>
+__device__ __forceinline__ void stage_tile(const char* L, u32x4 rs, int stride_bytes, int w) {
   using RT = RowTile<T, D>;
   constexpr int PER = 1024 / RT::ROW;          // rows per wave and instruction
   static_assert(PER >= 1 && ROWS % PER == 0, "rows of a staged tile");
   constexpr int STEPS = ROWS / PER;
-  const int l = lane();
+  const int l = threadIdx.x % WAVE;
   const int lr = l / RT::CH, lc = l % RT::CH;
   const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) const char*)L;
 #pragma unroll
@@ -416,8 +408,8 @@ __device__ __forceinline__ void stage_tile(const char* L, u32x4 rs, int stride_b
 }
 
 // Linear copy of 1024 N bytes to LDS, one instruction per 1024 bytes, by NW waves.
-template <int N, int NW, class Lane = ThisLane>
-__device__ __forceinline__ void stage_linear(const char* L, const void* src, int w, Lane lane = {}) {
+template <int N, int NW>
+__device__ __forceinline__ void stage_linear(const char* L, const void* src, int w) {
   u32x4 d;
   const uint64_t p = reinterpret_cast<uint64_t>(src);
   d[0] = __builtin_amdgcn_readfirstlane((unsigned)p);
@@ -425,7 +417,7 @@ __device__ __forceinline__ void stage_linear(const char* L, const void* src, int
   d[2] = N * 1024;
   d[3] = BUF_FLAGS;
   const unsigned base = (unsigned)(size_t)(__attribute__((address_space(3))) const char*)L;
-  const int l = lane();
+  const int l = threadIdx.x % WAVE;
 #pragma unroll
   for (int n = 0; n < (N + NW - 1) / NW; ++n) {
     const int step = n * NW + w;
