@@ -90,7 +90,7 @@ __device__ __forceinline__ bool not_finite(const Frag<float> (&x)[4]) {
 // taken from the last one, so that their weights are known and the sum has no decay in it.
 // The segment that nothing starts from is left out, and of the first one state0 is a part.
 // Bound by the vector instructions that form the weighted rows' terms, between the products of two waves a SIMD: 17152 tokens in 16
-// prompts, 64 heads of 64, N = 128, bf16: 73 us (141 MB of x).  With one buffer and two workgroups a CU 99.
+// prompts, 64 heads of 64, N = 128, bf16: 72 us (141 MB of x).  With one buffer and two workgroups a CU 99.
 template <class T, int N, bool REV>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_carry(ScanArgs a) {
   using S = typename Io<T>::type;
@@ -135,9 +135,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   fetch(REV ? 0 : nchunks - 1);
   for (int k = 0; k < nchunks; ++k) {
     const int next = REV ? k + 1 : nchunks - 2 - k;
-    int x = l;   // places in LDS are formed anew: kept over the loop they would take the registers that it is short of
-    asm volatile("" : "+v"(x));
-    const int h = x / 32;
+    const int h = l / 32;
     const char* L = buf(k);
     sync_tiles();   // the chunk is in LDS, and the buffer of the one before is free
     if (BUFS == 2 && k + 1 < nchunks) stage(k + 1, next);
@@ -148,8 +146,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     const char* LX = L + ROWS + w * XROWS;
     Frag<T> xf[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) xf[q] = XT::colp(LX, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 0, x);
-    form_rows<T, N>(st, L, xf, sc, x);
+    for (int q = 0; q < 4; ++q) xf[q] = XT::colp(LX, 16 * q + 4 * h, 16 * q + 8 + 4 * h, 0, l);
+    form_rows<T, N>(st, L, xf, sc, l);
     if (BUFS == 1) {
       sync_lds();
       if (k + 1 < nchunks) stage(k + 1, next);
@@ -270,8 +268,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   for (int k = 0; k < nchunks; ++k) {
     const int chunk = REV ? nchunks - 1 - k : k, next = REV ? chunk - 1 : chunk + 1;
     const char* L = buf(k);
-    int x = l;   // as above
-    asm volatile("" : "+v"(x));
+    int x = l;
+    if (Y) asm volatile("" : "+v"(x));   // places in LDS are formed anew: kept over the loop they take more registers than there are
     const int c = x % 32, h = x / 32;
     sync_tiles_but<LATER>();   // the chunk is in LDS, and the buffer of the one before is free
     if (BUFS == 2 && k + 1 < nchunks) stage(k + 1, next);
