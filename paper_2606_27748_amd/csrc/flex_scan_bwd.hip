@@ -40,7 +40,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   constexpr int BLOCK = 2 * XROWS + (ONE ? 1 : 2) * ROWS, BUFS = 2 * ROWS + 2 * BLOCK <= 144 * 1024 ? 2 : 1;
   __shared__ __attribute__((aligned(16))) char lds[2 * ROWS + BUFS * BLOCK];
   // of a head, two in turn: decays as factors from a half's middle (or L, hi and lo), dt, e^L, v; whether they are
-  // factors, that from one middle to the other, the whole decay
+  // factors, that from one middle to the other, the whole decay, D
   __shared__ __attribute__((aligned(16))) float scal[2][6 * SC + 4];
   // what the waves leave for dg and ddt
   struct Dots {
@@ -88,9 +88,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     stage_linear<ROWS / 1024, 8>(L + 2 * XROWS, static_cast<const S*>(a.st) + state_at(it), w);
     if (!ONE) stage_linear<ROWS / 1024, 8>(L + 2 * XROWS + ROWS, static_cast<const S*>(a.dst) + state_at(it), w);
   };
-  float gn = 0.f, dn = 0.f;   // of the next head, lane = token
+  float gn = 0.f, dn = 0.f, Dn = 0.f;   // of the next head, lane = token
   auto fetch = [&](int hd) {
     const int l = again();
+    if (a.D) Dn = a.D[head0 + hd];
     if (l < n) {
       const size_t at = (size_t)(row0 + l) * a.H + head0 + hd;
       gn = a.g[at];
@@ -114,6 +115,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
       sc[6 * SC] = product ? 1.f : 0.f;
       sc[6 * SC + 1] = __builtin_amdgcn_exp2f((float)(m1 - m0));
       sc[6 * SC + 2] = __builtin_amdgcn_exp2f((float)d.end);
+      sc[6 * SC + 3] = Dn;
     }
   };
   // dg, ddt and the chunk's part of dD of a head, by one wave; lane = token
@@ -168,7 +170,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
       sync_lds();   // what was staged before is no longer read
       stage(it);
     }
-    if (BUFS == 1 || it > 0) sync_tiles();
+    // the block is in LDS; the stores of dx, behind its loads, may be on their way
+    if (BUFS == 2 && w < 4)
+      sync_tiles_but<BF ? 2 : 4>();
+    else
+      sync_tiles();
     if (BUFS == 2 && it + 1 < items) stage(it + 1);
     // fp32 rows of N = 128 have no registers for places that are kept over the loop
     const int x = BF ? l : again(), c = x % 32, h = x / 32, tok = 32 * tj + c;
@@ -273,7 +279,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
           for (int s = 0; s < 2; ++s)
             mma32(xa, XT::colp(LY, 32 * i + 16 * s + 4 * h, 32 * i + 16 * s + 8 + 4 * h, p0, x), frag_of<T>(q, s));
         }
-        const float Dh = a.D ? a.D[head] : 0.f;
+      const float Dh = sc[6 * SC + 3];   // not from memory: its wait would be one for the block that is on its way
       const auto rx = row_window(static_cast<S*>(a.dX) + (size_t)head * a.P + pb * 64 + p0, row0, a.dxs, n, 32);
       float o[2][8];
 #pragma unroll

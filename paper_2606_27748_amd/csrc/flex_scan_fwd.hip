@@ -90,7 +90,7 @@ __device__ __forceinline__ bool not_finite(const Frag<float> (&x)[4]) {
 // taken from the last one, so that their weights are known and the sum has no decay in it.
 // The segment that nothing starts from is left out, and of the first one state0 is a part.
 // Bound by the vector instructions that form the weighted rows' terms, between the products of two waves a SIMD: 17152 tokens in 16
-// prompts, 64 heads of 64, N = 128, bf16: 72 us (141 MB of x).  With one buffer and two workgroups a CU 99.
+// prompts, 64 heads of 64, N = 128, bf16: 71 us (141 MB of x).  With one buffer and two workgroups a CU 99.
 template <class T, int N, bool REV>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_carry(ScanArgs a) {
   using S = typename Io<T>::type;
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 // are read from memory once for eight of them.  A wave's chunk is 94 matrix instructions (N = 128, 3000 clocks) and some
 // 9000 clocks of vector instructions: decays, three terms of each weighted row, roundings.  Both waves of a SIMD are at the
 // same place of a chunk and hardly overlap; a wave of 64 columns by itself on a SIMD takes as long (3 % more), C B^T
-// formed once for all heads beforehand costs more than it saves (162 and 47 us for 195).  The prompts above: 188 us (281 MB of x and y).
+// formed once for all heads beforehand costs more than it saves (162 and 47 us for 195).  The prompts above: 180 us (281 MB of x and y).
 template <class T, int N, int MODE>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_sweep(ScanArgs a) {
   using S = typename Io<T>::type;
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     for (int s = 0; s < NS; ++s) f[s] = frag_of<T>(st[s / 2], s % 2);
   };
   // stores of a step, behind its loads
-  constexpr int LATER = BUFS == 1 ? 0 : Y ? (BF ? 4 : 8) : (BF ? NS : 2 * NS);
+  constexpr int LATER = BUFS == 1 ? 0 : (Y ? (BF ? 4 : 8) : 0) + (MODE == SWEEP ? 0 : BF ? NS : 2 * NS);
 
   float* sc = scal[w];
   const float Dh = Y && a.D ? a.D[head] : 0.f;
@@ -263,8 +263,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     const int first = REV ? nchunks - 1 : 0;
     stage(0, first);
     fetch(first);
-    wait_lds_loads();
   }
+  // on every way to the loop: where a state's loads are not known to have arrived, the compiler waits for them at their first
+  // use in every chunk, and so for the rows that are on their way
+  wait_lds_loads();
   for (int k = 0; k < nchunks; ++k) {
     const int chunk = REV ? nchunks - 1 - k : k, next = REV ? chunk - 1 : chunk + 1;
     const char* L = buf(k);
