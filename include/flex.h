@@ -500,7 +500,8 @@ int32_t flex_scan_fwd(const flex_scan_desc* desc, const void* X, const void* Bt,
  *   saved             written by the forward of the same descriptor and inputs
  *   dY [T,H,P]        io_dtype
  *   dX [T,H,P], dB, dC [T,G,N], ddt, dg [T,H]   io_dtype outputs: the rows of the sequences are
- *                     overwritten.  dt's and g's are those of independent inputs.
+ *                     overwritten.  dt's and g's are those of independent inputs; dg is zero where g is
+ *                     below -1000.
  *   dD [H] fp32       output, or NULL
  * A group's dB and dC are sums over its heads, in fp32 and in a fixed order.  With FLEX_BF16 the products that a result
  * sums have operands rounded to bf16 once (a state with its gradient in dg both).  What is not finite in a

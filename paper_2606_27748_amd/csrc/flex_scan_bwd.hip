@@ -24,9 +24,9 @@ void launch_scan_states(const ScanArgs& a, bool bf16, hipStream_t st);
 // the rows of dB and dC of 32 tokens and 32 elements n (N = 64: the upper four); the lower four form dx of 32
 // tokens and columns each, three of the others the tiles of M and the sums of Z; the last one forms the
 // decays of the next head and puts out dg and ddt of the one before.  A lane is a token j throughout (of M too).
-// Bound by what each wave does one after the other between two barriers, vector instructions above all (4.3 us a head of 64 columns
-// and chunk), with two waves a SIMD: the registers hold no more, nor does LDS a second workgroup.  16384 tokens, 64
-// heads of 64, N = 128, bf16: 275 us (0.95 GB, S and dS more than half of it).
+// Bound by memory and by the waves in turn: with two waves a SIMD (registers and LDS hold no more) only the next block is on its
+// way while one is worked on.  16384 tokens, 64 heads of 64, N = 128, bf16: 275 us (0.95 GB, S and dS more than
+// half of it), where the reads alone take 196 and the work on blocks that are at hand 234.
 template <class T, int N>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_grad(ScanArgs a) {
   using S = typename Io<T>::type;

@@ -175,10 +175,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 // state is its gradient dS, the rows are C's, x is dy and the weights are e^L:
 //   dS <- e^{L_63} dS + C^T (e^L dy)
 // 32 columns a wave and eight waves: two a SIMD, with S, C B^T and the terms of a chunk in 256 registers each, and the rows of B and C
-// are read from memory once for eight of them.  A wave's chunk is 94 matrix instructions (N = 128, 3000 clocks) and some
-// 9000 clocks of vector instructions: decays, three terms of each weighted row, roundings.  Both waves of a SIMD are at the
-// same place of a chunk and hardly overlap; a wave of 64 columns by itself on a SIMD takes as long (3 % more), C B^T
-// formed once for all heads beforehand costs more than it saves (162 and 47 us for 195).  The prompts above: 180 us (281 MB of x and y).
+// are read from memory once for eight of them.  A wave's chunk is 94 matrix instructions (N = 128; 3000 clocks of its SIMD)
+// and some 950 vector instructions (4000): decays, three terms of each weighted row, roundings.  It takes some 8200: both
+// waves of a SIMD are at the same place of a chunk, behind one barrier, and wait for LDS and for results at the same time.
+// A wave of 64 columns by itself on a SIMD takes 3 % longer, C B^T formed once for all heads beforehand costs more than it saves
+// (162 and 47 us for 195).  The prompts above: 180 us (281 MB of x and y).
 template <class T, int N, int MODE>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_sweep(ScanArgs a) {
   using S = typename Io<T>::type;

@@ -4,7 +4,7 @@ from __future__ import annotations
 
 import torch
 
-from tests.seq_util import BF16, F32, offsets
+from tests.seq_util import BF16, offsets
 
 U32 = 2.0 ** -24   # half a step of fp32, relative to the value
 
