@@ -83,6 +83,7 @@ int norm_rows(const flex_norm_desc* d) {
 }
 // Rows of a workgroup of the backward at a time, which leaves one row of partial sums of dW: of rows that up to a wave's
 // lanes have, a piece each.  Wider ones leave a row of sums for each that is walked.
+// (2^20 rows of 64 channels, bf16: backward 137 us, forward 76; with a row of sums each, and so 4096 rows at once, 261 and 194.)
 int norm_wg_rows(const flex_norm_desc* d) {
   const int64_t lanes = (int64_t)norm_team(d->group) * (d->D / d->group);
   return lanes <= 64 && d->group <= 64 * 8 ? (int)(256 / lanes) : 1;
