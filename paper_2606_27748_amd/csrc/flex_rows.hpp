@@ -68,18 +68,20 @@ __device__ __forceinline__ float dsilu(float z, float sig) { return sig * __buil
 struct RowSeq {
   int b, first, end;
 };
+// From what a search says: `cnt` sequences start at row t or before it, the last of them from row `first` on, the next one from row
+// `end`.  Where offsets fall the search may be wrong: a sequence that does not hold row t is none, for this row.
+__host__ __device__ inline RowSeq row_seq(int cnt, int first, int end, int B, int T, int t) {
+  const bool holds = cnt > 0 && first <= t && end > t;
+  RowSeq s;
+  s.b = holds ? cnt - 1 : -1;
+  s.first = first;
+  s.end = holds ? end : cnt == 0 ? (end > t ? end : t + 1) : cnt == B ? T : t + 1;
+  return s;
+}
 __device__ __forceinline__ RowSeq find_row(const int32_t* __restrict__ off, int B, int T, int t) {
   const int cnt = leading(B, [=](int b) { return clamp_off(off[b], T) <= t; });
-  RowSeq s;
-  s.b = cnt - 1;
-  s.first = __builtin_amdgcn_readfirstlane(clamp_off(off[max(cnt - 1, 0)], T));
-  s.end = __builtin_amdgcn_readfirstlane(clamp_off(off[cnt], T));
-  if (cnt == 0) s.end = max(s.end, t + 1);
-  if (cnt > 0 && s.end <= t) {
-    s.b = -1;
-    s.end = cnt == B ? T : t + 1;
-  }
-  return s;
+  return row_seq(cnt, __builtin_amdgcn_readfirstlane(clamp_off(off[max(cnt - 1, 0)], T)),
+                 __builtin_amdgcn_readfirstlane(clamp_off(off[cnt], T)), B, T, t);
 }
 
 }  // namespace flex
