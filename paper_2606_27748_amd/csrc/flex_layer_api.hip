@@ -118,6 +118,14 @@ int scan_heads(const flex_scan_desc* d) {
 }
 int64_t scan_slots(const flex_scan_desc* d, int rows) { return (int64_t)d->T / rows + d->B; }
 
+// Parts of a group's heads in the gradients, each a workgroup's: as many as give the card two workgroups per CU.
+int scan_parts(const flex_scan_desc* d) {
+  const int r = d->H / d->G;
+  const int64_t wgs = scan_slots(d, SCAN_CHUNK) * d->G;
+  int n = 1;
+  while (n < r && (r % (2 * n) == 0) && wgs * n < 512) n *= 2;
+  return n;
+}
 int32_t check_scan(const flex_scan_desc* d, bool step) {
   if (!d) return FLEX_ERR_INVALID_ARG;
   if (d->B <= 0 || d->T < 0 || d->G <= 0 || d->H <= 0 || d->N <= 0 || d->P <= 0) return FLEX_ERR_INVALID_ARG;
@@ -134,6 +142,8 @@ int32_t check_scan(const flex_scan_desc* d, bool step) {
   const int64_t states = (int64_t)d->B * d->H, slots = step ? 0 : scan_slots(d, SCAN_CHUNK);
   if (states * 4096 > kMaxThreads || slots * d->H * 512 > kMaxThreads || (int64_t)d->T + d->B >= (1LL << 30))
     return FLEX_ERR_INVALID_ARG;
+  // the gradients' chunks go by as many at once as there are XCDs
+  if (!step && ceil_div(slots, 8) * 8 * d->G * scan_parts(d) * 512 > kMaxThreads) return FLEX_ERR_INVALID_ARG;
   return FLEX_OK;
 }
 
@@ -159,14 +169,6 @@ size_t scan_tot_bytes(const flex_scan_desc* d) {
 }
 size_t scan_saved_bytes(const flex_scan_desc* d) {
   return (size_t)scan_slots(d, SCAN_CHUNK) * scan_state(d) * esize(d->io_dtype);
-}
-// Parts of a group's heads in the gradients, each a workgroup's: as many as give the card two workgroups per CU.
-int scan_parts(const flex_scan_desc* d) {
-  const int r = d->H / d->G;
-  const int64_t wgs = scan_slots(d, SCAN_CHUNK) * d->G;
-  int n = 1;
-  while (n < r && (r % (2 * n) == 0) && wgs * n < 512) n *= 2;
-  return n;
 }
 size_t scan_part_bytes(const flex_scan_desc* d) {
   return scan_parts(d) > 1 ? (size_t)scan_parts(d) * scan_slots(d, SCAN_CHUNK) * SCAN_CHUNK * d->G * d->N * sizeof(float) : 0;
