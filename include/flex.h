@@ -523,7 +523,8 @@ int32_t flex_scan_step(const flex_scan_desc* desc, const void* x, const void* Bt
  *     FLEX_GATE_NONE   y = x r(x) w
  *     FLEX_GATE_FIRST  y = u r(u) w,  u = x silu(z)
  *     FLEX_GATE_LAST   y = x r(x) w silu(z)
- * Every row is for itself: there are no sequences. */
+ * Every row is for itself: there are no sequences.  Finite rows whose mean square leaves fp32's range (eps of 0 or next
+ * to it, or values from 1e19 on) have it from scaled values; a row of zeros with eps 0 is 0 / 0. */
 typedef enum { FLEX_GATE_NONE = 0, FLEX_GATE_FIRST = 1, FLEX_GATE_LAST = 2 } flex_gate;
 typedef struct {
   int32_t T, D;           /* rows; channels                                        */

@@ -6,7 +6,8 @@
 // A team of lanes has a group: 8 channels a lane and piece, the pieces of a group TEAM * 8 channels
 // apart.  Teams stay on their channels, with their part of W (and the sum of dW) in registers, and go
 // from row to row, the next row on its way while one is worked on.  One pass over the data: bound by
-// memory.  bf16, forward of 17973 rows of 4096 channels, one group: 79 us (442 MB, 5.6 TB/s); forward and backward of 16384 rows of
+// memory.  Where a mean square leaves what fp32 holds, the row's sums are formed again from scaled values.
+// bf16, forward of 17973 rows of 4096 channels, one group: 79 us (442 MB, 5.6 TB/s); forward and backward of 16384 rows of
 // 2048 channels in groups of 128: 34.5 us (201 MB) and 55 us (335 MB, 6.1 TB/s), and 5 for the sum of dW.
 #include <type_traits>
 #include "flex_rows.hpp"
@@ -65,6 +66,17 @@ __device__ __forceinline__ void team_sum(float (&x)[N], int team, float (*box)[4
     for (int i = 0; i < N; ++i) x[i] = (box[turn * N + i][0] + box[turn * N + i][1]) + (box[turn * N + i][2] + box[turn * N + i][3]);
   }
 }
+
+// Mean squares from 2^-96 on have their squares' bits, and no sum behind infinity has.  Others (eps = 0 allows any) are formed
+// from values times a power of two, whose halves `half` are multiplied to the two factors of a product.
+constexpr float NORM_LOW = 0x1p-96f, NORM_HALF = 0x1p48f;
+__device__ __forceinline__ bool norm_plain(float mean) { return mean >= NORM_LOW && mean < INFINITY; }
+__device__ __forceinline__ float norm_half(float mean) { return mean < NORM_LOW ? NORM_HALF : 1.f / NORM_HALF; }
+// 1 / sqrt(mean + eps) of scaled values
+__device__ __forceinline__ float norm_rsq(float sum, float inv, float eps, float half) {
+  const float k = half * half;
+  return __builtin_amdgcn_rsqf(__builtin_fmaf(sum, inv, eps * k * k));
+}
 }  // namespace
 
 // Where a lane works: rows row0, row0 + step, ... and pieces at channels c + i * team * 8 of them
@@ -89,7 +101,7 @@ struct NormPlace {
 
 template <class S, int GATE, int PIECES, bool WG>
 __global__ __launch_bounds__(256) void k_norm_fwd(NormArgs a, int team, float inv) {
-  __shared__ float box[2][4];
+  __shared__ float box[3][4];
   const NormPlace p = NormPlace::of<WG>(a, team, false);
   if (p.row0 >= a.rows) return;   // never a part of a team
   Eight w[PIECES];
@@ -132,7 +144,34 @@ __global__ __launch_bounds__(256) void k_norm_fwd(NormArgs a, int team, float in
     }
     if (row + p.step < a.T) fetch(row + p.step);
     team_sum<WG>(sum, team, box, turn);
-    const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[0], inv, a.eps));
+    const float mean = __builtin_fmaf(sum[0], inv, a.eps);
+    float r = __builtin_amdgcn_rsqf(mean);
+    if (!norm_plain(mean)) {
+      const float half = norm_half(mean);
+      sum[0] = 0.f;
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i)
+        if (in[i]) {
+          // the present row again: its X and Z are no longer in registers, and u may have lost what the factors have
+          Raw8<S> rx, rz;
+          Eight x, z;
+          const int c = p.c + i * p.team * 8;
+          rx.load(static_cast<const S*>(a.X) + (size_t)row * a.xs + c, true);
+          rx.get(x);
+          if (GATE == FLEX_GATE_FIRST) {
+            rz.load(static_cast<const S*>(a.Z) + (size_t)row * a.zs + c, true);
+            rz.get(z);
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float s = GATE == FLEX_GATE_FIRST ? z.v[e] * sigmoid(z.v[e]) : 1.f;
+            u[i].v[e] = (x.v[e] * half) * (s * half);
+            sum[0] = __builtin_fmaf(u[i].v[e], u[i].v[e], sum[0]);
+          }
+        }
+      team_sum<WG>(sum, team, box + 2, 0);
+      r = norm_rsq(sum[0], inv, a.eps, half);
+    }
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
 #pragma unroll
@@ -149,7 +188,7 @@ __global__ __launch_bounds__(256) void k_norm_fwd(NormArgs a, int team, float in
 // row that is walked has its own.
 template <class S, int GATE, int PIECES, bool WG, bool NARROW>
 __global__ __launch_bounds__(256) void k_norm_bwd(NormArgs a, int team, float inv) {
-  __shared__ float box[4][4];
+  __shared__ float box[6][4];
   __shared__ float sums[NARROW ? 256 * 8 : 1];
   const NormPlace p = NormPlace::of<WG>(a, team, NARROW);
   if (!NARROW && p.row0 >= a.rows) return;
@@ -200,29 +239,54 @@ __global__ __launch_bounds__(256) void k_norm_bwd(NormArgs a, int team, float in
     }
     if (row + p.step < a.T) fetch(row + p.step);
     team_sum<WG>(sum, team, box, turn);
-    const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[0], inv, a.eps));
-    const float m = sum[1] * r * inv;   // mean(dn n)
+    const float mean = __builtin_fmaf(sum[0], inv, a.eps);
+    // the row's gradients, with r for values scaled by half^2
+    auto put = [&](auto scaled, float half, float r) {
+      constexpr bool SCALED = decltype(scaled)::value;
+      const float m = sum[1] * r * inv;   // mean(dn n)
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      Eight dz;
+      for (int i = 0; i < PIECES; ++i) {
+        Eight dz;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float s = GATE != FLEX_GATE_NONE ? z[i].v[e] * sig[i].v[e] : 1.f;
-        const float ds = GATE != FLEX_GATE_NONE ? dsilu(z[i].v[e], sig[i].v[e]) : 0.f;
-        const float n = (GATE == FLEX_GATE_FIRST ? x[i].v[e] * s : x[i].v[e]) * r;
-        const float gn = g[i].v[e] * n;
-        float dn = g[i].v[e] * w[i].v[e];
-        if (GATE == FLEX_GATE_LAST) dn *= s;
-        const float du = r * (dn - n * m);
-        dw[i].v[e] += GATE == FLEX_GATE_LAST ? gn * s : gn;
-        dz.v[e] = (GATE == FLEX_GATE_FIRST ? du * x[i].v[e] : gn * w[i].v[e]) * ds;
-        x[i].v[e] = GATE == FLEX_GATE_FIRST ? du * s : du;
+        for (int e = 0; e < 8; ++e) {
+          const float s = GATE != FLEX_GATE_NONE ? z[i].v[e] * sig[i].v[e] : 1.f;
+          const float ds = GATE != FLEX_GATE_NONE ? dsilu(z[i].v[e], sig[i].v[e]) : 0.f;
+          const float xk = SCALED ? x[i].v[e] * half : x[i].v[e], sk = SCALED ? s * half : s;
+          const float n = (GATE == FLEX_GATE_FIRST ? xk * sk : SCALED ? xk * half : xk) * r;
+          const float gn = g[i].v[e] * n;
+          float dn = g[i].v[e] * w[i].v[e];
+          if (GATE == FLEX_GATE_LAST) dn *= s;
+          float du = r * (dn - n * m);
+          if (SCALED) du *= half;   // and by half once more below
+          dw[i].v[e] += GATE == FLEX_GATE_LAST ? gn * s : gn;
+          dz.v[e] = (GATE == FLEX_GATE_FIRST ? du * xk : gn * w[i].v[e]) * ds;
+          x[i].v[e] = GATE == FLEX_GATE_FIRST ? du * sk : SCALED ? du * half : du;
+        }
+        const int c = p.c + i * p.team * 8;
+        if (in[i]) {
+          Raw8<S>::store(static_cast<S*>(a.dX) + (size_t)row * a.dxs + c, x[i]);
+          if (GATE != FLEX_GATE_NONE) Raw8<S>::store(static_cast<S*>(a.dZ) + (size_t)row * a.dzs + c, dz);
+        }
       }
-      const int c = p.c + i * p.team * 8;
-      if (in[i]) {
-        Raw8<S>::store(static_cast<S*>(a.dX) + (size_t)row * a.dxs + c, x[i]);
-        if (GATE != FLEX_GATE_NONE) Raw8<S>::store(static_cast<S*>(a.dZ) + (size_t)row * a.dzs + c, dz);
-      }
+    };
+    if (norm_plain(mean)) {
+      put(std::false_type{}, 1.f, __builtin_amdgcn_rsqf(mean));
+    } else {
+      const float half = norm_half(mean);
+      sum[0] = sum[1] = 0.f;
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float s = GATE != FLEX_GATE_NONE ? z[i].v[e] * sig[i].v[e] : 1.f;
+          const float u = (x[i].v[e] * half) * (GATE == FLEX_GATE_FIRST ? s * half : half);
+          float dn = g[i].v[e] * w[i].v[e];
+          if (GATE == FLEX_GATE_LAST) dn *= s;
+          sum[0] = __builtin_fmaf(u, u, sum[0]);
+          sum[1] = __builtin_fmaf(dn, u, sum[1]);
+        }
+      team_sum<WG>(sum, team, box + 4, 0);
+      put(std::true_type{}, half, norm_rsq(sum[0], inv, a.eps, half));
     }
   }
   if constexpr (NARROW) {
