@@ -68,14 +68,15 @@ __device__ __forceinline__ void team_sum(float (&x)[N], int team, float (*box)[4
 }
 
 // Mean squares from 2^-96 on have their squares' bits, and no sum behind infinity has.  Others (eps = 0 allows any) are formed
-// from values times a power of two, whose halves `half` are multiplied to the two factors of a product.
-constexpr float NORM_LOW = 0x1p-96f, NORM_HALF = 0x1p48f;
+// again from values times 2^96 or 2^-96, in place: with a way of its own for such rows behind the sums, other rows' registers grew by
+// up to half (backward of 20000 rows of 2056 channels, bf16: 154 us for 143).
+constexpr float NORM_LOW = 0x1p-96f;
 __device__ __forceinline__ bool norm_plain(float mean) { return mean >= NORM_LOW && mean < INFINITY; }
-__device__ __forceinline__ float norm_half(float mean) { return mean < NORM_LOW ? NORM_HALF : 1.f / NORM_HALF; }
-// 1 / sqrt(mean + eps) of scaled values
-__device__ __forceinline__ float norm_rsq(float sum, float inv, float eps, float half) {
-  const float k = half * half;
-  return __builtin_amdgcn_rsqf(__builtin_fmaf(sum, inv, eps * k * k));
+__device__ __forceinline__ float norm_scale(float mean) { return mean < NORM_LOW ? 1.f / NORM_LOW : NORM_LOW; }
+// whether a row's team has such a mean: of a workgroup, which has one row, as a scalar
+template <bool WG>
+__device__ __forceinline__ bool norm_rare(float mean) {
+  return WG ? !norm_plain(__uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(mean)))) : !norm_plain(mean);
 }
 }  // namespace
 
@@ -146,31 +147,18 @@ __global__ __launch_bounds__(256) void k_norm_fwd(NormArgs a, int team, float in
     team_sum<WG>(sum, team, box, turn);
     const float mean = __builtin_fmaf(sum[0], inv, a.eps);
     float r = __builtin_amdgcn_rsqf(mean);
-    if (!norm_plain(mean)) {
-      const float half = norm_half(mean);
+    if (norm_rare<WG>(mean)) {
+      const float k = norm_scale(mean);
       sum[0] = 0.f;
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
-        if (in[i]) {
-          // the present row again: its X and Z are no longer in registers, and u may have lost what the factors have
-          Raw8<S> rx, rz;
-          Eight x, z;
-          const int c = p.c + i * p.team * 8;
-          rx.load(static_cast<const S*>(a.X) + (size_t)row * a.xs + c, true);
-          rx.get(x);
-          if (GATE == FLEX_GATE_FIRST) {
-            rz.load(static_cast<const S*>(a.Z) + (size_t)row * a.zs + c, true);
-            rz.get(z);
-          }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float s = GATE == FLEX_GATE_FIRST ? z.v[e] * sigmoid(z.v[e]) : 1.f;
-            u[i].v[e] = (x.v[e] * half) * (s * half);
-            sum[0] = __builtin_fmaf(u[i].v[e], u[i].v[e], sum[0]);
-          }
+        for (int e = 0; e < 8; ++e) {
+          u[i].v[e] *= k;
+          sum[0] = __builtin_fmaf(u[i].v[e], u[i].v[e], sum[0]);
         }
       team_sum<WG>(sum, team, box + 2, 0);
-      r = norm_rsq(sum[0], inv, a.eps, half);
+      r = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[0], inv, a.eps * k * k));
     }
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
@@ -240,53 +228,47 @@ __global__ __launch_bounds__(256) void k_norm_bwd(NormArgs a, int team, float in
     if (row + p.step < a.T) fetch(row + p.step);
     team_sum<WG>(sum, team, box, turn);
     const float mean = __builtin_fmaf(sum[0], inv, a.eps);
-    // the row's gradients, with r for values scaled by half^2
-    auto put = [&](auto scaled, float half, float r) {
-      constexpr bool SCALED = decltype(scaled)::value;
-      const float m = sum[1] * r * inv;   // mean(dn n)
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        Eight dz;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float s = GATE != FLEX_GATE_NONE ? z[i].v[e] * sig[i].v[e] : 1.f;
-          const float ds = GATE != FLEX_GATE_NONE ? dsilu(z[i].v[e], sig[i].v[e]) : 0.f;
-          const float xk = SCALED ? x[i].v[e] * half : x[i].v[e], sk = SCALED ? s * half : s;
-          const float n = (GATE == FLEX_GATE_FIRST ? xk * sk : SCALED ? xk * half : xk) * r;
-          const float gn = g[i].v[e] * n;
-          float dn = g[i].v[e] * w[i].v[e];
-          if (GATE == FLEX_GATE_LAST) dn *= s;
-          float du = r * (dn - n * m);
-          if (SCALED) du *= half;   // and by half once more below
-          dw[i].v[e] += GATE == FLEX_GATE_LAST ? gn * s : gn;
-          dz.v[e] = (GATE == FLEX_GATE_FIRST ? du * xk : gn * w[i].v[e]) * ds;
-          x[i].v[e] = GATE == FLEX_GATE_FIRST ? du * sk : SCALED ? du * half : du;
-        }
-        const int c = p.c + i * p.team * 8;
-        if (in[i]) {
-          Raw8<S>::store(static_cast<S*>(a.dX) + (size_t)row * a.dxs + c, x[i]);
-          if (GATE != FLEX_GATE_NONE) Raw8<S>::store(static_cast<S*>(a.dZ) + (size_t)row * a.dzs + c, dz);
-        }
-      }
-    };
-    if (norm_plain(mean)) {
-      put(std::false_type{}, 1.f, __builtin_amdgcn_rsqf(mean));
-    } else {
-      const float half = norm_half(mean);
+    float r = __builtin_amdgcn_rsqf(mean), k = 1.f;
+    if (norm_rare<WG>(mean)) {   // x and r of the scaled row from here on
+      k = norm_scale(mean);
       sum[0] = sum[1] = 0.f;
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
+          x[i].v[e] *= k;
           const float s = GATE != FLEX_GATE_NONE ? z[i].v[e] * sig[i].v[e] : 1.f;
-          const float u = (x[i].v[e] * half) * (GATE == FLEX_GATE_FIRST ? s * half : half);
+          const float u = GATE == FLEX_GATE_FIRST ? x[i].v[e] * s : x[i].v[e];
           float dn = g[i].v[e] * w[i].v[e];
           if (GATE == FLEX_GATE_LAST) dn *= s;
           sum[0] = __builtin_fmaf(u, u, sum[0]);
           sum[1] = __builtin_fmaf(dn, u, sum[1]);
         }
       team_sum<WG>(sum, team, box + 4, 0);
-      put(std::true_type{}, half, norm_rsq(sum[0], inv, a.eps, half));
+      r = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[0], inv, a.eps * k * k));
+    }
+    const float m = sum[1] * r * inv;   // mean(dn n)
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      Eight dz;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float s = GATE != FLEX_GATE_NONE ? z[i].v[e] * sig[i].v[e] : 1.f;
+        const float ds = GATE != FLEX_GATE_NONE ? dsilu(z[i].v[e], sig[i].v[e]) : 0.f;
+        const float n = (GATE == FLEX_GATE_FIRST ? x[i].v[e] * s : x[i].v[e]) * r;
+        const float gn = g[i].v[e] * n;
+        float dn = g[i].v[e] * w[i].v[e];
+        if (GATE == FLEX_GATE_LAST) dn *= s;
+        const float du = r * (dn - n * m);
+        dw[i].v[e] += GATE == FLEX_GATE_LAST ? gn * s : gn;
+        dz.v[e] = (GATE == FLEX_GATE_FIRST ? du * x[i].v[e] : gn * w[i].v[e]) * ds;
+        x[i].v[e] = (GATE == FLEX_GATE_FIRST ? du * s : du) * k;
+      }
+      const int c = p.c + i * p.team * 8;
+      if (in[i]) {
+        Raw8<S>::store(static_cast<S*>(a.dX) + (size_t)row * a.dxs + c, x[i]);
+        if (GATE != FLEX_GATE_NONE) Raw8<S>::store(static_cast<S*>(a.dZ) + (size_t)row * a.dzs + c, dz);
+      }
     }
   }
   if constexpr (NARROW) {
