@@ -169,9 +169,10 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvArgs a, int spans, int til
 
 // As the forward, over CONV_BWD_ROWS rows and the K-1 behind them, whose dz the last rows' dx take: at row
 // t, dz_t is formed and dx of row t - (K-1) is complete.  A workgroup's waves have consecutive rows and
-// leave one row of partial sums of dW and dbias.  29 instructions an element, two of them exponential and reciprocal,
-// keep the SIMDs busy 65 % of the time: bound by them and by memory.  Two channels a lane leave five
-// waves a SIMD: 2 x 8192 rows of 4352 channels, bf16, 91 us (342 MB, 3.8 TB/s); with four channels 106, with eight 143.
+// leave one row of partial sums of dW and dbias.  Bound nearly by memory: 2 x 8192 rows of 4352 channels, bf16, 92 us (428 MB of
+// x, dy and dx, and 454 MB by the counters: 4.9 TB/s, where a large copy has 5.2), with the SIMDs busy 76 % of the time by 29
+// vector instructions an element, two of them exponential and reciprocal.  Two channels a lane leave five waves
+// a SIMD; with four channels 106 us, with eight 143.
 template <class S, int K, bool SILU>
 __global__ __launch_bounds__(256) void k_conv_bwd(ConvArgs a, int spans) {
   constexpr int E = CONV_BWD_CH, U = 4;
@@ -352,7 +353,8 @@ __global__ __launch_bounds__(1024) void k_conv_sum(ConvArgs a, int spans) {
     a.dbias[c] = (float)s;
 }
 
-// One token of every sequence; a thread has 16 bytes of channels of one sequence.
+// One token of every sequence; a thread has 16 bytes of channels of one sequence.  256 rows of 4352 channels, bf16: 8.3 us, 2.8 of
+// them for the taps and the bias, 12 of a thread's 16 loads, which each sequence reads again; fp32 8.1, 0.4 of them.
 template <class S, int K, bool SILU>
 __global__ __launch_bounds__(256) void k_conv_step(ConvArgs a, int units) {
   constexpr int E = Piece<S>::N;

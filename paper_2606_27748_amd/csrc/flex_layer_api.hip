@@ -150,8 +150,10 @@ int32_t check_scan(const flex_scan_desc* d, bool step) {
 // Tokens of a segment.  A sweep's workgroup takes a CU, its sequences are walked in order, and a
 // segment that is not its sequence's last has its rows read twice: segments so long that the card has one
 // workgroup per CU of them, 64 to 4096 tokens (a prompt of 32768 tokens, 16 heads of 128: 207 us; with twice as many
-// 235).  Many sequences, whose ends leave workgroups of any length, have twice as many (16 prompts of 17152 tokens, 64 heads
-// of 64: 274 us; with one per CU 277).
+// 235).  Many sequences, whose ends leave workgroups of any length, have twice as many.  Heads of 64, N = 128, forward with twice as
+// many against one per CU: 16 prompts of 17152 tokens 253 and 265 us, of 31149 393 and 484, of 26818 360 and 349; 24 of 47020 610 and 686;
+// training of 12 of 15190 689 and 716.  Where as few as eight are of one length, one per CU is better (8 x 2048: 197 and 179,
+// training 665 and 609), but the host knows no lengths.
 int scan_seg(const flex_scan_desc* d) {
   const int64_t sets = d->H / scan_heads(d), wgs = d->B * sets < 128 ? 256 : 512;
   int64_t n = ceil_div((int64_t)d->T * sets, wgs * SCAN_CHUNK) * SCAN_CHUNK;

@@ -178,8 +178,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
 // are read from memory once for eight of them.  A wave's chunk is 94 matrix instructions (N = 128; 3000 clocks of its SIMD)
 // and some 950 vector instructions (4000): decays, three terms of each weighted row, roundings.  It takes some 8200: both
 // waves of a SIMD are at the same place of a chunk, behind one barrier, and wait for LDS and for results at the same time.
-// A wave of 64 columns by itself on a SIMD takes 3 % longer, C B^T formed once for all heads beforehand costs more than it saves
-// (162 and 47 us for 195).  The prompts above: 180 us (281 MB of x and y).
+// A wave of 64 columns by itself on a SIMD takes 3 % longer.  P of every head formed beforehand by a kernel of its own, decays
+// and all, took 47 us and left 162 of the sweep's 195 then.  C B^T alone, of which a group has one where P is each head's, is 24 of the
+// 94 and the same in all eight waves: sharing it has not been measured.  The prompts above: 178 us (281 MB of x and y).
+// Fp32 rows: one buffer (96 KB with N = 64, 128 KB with N = 128), whose loads are waited for in full, and products at a tenth of bf16's
+// rate: matrix cores busy 67 % of the time over 16384 tokens, 16 heads of 64, N = 128 (187 us).
 template <class T, int N, int MODE>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_scan_sweep(ScanArgs a) {
   using S = typename Io<T>::type;
