@@ -444,7 +444,8 @@ int32_t flex_conv_workspace_size(const flex_conv_desc* desc, size_t* bytes);
 int32_t flex_conv_fwd(const flex_conv_desc* desc, const void* X, const float* W, const float* bias,
                       const int32_t* off, const void* state0, void* Y, void* state, void* stream);
 
-/* Backward of flex_conv_fwd, state0 a constant.
+/* Backward of flex_conv_fwd, state0 a constant: the rows that the forward read (of a forward in place, a copy from
+ * before it).
  *   dY [T,D] io_dtype
  *   dX [T,D] io_dtype output: the rows of the sequences are overwritten
  *   dW [D,K] fp32, dbias [D] fp32 or NULL   outputs, summed in a fixed order */

@@ -640,7 +640,7 @@ def flex_conv_fwd(desc: flex_conv_desc, X, W, bias, off, state0=None, Y=None, st
 
 
 def flex_conv_bwd(desc: flex_conv_desc, X, W, bias, off, dY, state0=None, dX=None, dW=None, dbias=None, ws=None):
-    """Backward of flex_conv_fwd, its state0 a constant.  Returns dict(dX, dW, dbias): dX in the io dtype (rows of no
+    """Backward of flex_conv_fwd, its state0 a constant, as it was before a forward in place.  Returns dict(dX, dW, dbias): dX in the io dtype (rows of no
     sequence are not written), dW [D,K] and dbias [D] (None without a bias) fp32."""
     import torch
     io, f32, rows = _io(desc), torch.float32, (desc.T, desc.D)
